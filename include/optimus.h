@@ -402,6 +402,39 @@ int optimus_cross_entropy2d(const void* logits, const int32_t* labels, float* lo
 int optimus_cross_entropy2d_bwd(const void* logits, const int32_t* labels, const float* lse, void* d_logits,
                                 float scale, int64_t M, int64_t v, int q, int i, int j, int dtype, void* stream);
 
+/* ---- one AdamW step over many tensors (the update of Section 3.2.3, which lets the layers share one parameter-gradient buffer) ----
+ * Per element, in fp32 whatever the types:  g = grad_scale * sum over the parts of grad;  m = beta1 m + (1 - beta1) g;
+ *   v = beta2 v + (1 - beta2) g^2;  w = w - (lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps) + lr * weight_decay * w).
+ * A vector's partial gradients [q][q][N/q] of optimus_layer_bwd are q parts of N elements: they are added in order here.
+ * Weights: fp32; or bf16 with an fp32 `master` (which is updated; param receives it rounded to nearest even); or bf16 alone, rounded
+ *   up or down at random in proportion to the place between the two neighbours (to nearest, updates below half a step would be lost).
+ * Moments: fp32 m, v [n]; or, with m_scale and v_scale, 8 bits: e4m3 numbers (OCP: 1 sign, 4 exponent, 3 mantissa bits), element k
+ *   standing for number * 2^(scale[k / 128] - 127) (scale 255: NaN), rounded at random like the weights; a v above zero stays above zero.
+ *   Zeroed memory is a valid state of either kind.  A group with a gradient that is not finite turns NaN as a whole.
+ * The random bits are a hash of (seed, step, index in `tensors`, element): the same call gives the same bits.
+ * grad_scale, lr_on_device, step_on_device: NULL, or device memory that is read when the step runs, in place of 1, lr and step: what
+ *   a captured step changes between its replays.
+ * tensors: host array, read before the call returns.  Pointers need the alignment of their elements only.  The parameters may not
+ *   overlap (OPTIMUS_EINVAL); nor may any other memory that is written (not checked).  n from 1 to 2^40, any number. */
+typedef struct {
+  void* param;
+  float* master;
+  const void* grad;         /* [grad_parts][n] */
+  void* m; void* v;
+  uint8_t* m_scale; uint8_t* v_scale;   /* [(n + 127) / 128] each, or both NULL */
+  int64_t n;
+  int param_dtype, grad_dtype;          /* OPTIMUS_FP32 / OPTIMUS_BF16 */
+  int grad_parts;
+  float weight_decay;
+} optimus_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps;         /* 0 <= beta < 1, eps > 0 */
+  int64_t step;                         /* 1 in the first step */
+  uint64_t seed;
+  const float* grad_scale; const float* lr_on_device; const int64_t* step_on_device;
+} optimus_adamw_cfg;
+int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count, void* stream);
+
 /* ---- flop accounting (Table 1) ----
  * optimus_gemm_flops: 2*(M/q)*K*(N/q), one device's share of one product.
  * optimus_layer_flops: one device's share of a layer; what = 0 forward,

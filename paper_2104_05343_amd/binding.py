@@ -73,6 +73,17 @@ class StackBuffers(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in ("workspace", "forward", "backward", "conjunction", "checkpoint")]
 
 
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int), ("grad_dtype", C.c_int),
+                ("grad_parts", C.c_int), ("weight_decay", C.c_float)]
+
+
+class AdamwCfg(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("seed", C.c_uint64), ("grad_scale", C.c_void_p), ("lr_on_device", C.c_void_p), ("step_on_device", C.c_void_p)]
+
+
 LAYER_DONE_FN = C.CFUNCTYPE(None, C.c_int, C.c_void_p)
 
 
@@ -120,6 +131,7 @@ SIGNATURES = {
     "optimus_layer_workspace_bytes_grid": (_SZ, [C.POINTER(LayerCfg)]),
     "optimus_layer_fwd": (_INT, [C.POINTER(LayerCfg), C.POINTER(LayerTensors), _INT, _INT, _P, _SZ, _P]),
     "optimus_layer_bwd": (_INT, [C.POINTER(LayerCfg), C.POINTER(LayerTensors), _INT, _INT, _P, _SZ, _P]),
+    "optimus_adamw_step": (_INT, [C.POINTER(AdamwCfg), C.POINTER(AdamwTensor), _INT, _P]),
     "optimus_gemm_flops": (_I64, [_I64, _I64, _I64, _INT]),
     "optimus_layer_flops": (_I64, [C.POINTER(LayerCfg), _INT]),
     "optimus_debug_set_gemm_variant": (None, [_INT]),
@@ -405,6 +417,25 @@ def stack_bwd(cfg: LayerCfg, params, grads, d_out, buf: StackBuffers, d_x, done=
     cb = LAYER_DONE_FN((lambda layer, user: done(layer)) if done is not None else 0)
     _check(lib().optimus_stack_bwd(C.byref(cfg), len(params), pa, ga, _ptr(d_out), C.byref(buf), _ptr(d_x), cb, None,
                                    _stream(stream)), "optimus_stack_bwd")
+
+
+def make_adamw_tensors(tensors):
+    """tensors: list of dicts param, grad, m, v (torch tensors) and, where they differ from these defaults, master=None, m_scale=None,
+    v_scale=None, n=param.numel(), grad_parts=1, weight_decay=0.0.  The array holds addresses: keep the tensors alive."""
+    codes = {torch.float32: FP32, torch.bfloat16: BF16}
+    out = (AdamwTensor * len(tensors))()
+    for a, t in zip(out, tensors):
+        for name in ("param", "master", "grad", "m", "v", "m_scale", "v_scale"):
+            setattr(a, name, _ptr(t.get(name)))
+        a.n = t.get("n", t["param"].numel())
+        a.param_dtype, a.grad_dtype = (codes.get(t[k].dtype, -1) for k in ("param", "grad"))
+        a.grad_parts, a.weight_decay = t.get("grad_parts", 1), t.get("weight_decay", 0.0)
+    return out
+
+
+def adamw_step(cfg: AdamwCfg, tensors, stream=None):
+    """tensors: what make_adamw_tensors returned."""
+    _check(lib().optimus_adamw_step(C.byref(cfg), tensors, len(tensors), _stream(stream)), "optimus_adamw_step")
 
 
 def gemm_flops(M, K, N, q) -> int:

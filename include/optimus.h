@@ -242,6 +242,41 @@ int optimus_attention_fused_bwd_static(const void* qkv, const void* attn, const 
                                        void* d_qkv, int b, int s, int h, int n, int q, int i, int j,
                                        int causal, int dtype, void* stream);
 
+/* ---- the same attention with changed scores: capped, biased by distance, masked by documents or opened by a prefix ----
+ * Layouts, lse, d_qkv, coordinates and limits as in optimus_attention_fused_*; per pair (t, u) of a (sequence, head):
+ *   S = Q K^T / sqrt(d);  with cap > 0: S = cap tanh(S / cap);
+ *   with slopes: S -= slopes[head] |t - u|;  or, with table: S += table[head][bucket(t - u)] (not both: EINVAL).
+ * A pair is left out
+ *   with causal != 0 where u > t, unless u < prefix[sequence] (prefix needs causal != 0: EINVAL; values are clamped to 0 .. s);
+ *   with documents where documents[t] != documents[u], or either is negative: a token of a negative document is padding;
+ *   where the table's number is -1e30 or less (-infinity included).
+ * A row without a pair has attn 0, lse -infinity and gradients 0.  What qkv, attn and d_attn hold in rows of padding is not looked at,
+ * NaN included; their rows of attn and d_qkv are written as zeros.
+ * bucket(n) of the distance n = t - u: a side has `side` buckets: buckets, or buckets / 2 with two_sided; near = side / 2.  Distances
+ * 0 .. near - 1 have a bucket each; bucket near + k begins at the first whole number not below near * (max_distance / near)^(k / (side -
+ * near)); the last has no end.  n < 0 (a later key): bucket 0, or with two_sided side + bucket(-n).  2 <= side, even `buckets` with
+ * two_sided, buckets <= 128, near < max_distance <= 1024 (ESHAPE).
+ * Backward: S is rebuilt and P = exp(S - lse); dS = P (dO V^T - rowsum(dO attn)); d_table sums dS over the pairs of a bucket; then
+ * dS (1 - tanh^2) is the gradient of Q K^T / sqrt(d).  d_table: fp32 [q][q][n/q * buckets], entry (i, j) written: device (i, j)'s partial,
+ * the gradient of table rows j*n/q .. is the sum over i; NULL: not computed.  No gradient of slopes.
+ * slopes: fp32 [n]; table: fp32 [n][buckets]; documents: int32 [b*s], in any order; prefix: int32 [b]: device memory or NULL.
+ * ws: optimus_attention_biased_workspace_bytes(...) bytes (0 for arguments that are refused), 16-byte aligned; the forward needs it with
+ * documents only.  Calls that may overlap need a workspace each.  (n/q + 1) * b/q <= 65535, b/q * n/q * ceil(s/64) < 2^23 (ESHAPE). */
+typedef struct {
+  float cap;
+  const float* slopes;
+  const float* table;
+  int buckets, max_distance, two_sided;
+  const int32_t* documents;
+  const int32_t* prefix;
+} optimus_attention_bias;
+int optimus_attention_biased_fwd(const void* qkv, void* attn, float* lse, int b, int s, int h, int n, int q, int i, int j, int causal,
+                                 int dtype, const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream);
+int optimus_attention_biased_bwd(const void* qkv, const void* attn, const float* lse, const void* d_attn, void* d_qkv, float* d_table,
+                                 int b, int s, int h, int n, int q, int i, int j, int causal, int dtype,
+                                 const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream);
+size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int q, const optimus_attention_bias* bias);
+
 /* ---- one transformer layer on device (i, j) (Section 3.2; Eq. 1) ----
  * Wiring: a1 = LN1(x); qkv = a1 Wqkv + b; attn = local attention;
  * h_mid = x + attn Wo + b; a2 = LN2(h_mid); pre = a2 W1 + b; g = GeLU(pre);

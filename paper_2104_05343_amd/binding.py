@@ -73,6 +73,11 @@ class StackBuffers(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in ("workspace", "forward", "backward", "conjunction", "checkpoint")]
 
 
+class AttentionBias(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("table", C.c_void_p), ("buckets", C.c_int), ("max_distance", C.c_int),
+                ("two_sided", C.c_int), ("documents", C.c_void_p), ("prefix", C.c_void_p)]
+
+
 class AdamwTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int), ("grad_dtype", C.c_int),
@@ -117,6 +122,11 @@ SIGNATURES = {
     "optimus_attention_fused_bwd": (_INT, [_P, _P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _P, _SZ, _P]),
     "optimus_attention_fused_workspace_bytes": (_SZ, [_INT, _INT, _INT, _INT, _INT]),
     "optimus_attention_fused_bwd_static": (_INT, [_P, _P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _P]),
+    "optimus_attention_biased_fwd": (_INT, [_P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias), _P,
+                                            _SZ, _P]),
+    "optimus_attention_biased_bwd": (_INT, [_P, _P, _P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT,
+                                            C.POINTER(AttentionBias), _P, _SZ, _P]),
+    "optimus_attention_biased_workspace_bytes": (_SZ, [_INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias)]),
     "optimus_embedding_fwd": (_INT, [_P, _P, _P, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
     "optimus_embedding_bwd": (_INT, [_P, _P, _P, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
     "optimus_cross_entropy2d_stats": (_INT, [_P, _P, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
@@ -319,6 +329,27 @@ def attention_fused_bwd(qkv, attn, lse, d_attn, d_qkv, b, s, h, n, q, i, j, caus
     p, nb = _ws(ws)
     _check(lib().optimus_attention_fused_bwd(_ptr(qkv), _ptr(attn), _ptr(lse), _ptr(d_attn), _ptr(d_qkv), b, s, h, n, q, i, j,
                                              int(causal), dtype, p, nb, _stream(stream)), "optimus_attention_fused_bwd")
+
+
+def make_attention_bias(cap=0.0, slopes=None, table=None, buckets=0, max_distance=0, two_sided=False, documents=None, prefix=None) -> AttentionBias:
+    """What changes the scores (optimus_attention_bias).  Holds addresses: keep the tensors alive."""
+    return AttentionBias(float(cap), _ptr(slopes), _ptr(table), buckets, max_distance, int(two_sided), _ptr(documents), _ptr(prefix))
+
+
+def attention_biased_workspace_bytes(b, s, h, n, q, bias: AttentionBias) -> int:
+    return lib().optimus_attention_biased_workspace_bytes(b, s, h, n, q, C.byref(bias))
+
+
+def attention_biased_fwd(qkv, attn, lse, b, s, h, n, q, i, j, causal, dtype, bias: AttentionBias, ws=None, stream=None):
+    p, nb = _ws(ws)
+    _check(lib().optimus_attention_biased_fwd(_ptr(qkv), _ptr(attn), _ptr(lse), b, s, h, n, q, i, j, int(causal), dtype, C.byref(bias),
+                                              p, nb, _stream(stream)), "optimus_attention_biased_fwd")
+
+
+def attention_biased_bwd(qkv, attn, lse, d_attn, d_qkv, d_table, b, s, h, n, q, i, j, causal, dtype, bias: AttentionBias, ws, stream=None):
+    p, nb = _ws(ws)
+    _check(lib().optimus_attention_biased_bwd(_ptr(qkv), _ptr(attn), _ptr(lse), _ptr(d_attn), _ptr(d_qkv), _ptr(d_table), b, s, h, n, q, i, j,
+                                              int(causal), dtype, C.byref(bias), p, nb, _stream(stream)), "optimus_attention_biased_bwd")
 
 
 def layer_workspace_bytes(cfg: LayerCfg) -> int:

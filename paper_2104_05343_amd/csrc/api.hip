@@ -347,6 +347,71 @@ int run_attention_fused(bool bwd, const void* qkv, void* attn, float* lse, const
   return bwd ? launch_attn_fused_bwd(d, as_stream(stream)) : launch_attn_fused_fwd(d, as_stream(stream));
 }
 
+// ---- fused attention with changed scores ----
+// First distance of every bucket of a side (see the header): the smallest whole number not below near * ratio^(k / (side - near)), where
+// a power next to a whole number is that number.
+int bias_desc(const optimus_attention_bias* b, int causal, AttnBiasedDesc* d) {
+  if (!b) return OPTIMUS_EINVAL;
+  if (!(b->cap >= 0) || isinf(b->cap) || (b->slopes && b->table) || (b->prefix && !causal)) return OPTIMUS_EINVAL;
+  d->cap = b->cap; d->slopes = b->slopes; d->table = b->table; d->documents = b->documents; d->prefix = b->prefix;
+  if (!b->table) return OPTIMUS_OK;
+  d->buckets = b->buckets; d->two_sided = b->two_sided ? 1 : 0;
+  const int side = d->two_sided ? b->buckets / 2 : b->buckets, near = side / 2;
+  if (side < 2 || b->buckets > 128 || (d->two_sided && b->buckets % 2) || b->max_distance <= near || b->max_distance > 1024) return OPTIMUS_ESHAPE;
+  for (int k = 0; k < side; ++k)
+    d->first[k] = (unsigned short)(k < near ? k : ceil(near * pow((double)b->max_distance / near, (double)(k - near) / (side - near)) - 1e-9));
+  d->first[side] = 0xffff;
+  return OPTIMUS_OK;
+}
+// a launch has 65535 matrices and sequences, and 2^32 threads, at most
+int attn_biased_dims(int b, int s, int h, int n, int q, AttnDims* a) {
+  if (const int rc = attn_fused_dims(b, s, h, n, q, a)) return rc;
+  return a->nmat + a->nb > 65535 || (s + 63ll) / 64 * a->nmat >= (1 << 23) ? OPTIMUS_ESHAPE : OPTIMUS_OK;
+}
+struct BiasedWs { size_t blocks, delta, parts, total; };   // bytes of each, in this order
+BiasedWs biased_ws(const AttnDims& a, int b, int q, const AttnBiasedDesc& d) {
+  BiasedWs w;
+  const size_t nblk = ((size_t)a.s + 63) / 64, mats = (size_t)q * q * a.nmat;
+  w.blocks = d.documents ? align256((size_t)b * nblk * 16) : 0;
+  w.delta = align256(mats * a.s * sizeof(float));
+  w.parts = d.table ? align256(mats * nblk * d.buckets * sizeof(float)) : 0;
+  w.total = w.blocks + w.delta + w.parts;
+  return w;
+}
+int run_attention_biased(bool bwd, const void* qkv, void* attn, float* lse, const void* d_attn, void* d_qkv, float* d_table, int b, int s, int h,
+                         int n, int q, int i, int j, int causal, int dtype, const optimus_attention_bias* bias, void* ws, size_t ws_bytes,
+                         void* stream) {
+  if (!qkv || !attn || !lse || (bwd && (!d_attn || !d_qkv))) return OPTIMUS_EINVAL;
+  if (dtype != OPTIMUS_BF16) return OPTIMUS_EDTYPE;
+  AttnDims a;
+  int rc = attn_biased_dims(b, s, h, n, q, &a);
+  if (rc) return rc;
+  if ((rc = check_coords(q, i, j))) return rc;
+  AttnBiasedDesc d = {};
+  if ((rc = bias_desc(bias, causal, &d))) return rc;
+  if (d_table && !d.table) return OPTIMUS_EINVAL;
+  const BiasedWs w = biased_ws(a, b, q, d);
+  if ((bwd || d.documents) && (!ws || ws_bytes < w.total || (uintptr_t)ws & 15)) return OPTIMUS_EWORKSPACE;
+  const bool grid = is_grid(i, j);
+  const long long dev = grid ? 0 : (long long)i * q + j;
+  AttnFusedDesc& f = d.base;
+  f.qkv = (const bf16_t*)qkv + dev * a.blk_qkv;
+  f.attn = (bf16_t*)attn + dev * a.blk_attn;
+  f.lse = lse + dev * a.nmat * s;
+  f.d_attn = d_attn ? (const bf16_t*)d_attn + dev * a.blk_attn : nullptr;
+  f.d_qkv = d_qkv ? (bf16_t*)d_qkv + dev * a.blk_qkv : nullptr;
+  f.s = s; f.d = a.d; f.nb = a.nb; f.nh = a.nh; f.ld = a.ld; f.ldo = a.ldo;
+  f.ndev = grid ? q * q : 1;
+  f.dev_qkv = a.blk_qkv; f.dev_attn = a.blk_attn;
+  f.causal = causal;
+  d.q = q; d.dev0 = (int)dev;
+  d.blocks = ws;
+  f.delta = (float*)off(ws, (long long)w.blocks, 1);
+  d.table_parts = (float*)off(ws, (long long)(w.blocks + w.delta), 1);
+  d.d_table = d_table ? d_table + dev * a.nh * d.buckets : nullptr;
+  return bwd ? launch_attn_biased_bwd(d, as_stream(stream)) : launch_attn_biased_fwd(d, as_stream(stream));
+}
+
 int end_desc(int64_t M, int64_t v, int64_t h, int q, int i, int j, int dtype, EndDesc* d) {
   if (dtype != OPTIMUS_FP32 && dtype != OPTIMUS_BF16) return OPTIMUS_EDTYPE;
   if (q <= 0 || M <= 0 || v <= 0 || h <= 0 || M % q || v % q || h % q) return OPTIMUS_ESHAPE;
@@ -813,6 +878,23 @@ int optimus_attention_fused_bwd_static(const void* qkv, const void* attn, const 
   // check of the shared code path is against the whole-grid size, which the array is not required to hold
   return run_attention_fused(true, qkv, const_cast<void*>(attn), const_cast<float*>(lse), d_attn, d_qkv, b, s, h, n, q, i, j,
                              causal ? 1 : 0, dtype, ws, attn_fused_ws_bytes(a, q), stream);
+}
+
+size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int q, const optimus_attention_bias* bias) {
+  AttnDims a;
+  AttnBiasedDesc d = {};
+  if (attn_biased_dims(b, s, h, n, q, &a) || bias_desc(bias, 1, &d)) return 0;
+  return biased_ws(a, b, q, d).total;
+}
+int optimus_attention_biased_fwd(const void* qkv, void* attn, float* lse, int b, int s, int h, int n, int q, int i, int j, int causal,
+                                 int dtype, const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream) {
+  return run_attention_biased(false, qkv, attn, lse, nullptr, nullptr, nullptr, b, s, h, n, q, i, j, causal ? 1 : 0, dtype, bias, ws, ws_bytes, stream);
+}
+int optimus_attention_biased_bwd(const void* qkv, const void* attn, const float* lse, const void* d_attn, void* d_qkv, float* d_table,
+                                 int b, int s, int h, int n, int q, int i, int j, int causal, int dtype,
+                                 const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream) {
+  return run_attention_biased(true, qkv, const_cast<void*>(attn), const_cast<float*>(lse), d_attn, d_qkv, d_table, b, s, h, n, q, i, j,
+                              causal ? 1 : 0, dtype, bias, ws, ws_bytes, stream);
 }
 
 size_t layer_attn_ws(const optimus_layer_cfg* c, const AttnDims& a) {

@@ -1,0 +1,330 @@
+// Forward of the attention with changed scores (attention_biased_kernel.hpp), the kernel that both directions run first, the choice
+// between the forms.
+#include "attention_biased_kernel.hpp"
+
+namespace optimus {
+namespace {
+
+// Forward.  NRG: row groups of 32 queries per workgroup, as in the attention without changes.
+template <int D, int NRG, bool CAP, int BIAS>
+__global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_biased_fwd_kernel(BiasedArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, BQ = NRG * 32, AHEAD = D == 64 ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][PAIR * D];  // [stage][K, V][pair tile]
+  __shared__ BiasLds<BIAS> bias_lds;
+  __shared__ __attribute__((aligned(16))) int key_docs[2 * NRG][BLK];    // of the wavefront's block
+  __shared__ int live[2];
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave % NRG, par = wave / NRG;
+  const int tile = gridDim.y - 1 - blockIdx.y, s = f.s;   // the longest causal loops first
+  const Matrix m = matrix_of<D>(a, blockIdx.x, blockIdx.z);
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const bf16_t* Kp = Qp + D;
+  const bf16_t* Vp = Qp + 2 * D;
+  const int q0 = tile * BQ + rg * 32;
+  const int query = q0 + (lane & 31);
+  const int qrow = min(query, s - 1);
+  const int qdoc = m.docs ? m.docs[qrow] : 0;
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = zero_if(qdoc < 0, *(const bf16x8*)(Qp + (long long)qrow * f.ld + ks * 16 + g * 8));
+  const Bias<BIAS> bias = make_bias<BIAS>(a, m.ghead, bias_lds);
+
+  const int wg_hi = min(tile * BQ + BQ, s) - 1;   // last query row of the workgroup
+  int kb_lo = 0, kb_hi = a.causal ? max(wg_hi, m.prefix - 1) / BLK + 1 : a.nblk;
+  if (m.docs) live_blocks(m.blocks, tile * BQ / BLK, wg_hi / BLK, kb_lo, kb_hi, live);
+  const int it_lo = kb_lo / 2, n_it = (kb_hi + 1) / 2;
+  // last key that a row of the wavefront may see, and that this lane's may
+  const int wave_last = q0 >= s ? -1 : a.causal ? max(min(q0 + 31, s - 1), m.prefix - 1) : s - 1;
+  const int limit = a.causal ? max(qrow, m.prefix - 1) : s - 1;
+  const i32x4_t none = {0x7fffffff, -1, 0, 0};
+  const i32x4_t own = m.docs && q0 < s ? m.blocks[q0 / BLK] : none;
+
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+  float m_run = -INFINITY, l_run = 0.f;
+
+  RowLoader<D, 2 * NRG, PAIR> ldr;
+  ldr.init(f.ld, wave, lane);
+  // documents of a pair's blocks, known an iteration before they are used
+  struct Pair { i32x4_t even, odd; };
+  auto pair_of = [&](int it) {
+    Pair p = {none, none};
+    if (m.docs) {
+      if (2 * it < a.nblk) p.even = m.blocks[2 * it];
+      if (2 * it + 1 < a.nblk) p.odd = m.blocks[2 * it + 1];
+    }
+    return p;
+  };
+  auto issue = [&](int it, int st, const Pair& p) {
+    const int* docs = p.even.z | p.odd.z ? m.docs : nullptr;
+    ldr.issue(Kp, it * PAIR, s, lds[st][0], docs);
+    ldr.issue(Vp, it * PAIR, s, lds[st][1], docs);
+  };
+  Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
+  if (it_lo < n_it) {
+    if (m.docs) key_docs[wave][lane] = m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)];
+    issue(it_lo, 0, cur);
+  }
+  wait_loads_and_barrier();
+  for (int it = it_lo; it < n_it; ++it) {
+    const int st = (it - it_lo) & 1;
+    int next_doc = -1;
+    Pair after = next;
+    if (it + 1 < n_it) {
+      if (m.docs) {
+        next_doc = m.docs[min((2 * (it + 1) + par) * BLK + lane, s - 1)];
+        after = pair_of(it + 2);
+      }
+      issue(it + 1, st ^ 1, next);
+    }
+    const int kb = 2 * it + par, kbase = kb * BLK;
+    const i32x4_t blk = par ? cur.odd : cur.even;
+    const bool shared = !m.docs || share_documents(blk, own);
+    if (kb >= kb_lo && kb < kb_hi && kbase <= wave_last && shared) {
+      const bf16_t* tK = lds[st][0] + par * BLK * D;
+      const bf16_t* tV = lds[st][1] + par * BLK * D;
+      f32x16 sacc[2];
+      sacc[0] = zero16();
+      sacc[1] = zero16();
+      pipelined<2 * KS, AHEAD>([&](int n) { return frag_rows<D>(tK, n / KS * 32, n % KS, lane); },
+                               [&](int n, const bf16x8& x) {
+                                 sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
+                               });
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        if (CAP) tanh16(sacc[t2], a);
+        const int k0 = kbase + t2 * 32;
+        scores16<CAP, BIAS, -1>(sacc[t2], a, bias, tile_bias<BIAS>(bias, query - k0 - 4 * g, q0 - k0 - 31, q0 - k0 + 31));
+      }
+      // keys past a row's limit, and those past the end, exist only in the last blocks (wave-uniform tests)
+      if (a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) {
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (kbase + t2 * 32 + slot(r) + 4 * g > limit) sacc[t2][r] = -INFINITY;
+      }
+      if (m.docs && !one_document(blk, own)) {
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int4 kd = *(const int4*)&key_docs[wave][t2 * 32 + 8 * c + 4 * g];
+            const int k4[4] = {kd.x, kd.y, kd.z, kd.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (k4[e] != qdoc || qdoc < 0) sacc[t2][4 * c + e] = -INFINITY;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
+      mx = halfwave_max(mx);
+      // The running maximum follows the block's only when that is more than 2^8 above it (see the attention without changes).  A row
+      // that has met no key yet keeps -infinity, and 0 in its place where it is subtracted: its terms are exp2(-infinity) = 0.
+      const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
+      const float m_new = move ? fmaxf(m_run, mx) : m_run;
+      const float m_sub = m_new == -INFINITY ? 0.f : m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = __builtin_amdgcn_exp2f(sacc[t2][r] - m_sub);
+          sacc[t2][r] = p;
+          sum += p;
+        }
+      sum = halfwave_sum(sum);
+      if (move) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_sub);
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+        m_run = m_new;
+      }
+      l_run += sum;
+      bf16x8 pf[2][2];
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        pf[t2][0] = pack_acc<0>(sacc[t2]);
+        pf[t2][1] = pack_acc<1>(sacc[t2]);
+      }
+      pipelined<4 * DT, AHEAD>([&](int n) { return frag_cols_acc_order<D>(tV, n / DT * 16, n % DT * 32, lane); },
+                               [&](int n, const bf16x8& x) {
+                                 oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[n / (2 * DT)][n / DT & 1], oacc[n % DT], 0, 0, 0);
+                               });
+    }
+    if (m.docs && it + 1 < n_it) key_docs[wave][lane] = next_doc;
+    cur = next;
+    next = after;
+    wait_loads_and_barrier();
+  }
+  // merge the two parities: the odd one hands (m, l, O) over through LDS (all tiles are free after the last barrier)
+  float* xch = (float*)&lds[0][0][0] + rg * (DT * 16 + 2) * 64;
+  if (par == 1) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) xch[(dt * 16 + r) * 64 + lane] = oacc[dt][r];
+    xch[(DT * 16) * 64 + lane] = m_run;
+    xch[(DT * 16 + 1) * 64 + lane] = l_run;
+  }
+  __syncthreads();
+  if (par == 0 && query < s) {
+    const float m1 = xch[(DT * 16) * 64 + lane], l1 = xch[(DT * 16 + 1) * 64 + lane];
+    const float top = fmaxf(m_run, m1), m_sub = top == -INFINITY ? 0.f : top;
+    const float a0 = __builtin_amdgcn_exp2f(m_run - m_sub), a1 = __builtin_amdgcn_exp2f(m1 - m_sub);
+    const float l = l_run * a0 + l1 * a1;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;   // (no pair left: zeros)
+    const float w0 = a0 * inv, w1 = a1 * inv;
+    bf16_t* Op = f.attn + m.attn + (long long)query * f.ldo;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = oacc[dt][4 * c + e] * w0 + xch[(dt * 16 + 4 * c + e) * 64 + lane] * w1;
+        u32x2 w = {pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])};
+        *(u32x2*)(Op + dt * 32 + 8 * c + 4 * g) = w;
+      }
+    if (g == 0) f.lse[m.vec + query] = l == 0.f ? -INFINITY : (m_sub + __log2f(l)) * LN2;
+  }
+}
+
+// Ahead of the other kernels.  Workgroups y < nmat (backward): rowsum(dO * O) of every query row, 0 for padding.  The others: documents
+// of every block of 64 tokens, a wavefront each.
+template <int D>
+__global__ __launch_bounds__(256) void attn_biased_prepare_kernel(BiasedArgs a, int nmat) {
+  const FusedArgs& f = a.f;
+  const int lane = threadIdx.x & 63, g = lane >> 5, wave = threadIdx.x >> 6, s = f.s;
+  if ((int)blockIdx.y < nmat) {
+    const Matrix m = matrix_of<D>(a, blockIdx.y, blockIdx.z);
+    const int query = blockIdx.x * 128 + wave * 32 + (lane & 31);
+    const int qrow = min(query, s - 1);
+    float delta = 0.f;
+    const bf16_t* G = f.d_attn + m.attn + (long long)qrow * f.ldo;
+    const bf16_t* O = f.attn + m.attn + (long long)qrow * f.ldo;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) delta += delta_piece(*(const bf16x8*)(G + ks * 16 + g * 8), *(const bf16x8*)(O + ks * 16 + g * 8));
+    delta = halfwave_sum(delta);
+    if (m.docs && m.docs[qrow] < 0) delta = 0.f;
+    if (g == 0 && query < s) f.delta[m.vec + qrow] = delta;
+    return;
+  }
+  // sequences of the launch's device rows: device z's, the first of a row speaks for the others
+  const int at = a.dev0 + (int)blockIdx.z, seq = (int)blockIdx.y - nmat;
+  if (blockIdx.z > 0 && at % a.q != 0) return;
+  const long long gseq = (long long)(at / a.q) * a.nb + seq;
+  for (int blk = blockIdx.x * 2 + (wave & 1); blk < a.nblk && wave < 2; blk += 2 * gridDim.x) {
+    const int t = blk * BLK + lane;
+    const int doc = t < s ? a.documents[gseq * s + t] : 0x7fffffff;   // (past the end: no part)
+    const bool pad = t < s && doc < 0;
+    int lo = t < s && doc >= 0 ? doc : 0x7fffffff, hi = t < s && doc >= 0 ? doc : -1;
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) {
+      lo = min(lo, __shfl_xor(lo, step));
+      hi = max(hi, __shfl_xor(hi, step));
+    }
+    const int any = __builtin_amdgcn_ballot_w64(pad) != 0;
+    if (lane == 0) const_cast<i32x4_t*>(a.blocks)[gseq * a.nblk + blk] = i32x4_t{lo, hi, any, 0};
+  }
+}
+
+bool desc_ok(const AttnBiasedDesc& b) {
+  const AttnFusedDesc& d = b.base;
+  if (!attn_fused_supported(d.d)) return false;
+  if (d.s < 1 || d.nb < 1 || d.nh < 1 || d.ndev < 1 || d.ndev > 65535) return false;
+  if ((long long)d.nb * d.nh + d.nb > 65535) return false;
+  if (d.ld % 8 || d.ldo % 8 || d.ld < 3 * d.d * d.nh || d.ldo < d.d * d.nh) return false;
+  if ((long long)((d.s + BLK - 1) / BLK) * d.nb * d.nh >= (1 << 23)) return false;   // 2^32 threads in a launch
+  return (long long)PAIR * d.ld * 2 < (1ll << 31);
+}
+
+BiasedArgs make_args(const AttnBiasedDesc& b) {
+  const AttnFusedDesc& d = b.base;
+  BiasedArgs a = {};
+  FusedArgs& f = a.f;
+  f.qkv = (const bf16_t*)d.qkv; f.attn = (bf16_t*)d.attn; f.lse = d.lse;
+  f.d_attn = (const bf16_t*)d.d_attn; f.d_qkv = (bf16_t*)d.d_qkv; f.delta = d.delta;
+  f.s = d.s; f.nh = d.nh; f.ld = d.ld; f.ldo = d.ldo;
+  f.dev_qkv = d.dev_qkv; f.dev_attn = d.dev_attn; f.dev_vec = (long long)d.nb * d.nh * d.s;
+  f.scale = 1.0f / sqrtf((float)d.d);
+  f.scale_log2 = f.scale * LOG2E;
+  a.nb = d.nb; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal; a.nblk = (d.s + BLK - 1) / BLK;
+  if (b.cap > 0) {
+    const double in = 1.0 / (sqrt((double)d.d) * b.cap);
+    a.cap_log2 = (float)(b.cap * 1.4426950408889634);
+    a.cap_in = (float)in;
+    a.cap_exp = (float)(2.0 * in * 1.4426950408889634);
+    a.cap_small = (float)(0.25 / in);
+  }
+  a.slopes = b.slopes; a.table = b.table; a.documents = b.documents; a.prefix = b.prefix;
+  a.blocks = (const i32x4_t*)b.blocks; a.table_parts = b.table_parts;
+  if (b.table) {
+    a.buckets = b.buckets; a.two_sided = b.two_sided;
+    a.side = b.two_sided ? b.buckets / 2 : b.buckets;
+    for (int k = 0; k <= a.side; ++k) a.first[k] = b.first[k];
+    a.far = a.first[a.side - 1];
+  }
+  return a;
+}
+
+template <int D, bool CAP, int BIAS>
+void fwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
+  // 128-row workgroups from one per two compute units on, as without changes
+  const bool big = (long long)((d.s + 127) / 128) * d.nb * d.nh * d.ndev >= 128;
+  const int rows = big ? 128 : BLK;
+  const dim3 grid(d.nb * d.nh, (d.s + rows - 1) / rows, d.ndev);
+  if (big) attn_biased_fwd_kernel<D, 4, CAP, BIAS><<<grid, 512, 0, st>>>(a);
+  else attn_biased_fwd_kernel<D, 2, CAP, BIAS><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+void launch_attn_biased_prepare(const BiasedArgs& a, int d, bool delta, int nmat, int ndev, hipStream_t st) {
+  const int mats = delta ? nmat : 0, seqs = a.documents ? a.nb : 0;
+  if (mats + seqs == 0) return;
+  const dim3 grid((a.f.s + 127) / 128, mats + seqs, ndev);
+  if (d == 64) attn_biased_prepare_kernel<64><<<grid, 256, 0, st>>>(a, mats);
+  else attn_biased_prepare_kernel<128><<<grid, 256, 0, st>>>(a, mats);
+}
+
+int launch_attn_biased_fwd(const AttnBiasedDesc& b, hipStream_t st) {
+  const AttnFusedDesc& d = b.base;
+  if (!desc_ok(b) || !d.qkv || !d.attn || !d.lse) return OPTIMUS_ESHAPE;
+  const BiasedArgs a = make_args(b);
+  launch_attn_biased_prepare(a, d.d, false, d.nb * d.nh, d.ndev, st);
+  const int kind = (b.cap > 0 ? 3 : 0) + (b.table ? 2 : b.slopes ? 1 : 0);
+  auto run = [&](auto width) {
+    constexpr int D = decltype(width)::value;
+    switch (kind) {
+      case 0: fwd_launch<D, false, 0>(a, d, st); break;
+      case 1: fwd_launch<D, false, 1>(a, d, st); break;
+      case 2: fwd_launch<D, false, 2>(a, d, st); break;
+      case 3: fwd_launch<D, true, 0>(a, d, st); break;
+      case 4: fwd_launch<D, true, 1>(a, d, st); break;
+      default: fwd_launch<D, true, 2>(a, d, st);
+    }
+  };
+  if (d.d == 64) run(std::integral_constant<int, 64>());
+  else run(std::integral_constant<int, 128>());
+  return hip_launch_status();
+}
+
+int launch_attn_biased_bwd(const AttnBiasedDesc& b, hipStream_t st) {
+  const AttnFusedDesc& d = b.base;
+  if (!desc_ok(b) || !d.qkv || !d.attn || !d.lse || !d.d_attn || !d.d_qkv || !d.delta) return OPTIMUS_ESHAPE;
+  const BiasedArgs a = make_args(b);
+  launch_attn_biased_prepare(a, d.d, true, d.nb * d.nh, d.ndev, st);
+  return launch_attn_biased_bwd_kernels(a, b, st);
+}
+
+}  // namespace optimus

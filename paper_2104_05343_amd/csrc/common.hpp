@@ -189,6 +189,24 @@ bool attn_fused_supported(int d);
 int launch_attn_fused_fwd(const AttnFusedDesc& d, hipStream_t stream);
 int launch_attn_fused_bwd(const AttnFusedDesc& d, hipStream_t stream);
 
+// The same with changed scores (attention_biased_kernel.hpp).
+struct AttnBiasedDesc {
+  AttnFusedDesc base;
+  int q, dev0;              // grid, first device of the launch
+  float cap;                // 0: none
+  const float* slopes;      // [heads of the grid], or nullptr
+  const float* table;       // [heads of the grid][buckets], or nullptr
+  int buckets, two_sided;
+  unsigned short first[129];   // first distance of each bucket of a side, then a distance that is never reached
+  const int* documents;     // [sequences of the grid][s], or nullptr
+  const int* prefix;        // [sequences of the grid], or nullptr
+  void* blocks;             // scratch with documents: 16 bytes per 64 tokens of every sequence of the grid
+  float* table_parts;       // scratch with d_table: attn_biased_parts(...) floats
+  float* d_table;           // backward: [device][heads of a device][buckets] of the launch's devices, or nullptr
+};
+int launch_attn_biased_fwd(const AttnBiasedDesc& d, hipStream_t stream);
+int launch_attn_biased_bwd(const AttnBiasedDesc& d, hipStream_t stream);
+
 // Attention that keeps the probabilities, head widths 64 and 128 (attention_probs.hip): nmat matrices of consecutive sequences,
 // nh heads each.
 struct AttnProbsDesc {

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
   bf16x8 qf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) qf[ks] = zero_if(qdoc < 0, *(const bf16x8*)(Qp + (long long)qrow * f.ld + ks * 16 + g * 8));
-  const Bias<BIAS> bias = make_bias<BIAS>(a, m.ghead, bias_lds);
+  const Bias bias = make_bias<BIAS>(a, m.ghead, bias_lds);
 
   const int wg_hi = min(tile * BQ + BQ, s) - 1;   // last query row of the workgroup
   int kb_lo = 0, kb_hi = a.causal ? max(wg_hi, m.prefix - 1) / BLK + 1 : a.nblk;
@@ -46,6 +46,7 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
   for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
   float m_run = -INFINITY, l_run = 0.f;
 
+  const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane);
   RowLoader<D, 2 * NRG, PAIR> ldr;
   ldr.init(f.ld, wave, lane);
   // documents of a pair's blocks, known an iteration before they are used
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
   };
   Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
   if (it_lo < n_it) {
-    if (m.docs) key_docs[wave][lane] = m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)];
+    key_docs[wave][lane] = m.docs ? m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)] : 0;
     issue(it_lo, 0, cur);
   }
   wait_loads_and_barrier();
@@ -84,58 +85,49 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
     const i32x4_t blk = par ? cur.odd : cur.even;
     const bool shared = !m.docs || share_documents(blk, own);
     if (kb >= kb_lo && kb < kb_hi && kbase <= wave_last && shared) {
-      const bf16_t* tK = lds[st][0] + par * BLK * D;
-      const bf16_t* tV = lds[st][1] + par * BLK * D;
+      const unsigned stage = (unsigned)((st * 2 * PAIR + par * BLK) * D * 2);
+      const unsigned kt = in_rows + stage, vt = in_cols + stage;
       f32x16 sacc[2];
       sacc[0] = zero16();
       sacc[1] = zero16();
-      pipelined<2 * KS, AHEAD>([&](int n) { return frag_rows<D>(tK, n / KS * 32, n % KS, lane); },
+      pipelined<2 * KS, AHEAD>([&](int n) { return rows_at<D>(kt, n / KS * 32, n % KS); },
                                [&](int n, const bf16x8& x) {
                                  sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
                                });
-#pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        if (CAP) tanh16(sacc[t2], a);
-        const int k0 = kbase + t2 * 32;
-        scores16<CAP, BIAS, -1>(sacc[t2], a, bias, tile_bias<BIAS>(bias, query - k0 - 4 * g, q0 - k0 - 31, q0 - k0 + 31));
+      if (CAP) {
+        tanh16(sacc[0], a);
+        tanh16(sacc[1], a);
       }
-      // keys past a row's limit, and those past the end, exist only in the last blocks (wave-uniform tests)
-      if (a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) {
+      const int dist0 = query - kbase - 4 * g, lo = q0 - kbase - (BLK - 1), hi = q0 + 31 - kbase;
+      float w = 1.0f, c = 0.f;
+      // pairs to leave out exist only in the last blocks and where documents meet (wave-uniform tests)
+      if ((a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) || (m.docs && !one_document(blk, own)) || !plain_tile<BIAS>(bias, lo, hi)) {
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (kbase + t2 * 32 + slot(r) + 4 * g > limit) sacc[t2][r] = -INFINITY;
-      }
-      if (m.docs && !one_document(blk, own)) {
-#pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int4 kd = *(const int4*)&key_docs[wave][t2 * 32 + 8 * c + 4 * g];
-            const int k4[4] = {kd.x, kd.y, kd.z, kd.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (k4[e] != qdoc || qdoc < 0) sacc[t2][4 * c + e] = -INFINITY;
-          }
+          any16<CAP, BIAS, -1>(sacc[t2], a, bias, dist0 - 32 * t2, kbase + 32 * t2 + 4 * g, limit, &key_docs[wave][32 * t2 + 4 * g], qdoc);
+      } else {
+        plain_weights<CAP, BIAS>(a, bias, lo, w, c);
+        plain16<CAP, BIAS, -1>(sacc[0], a, bias, dist0, lo);
+        plain16<CAP, BIAS, -1>(sacc[1], a, bias, dist0 - 32, lo);
       }
       float mx = -INFINITY;
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
-      mx = halfwave_max(mx);
+      mx = fmaf(halfwave_max(mx), w, c);   // (w is positive: it commutes with the maximum)
       // The running maximum follows the block's only when that is more than 2^8 above it (see the attention without changes).  A row
       // that has met no key yet keeps -infinity, and 0 in its place where it is subtracted: its terms are exp2(-infinity) = 0.
       const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
       const float m_new = move ? fmaxf(m_run, mx) : m_run;
       const float m_sub = m_new == -INFINITY ? 0.f : m_new;
+      const float off = c - m_sub;
       float sum = 0.f;
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(sacc[t2][r] - m_sub);
+          const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], w, off));
           sacc[t2][r] = p;
           sum += p;
         }
@@ -156,7 +148,7 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
         pf[t2][0] = pack_acc<0>(sacc[t2]);
         pf[t2][1] = pack_acc<1>(sacc[t2]);
       }
-      pipelined<4 * DT, AHEAD>([&](int n) { return frag_cols_acc_order<D>(tV, n / DT * 16, n % DT * 32, lane); },
+      pipelined<4 * DT, AHEAD>([&](int n) { return cols_at<D>(vt, PAIR + n / DT * 16, n % DT); },
                                [&](int n, const bf16x8& x) {
                                  oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[n / (2 * DT)][n / DT & 1], oacc[n % DT], 0, 0, 0);
                                });

@@ -82,7 +82,7 @@ template <int D, int NRG, int BIAS>
 struct DqLds {
   bf16_t tile[2][2][PAIR * D];   // [stage][K, V]
   BiasLds<BIAS> bias;
-  int key_docs[2 * NRG][BLK];
+  alignas(16) int key_docs[2 * NRG][BLK];   // (read sixteen bytes at a time)
   float diag[BIAS == 2 ? 2 * NRG : 1][128];
   int live[2];
 };
@@ -90,8 +90,9 @@ template <int D, int NRG, int BIAS>
 struct DkvLds {
   bf16_t tile[2][2][PAIR * D];   // [stage][Q, dO]
   BiasLds<BIAS> bias;
-  float l[2][PAIR], d[2][PAIR];
-  int docs[2][PAIR];
+  alignas(16) float l[2][PAIR];   // (read sixteen bytes at a time, as the next two)
+  alignas(16) float d[2][PAIR];
+  alignas(16) int docs[2][PAIR];
   int live[2];
 };
 
@@ -122,7 +123,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   }
   const float delta = f.delta[m.vec + qrow];
   const float lse2 = query < s && qdoc >= 0 ? lse2_of(f.lse[m.vec + qrow]) : INFINITY;
-  const Bias<BIAS> bias = make_bias<BIAS>(a, m.ghead, lds.bias);
+  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
   BucketSums sums;
   const bool table_grad = BIAS == 2 && a.table_parts;
   if (BIAS == 2) sums.init(a, lds.diag[wave], lds.bias.first, lane);
@@ -140,6 +141,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt] = zero16();
 
+  const unsigned in_rows = lds_address(lds.tile) + lane_rows<D>(lane), in_cols = lds_address(lds.tile) + lane_cols<D>(lane);
   RowLoader<D, 2 * NRG, PAIR> ldr;
   ldr.init(f.ld, wave, lane);
   struct Pair { i32x4_t even, odd; };
@@ -158,7 +160,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   };
   Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
   if (it_lo < n_it) {
-    if (m.docs) lds.key_docs[wave][lane] = m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)];
+    lds.key_docs[wave][lane] = m.docs ? m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)] : 0;
     issue(it_lo, 0, cur);
   }
   wait_loads_and_barrier();
@@ -177,55 +179,50 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
     const i32x4_t blk = par ? cur.odd : cur.even;
     const bool shared = !m.docs || share_documents(blk, own);
     if (kb >= kb_lo && kb < kb_hi && kbase <= wave_last && shared) {
-      const bf16_t* tK = lds.tile[st][0] + par * BLK * D;
-      const bf16_t* tV = lds.tile[st][1] + par * BLK * D;
-      const bool need_limit = a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s;
-      const bool need_docs = m.docs && !one_document(blk, own);
+      const unsigned stage = (unsigned)((st * 2 * PAIR + par * BLK) * D * 2);
+      const unsigned kt = in_rows + stage, kc = in_cols + stage;
+      const bool masked = (a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) || (m.docs && !one_document(blk, own));
       bf16x8 dsf[2][2];
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2) {
         f32x16 sacc = zero16(), pacc = zero16();
-        pipelined<2 * KS, 2>([&](int n) { return frag_rows<D>(n & 1 ? tV : tK, t2 * 32, n / 2, lane); },
+        pipelined<2 * KS, 2>([&](int n) { return rows_at<D>(kt, (n & 1 ? PAIR : 0) + t2 * 32, n / 2); },
                             [&](int n, const bf16x8& x) {
                               f32x16& acc = n & 1 ? pacc : sacc;
                               acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dof[n / 2] : qf[n / 2], acc, 0, 0, 0);
                             });
         const int k0 = kbase + t2 * 32, dist0 = query - k0 - 4 * g;
-        f32x16 th;
-        if (CAP) {
-          tanh16(sacc, a);
-          th = sacc;
-        }
-        scores16<CAP, BIAS, -1>(sacc, a, bias, tile_bias<BIAS>(bias, dist0, q0 - k0 - 31, q0 - k0 + 31));
+        // the table's gradient wants dS before the tanh's part: that waits in `part` then; else it goes into dP first
+        f32x16 part;
+        if (CAP) tanh16(sacc, a);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(sacc[r] - lse2);
-          sacc[r] = p * (pacc[r] - delta);  // dS^T
+          pacc[r] -= delta;
+          if (CAP && BIAS != 2) pacc[r] *= fmaf(-sacc[r], sacc[r], 1.0f);
+          if (CAP && BIAS == 2) part[r] = fmaf(-sacc[r], sacc[r], 1.0f);
         }
-        if (need_limit) {
+        const int lo = q0 - k0 - 31;
+        if (masked || !plain_tile<BIAS>(bias, lo, lo + 62)) {
+          any16<CAP, BIAS, -1>(sacc, a, bias, dist0, k0 + 4 * g, limit, &lds.key_docs[wave][t2 * 32 + 4 * g], qdoc);
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (k0 + slot(r) + 4 * g > limit) sacc[r] = 0.f;
-        }
-        if (need_docs) {
+          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(sacc[r] - lse2) * pacc[r];  // dS^T
+        } else {
+          float w, c;
+          plain_weights<CAP, BIAS>(a, bias, lo, w, c);
+          plain16<CAP, BIAS, -1>(sacc, a, bias, dist0, lo);
+          c -= lse2;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int4 kd = *(const int4*)&lds.key_docs[wave][t2 * 32 + 8 * c + 4 * g];
-            const int k4[4] = {kd.x, kd.y, kd.z, kd.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (k4[e] != qdoc || qdoc < 0) sacc[4 * c + e] = 0.f;
-          }
+          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], w, c)) * pacc[r];
         }
         if (BIAS == 2 && table_grad) sums.add(sacc, q0 - k0 - 31, (lane & 31) + 31 - 4 * g, g, lane, a.buckets > 64);
-        if (CAP) {
+        if (CAP && BIAS == 2) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[r] *= fmaf(-th[r], th[r], 1.0f);
+          for (int r = 0; r < 16; ++r) sacc[r] *= part[r];
         }
         dsf[t2][0] = pack_acc<0>(sacc);
         dsf[t2][1] = pack_acc<1>(sacc);
       }
-      pipelined<4 * DT, 2>([&](int n) { return frag_cols_acc_order<D>(tK, n / DT * 16, n % DT * 32, lane); },
+      pipelined<4 * DT, 2>([&](int n) { return cols_at<D>(kc, n / DT * 16, n % DT); },
                           [&](int n, const bf16x8& x) {
                             const int dt = n % DT;
                             dqacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, dsf[n / (2 * DT)][n / DT & 1], dqacc[dt], 0, 0, 0);
@@ -271,43 +268,41 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
 }
 
 // 32 x 32 scores S (rows: queries q0 .., columns: keys) and dP = dO V^T in accumulators -> P and dS (the gradient of Q K^T) in their place.
-// l, d, docs: of the 32 queries.
+// l, d, docs: of the 32 queries.  (dP - rowsum) (1 - tanh^2) comes before the scores, so that the tanh needs no place of its own.
+// first: query from which on the key is seen.
 template <bool CAP, int BIAS>
 __device__ __forceinline__ void biased_dkv_scores(f32x16& sacc, f32x16& pacc, const float* l, const float* d, const int* docs, int q0, int k0, int key,
-                                                  int kdoc, bool need_limit, bool need_docs, int prefix, const BiasedArgs& a, const Bias<BIAS>& bias,
-                                                  int g) {
-  f32x16 th;
-  if (CAP) {
-    tanh16(sacc, a);
-    th = sacc;
-  }
-  scores16<CAP, BIAS, 1>(sacc, a, bias, tile_bias<BIAS>(bias, q0 + 4 * g - key, q0 - k0 - 31, q0 - k0 + 31));
+                                                  int first, int kdoc, bool masked, const BiasedArgs& a, const Bias& bias, int g) {
+  if (CAP) tanh16(sacc, a);
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const int qi = 8 * c + 4 * g;
-    const float4 l4 = *(const float4*)(l + qi);
-    const float4 d4 = *(const float4*)(d + qi);
-    const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+    const float4 d4 = *(const float4*)(d + 8 * c + 4 * g);
+    const float dv[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 4 * c + e;
-      float p = __builtin_amdgcn_exp2f(sacc[r] - lv[e]);   // (of a row without pairs, and past the end: 0)
-      if (need_limit && q0 + qi + e < key && key >= prefix) p = 0.f;
+      pacc[r] -= dv[e];
+      if (CAP) pacc[r] *= fmaf(-sacc[r], sacc[r], 1.0f);
+    }
+  }
+  const int lo = q0 - k0 - 31, dist0 = q0 + 4 * g - key;
+  float w = 1.0f, c0 = 0.f;
+  if (masked || !plain_tile<BIAS>(bias, lo, lo + 62)) {
+    any16<CAP, BIAS, 1>(sacc, a, bias, dist0, q0 + 4 * g, first, docs + 4 * g, kdoc);
+  } else {
+    plain_weights<CAP, BIAS>(a, bias, lo, w, c0);
+    plain16<CAP, BIAS, 1>(sacc, a, bias, dist0, lo);
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const float4 l4 = *(const float4*)(l + 8 * c + 4 * g);
+    const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * c + e;
+      const float p = __builtin_amdgcn_exp2f(fmaf(sacc[r], w, BIAS == 2 ? c0 - lv[e] : -lv[e]));   // (of a row without pairs, and past the end: 0)
       sacc[r] = p;
-    }
-    if (need_docs) {
-      const int4 o4 = *(const int4*)(docs + qi);
-      const int ov[4] = {o4.x, o4.y, o4.z, o4.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (ov[e] != kdoc || kdoc < 0) sacc[4 * c + e] = 0.f;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = 4 * c + e;
-      float ds = sacc[r] * (pacc[r] - dv[e]);
-      if (CAP) ds *= fmaf(-th[r], th[r], 1.0f);
-      pacc[r] = ds;
+      pacc[r] *= p;
     }
   }
 }
@@ -331,13 +326,14 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   const int key = k0 + (lane & 31);
   const int krow = min(key, s - 1);
   const int kdoc = m.docs ? m.docs[krow] : 0;
+  const int first = a.causal && key >= m.prefix ? key : 0;   // query from which on the key is seen
   bf16x8 kf[KS], vf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     kf[ks] = zero_if(kdoc < 0, *(const bf16x8*)(Kp + (long long)krow * f.ld + ks * 16 + g * 8));
     vf[ks] = zero_if(kdoc < 0, *(const bf16x8*)(Vp + (long long)krow * f.ld + ks * 16 + g * 8));
   }
-  const Bias<BIAS> bias = make_bias<BIAS>(a, m.ghead, lds.bias);
+  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
   // the first block with a query that sees the workgroup's first key
   int qb_lo = a.causal && kt0 >= m.prefix ? kt0 / BLK : 0, qb_hi = a.nblk;
   if (m.docs) live_blocks(m.blocks, kt0 / BLK, (min(kt0 + BKW, s) - 1) / BLK, qb_lo, qb_hi, lds.live);
@@ -351,6 +347,7 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
     dkacc[dt] = zero16();
     dvacc[dt] = zero16();
   }
+  const unsigned in_rows = lds_address(lds.tile) + lane_rows<D>(lane), in_cols = lds_address(lds.tile) + lane_cols<D>(lane);
   RowLoader<D, 2 * NRG, PAIR> ldq, ldg;
   ldq.init(f.ld, wave, lane);
   ldg.init(f.ldo, wave, lane);
@@ -366,18 +363,18 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   // the queries' numbers go through registers and reach LDS at the end of an iteration: stored at its top, they would wait for their
   // loads and for the tiles requested before them
   float next_l = 0.f, next_d = 0.f;
-  int next_doc = -1;
+  int next_doc = 0;
   auto load_rows = [&](int it) {
     if (tid < PAIR) {
-      const int row = it * PAIR + tid, at = min(row, s - 1);
-      next_doc = m.docs ? m.docs[at] : 0;
-      next_l = row < s ? Lp[at] : -INFINITY;
+      const int at = min(it * PAIR + tid, s - 1);
+      if (m.docs) next_doc = m.docs[at];
+      next_l = Lp[at];
       next_d = Dp[at];
     }
   };
-  auto store_rows = [&](int st) {
+  auto store_rows = [&](int it, int st) {   // (past the end as padding)
     if (tid < PAIR) {
-      lds.l[st][tid] = next_doc < 0 ? INFINITY : lse2_of(next_l);
+      lds.l[st][tid] = next_doc < 0 || it * PAIR + tid >= s ? INFINITY : lse2_of(next_l);
       lds.d[st][tid] = next_d;
       lds.docs[st][tid] = next_doc;
     }
@@ -390,7 +387,7 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
   if (it_lo < n_it) {
     load_rows(it_lo);
-    store_rows(0);
+    store_rows(it_lo, 0);
     issue(it_lo, 0, cur);
   }
   wait_loads_and_barrier();
@@ -406,41 +403,35 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
     const i32x4_t blk = par ? cur.odd : cur.even;
     const bool shared = !m.docs || share_documents(blk, own);
     if (k0 < s && qb >= qb_lo && qb < qb_hi && (!a.causal || qbase + BLK - 1 >= k0 || k0 < m.prefix) && shared) {
-      const bf16_t* tQ = lds.tile[st][0] + par * BLK * D;
-      const bf16_t* tG = lds.tile[st][1] + par * BLK * D;
-      f32x16 sacc[2], pacc[2];
-#pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        sacc[t2] = zero16();
-        pacc[t2] = zero16();
-      }
-      pipelined<4 * KS, 2>([&](int n) { return frag_rows<D>(n & 1 ? tG : tQ, n / (2 * KS) * 32, n / 2 % KS, lane); },
-                          [&](int n, const bf16x8& x) {
-                            const int t2 = n / (2 * KS), ks = n / 2 % KS;
-                            f32x16& acc = n & 1 ? pacc[t2] : sacc[t2];
-                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? vf[ks] : kf[ks], acc, 0, 0, 0);
-                          });
-      const bool need_limit = a.causal && qbase < k0 + 31 && k0 + 31 >= m.prefix;
-      const bool need_docs = m.docs && !one_document(blk, own);
+      const unsigned stage = (unsigned)((st * 2 * PAIR + par * BLK) * D * 2);
+      const unsigned qt = in_rows + stage, qc = in_cols + stage;
+      const bool masked = (a.causal && qbase < k0 + 31 && k0 + 31 >= m.prefix) || (m.docs && !one_document(blk, own));
       bf16x8 pf[2][2], dsf[2][2];
+      // 32 queries at a time: with the scores of all 64 live, fragments on their way have no registers
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2) {
+        f32x16 sacc = zero16(), pacc = zero16();
+        pipelined<2 * KS, 2>([&](int n) { return rows_at<D>(qt, (n & 1 ? PAIR : 0) + t2 * 32, n / 2); },
+                            [&](int n, const bf16x8& x) {
+                              f32x16& acc = n & 1 ? pacc : sacc;
+                              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? vf[n / 2] : kf[n / 2], acc, 0, 0, 0);
+                            });
         const int at = par * BLK + t2 * 32;
-        biased_dkv_scores<CAP, BIAS>(sacc[t2], pacc[t2], lds.l[st] + at, lds.d[st] + at, lds.docs[st] + at, qbase + t2 * 32, k0, key, kdoc, need_limit,
-                                     need_docs, m.prefix, a, bias, g);
-        pf[t2][0] = pack_acc<0>(sacc[t2]);
-        pf[t2][1] = pack_acc<1>(sacc[t2]);
-        dsf[t2][0] = pack_acc<0>(pacc[t2]);
-        dsf[t2][1] = pack_acc<1>(pacc[t2]);
+        biased_dkv_scores<CAP, BIAS>(sacc, pacc, lds.l[st] + at, lds.d[st] + at, lds.docs[st] + at, qbase + t2 * 32, k0, key, first, kdoc,
+                                     masked, a, bias, g);
+        pf[t2][0] = pack_acc<0>(sacc);
+        pf[t2][1] = pack_acc<1>(sacc);
+        dsf[t2][0] = pack_acc<0>(pacc);
+        dsf[t2][1] = pack_acc<1>(pacc);
       }
-      pipelined<8 * DT, 2>([&](int n) { return frag_cols_acc_order<D>(n & 1 ? tQ : tG, n / (2 * DT) * 16, n / 2 % DT * 32, lane); },
+      pipelined<8 * DT, 2>([&](int n) { return cols_at<D>(qc, (n & 1 ? 0 : PAIR) + n / (2 * DT) * 16, n / 2 % DT); },
                           [&](int n, const bf16x8& x) {
                             const int dt = n / 2 % DT, t2 = n / (4 * DT), u = n / (2 * DT) & 1;
                             f32x16& acc = n & 1 ? dkacc[dt] : dvacc[dt];
                             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dsf[t2][u] : pf[t2][u], acc, 0, 0, 0);
                           });
     }
-    if (it + 1 < n_it) store_rows(st ^ 1);
+    if (it + 1 < n_it) store_rows(it + 1, st ^ 1);
     cur = next;
     next = after;
     wait_loads_and_barrier();
@@ -477,6 +468,166 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   }
 }
 
+// Head width 128, 128 keys per workgroup, eight wavefronts: as without changes, the own V rows and half of the K fragments stay in
+// LDS, blocks come one at a time, a wavefront takes one 32-query half (par) of every block.
+template <int BIAS>
+struct WideDkvLds {
+  bf16_t block[2][2][BLK * 128];   // [stage][Q, dO]
+  bf16_t v[128 * 128], k[128 * 128];
+  BiasLds<BIAS> bias;
+  alignas(16) float l[2][BLK];
+  alignas(16) float d[2][BLK];
+  alignas(16) int docs[2][BLK];
+  int live[2];
+};
+template <bool CAP, int BIAS>
+__device__ __forceinline__ void biased_dkv_wide_body(const BiasedArgs& a, WideDkvLds<BIAS>& lds, int tile, int mat, int dev) {
+  constexpr int D = 128, KS = D / 16, DT = D / 32, BKW = 128, KREG = KS / 2;   // KREG: K fragments kept in registers
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave & 3, par = wave >> 2;
+  const int s = f.s;
+  const Matrix m = matrix_of<D>(a, mat, dev);
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const bf16_t* Kp = Qp + D;
+  const bf16_t* Gp = f.d_attn + m.attn;
+  const float* Lp = f.lse + m.vec;
+  const float* Dp = f.delta + m.vec;
+  const int kt0 = tile * BKW, k0 = kt0 + rg * 32;
+  const int key = k0 + (lane & 31);
+  const int krow = min(key, s - 1);
+  const int kdoc = m.docs ? m.docs[krow] : 0;
+  const int first = a.causal && key >= m.prefix ? key : 0;   // query from which on the key is seen
+  bf16x8 kf[KREG];
+#pragma unroll
+  for (int ks = 0; ks < KREG; ++ks) kf[ks] = zero_if(kdoc < 0, *(const bf16x8*)(Kp + (long long)krow * f.ld + ks * 16 + g * 8));
+  const int last_blk = (min(kt0 + BKW, s) - 1) / BLK;
+  {
+    const int* docs = m.docs && m.blocks[kt0 / BLK].z | m.blocks[last_blk].z ? m.docs : nullptr;
+    RowLoader<D, 8, BKW> own;
+    own.init(f.ld, wave, lane);
+    own.issue(Qp + 2 * D, kt0, s, lds.v, docs);
+    own.issue(Kp, kt0, s, lds.k, docs);
+  }
+  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
+  int qb_lo = a.causal && kt0 >= m.prefix ? kt0 / BLK : 0, qb_hi = a.nblk;
+  if (m.docs) live_blocks(m.blocks, kt0 / BLK, last_blk, qb_lo, qb_hi, lds.live);
+  const i32x4_t none = {0x7fffffff, -1, 0, 0};
+  const i32x4_t own_docs = m.docs && k0 < s ? m.blocks[k0 / BLK] : none;
+
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    dkacc[dt] = zero16();
+    dvacc[dt] = zero16();
+  }
+  // (a wavefront's 32 rows of a block, and its own 32 rows of V and K)
+  const unsigned in_rows = lds_address(lds.block) + lane_rows<D>(lane) + par * 32 * D * 2, in_cols = lds_address(lds.block) + lane_cols<D>(lane) + par * 32 * D * 2;
+  const unsigned own_rows = lds_address(lds.v) + lane_rows<D>(lane) + rg * 32 * D * 2;
+  RowLoader<D, 8, BLK> ldq, ldg;
+  ldq.init(f.ld, wave, lane);
+  ldg.init(f.ldo, wave, lane);
+  auto block_of = [&](int qb) { return m.docs && qb < a.nblk ? (i32x4_t)m.blocks[qb] : none; };
+  float next_l = 0.f, next_d = 0.f;
+  int next_doc = 0;
+  auto load_block = [&](int qb, int st, i32x4_t blk) {
+    if (tid < BLK) {
+      const int at = min(qb * BLK + tid, s - 1);
+      if (m.docs) next_doc = m.docs[at];
+      next_l = Lp[at];
+      next_d = Dp[at];
+    }
+    const int* docs = blk.z ? m.docs : nullptr;
+    ldq.issue(Qp, qb * BLK, s, lds.block[st][0], docs);
+    ldg.issue(Gp, qb * BLK, s, lds.block[st][1], docs);
+  };
+  auto store_rows = [&](int qb, int st) {   // (past the end as padding)
+    if (tid < BLK) {
+      lds.l[st][tid] = next_doc < 0 || qb * BLK + tid >= s ? INFINITY : lse2_of(next_l);
+      lds.d[st][tid] = next_d;
+      lds.docs[st][tid] = next_doc;
+    }
+  };
+  i32x4_t cur = block_of(qb_lo), next = block_of(qb_lo + 1);
+  if (qb_lo < qb_hi) {
+    load_block(qb_lo, 0, cur);
+    store_rows(qb_lo, 0);
+  }
+  wait_loads_and_barrier();
+  for (int qb = qb_lo; qb < qb_hi; ++qb) {
+    const int st = (qb - qb_lo) & 1;
+    i32x4_t after = next;
+    if (qb + 1 < qb_hi) {
+      after = block_of(qb + 2);
+      load_block(qb + 1, st ^ 1, next);
+    }
+    const int q0 = qb * BLK + par * 32;   // this wavefront's queries
+    if (k0 < s && q0 < s && (!a.causal || q0 + 31 >= k0 || k0 < m.prefix) && (!m.docs || share_documents(cur, own_docs))) {
+      const unsigned stage = (unsigned)(st * 2 * BLK * D * 2);
+      const unsigned qt = in_rows + stage, qc = in_cols + stage;
+      f32x16 sacc = zero16(), pacc = zero16();
+      struct Two { bf16x8 q, own; };
+      pipelined<2 * KS, 2>([&](int n) {
+                            const int ks = n / 2;
+                            Two x;
+                            x.q = rows_at<D>(qt, n & 1 ? BLK : 0, ks);
+                            if (n & 1) x.own = rows_at<D>(own_rows, 0, ks);
+                            else x.own = ks < KREG ? kf[ks < KREG ? ks : 0] : rows_at<D>(own_rows, BKW, ks);
+                            return x;
+                          },
+                          [&](int n, const Two& x) {
+                            f32x16& acc = n & 1 ? pacc : sacc;
+                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.q, x.own, acc, 0, 0, 0);
+                          });
+      biased_dkv_scores<CAP, BIAS>(sacc, pacc, lds.l[st] + par * 32, lds.d[st] + par * 32, lds.docs[st] + par * 32, q0, k0, key, first, kdoc,
+                                   (a.causal && q0 < k0 + 31 && k0 + 31 >= m.prefix) || (m.docs && !one_document(cur, own_docs)), a, bias, g);
+      const bf16x8 pf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)}, dsf[2] = {pack_acc<0>(pacc), pack_acc<1>(pacc)};
+      pipelined<4 * DT, 2>([&](int n) { return cols_at<D>(qc, (n & 1 ? 0 : BLK) + n / (2 * DT) * 16, n / 2 % DT); },
+                          [&](int n, const bf16x8& x) {
+                            const int dt = n / 2 % DT, u = n / (2 * DT);
+                            f32x16& acc = n & 1 ? dkacc[dt] : dvacc[dt];
+                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dsf[u] : pf[u], acc, 0, 0, 0);
+                          });
+    }
+    if (qb + 1 < qb_hi) store_rows(qb + 1, st ^ 1);
+    cur = next;
+    next = after;
+    wait_loads_and_barrier();
+  }
+  // merge the two halves' sums, dV first: the odd one hands over through LDS (64 KiB, all block tiles are free)
+  float* xch = (float*)&lds.block[0][0][0] + rg * (DT * 16) * 64;
+  bf16_t* dKp = f.d_qkv + m.qkv + (long long)key * f.ld + D;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    f32x16 (&acc)[DT] = which == 0 ? dvacc : dkacc;
+    if (which == 1) __syncthreads();
+    if (par == 1) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) xch[(dt * 16 + r) * 64 + lane] = acc[dt][r];
+    }
+    __syncthreads();
+    if (par == 0 && key < s) {
+      const float w = which == 0 ? 1.0f : f.scale;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = (acc[dt][4 * c + e] + xch[(dt * 16 + 4 * c + e) * 64 + lane]) * w;
+          u32x2 x = {pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])};
+          *(u32x2*)(dKp + (which == 0 ? D : 0) + dt * 32 + 8 * c + 4 * g) = x;
+        }
+    }
+  }
+}
+
+template <size_t A, size_t B>
+constexpr size_t larger() { return A > B ? A : B; }
+
 // Both kinds in one grid ordered by loop length, longest first, the kinds alternating: x = (rank, matrix, kind), y = device.
 template <int D, bool CAP, int BIAS>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_biased_bwd_kernel(BiasedArgs a, int ntiles, int nmat) {
@@ -487,6 +638,21 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_biased_bwd_kernel(B
   const int mat = (int)(rem >> 1), dev = (int)blockIdx.y;
   if (rem & 1) biased_dq_body<D, 2, CAP, BIAS>(a, *(DqLds<D, 2, BIAS>*)lds, ntiles - 1 - (int)rank, mat, dev);
   else biased_dkv_body<D, 2, CAP, BIAS>(a, *(DkvLds<D, 2, BIAS>*)lds, (int)rank, mat, dev);
+}
+
+// The same in workgroups of eight wavefronts and 128 rows: x = (matrix, kind), y = rank, z = device.
+template <int D, bool CAP, int BIAS>
+__global__ __launch_bounds__(512, 2) void attn_biased_bwd_wide_kernel(BiasedArgs a) {
+  const int rank = blockIdx.y, mat = blockIdx.x >> 1, kind = blockIdx.x & 1, ntiles = gridDim.y, dev = blockIdx.z;
+  if constexpr (D == 128) {
+    __shared__ __attribute__((aligned(1024))) char lds[larger<sizeof(WideDkvLds<BIAS>), sizeof(DqLds<D, 4, BIAS>)>()];
+    if (kind) biased_dq_body<D, 4, CAP, BIAS>(a, *(DqLds<D, 4, BIAS>*)lds, ntiles - 1 - rank, mat, dev);
+    else biased_dkv_wide_body<CAP, BIAS>(a, *(WideDkvLds<BIAS>*)lds, rank, mat, dev);
+  } else {
+    __shared__ __attribute__((aligned(1024))) char lds[larger<sizeof(DkvLds<D, 4, BIAS>), sizeof(DqLds<D, 4, BIAS>)>()];
+    if (kind) biased_dq_body<D, 4, CAP, BIAS>(a, *(DqLds<D, 4, BIAS>*)lds, ntiles - 1 - rank, mat, dev);
+    else biased_dkv_body<D, 4, CAP, BIAS>(a, *(DkvLds<D, 4, BIAS>*)lds, rank, mat, dev);
+  }
 }
 
 // d_table[device][head][bucket]: the parts of the head's matrices and tiles, added in that order by 1024 / 128 threads a bucket, then
@@ -510,10 +676,15 @@ __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, f
   }
 }
 
+// 128-row workgroups from one per compute unit on.  The two forms add dK and dV (width 128) and the table's gradient up in different
+// orders, so the choice follows one device's matrices, whatever the launch covers.
+bool wide_form(const AttnFusedDesc& d) { return 2ll * ((d.s + 127) / 128) * d.nb * d.nh >= 256; }
+
 template <int D, bool CAP, int BIAS>
 void bwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
-  const int ntiles = (d.s + BLK - 1) / BLK, nmat = d.nb * d.nh;
-  attn_biased_bwd_kernel<D, CAP, BIAS><<<dim3((unsigned)(2ll * ntiles * nmat), d.ndev), 256, 0, st>>>(a, ntiles, nmat);
+  const int nmat = d.nb * d.nh;
+  if (wide_form(d)) attn_biased_bwd_wide_kernel<D, CAP, BIAS><<<dim3(2 * nmat, a.ntiles, d.ndev), 512, 0, st>>>(a);
+  else attn_biased_bwd_kernel<D, CAP, BIAS><<<dim3((unsigned)(2ll * a.ntiles * nmat), d.ndev), 256, 0, st>>>(a, a.ntiles, nmat);
 }
 
 }  // namespace
@@ -521,7 +692,7 @@ void bwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
 int launch_attn_biased_bwd_kernels(const BiasedArgs& given, const AttnBiasedDesc& b, hipStream_t st) {
   const AttnFusedDesc& d = b.base;
   BiasedArgs a = given;
-  a.ntiles = (d.s + BLK - 1) / BLK;
+  a.ntiles = wide_form(d) ? (d.s + 127) / 128 : (d.s + BLK - 1) / BLK;
   a.table_parts = b.d_table ? b.table_parts : nullptr;
   const int kind = (b.cap > 0 ? 3 : 0) + (b.table ? 2 : b.slopes ? 1 : 0);
   auto run = [&](auto width) {

@@ -17,7 +17,7 @@
 
 namespace optimus {
 
-constexpr int kMaxBuckets = 128, kMaxDistance = 1024, kTableMargin = 64;
+constexpr int kMaxBuckets = 128, kMaxDistance = 1024;
 
 typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 // read through the scalar cache: the same address in every lane, written by an earlier kernel
@@ -128,6 +128,36 @@ __device__ __forceinline__ bf16x8 zero_if(bool z, bf16x8 v) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// ---- fragments by byte addresses in LDS ----
+// A lane's place in a tile is one number; the swizzle makes the step along a row (16 contraction elements, 32 columns) an exclusive or
+// with a constant, since tiles are aligned to their rows, and whole groups of 16 rows an offset in the instruction.  One register a
+// tile then: kept apart, the places of a block's fragments are 16 to 24 registers, and were spilled.
+template <int D>
+__device__ __forceinline__ unsigned lane_rows(int lane) {
+  const int row = lane & 31;
+  return (unsigned)(row * D * 2 + (((lane >> 5) ^ swz<D>(row)) << 4));
+}
+template <int D>
+__device__ __forceinline__ unsigned lane_cols(int lane) {
+  const int lg = lane & 15, col = (((lane >> 4) & 1) << 4) + ((lg & 3) << 2), row = ((lane >> 5) << 2) + (lg >> 2);
+  return (unsigned)((row * D + (((col >> 3) ^ swz<D>(row)) << 3) + (col & 7)) * 2);
+}
+__device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p; }
+// at: address of the tile plus lane_rows; fragment frag_rows<D>(tile, row0, ks, lane)
+template <int D>
+__device__ __forceinline__ bf16x8 rows_at(unsigned at, int row0, int ks) {
+  return *(__attribute__((address_space(3))) const bf16x8*)(size_t)((at ^ (unsigned)(ks * 32)) + (unsigned)(row0 * D * 2));
+}
+// at: address of the tile plus lane_cols; fragment frag_cols_acc_order<D>(tile, row0, 32 * dt, lane)
+template <int D>
+__device__ __forceinline__ bf16x8 cols_at(unsigned at, int row0, int dt) {
+  typedef __attribute__((address_space(3))) s16x4* P;
+  s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(size_t)((at ^ (unsigned)(dt * 64)) + (unsigned)(row0 * D * 2)));
+  s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(size_t)((at ^ (unsigned)(dt * 64 + 32)) + (unsigned)((row0 + 8) * D * 2)));
+  s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(bf16x8, v);
+}
+
 // ---- the scores ----
 // place of accumulator slot r in its 32 x 32 tile, without the lane's 4 * (lane / 32)
 __device__ constexpr int slot(int r) { return 8 * (r >> 2) + (r & 3); }
@@ -152,16 +182,15 @@ __device__ __forceinline__ void tanh16(f32x16& v, const BiasedArgs& a) {
 
 // The bias of a wavefront's head, in units of log2.  BIAS: 0 none, 1 slopes, 2 table.
 template <int BIAS>
+struct BiasLds {
+  float numbers[BIAS == 2 ? 2 * kMaxDistance + 1 : 1];   // by distance, -far .. far
+  int first[BIAS == 2 ? kMaxBuckets + 1 : 1];
+};
 struct Bias {
   float slope2;
   const float* at0;          // LDS: entry of distance 0
   float far_pos, far_neg;    // from `far` on, and down from `-back` on
   int far, back;
-  // lds: [2 (far + kTableMargin) + 1] numbers and kMaxBuckets + 1 first distances; the caller's barrier follows
-  __device__ __forceinline__ void init(const BiasedArgs& a, int ghead) {
-    if (BIAS == 1) slope2 = a.slopes[ghead] * LOG2E;
-    if (BIAS == 2) { far = a.far; back = a.two_sided ? a.far : 0; }
-  }
 };
 __device__ __forceinline__ int bucket_of(const BiasedArgs& a, const int* first, int dist) {
   if (dist < 0 && !a.two_sided) return 0;
@@ -172,74 +201,72 @@ __device__ __forceinline__ int bucket_of(const BiasedArgs& a, const int* first, 
     if (k + step < a.side && first[k + step] <= n) k += step;
   return dist < 0 ? k + a.side : k;
 }
-// The head's table by distance.  Two barriers: behind the first distances, behind the numbers.
-__device__ __forceinline__ void fill_table(const BiasedArgs& a, int ghead, float* numbers, int* first) {
-  for (int k = threadIdx.x; k <= a.side; k += blockDim.x) first[k] = a.first[k];
-  __syncthreads();
-  const int reach = a.far + kTableMargin;
-  for (int k = threadIdx.x; k <= 2 * reach; k += blockDim.x) {
-    const float x = a.table[(long long)ghead * a.buckets + bucket_of(a, first, k - reach)];
-    numbers[k] = x <= -1e30f ? -INFINITY : x * LOG2E;
-  }
-  __syncthreads();
-}
-
-// v: 32 x 32 scores (tanh of them with CAP) -> log2(e) times the score.  The lane's slot r lies at distance t - u =
-// dist0 + SIGN * slot(r); lo, hi: smallest and largest distance of the tile.
-template <bool CAP, int BIAS, int SIGN>
-__device__ __forceinline__ float score2(float v, int r, const BiasedArgs& a, const Bias<BIAS>& b, float base, float dist0f, const float* near) {
-  // base: a constant added to every score of the tile (BIAS 2, far), near: its entries in LDS
-  const float w = CAP ? a.cap_log2 : a.f.scale_log2;
-  if (BIAS == 1) return fmaf(-b.slope2, fabsf(dist0f + (float)(SIGN * slot(r))), v * w);
-  if (BIAS == 2) return fmaf(v, w, near ? near[SIGN * slot(r)] : base);
-  return v * w;
-}
+// With a table two barriers: behind the first distances of the buckets, behind the numbers.
 template <int BIAS>
-struct TileBias {
-  float base, dist0f;
-  bool near;
-  const float* entry;
-};
-template <int BIAS>
-__device__ __forceinline__ TileBias<BIAS> tile_bias(const Bias<BIAS>& b, int dist0, int lo, int hi) {
-  TileBias<BIAS> t = {};
-  if (BIAS == 1) t.dist0f = (float)dist0;
+__device__ __forceinline__ Bias make_bias(const BiasedArgs& a, int ghead, BiasLds<BIAS>& lds) {
+  Bias b = {};
+  // (the same in every lane: scalar registers)
+  auto uniform = [](float x) { return __uint_as_float((unsigned)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x))); };
+  if (BIAS == 1) b.slope2 = uniform(a.slopes[ghead] * LOG2E);
   if (BIAS == 2) {
-    t.near = lo < b.far && hi > -b.back;
-    t.base = lo >= b.far ? b.far_pos : b.far_neg;
-    t.entry = b.at0 + dist0;
-  }
-  return t;
-}
-// all sixteen, in place
-template <bool CAP, int BIAS, int SIGN>
-__device__ __forceinline__ void scores16(f32x16& v, const BiasedArgs& a, const Bias<BIAS>& b, const TileBias<BIAS>& t) {
-  if (BIAS == 2 && t.near) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = score2<CAP, BIAS, SIGN>(v[r], r, a, b, 0.f, 0.f, t.entry);
-  } else {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = score2<CAP, BIAS, SIGN>(v[r], r, a, b, t.base, t.dist0f, nullptr);
-  }
-}
-
-template <int BIAS>
-struct BiasLds {
-  static constexpr int kNumbers = BIAS == 2 ? 2 * (kMaxDistance + kTableMargin) + 1 : 1;
-  float numbers[kNumbers];
-  int first[BIAS == 2 ? kMaxBuckets + 1 : 1];
-};
-template <int BIAS>
-__device__ __forceinline__ Bias<BIAS> make_bias(const BiasedArgs& a, int ghead, BiasLds<BIAS>& lds) {
-  Bias<BIAS> b = {};
-  b.init(a, ghead);
-  if (BIAS == 2) {
-    fill_table(a, ghead, lds.numbers, lds.first);
-    b.at0 = lds.numbers + a.far + kTableMargin;
-    b.far_pos = b.at0[a.far];
-    b.far_neg = b.at0[-b.back];
+    for (int k = threadIdx.x; k <= a.side; k += blockDim.x) lds.first[k] = a.first[k];
+    __syncthreads();
+    for (int k = threadIdx.x; k <= 2 * a.far; k += blockDim.x) {
+      const float x = a.table[(long long)ghead * a.buckets + bucket_of(a, lds.first, k - a.far)];
+      lds.numbers[k] = x <= -1e30f ? -INFINITY : x * LOG2E;
+    }
+    __syncthreads();
+    b.at0 = lds.numbers + a.far;
+    b.far = a.far;
+    b.back = a.two_sided ? a.far : 0;
+    b.far_pos = uniform(b.at0[b.far]);
+    b.far_neg = uniform(b.at0[-b.back]);
   }
   return b;
+}
+
+// Tiles of n columns or rows whose smallest distance t - u is lo and largest hi, scores (their tanh with CAP) in v.  SIGN: of the
+// distance along a lane's slots; the lane's slot r lies at dist0 + SIGN * slot(r).
+//
+// plain: every pair of the tile has one sign (slopes) or one bucket (table), so that log2(e) times the score is v * w + c.
+template <int BIAS>
+__device__ __forceinline__ bool plain_tile(const Bias& b, int lo, int hi) {
+  return BIAS == 1 ? lo >= 0 || hi <= 0 : BIAS == 2 ? lo >= b.far || hi <= -b.back : true;
+}
+template <bool CAP, int BIAS>
+__device__ __forceinline__ void plain_weights(const BiasedArgs& a, const Bias& b, int lo, float& w, float& c) {
+  w = BIAS == 1 ? 1.0f : CAP ? a.cap_log2 : a.f.scale_log2;
+  c = BIAS == 2 ? (lo >= b.far ? b.far_pos : b.far_neg) : 0.f;
+}
+template <bool CAP, int BIAS, int SIGN>
+__device__ __forceinline__ void plain16(f32x16& v, const BiasedArgs& a, const Bias& b, int dist0, int lo) {
+  if (BIAS == 1) {
+    const float sg = lo >= 0 ? -b.slope2 : b.slope2, base = sg * (float)dist0, w = CAP ? a.cap_log2 : a.f.scale_log2;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = fmaf(v[r], w, fmaf(sg, (float)(SIGN * slot(r)), base));
+  }
+}
+// Any tile: log2(e) times the score, -infinity where the pair is left out: the other token's place (at + slot(r)) behind `bound`
+// (SIGN < 0) or ahead of it, or of another document than `doc`.  docs: LDS, the other tokens' from the lane's slot 0 on.
+template <bool CAP, int BIAS, int SIGN>
+__device__ __forceinline__ void any16(f32x16& v, const BiasedArgs& a, const Bias& b, int dist0, int at, int bound, const int* docs, int doc) {
+  asm volatile("");   // a branch, not selects: taken by few tiles, and seven operations a score
+  const float w = CAP ? a.cap_log2 : a.f.scale_log2;
+  const int reach = bound - at;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int4 o = *(const int4*)(docs + 8 * c);
+    const int other[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * c + e, dist = dist0 + SIGN * slot(r);
+      float x = v[r] * w;
+      if (BIAS == 1) x = fmaf(-b.slope2, fabsf((float)dist), x);
+      if (BIAS == 2) x += b.at0[min(max(dist, -b.far), b.far)];
+      const bool out = (SIGN < 0 ? slot(r) > reach : slot(r) < reach) | (other[e] != doc) | (doc < 0);
+      v[r] = out ? -INFINITY : x;
+    }
+  }
 }
 
 }  // namespace

@@ -6,17 +6,21 @@ namespace optimus {
 namespace {
 
 // The sums of dS over the buckets, of one wavefront.  A lane owns a bucket (and the one 64 further).  A 32 x 32 tile that lies in the
-// last bucket as a whole is summed lane by lane; another one is summed along its 63 diagonals first: slot r of 32 lanes lies on 32
-// diagonals, so the adds into LDS of one instruction go to different places (the halves have an array each) and come one instruction
-// after the other: the same bits in every run.
+// last bucket as a whole is summed lane by lane; another one is summed along its 63 diagonals first.  Eight keys at a time go to LDS,
+// each moved by its place, so that the diagonals are columns, which a lane each adds up; places that no score reaches stay zero.
+// (Adding into 63 places with LDS's float additions took some 6000 clk a tile: 8 sequences of 8 heads, s = 2048, width 64, causal,
+// backward 426 us, so 240, without the table's gradient 227.)
+constexpr int kSkew = 41;   // places of a key: 39 diagonals, zeros behind them; of the halves' rows, four apart, in different banks
+constexpr int kSkewed = 8 * kSkew;
 struct BucketSums {
   float own[2], far_pos, far_neg;
   int lo[2], hi[2];      // distances of the lane's buckets
   int far, back;
-  float* diag;           // LDS, [2][64] of the wavefront
-  int* first;
-  __device__ __forceinline__ void init(const BiasedArgs& a, float* diag_, const int* first_, int lane) {
-    diag = diag_;
+  float* skewed;         // LDS of the wavefront: [8][kSkew], and [64] behind it
+  float* line;
+  __device__ __forceinline__ void init(const BiasedArgs& a, float* lds, const int* first_, int lane) {
+    skewed = lds;
+    line = lds + kSkewed;
     own[0] = own[1] = far_pos = far_neg = 0.f;
     far = a.far; back = a.two_sided ? a.far : 0;
 #pragma unroll
@@ -32,10 +36,10 @@ struct BucketSums {
         hi[k] = -max(first_[n], 1);
       }
     }
-    diag[lane] = diag[64 + lane] = 0.f;
+    for (int k = lane; k < kSkewed; k += 64) skewed[k] = 0.f;
   }
-  // ds: lane's slots at distance dist0 - slot(r); the tile's distances are base .. base + 62, the lane's slot 0 at `at` = dist0 - base
-  __device__ __forceinline__ void add(const f32x16& ds, int base, int at, int g, int lane, bool wide) {
+  // ds: the tile's scores, whose distances are base .. base + 62
+  __device__ __forceinline__ void add(const f32x16& ds, int base, int g, int lane, bool wide) {
     if (base >= far || base + 62 <= -back) {
       float t[8];
 #pragma unroll
@@ -45,22 +49,37 @@ struct BucketSums {
       else far_neg += sum;
       return;
     }
-    float* mine = diag + 64 * g + at;
+    // key 8c + 4g + e against query t: diagonal t - key + 31, place t - (4g + e) + 7 of row 4g + e
+    float* to_place = skewed + 4 * g * kSkew + (lane & 31) - 4 * g + 7;
+    float run = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(mine - slot(r), ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to_place[e * (kSkew - 1)] = ds[4 * c + e];
+      __builtin_amdgcn_wave_barrier();
+      const int place = lane - 24 + 8 * c;   // of the lane's diagonal
+      const float* column = skewed + (place >= 0 && place < 39 ? place : 39);
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = column[k * kSkew];
+      run += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      __builtin_amdgcn_wave_barrier();
+    }
+    line[lane] = run;   // (63 diagonals: the last place is zero)
     __builtin_amdgcn_wave_barrier();
-    const float both = diag[lane] + diag[64 + lane];
-    __builtin_amdgcn_wave_barrier();
-    diag[lane] = both;
-    __builtin_amdgcn_wave_barrier();
+    // A lane adds its buckets' diagonals up, eight reads in flight.  (Differences of one running sum over all of them are shorter, but
+    // leave a small bucket the rounding errors of its neighbours.)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       if (k == 1 && !wide) break;
       const int from = max(lo[k] - base, 0), to = min(hi[k] - base, 62);
-      for (int d = from; d <= to; ++d) own[k] += diag[d];
+      for (int d = from; d <= to; d += 8) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = line[d + e <= to ? d + e : 63];
+        own[k] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      }
     }
-    __builtin_amdgcn_wave_barrier();
-    diag[lane] = diag[64 + lane] = 0.f;
     __builtin_amdgcn_wave_barrier();
   }
   __device__ __forceinline__ void finish(const BiasedArgs& a, int lane) {   // the far sums to their buckets' lanes
@@ -83,7 +102,7 @@ struct DqLds {
   bf16_t tile[2][2][PAIR * D];   // [stage][K, V]
   BiasLds<BIAS> bias;
   alignas(16) int key_docs[2 * NRG][BLK];   // (read sixteen bytes at a time)
-  float diag[BIAS == 2 ? 2 * NRG : 1][128];
+  float sums[BIAS == 2 ? 2 * NRG : 1][kSkewed + 64];   // BucketSums; at the end the buckets (128)
   int live[2];
 };
 template <int D, int NRG, int BIAS>
@@ -126,7 +145,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
   BucketSums sums;
   const bool table_grad = BIAS == 2 && a.table_parts;
-  if (BIAS == 2) sums.init(a, lds.diag[wave], lds.bias.first, lane);
+  if (BIAS == 2) sums.init(a, lds.sums[wave], lds.bias.first, lane);
 
   const int wg_hi = min(tile * BQ + BQ, s) - 1;
   int kb_lo = 0, kb_hi = a.causal ? max(wg_hi, m.prefix - 1) / BLK + 1 : a.nblk;
@@ -182,7 +201,6 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
       const unsigned stage = (unsigned)((st * 2 * PAIR + par * BLK) * D * 2);
       const unsigned kt = in_rows + stage, kc = in_cols + stage;
       const bool masked = (a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) || (m.docs && !one_document(blk, own));
-      bf16x8 dsf[2][2];
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2) {
         f32x16 sacc = zero16(), pacc = zero16();
@@ -214,19 +232,18 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
 #pragma unroll
           for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], w, c)) * pacc[r];
         }
-        if (BIAS == 2 && table_grad) sums.add(sacc, q0 - k0 - 31, (lane & 31) + 31 - 4 * g, g, lane, a.buckets > 64);
+        if (BIAS == 2 && table_grad) sums.add(sacc, lo, g, lane, a.buckets > 64);
         if (CAP && BIAS == 2) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) sacc[r] *= part[r];
         }
-        dsf[t2][0] = pack_acc<0>(sacc);
-        dsf[t2][1] = pack_acc<1>(sacc);
+        const bf16x8 dsf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)};
+        pipelined<2 * DT, 2>([&](int n) { return cols_at<D>(kc, t2 * 32 + n / DT * 16, n % DT); },
+                            [&](int n, const bf16x8& x) {
+                              const int dt = n % DT;
+                              dqacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, dsf[n / DT], dqacc[dt], 0, 0, 0);
+                            });
       }
-      pipelined<4 * DT, 2>([&](int n) { return cols_at<D>(kc, n / DT * 16, n % DT); },
-                          [&](int n, const bf16x8& x) {
-                            const int dt = n % DT;
-                            dqacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, dsf[n / (2 * DT)][n / DT & 1], dqacc[dt], 0, 0, 0);
-                          });
     }
     if (m.docs && it + 1 < n_it) lds.key_docs[wave][lane] = next_doc;
     cur = next;
@@ -240,16 +257,16 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
 #pragma unroll
       for (int r = 0; r < 16; ++r) xch[(dt * 16 + r) * 64 + lane] = dqacc[dt][r];
   }
-  if (BIAS == 2 && table_grad) {   // (the wavefront's buckets over its diagonals)
+  if (BIAS == 2 && table_grad) {   // (in the wavefront's own place)
     sums.finish(a, lane);
-    lds.diag[wave][lane] = sums.own[0];
-    lds.diag[wave][64 + lane] = sums.own[1];
+    lds.sums[wave][lane] = sums.own[0];
+    lds.sums[wave][64 + lane] = sums.own[1];
   }
   __syncthreads();
   if (BIAS == 2 && table_grad && tid < a.buckets) {
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 2 * NRG; ++w) sum += lds.diag[w][tid];
+    for (int w = 0; w < 2 * NRG; ++w) sum += lds.sums[w][tid];
     a.table_parts[(((long long)dev * a.nb * f.nh + mat) * a.ntiles + tile) * a.buckets + tid] = sum;
   }
   if (par == 0 && query < s) {
@@ -406,7 +423,6 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
       const unsigned stage = (unsigned)((st * 2 * PAIR + par * BLK) * D * 2);
       const unsigned qt = in_rows + stage, qc = in_cols + stage;
       const bool masked = (a.causal && qbase < k0 + 31 && k0 + 31 >= m.prefix) || (m.docs && !one_document(blk, own));
-      bf16x8 pf[2][2], dsf[2][2];
       // 32 queries at a time: with the scores of all 64 live, fragments on their way have no registers
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2) {
@@ -419,17 +435,14 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
         const int at = par * BLK + t2 * 32;
         biased_dkv_scores<CAP, BIAS>(sacc, pacc, lds.l[st] + at, lds.d[st] + at, lds.docs[st] + at, qbase + t2 * 32, k0, key, first, kdoc,
                                      masked, a, bias, g);
-        pf[t2][0] = pack_acc<0>(sacc);
-        pf[t2][1] = pack_acc<1>(sacc);
-        dsf[t2][0] = pack_acc<0>(pacc);
-        dsf[t2][1] = pack_acc<1>(pacc);
+        const bf16x8 pf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)}, dsf[2] = {pack_acc<0>(pacc), pack_acc<1>(pacc)};
+        pipelined<4 * DT, 2>([&](int n) { return cols_at<D>(qc, (n & 1 ? 0 : PAIR) + t2 * 32 + n / (2 * DT) * 16, n / 2 % DT); },
+                            [&](int n, const bf16x8& x) {
+                              const int dt = n / 2 % DT, u = n / (2 * DT);
+                              f32x16& acc = n & 1 ? dkacc[dt] : dvacc[dt];
+                              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dsf[u] : pf[u], acc, 0, 0, 0);
+                            });
       }
-      pipelined<8 * DT, 2>([&](int n) { return cols_at<D>(qc, (n & 1 ? 0 : PAIR) + n / (2 * DT) * 16, n / 2 % DT); },
-                          [&](int n, const bf16x8& x) {
-                            const int dt = n / 2 % DT, t2 = n / (4 * DT), u = n / (2 * DT) & 1;
-                            f32x16& acc = n & 1 ? dkacc[dt] : dvacc[dt];
-                            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dsf[t2][u] : pf[t2][u], acc, 0, 0, 0);
-                          });
     }
     if (it + 1 < n_it) store_rows(it + 1, st ^ 1);
     cur = next;

@@ -244,7 +244,7 @@ int optimus_attention_fused_bwd_static(const void* qkv, const void* attn, const 
 
 /* ---- the same attention with changed scores: capped, biased by distance, masked by documents or opened by a prefix ----
  * Layouts, lse, d_qkv, coordinates and limits as in optimus_attention_fused_*; per pair (t, u) of a (sequence, head):
- *   S = Q K^T / sqrt(d);  with cap > 0: S = cap tanh(S / cap);
+ *   S = Q K^T / sqrt(d);  with cap from 1e-3 to 1e30: S = cap tanh(S / cap), 0: none, others EINVAL;
  *   with slopes: S -= slopes[head] |t - u|;  or, with table: S += table[head][bucket(t - u)] (not both: EINVAL).
  * A pair is left out
  *   with causal != 0 where u > t, unless u < prefix[sequence] (prefix needs causal != 0: EINVAL; values are clamped to 0 .. s);

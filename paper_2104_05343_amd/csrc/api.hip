@@ -352,7 +352,7 @@ int run_attention_fused(bool bwd, const void* qkv, void* attn, float* lse, const
 // a power next to a whole number is that number.
 int bias_desc(const optimus_attention_bias* b, int causal, AttnBiasedDesc* d) {
   if (!b) return OPTIMUS_EINVAL;
-  if (!(b->cap >= 0) || isinf(b->cap) || (b->slopes && b->table) || (b->prefix && !causal)) return OPTIMUS_EINVAL;
+  if (!(b->cap == 0 || (b->cap >= 1e-3f && b->cap <= 1e30f)) || (b->slopes && b->table) || (b->prefix && !causal)) return OPTIMUS_EINVAL;
   d->cap = b->cap; d->slopes = b->slopes; d->table = b->table; d->documents = b->documents; d->prefix = b->prefix;
   if (!b->table) return OPTIMUS_OK;
   d->buckets = b->buckets; d->two_sided = b->two_sided ? 1 : 0;

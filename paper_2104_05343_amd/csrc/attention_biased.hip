@@ -12,7 +12,6 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][PAIR * D];  // [stage][K, V][pair tile]
   __shared__ BiasLds<BIAS> bias_lds;
   __shared__ __attribute__((aligned(16))) int key_docs[2 * NRG][BLK];    // of the wavefront's block
-  __shared__ int live[2];
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -28,12 +27,11 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
   const int qdoc = m.docs ? m.docs[qrow] : 0;
   bf16x8 qf[KS];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) qf[ks] = zero_if(qdoc < 0, *(const bf16x8*)(Qp + (long long)qrow * f.ld + ks * 16 + g * 8));
-  const Bias bias = make_bias<BIAS>(a, m.ghead, bias_lds);
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(Qp + (long long)qrow * f.ld + ks * 16 + g * 8);
 
   const int wg_hi = min(tile * BQ + BQ, s) - 1;   // last query row of the workgroup
   int kb_lo = 0, kb_hi = a.causal ? max(wg_hi, m.prefix - 1) / BLK + 1 : a.nblk;
-  if (m.docs) live_blocks(m.blocks, tile * BQ / BLK, wg_hi / BLK, kb_lo, kb_hi, live);
+  if (m.docs) live_blocks(m.blocks, tile * BQ / BLK, wg_hi / BLK, kb_lo, kb_hi);
   const int it_lo = kb_lo / 2, n_it = (kb_hi + 1) / 2;
   // last key that a row of the wavefront may see, and that this lane's may
   const int wave_last = q0 >= s ? -1 : a.causal ? max(min(q0 + 31, s - 1), m.prefix - 1) : s - 1;
@@ -65,10 +63,16 @@ __global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_b
     ldr.issue(Vp, it * PAIR, s, lds[st][1], docs);
   };
   Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
+  int first_doc = 0;
   if (it_lo < n_it) {
-    key_docs[wave][lane] = m.docs ? m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)] : 0;
+    if (m.docs) first_doc = m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)];
     issue(it_lo, 0, cur);
   }
+  // (behind the first tiles' request: it waits for loads of its own)
+  const Bias bias = make_bias<BIAS>(a, m.ghead, bias_lds);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = zero_if(qdoc < 0, qf[ks]);
+  key_docs[wave][lane] = first_doc;
   wait_loads_and_barrier();
   for (int it = it_lo; it < n_it; ++it) {
     const int st = (it - it_lo) & 1;
@@ -254,7 +258,9 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
   if (b.cap > 0) {
     const double in = 1.0 / (sqrt((double)d.d) * b.cap);
     a.cap_log2 = (float)(b.cap * 1.4426950408889634);
-    a.cap_in = (float)in;
+    const double of[5] = {1.0, -1.0 / 3, 2.0 / 15, -17.0 / 315, 62.0 / 2835};
+    double power = in;
+    for (int k = 0; k < 5; ++k, power *= in * in) a.tanh_of[k] = (float)(of[k] * power);
     a.cap_exp = (float)(2.0 * in * 1.4426950408889634);
     a.cap_small = (float)(0.25 / in);
   }

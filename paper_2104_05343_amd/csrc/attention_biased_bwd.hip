@@ -102,8 +102,7 @@ struct DqLds {
   bf16_t tile[2][2][PAIR * D];   // [stage][K, V]
   BiasLds<BIAS> bias;
   alignas(16) int key_docs[2 * NRG][BLK];   // (read sixteen bytes at a time)
-  float sums[BIAS == 2 ? 2 * NRG : 1][kSkewed + 64];   // BucketSums; at the end the buckets (128)
-  int live[2];
+  float sums[BIAS == 2 ? 2 * NRG : 1][BIAS == 2 ? kSkewed + 64 : 1];   // BucketSums; at the end the buckets (128)
 };
 template <int D, int NRG, int BIAS>
 struct DkvLds {
@@ -112,7 +111,6 @@ struct DkvLds {
   alignas(16) float l[2][PAIR];   // (read sixteen bytes at a time, as the next two)
   alignas(16) float d[2][PAIR];
   alignas(16) int docs[2][PAIR];
-  int live[2];
 };
 
 // log-sum-exp of a row -> what is subtracted from its scores.  Of a row without pairs +infinity, which makes every P of it zero.
@@ -137,19 +135,14 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   bf16x8 qf[KS], dof[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
-    qf[ks] = zero_if(qdoc < 0, *(const bf16x8*)(Qp + (long long)qrow * f.ld + ks * 16 + g * 8));
-    dof[ks] = zero_if(qdoc < 0, *(const bf16x8*)(f.d_attn + m.attn + (long long)qrow * f.ldo + ks * 16 + g * 8));
+    qf[ks] = *(const bf16x8*)(Qp + (long long)qrow * f.ld + ks * 16 + g * 8);
+    dof[ks] = *(const bf16x8*)(f.d_attn + m.attn + (long long)qrow * f.ldo + ks * 16 + g * 8);
   }
-  const float delta = f.delta[m.vec + qrow];
-  const float lse2 = query < s && qdoc >= 0 ? lse2_of(f.lse[m.vec + qrow]) : INFINITY;
-  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
-  BucketSums sums;
-  const bool table_grad = BIAS == 2 && a.table_parts;
-  if (BIAS == 2) sums.init(a, lds.sums[wave], lds.bias.first, lane);
+  const float delta = f.delta[m.vec + qrow], lse = f.lse[m.vec + qrow];
 
   const int wg_hi = min(tile * BQ + BQ, s) - 1;
   int kb_lo = 0, kb_hi = a.causal ? max(wg_hi, m.prefix - 1) / BLK + 1 : a.nblk;
-  if (m.docs) live_blocks(m.blocks, tile * BQ / BLK, wg_hi / BLK, kb_lo, kb_hi, lds.live);
+  if (m.docs) live_blocks(m.blocks, tile * BQ / BLK, wg_hi / BLK, kb_lo, kb_hi);
   const int it_lo = kb_lo / 2, n_it = (kb_hi + 1) / 2;
   const int wave_last = q0 >= s ? -1 : a.causal ? max(min(q0 + 31, s - 1), m.prefix - 1) : s - 1;
   const int limit = a.causal ? max(qrow, m.prefix - 1) : s - 1;
@@ -178,10 +171,23 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
     ldr.issue(Vp, it * PAIR, s, lds.tile[st][1], docs);
   };
   Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
+  int first_doc = 0;
   if (it_lo < n_it) {
-    lds.key_docs[wave][lane] = m.docs ? m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)] : 0;
+    if (m.docs) first_doc = m.docs[min((2 * it_lo + par) * BLK + lane, s - 1)];
     issue(it_lo, 0, cur);
   }
+  // (behind the first tiles' request: it waits for loads of its own)
+  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
+  BucketSums sums;
+  const bool table_grad = BIAS == 2 && a.table_parts;
+  if (BIAS == 2) sums.init(a, lds.sums[wave], lds.bias.first, lane);
+  const float lse2 = query < s && qdoc >= 0 ? lse2_of(lse) : INFINITY;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    qf[ks] = zero_if(qdoc < 0, qf[ks]);
+    dof[ks] = zero_if(qdoc < 0, dof[ks]);
+  }
+  lds.key_docs[wave][lane] = first_doc;
   wait_loads_and_barrier();
   for (int it = it_lo; it < n_it; ++it) {
     const int st = (it - it_lo) & 1;
@@ -347,13 +353,12 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   bf16x8 kf[KS], vf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
-    kf[ks] = zero_if(kdoc < 0, *(const bf16x8*)(Kp + (long long)krow * f.ld + ks * 16 + g * 8));
-    vf[ks] = zero_if(kdoc < 0, *(const bf16x8*)(Vp + (long long)krow * f.ld + ks * 16 + g * 8));
+    kf[ks] = *(const bf16x8*)(Kp + (long long)krow * f.ld + ks * 16 + g * 8);
+    vf[ks] = *(const bf16x8*)(Vp + (long long)krow * f.ld + ks * 16 + g * 8);
   }
-  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
   // the first block with a query that sees the workgroup's first key
   int qb_lo = a.causal && kt0 >= m.prefix ? kt0 / BLK : 0, qb_hi = a.nblk;
-  if (m.docs) live_blocks(m.blocks, kt0 / BLK, (min(kt0 + BKW, s) - 1) / BLK, qb_lo, qb_hi, lds.live);
+  if (m.docs) live_blocks(m.blocks, kt0 / BLK, (min(kt0 + BKW, s) - 1) / BLK, qb_lo, qb_hi);
   const int it_lo = qb_lo / 2, n_it = (qb_hi + 1) / 2;
   const i32x4_t none = {0x7fffffff, -1, 0, 0};
   const i32x4_t own = m.docs && k0 < s ? m.blocks[k0 / BLK] : none;
@@ -404,9 +409,15 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   Pair cur = pair_of(it_lo), next = pair_of(it_lo + 1);
   if (it_lo < n_it) {
     load_rows(it_lo);
-    store_rows(it_lo, 0);
     issue(it_lo, 0, cur);
   }
+  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = zero_if(kdoc < 0, kf[ks]);
+    vf[ks] = zero_if(kdoc < 0, vf[ks]);
+  }
+  store_rows(it_lo, 0);
   wait_loads_and_barrier();
   for (int it = it_lo; it < n_it; ++it) {
     const int st = (it - it_lo) & 1;
@@ -491,7 +502,6 @@ struct WideDkvLds {
   alignas(16) float l[2][BLK];
   alignas(16) float d[2][BLK];
   alignas(16) int docs[2][BLK];
-  int live[2];
 };
 template <bool CAP, int BIAS>
 __device__ __forceinline__ void biased_dkv_wide_body(const BiasedArgs& a, WideDkvLds<BIAS>& lds, int tile, int mat, int dev) {
@@ -514,7 +524,7 @@ __device__ __forceinline__ void biased_dkv_wide_body(const BiasedArgs& a, WideDk
   const int first = a.causal && key >= m.prefix ? key : 0;   // query from which on the key is seen
   bf16x8 kf[KREG];
 #pragma unroll
-  for (int ks = 0; ks < KREG; ++ks) kf[ks] = zero_if(kdoc < 0, *(const bf16x8*)(Kp + (long long)krow * f.ld + ks * 16 + g * 8));
+  for (int ks = 0; ks < KREG; ++ks) kf[ks] = *(const bf16x8*)(Kp + (long long)krow * f.ld + ks * 16 + g * 8);
   const int last_blk = (min(kt0 + BKW, s) - 1) / BLK;
   {
     const int* docs = m.docs && m.blocks[kt0 / BLK].z | m.blocks[last_blk].z ? m.docs : nullptr;
@@ -523,9 +533,8 @@ __device__ __forceinline__ void biased_dkv_wide_body(const BiasedArgs& a, WideDk
     own.issue(Qp + 2 * D, kt0, s, lds.v, docs);
     own.issue(Kp, kt0, s, lds.k, docs);
   }
-  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
   int qb_lo = a.causal && kt0 >= m.prefix ? kt0 / BLK : 0, qb_hi = a.nblk;
-  if (m.docs) live_blocks(m.blocks, kt0 / BLK, last_blk, qb_lo, qb_hi, lds.live);
+  if (m.docs) live_blocks(m.blocks, kt0 / BLK, last_blk, qb_lo, qb_hi);
   const i32x4_t none = {0x7fffffff, -1, 0, 0};
   const i32x4_t own_docs = m.docs && k0 < s ? m.blocks[k0 / BLK] : none;
 
@@ -565,8 +574,11 @@ __device__ __forceinline__ void biased_dkv_wide_body(const BiasedArgs& a, WideDk
   i32x4_t cur = block_of(qb_lo), next = block_of(qb_lo + 1);
   if (qb_lo < qb_hi) {
     load_block(qb_lo, 0, cur);
-    store_rows(qb_lo, 0);
   }
+  const Bias bias = make_bias<BIAS>(a, m.ghead, lds.bias);
+#pragma unroll
+  for (int ks = 0; ks < KREG; ++ks) kf[ks] = zero_if(kdoc < 0, kf[ks]);
+  store_rows(qb_lo, 0);
   wait_loads_and_barrier();
   for (int qb = qb_lo; qb < qb_hi; ++qb) {
     const int st = (qb - qb_lo) & 1;

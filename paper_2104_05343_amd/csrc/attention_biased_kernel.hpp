@@ -8,7 +8,7 @@
 // Backward: P = exp(S - lse), dS = P (dO V^T - rowsum(dO * O)); the table's gradient is the sum of dS over a bucket's pairs; from
 // there on dS (1 - tanh^2).
 //
-// What the additions cost beside the 32 to 64 clk a matrix instruction takes: the tanh 7 operations a score while a tile's scores stay
+// What the additions cost beside the 32 to 64 clk a matrix instruction takes: the tanh 7 operations a score (the largest of the tile among them) while a tile's scores stay
 // below a quarter of the cap (odd polynomial), else an exponential and a reciprocal; slopes 2; the table nothing but one fused
 // multiply-add where a whole tile lies in the last bucket, one LDS read where it does not.  Blocks of keys that share no document with
 // the workgroup's rows are not loaded: documents packed one after the other cost the sum of their squares.
@@ -28,7 +28,8 @@ struct BiasedArgs {
   int nb, q, dev0;           // sequences of a device, grid, first device of the launch
   int causal, nblk;          // nblk: blocks of 64 tokens of a sequence
   float cap_log2;            // cap * log2(e)
-  float cap_in, cap_exp;     // 1 / (sqrt(d) cap);  2 log2(e) / (sqrt(d) cap)
+  float cap_exp;             // 2 log2(e) / (sqrt(d) cap)
+  float tanh_of[5];          // coefficients of tanh(v / (sqrt(d) cap)) at v, v^3, .. v^9
   float cap_small;           // Q K^T below which the polynomial is taken: cap sqrt(d) / 4
   int buckets, side, two_sided, far;   // side: buckets of one side; far: first distance of its last one
   int ntiles;                // row tiles of a matrix in the parts of the table's gradient
@@ -77,22 +78,23 @@ __device__ __forceinline__ Matrix matrix_of(const BiasedArgs& a, int mat, int de
 __device__ __forceinline__ bool share_documents(i32x4_t x, i32x4_t y) { return x.x <= y.y && x.y >= y.x; }
 // every pair of the two blocks, which share documents, is of one document
 __device__ __forceinline__ bool one_document(i32x4_t x, i32x4_t y) { return x.x == x.y && y.x == y.y && !(x.z | y.z); }
-// First and last + 1 of the blocks lo .. hi - 1 that share documents with the blocks own0 .. own1 (the workgroup's rows).
-__device__ __forceinline__ void live_blocks(BlockList blocks, int own0, int own1, int& lo, int& hi, int* lds2) {
-  const int tid = threadIdx.x, n = blockDim.x;
-  if (tid == 0) { lds2[0] = 0x7fffffff; lds2[1] = -1; }
-  __syncthreads();
+// First and last + 1 of the blocks lo .. hi - 1 that share documents with the blocks own0 .. own1 (the workgroup's rows).  Every
+// wavefront looks at all of them, 64 at a time: no barrier.
+__device__ __forceinline__ void live_blocks(BlockList blocks, int own0, int own1, int& lo, int& hi) {
   const i32x4_t r0 = blocks[own0], r1 = blocks[own1];
-  int first = 0x7fffffff, last = -1;
-  for (int b = lo + tid; b < hi; b += n) {
-    const i32x4_t x = ((const i32x4_t*)(unsigned long long)blocks)[b];
-    if (share_documents(x, r0) || share_documents(x, r1)) { first = min(first, b); last = b; }
+  const i32x4_t* list = (const i32x4_t*)(unsigned long long)blocks;
+  const int lane = threadIdx.x & 63;
+  int first = 0, last = -1;
+  for (int b = lo; b < hi; b += 64) {
+    const i32x4_t x = list[min(b + lane, hi - 1)];
+    const unsigned long long m = __builtin_amdgcn_ballot_w64(b + lane < hi && (share_documents(x, r0) || share_documents(x, r1)));
+    if (m) {
+      if (last < 0) first = b + __builtin_ctzll(m);
+      last = b + 63 - __builtin_clzll(m);
+    }
   }
-  if (last >= 0) { atomicMin(&lds2[0], first); atomicMax(&lds2[1], last); }   // (of integers in LDS: the order does not matter)
-  __syncthreads();
-  const int x = __builtin_amdgcn_readfirstlane(lds2[0]), y = __builtin_amdgcn_readfirstlane(lds2[1]);
-  lo = y < 0 ? 0 : x;
-  hi = y + 1;
+  lo = first;
+  hi = last + 1;
 }
 
 // A tile whose padded rows (and those past the end) become zeros in LDS: what a padded token's rows hold is not looked at, and zero
@@ -162,8 +164,8 @@ __device__ __forceinline__ bf16x8 cols_at(unsigned at, int row0, int dt) {
 // place of accumulator slot r in its 32 x 32 tile, without the lane's 4 * (lane / 32)
 __device__ constexpr int slot(int r) { return 8 * (r >> 2) + (r & 3); }
 
-// v = Q K^T -> tanh(v / (sqrt(d) cap)).  Below a quarter the odd polynomial up to the ninth power (relative error 1e-8); above,
-// 1 - 2 / (exp(2x) + 1), whose absolute error of a unit in the last place of 1 is a relative one of 5e-7 of such a score.
+// v = Q K^T -> tanh(v / (sqrt(d) cap)).  Below a quarter the odd polynomial up to the ninth power, in v itself (relative error 1e-8);
+// above, 1 - 2 / (exp(2x) + 1), whose absolute error of a unit in the last place of 1 is a relative one of 5e-7 of such a score.
 __device__ __forceinline__ void tanh16(f32x16& v, const BiasedArgs& a) {
   float mx = 0.f;
 #pragma unroll
@@ -171,8 +173,8 @@ __device__ __forceinline__ void tanh16(f32x16& v, const BiasedArgs& a) {
   if (__builtin_amdgcn_ballot_w64(mx < a.cap_small) == ~0ull) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float x = v[r] * a.cap_in, y = x * x;
-      v[r] = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), x);
+      const float y = v[r] * v[r];
+      v[r] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, a.tanh_of[4], a.tanh_of[3]), a.tanh_of[2]), a.tanh_of[1]), a.tanh_of[0]);
     }
   } else {
 #pragma unroll

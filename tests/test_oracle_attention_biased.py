@@ -94,7 +94,7 @@ T = dict(table=4096, buckets=32, max_distance=128)
 @pytest.mark.parametrize("kw,code", [
     (dict(ptr=False), "EINVAL"), (dict(null_bias=True), "EINVAL"), (dict(dtype=0), "EDTYPE"), (dict(b=3), "ESHAPE"), (dict(n=3), "ESHAPE"),
     (dict(h=64), "ESHAPE"), (dict(s=0), "ESHAPE"), (dict(s=(1 << 20) + 1), "ESHAPE"), (dict(i=2), "ECOORD"), (dict(i=-1, j=0), "ECOORD"),
-    (dict(bias=dict(cap=-1.0)), "EINVAL"), (dict(bias=dict(cap=float("nan"))), "EINVAL"), (dict(bias=dict(cap=float("inf"))), "EINVAL"),
+    (dict(bias=dict(cap=-1.0)), "EINVAL"), (dict(bias=dict(cap=float("nan"))), "EINVAL"), (dict(bias=dict(cap=float("inf"))), "EINVAL"), (dict(bias=dict(cap=1e-4)), "EINVAL"), (dict(bias=dict(cap=1e31)), "EINVAL"),
     (dict(bias=dict(T, slopes=4096)), "EINVAL"), (dict(bias=dict(prefix=4096), causal=0), "EINVAL"),
     (dict(bias=dict(T, buckets=1)), "ESHAPE"), (dict(bias=dict(T, buckets=129)), "ESHAPE"), (dict(bias=dict(T, buckets=7, two_sided=True)), "ESHAPE"),
     (dict(bias=dict(T, buckets=2, two_sided=True)), "ESHAPE"), (dict(bias=dict(T, max_distance=16)), "ESHAPE"), (dict(bias=dict(T, max_distance=1025)), "ESHAPE"),

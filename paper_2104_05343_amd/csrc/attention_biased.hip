@@ -5,9 +5,11 @@
 namespace optimus {
 namespace {
 
-// Forward.  NRG: row groups of 32 queries per workgroup, as in the attention without changes.
+// Forward.  NRG: row groups of 32 queries per workgroup, as in the attention without changes.  Two workgroups of 128 rows a compute unit
+// of width 64, where 128 registers a lane are enough: with slopes a dozen would be spilled (16 matrices of 4096, causal, 76 us; one
+// workgroup 63).
 template <int D, int NRG, bool CAP, int BIAS>
-__global__ __launch_bounds__(NRG * 128, NRG == 4 || D == 64 ? 2 : 1) void attn_biased_fwd_kernel(BiasedArgs a) {
+__global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 && BIAS != 1 ? 4 : NRG == 4 || D == 64 ? 2 : 1) void attn_biased_fwd_kernel(BiasedArgs a) {
   constexpr int KS = D / 16, DT = D / 32, BQ = NRG * 32, AHEAD = D == 64 ? 1 : 2;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][PAIR * D];  // [stage][K, V][pair tile]
   __shared__ BiasLds<BIAS> bias_lds;
@@ -277,8 +279,11 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
 
 template <int D, bool CAP, int BIAS>
 void fwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
-  // 128-row workgroups from one per two compute units on, as without changes
-  const bool big = (long long)((d.s + 127) / 128) * d.nb * d.nh * d.ndev >= 128;
+  // 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64): a wavefront has the same loop
+  // either way and a SIMD to itself.  64 rows / 128 rows, us: width 128, causal with a cap, 16 matrices of 1024 (256 workgroups of 64
+  // rows) 23.7 / 26.8, 32 of them 31.3 / 27.5; width 64, 16 of 2048 (512) 29.7 / 37.7, 64 of 1024 (1024) 27.9 / 27.1, without a mask
+  // 40.1 / 34.2.  The bits are the same.
+  const bool big = (long long)((d.s + BLK - 1) / BLK) * d.nb * d.nh * d.ndev > num_cus() * (D == 64 ? 2 : 1);
   const int rows = big ? 128 : BLK;
   const dim3 grid(d.nb * d.nh, (d.s + rows - 1) / rows, d.ndev);
   if (big) attn_biased_fwd_kernel<D, 4, CAP, BIAS><<<grid, 512, 0, st>>>(a);

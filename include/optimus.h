@@ -450,7 +450,7 @@ int optimus_cross_entropy2d_bwd(const void* logits, const int32_t* labels, const
  * grad_scale, lr_on_device, step_on_device: NULL, or device memory that is read when the step runs, in place of 1, lr and step: what
  *   a captured step changes between its replays.
  * tensors: host array, read before the call returns.  Pointers need the alignment of their elements only.  The parameters may not
- *   overlap (OPTIMUS_EINVAL); nor may any other memory that is written (not checked).  n from 1 to 2^40, any number. */
+ *   overlap (OPTIMUS_EINVAL); nor may any other memory that is written (not checked).  n from 1 to 2^34. */
 typedef struct {
   void* param;
   float* master;
@@ -469,6 +469,18 @@ typedef struct {
   const float* grad_scale; const float* lr_on_device; const int64_t* step_on_device;
 } optimus_adamw_cfg;
 int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count, void* stream);
+
+/* optimus_stack_bwd that updates each layer as soon as its gradients are complete, so that all layers share ONE parameter-gradient
+ * buffer (Section 3.2.3): the parameters in `params` are written.  param_grad: optimus_stack_sizes.param_grad bytes.  states: host array
+ * of n_layers entries.  m, v, m_scale, v_scale: as in optimus_adamw_tensor, for optimus_stack_adamw_elements(cfg) elements: w_qkv, w_o,
+ * w1, w2, b_qkv, b_o, b1, b2, ln1_g, ln1_b, ln2_g, ln2_b one after the other, each from a multiple of 128 elements on.  master: fp32
+ * [12 h h], the four matrices, or NULL.  weight_decay: of the matrices; vectors have none.  Random bits: those of a list of these
+ * twelve tensors and the seed adamw->seed + layer.  No two parameters, of whatever layers, may overlap (OPTIMUS_EINVAL). */
+typedef struct { void* m; void* v; uint8_t* m_scale; uint8_t* v_scale; float* master; } optimus_adamw_state;
+int64_t optimus_stack_adamw_elements(const optimus_layer_cfg* cfg);   /* 0 for a cfg that is refused */
+int optimus_stack_bwd_adamw(const optimus_layer_cfg* cfg, int n_layers, const optimus_layer_params* params,
+                            const optimus_adamw_state* states, const optimus_adamw_cfg* adamw, float weight_decay, void* param_grad,
+                            const void* d_out, const optimus_stack_buffers* buf, void* d_x, void* stream);
 
 /* ---- flop accounting (Table 1) ----
  * optimus_gemm_flops: 2*(M/q)*K*(N/q), one device's share of one product.

@@ -89,6 +89,10 @@ class AdamwCfg(C.Structure):
                 ("seed", C.c_uint64), ("grad_scale", C.c_void_p), ("lr_on_device", C.c_void_p), ("step_on_device", C.c_void_p)]
 
 
+class AdamwState(C.Structure):
+    _fields_ = [("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("master", C.c_void_p)]
+
+
 LAYER_DONE_FN = C.CFUNCTYPE(None, C.c_int, C.c_void_p)
 
 
@@ -142,6 +146,9 @@ SIGNATURES = {
     "optimus_layer_fwd": (_INT, [C.POINTER(LayerCfg), C.POINTER(LayerTensors), _INT, _INT, _P, _SZ, _P]),
     "optimus_layer_bwd": (_INT, [C.POINTER(LayerCfg), C.POINTER(LayerTensors), _INT, _INT, _P, _SZ, _P]),
     "optimus_adamw_step": (_INT, [C.POINTER(AdamwCfg), C.POINTER(AdamwTensor), _INT, _P]),
+    "optimus_stack_adamw_elements": (_I64, [C.POINTER(LayerCfg)]),
+    "optimus_stack_bwd_adamw": (_INT, [C.POINTER(LayerCfg), _INT, C.POINTER(LayerParams), C.POINTER(AdamwState), C.POINTER(AdamwCfg), _F, _P, _P,
+                                       C.POINTER(StackBuffers), _P, _P]),
     "optimus_gemm_flops": (_I64, [_I64, _I64, _I64, _INT]),
     "optimus_layer_flops": (_I64, [C.POINTER(LayerCfg), _INT]),
     "optimus_debug_set_gemm_variant": (None, [_INT]),
@@ -467,6 +474,25 @@ def make_adamw_tensors(tensors):
 def adamw_step(cfg: AdamwCfg, tensors, stream=None):
     """tensors: what make_adamw_tensors returned."""
     _check(lib().optimus_adamw_step(C.byref(cfg), tensors, len(tensors), _stream(stream)), "optimus_adamw_step")
+
+
+def make_adamw_state(m, v, m_scale=None, v_scale=None, master=None) -> AdamwState:
+    """One layer's moments (stack_adamw_elements of them) and masters.  Holds addresses: keep the tensors alive."""
+    return AdamwState(_ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), _ptr(master))
+
+
+def stack_adamw_elements(cfg: LayerCfg) -> int:
+    return lib().optimus_stack_adamw_elements(C.byref(cfg))
+
+
+def stack_bwd_adamw(cfg: LayerCfg, params, states, adamw: AdamwCfg, weight_decay, param_grad, d_out, buf: StackBuffers, d_x, stream=None):
+    """params / states: lists of LayerParams / AdamwState, one per layer; the parameters are updated."""
+    pa = (LayerParams * len(params))(*params)
+    sa = (AdamwState * len(states))(*states)
+    if len(states) != len(params):
+        raise OptimusError(EINVAL, "optimus_stack_bwd_adamw")
+    _check(lib().optimus_stack_bwd_adamw(C.byref(cfg), len(params), pa, sa, C.byref(adamw), weight_decay, _ptr(param_grad), _ptr(d_out),
+                                         C.byref(buf), _ptr(d_x), _stream(stream)), "optimus_stack_bwd_adamw")
 
 
 def gemm_flops(M, K, N, q) -> int:

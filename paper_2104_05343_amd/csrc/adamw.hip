@@ -20,6 +20,7 @@ namespace {
 constexpr int kGroup = 128;                    // elements that share a scale
 constexpr int kPerLane = 8, kThreads = 256;
 constexpr int kChunk = kPerLane * kThreads;    // elements of a workgroup
+constexpr long long kMostGroups = (1ll << 32) / kThreads - 1;   // of a launch: 2^32 threads
 constexpr int kTensors = 40;                   // of one launch: its table travels in the kernel's arguments (4 KiB at most)
 
 struct AdamwJob {
@@ -281,7 +282,7 @@ int check_tensor(const optimus_adamw_tensor& t) {
   if ((t.param_dtype != OPTIMUS_BF16 && t.param_dtype != OPTIMUS_FP32) || (t.grad_dtype != OPTIMUS_BF16 && t.grad_dtype != OPTIMUS_FP32))
     return OPTIMUS_EDTYPE;
   if (t.master && t.param_dtype != OPTIMUS_BF16) return OPTIMUS_EINVAL;
-  if (t.n < 1 || t.n > (1ll << 40) || t.grad_parts < 1 || t.grad_parts > 65536) return OPTIMUS_ESHAPE;
+  if (t.n < 1 || t.n > (1ll << 34) || t.grad_parts < 1 || t.grad_parts > 65536) return OPTIMUS_ESHAPE;
   if (!isfinite(t.weight_decay)) return OPTIMUS_EINVAL;
   const uintptr_t pe = t.param_dtype == OPTIMUS_BF16 ? 1 : 3, ge = t.grad_dtype == OPTIMUS_BF16 ? 1 : 3, me = t.m_scale ? 0 : 3;
   if ((uintptr_t)t.param & pe || (uintptr_t)t.grad & ge || ((uintptr_t)t.m | (uintptr_t)t.v) & me || (uintptr_t)t.master & 3) return OPTIMUS_EINVAL;
@@ -289,11 +290,8 @@ int check_tensor(const optimus_adamw_tensor& t) {
 }
 
 }  // namespace
-}  // namespace optimus
 
-using namespace optimus;
-
-extern "C" int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count, void* stream) {
+int adamw_check(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count) {
   if (!cfg || !tensors) return OPTIMUS_EINVAL;
   if (count < 1 || count > (1 << 20)) return OPTIMUS_ESHAPE;
   if (!isfinite(cfg->lr) || !(cfg->beta1 >= 0 && cfg->beta1 < 1) || !(cfg->beta2 >= 0 && cfg->beta2 < 1) || !(cfg->eps > 0) || !isfinite(cfg->eps) ||
@@ -301,20 +299,21 @@ extern "C" int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_ad
     return OPTIMUS_EINVAL;
   for (int k = 0; k < count; ++k)
     if (const int rc = check_tensor(tensors[k])) return rc;
-  {
-    Range few[64];
-    Range* r = count <= 64 ? few : (Range*)malloc(sizeof(Range) * (size_t)count);
-    if (!r) return OPTIMUS_EHIP;
-    for (int k = 0; k < count; ++k) {
-      r[k].at = (uintptr_t)tensors[k].param;
-      r[k].end = r[k].at + (uintptr_t)tensors[k].n * (tensors[k].param_dtype == OPTIMUS_BF16 ? 2 : 4);
-    }
-    qsort(r, (size_t)count, sizeof(Range), compare_ranges);
-    bool meet = false;
-    for (int k = 1; k < count; ++k) meet = meet || r[k].at < r[k - 1].end;
-    if (r != few) free(r);
-    if (meet) return OPTIMUS_EINVAL;
+  Range few[64];
+  Range* r = count <= 64 ? few : (Range*)malloc(sizeof(Range) * (size_t)count);
+  if (!r) return OPTIMUS_EHIP;
+  for (int k = 0; k < count; ++k) {
+    r[k].at = (uintptr_t)tensors[k].param;
+    r[k].end = r[k].at + (uintptr_t)tensors[k].n * (tensors[k].param_dtype == OPTIMUS_BF16 ? 2 : 4);
   }
+  qsort(r, (size_t)count, sizeof(Range), compare_ranges);
+  bool meet = false;
+  for (int k = 1; k < count; ++k) meet = meet || r[k].at < r[k - 1].end;
+  if (r != few) free(r);
+  return meet ? OPTIMUS_EINVAL : OPTIMUS_OK;
+}
+
+int adamw_launch(const optimus_adamw_cfg* cfg, unsigned long long seed, const optimus_adamw_tensor* tensors, int count, hipStream_t st) {
   AdamwArgs a = {};
   a.b1 = (float)cfg->beta1; a.b2 = (float)cfg->beta2; a.c1 = (float)(1.0 - cfg->beta1); a.c2 = (float)(1.0 - cfg->beta2);
   a.eps = (float)cfg->eps; a.lr = (float)cfg->lr;
@@ -330,11 +329,11 @@ extern "C" int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_ad
     a.count = 0;
     while (k < count && a.count < kTensors) {
       const optimus_adamw_tensor& t = tensors[k];
-      const long long own = (t.n + kChunk - 1) / kChunk;   // at most 2^29
-      if (a.count > 0 && groups + own > (1ll << 30)) break;
+      const long long own = (t.n + kChunk - 1) / kChunk;   // at most 2^23
+      if (a.count > 0 && groups + own > kMostGroups) break;
       AdamwJob& j = a.job[a.count];
       j = {t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, (long long)t.n, 0, 0.f, 0.f, t.grad_parts, 0, 0};
-      j.key = mix(mix((unsigned)cfg->seed + 0x9E3779B1u * (unsigned)(k + 1)) ^ (unsigned)(cfg->seed >> 32));
+      j.key = mix(mix((unsigned)seed + 0x9E3779B1u * (unsigned)(k + 1)) ^ (unsigned)(seed >> 32));
       j.decay = t.weight_decay;
       j.shrink = (float)(cfg->lr * t.weight_decay);
       j.param_bf16 = t.param_dtype == OPTIMUS_BF16;
@@ -343,8 +342,17 @@ extern "C" int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_ad
       groups += (unsigned)own;
       ++k;
     }
-    adamw_kernel<<<groups, kThreads, 0, (hipStream_t)stream>>>(a);
+    adamw_kernel<<<groups, kThreads, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }
   return OPTIMUS_OK;
+}
+
+}  // namespace optimus
+
+using namespace optimus;
+
+extern "C" int optimus_adamw_step(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count, void* stream) {
+  if (const int rc = adamw_check(cfg, tensors, count)) return rc;
+  return adamw_launch(cfg, cfg->seed, tensors, count, (hipStream_t)stream);
 }

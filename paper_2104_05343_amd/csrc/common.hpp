@@ -239,6 +239,10 @@ int launch_ce_finalize(const void* logits, const int* labels, const float* stats
 int launch_ce_bwd(const void* logits, const int* labels, const float* lse, void* d_logits, float scale, const EndDesc& d,
                   hipStream_t stream);
 
+// AdamW (adamw.hip): what optimus_adamw_step checks, and the launches
+int adamw_check(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count);
+int adamw_launch(const optimus_adamw_cfg* cfg, unsigned long long seed, const optimus_adamw_tensor* tensors, int count, hipStream_t stream);
+
 // optimus_layer_fwd, optionally without its last product (used by the checkpointed stack's recomputation)
 int layer_forward(const optimus_layer_cfg* c, const optimus_layer_tensors* t, int i, int j, void* ws, size_t ws_bytes,
                   void* stream, bool skip_out);

@@ -19,6 +19,10 @@
 //
 // One GPU holds the whole q x q grid here, so these entry points run in grid mode only (all q*q devices' blocks, stage
 // by stage): the peers' blocks of every stage of every layer cannot stay resident in buffers that all layers share.
+// optimus_stack_bwd_adamw is the paper's "update immediately, then reuse" with AdamW as the consumer: a layer's step is enqueued behind
+// its backward pass and ahead of the next layer's, whose gradients then take the same buffer.
+#include <stdlib.h>
+
 #include "common.hpp"
 
 using namespace optimus;
@@ -95,6 +99,53 @@ bool params_ok(const optimus_layer_params& p) {
 bool grads_ok(const optimus_layer_grads& g) {
   return g.d_w_qkv && g.d_w_o && g.d_w1 && g.d_w2 && g.d_b_qkv && g.d_b_o && g.d_b1 && g.d_b2 && g.d_ln1_g && g.d_ln1_b &&
          g.d_ln2_g && g.d_ln2_b;
+}
+
+constexpr int kLayerTensors = 12;
+// elements of a layer's tensors: four matrices, then the vectors
+void layer_elements(const Dims& d, int64_t n[kLayerTensors]) {
+  const int64_t h = d.h, of[kLayerTensors] = {3 * h * h, h * h, 4 * h * h, 4 * h * h, 3 * h, h, 4 * h, h, h, h, h, h};
+  for (int k = 0; k < kLayerTensors; ++k) n[k] = of[k];
+}
+int64_t group_end(int64_t n) { return (n + 127) / 128 * 128; }
+void layer_adamw(const Dims& d, const optimus_layer_params& p, const optimus_layer_grads& g, const optimus_adamw_state& s, float decay,
+                 optimus_adamw_tensor out[kLayerTensors]) {
+  const void* param[kLayerTensors] = {p.w_qkv, p.w_o, p.w1, p.w2, p.b_qkv, p.b_o, p.b1, p.b2, p.ln1_g, p.ln1_b, p.ln2_g, p.ln2_b};
+  const float* grad[kLayerTensors] = {g.d_w_qkv, g.d_w_o, g.d_w1, g.d_w2, g.d_b_qkv, g.d_b_o, g.d_b1, g.d_b2, g.d_ln1_g, g.d_ln1_b, g.d_ln2_g, g.d_ln2_b};
+  const bool eight = s.m_scale || s.v_scale;
+  int64_t n[kLayerTensors], at = 0, master = 0;
+  layer_elements(d, n);
+  for (int k = 0; k < kLayerTensors; ++k) {
+    const bool matrix = k < 4;
+    optimus_adamw_tensor t = {};
+    t.param = const_cast<void*>(param[k]);
+    t.grad = grad[k];
+    t.m = s.m ? (char*)s.m + at * (eight ? 1 : 4) : nullptr;
+    t.v = s.v ? (char*)s.v + at * (eight ? 1 : 4) : nullptr;
+    t.m_scale = s.m_scale ? s.m_scale + at / 128 : nullptr;
+    t.v_scale = s.v_scale ? s.v_scale + at / 128 : nullptr;
+    t.master = matrix && s.master ? s.master + master : nullptr;
+    t.n = n[k];
+    t.param_dtype = matrix ? OPTIMUS_BF16 : OPTIMUS_FP32;
+    t.grad_dtype = OPTIMUS_FP32;
+    t.grad_parts = matrix ? 1 : d.q;   // a vector's partials [q][q][N/q]: the q of a grid column lie N apart
+    t.weight_decay = matrix ? decay : 0.f;
+    out[k] = t;
+    at += group_end(n[k]);
+    if (matrix) master += n[k];
+  }
+}
+
+struct UpdateJob {
+  const optimus_adamw_cfg* cfg;
+  const optimus_adamw_tensor* tensors;
+  hipStream_t stream;
+  int rc;
+};
+void update_layer(int layer, void* user) {
+  UpdateJob* j = (UpdateJob*)user;
+  if (j->rc) return;
+  j->rc = adamw_launch(j->cfg, j->cfg->seed + (unsigned long long)layer, j->tensors + (size_t)layer * kLayerTensors, kLayerTensors, j->stream);
 }
 
 }  // namespace
@@ -183,6 +234,50 @@ int optimus_stack_bwd(const optimus_layer_cfg* cfg, int n_layers, const optimus_
     g_in = g_out;
   }
   return OPTIMUS_OK;
+}
+
+int64_t optimus_stack_adamw_elements(const optimus_layer_cfg* cfg) {
+  Dims d;
+  if (dims_of(cfg, &d)) return 0;
+  int64_t n[kLayerTensors], total = 0;
+  layer_elements(d, n);
+  for (int k = 0; k < kLayerTensors; ++k) total += group_end(n[k]);
+  return total;
+}
+
+int optimus_stack_bwd_adamw(const optimus_layer_cfg* cfg, int n_layers, const optimus_layer_params* params,
+                            const optimus_adamw_state* states, const optimus_adamw_cfg* adamw, float weight_decay, void* param_grad,
+                            const void* d_out, const optimus_stack_buffers* buf, void* d_x, void* stream) {
+  Dims d;
+  int rc = dims_of(cfg, &d);
+  if (rc) return rc;
+  if (n_layers < 1 || n_layers > 65536) return OPTIMUS_ESHAPE;
+  if (!params || !states || !adamw || !param_grad || !d_out || !buf || !d_x || !buf->workspace || !buf->forward || !buf->backward ||
+      !buf->conjunction || !buf->checkpoint)
+    return OPTIMUS_EINVAL;
+  for (int l = 0; l < n_layers; ++l)
+    if (!params_ok(params[l])) return OPTIMUS_EINVAL;
+  optimus_layer_grads g = {};
+  carve_grads(d, param_grad, &g);
+  // both lists before anything is enqueued: the steps run from inside the backward pass
+  optimus_adamw_tensor* tensors = (optimus_adamw_tensor*)malloc(sizeof(optimus_adamw_tensor) * kLayerTensors * (size_t)n_layers);
+  optimus_layer_grads* grads = (optimus_layer_grads*)malloc(sizeof(optimus_layer_grads) * (size_t)n_layers);
+  rc = tensors && grads ? OPTIMUS_OK : OPTIMUS_EHIP;
+  if (!rc) {
+    for (int l = 0; l < n_layers; ++l) {
+      grads[l] = g;
+      layer_adamw(d, params[l], g, states[l], weight_decay, tensors + (size_t)l * kLayerTensors);
+    }
+    rc = adamw_check(adamw, tensors, kLayerTensors * n_layers);
+  }
+  if (!rc) {
+    UpdateJob job = {adamw, tensors, (hipStream_t)stream, OPTIMUS_OK};
+    rc = optimus_stack_bwd(cfg, n_layers, params, grads, d_out, buf, d_x, update_layer, &job, stream);
+    if (!rc) rc = job.rc;
+  }
+  free(tensors);
+  free(grads);
+  return rc;
 }
 
 }  // extern "C"

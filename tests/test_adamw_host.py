@@ -77,7 +77,7 @@ def _rc(cfg, tensors, count=None):
 @pytest.mark.parametrize("change,code", [
     (dict(param=None), opt.EINVAL), (dict(grad=None), opt.EINVAL), (dict(m=None), opt.EINVAL), (dict(v=None), opt.EINVAL),
     (dict(m_scale=4096), opt.EINVAL), (dict(v_scale=4096), opt.EINVAL), (dict(n=0), opt.ESHAPE), (dict(n=-5), opt.ESHAPE),
-    (dict(n=(1 << 40) + 1), opt.ESHAPE), (dict(param_dtype=2), opt.EDTYPE), (dict(grad_dtype=-1), opt.EDTYPE),
+    (dict(n=(1 << 34) + 1), opt.ESHAPE), (dict(param_dtype=2), opt.EDTYPE), (dict(grad_dtype=-1), opt.EDTYPE),
     (dict(grad_parts=0), opt.ESHAPE), (dict(master=32768), opt.EINVAL), (dict(weight_decay=float("nan")), opt.EINVAL),
     (dict(param=4098), opt.EINVAL), (dict(grad=8193), opt.EINVAL), (dict(m=12290), opt.EINVAL), (dict(v=16385), opt.EINVAL),
     (dict(param_dtype=opt.BF16, param=4097), opt.EINVAL), (dict(param_dtype=opt.BF16, master=32770), opt.EINVAL)])
@@ -104,3 +104,39 @@ def test_refuses_lists():
     assert _rc(cfg, [_tensor(), _tensor(param=4096 + 396)]) == opt.EINVAL
     many = [_tensor(param=1 << 20 | k << 12) for k in range(100)] + [_tensor(param=(1 << 20) + 399 & ~3)]
     assert _rc(cfg, many) == opt.EINVAL
+
+
+def test_stack_step_refusals():
+    """Before anything is enqueued, without a GPU."""
+    cfg = opt.LayerCfg(4, 64, 128, 4, 2, 1e-5, 1, opt.BF16, 0)
+    assert opt.stack_adamw_elements(cfg) == 12 * 128 * 128 + 13 * 128
+    assert opt.stack_adamw_elements(opt.LayerCfg(3, 64, 128, 4, 2, 1e-5, 1, opt.BF16, 0)) == 0
+    elements = opt.stack_adamw_elements(opt.LayerCfg(1, 8, 40, 1, 1, 1e-5, 1, opt.BF16, 0))   # vectors of 40 start 128 apart
+    assert elements == sum(-(-n // 128) * 128 for n in (4800, 1600, 6400, 6400, 120, 40, 160, 40, 40, 40, 40, 40))
+    adamw, place = opt.AdamwCfg(1e-3, 0.9, 0.99, 1e-8, 1, 0), iter(range(1 << 20, 1 << 40, 1 << 20))
+
+    def layer():
+        return opt.LayerParams(*[next(place) for _ in opt.LAYER_PARAM_FIELDS])
+
+    def rc(params, states=None, cfg=cfg, adamw=adamw, grad=next(place), buf=None):
+        pa = (opt.LayerParams * len(params))(*params)
+        states = states or [opt.AdamwState(next(place), next(place), None, None, None) for _ in params]
+        sa = (opt.AdamwState * len(states))(*states)
+        buf = buf or opt.StackBuffers(*[next(place) for _ in range(5)])
+        return opt.lib().optimus_stack_bwd_adamw(ctypes.byref(cfg), len(params), pa, sa, ctypes.byref(adamw), 0.1, grad, next(place), ctypes.byref(buf),
+                                                 next(place), None)
+
+    a, b = layer(), layer()
+    assert rc([a, b], cfg=opt.LayerCfg(3, 64, 128, 4, 2, 1e-5, 1, opt.BF16, 0)) == opt.ESHAPE
+    assert rc([a, b], adamw=opt.AdamwCfg(1e-3, 1.0, 0.99, 1e-8, 1, 0)) == opt.EINVAL
+    assert rc([a, b], grad=None) == opt.EINVAL
+    assert rc([a, a]) == opt.EINVAL                       # layers that share parameters
+    b.w2 = a.w1
+    assert rc([a, b]) == opt.EINVAL
+    b.w2 = None
+    assert rc([a, b]) == opt.EINVAL
+    assert rc([a], states=[opt.AdamwState(next(place), None, None, None, None)]) == opt.EINVAL
+    assert rc([a], states=[opt.AdamwState(next(place), next(place), next(place), None, None)]) == opt.EINVAL
+    assert rc([a], buf=opt.StackBuffers(next(place), None, next(place), next(place), next(place))) == opt.EINVAL
+    with pytest.raises(opt.OptimusError):
+        opt.stack_bwd_adamw(cfg, [a], [], adamw, 0.1, 4096, 4096, opt.StackBuffers(), 4096)

@@ -701,14 +701,25 @@ __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, f
   }
 }
 
-// 128-row workgroups from one per compute unit on.  The two forms add dK and dV (width 128) and the table's gradient up in different
-// orders, so the choice follows one device's matrices, whatever the launch covers.
-bool wide_form(const AttnFusedDesc& d) { return 2ll * ((d.s + 127) / 128) * d.nb * d.nh >= 256; }
+// 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64).  Width 64 keeps them where there
+// are documents or a cap: two workgroups a compute unit, each with barriers of its own, overlap one's arithmetic with the other's
+// products.  64 rows / 128 rows, us: width 128, causal, 16 matrices of 512 (256 workgroups of 64 rows) 25.3 / 25.3, 10 of 1000 without
+// a mask (320) 66.5 / 37.1, 16 of 4096 457 / 256; width 64, causal, 16 of 1024 (512) 23.4 / 25.2, 16 of 2048 (1024) 52.6 / 49.4, 16 of
+// 4096 157 / 153, with cap and slopes 212 / 233, with documents of 700 67 / 73.
+// The two forms add dK and dV (width 128) and the table's gradient up in different orders, so the choice follows one device's matrices,
+// whatever the launch covers.
+bool wide_form(const AttnBiasedDesc& b) {
+  const AttnFusedDesc& d = b.base;
+  const long long groups = 2ll * ((d.s + BLK - 1) / BLK) * d.nb * d.nh;
+  if (d.d == 64) return groups > 2 * num_cus() && !b.documents && !(b.cap > 0);
+  return groups > num_cus();
+}
 
 template <int D, bool CAP, int BIAS>
-void bwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
+void bwd_launch(const BiasedArgs& a, const AttnBiasedDesc& b, hipStream_t st) {
+  const AttnFusedDesc& d = b.base;
   const int nmat = d.nb * d.nh;
-  if (wide_form(d)) attn_biased_bwd_wide_kernel<D, CAP, BIAS><<<dim3(2 * nmat, a.ntiles, d.ndev), 512, 0, st>>>(a);
+  if (wide_form(b)) attn_biased_bwd_wide_kernel<D, CAP, BIAS><<<dim3(2 * nmat, a.ntiles, d.ndev), 512, 0, st>>>(a);
   else attn_biased_bwd_kernel<D, CAP, BIAS><<<dim3((unsigned)(2ll * a.ntiles * nmat), d.ndev), 256, 0, st>>>(a, a.ntiles, nmat);
 }
 
@@ -717,18 +728,18 @@ void bwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
 int launch_attn_biased_bwd_kernels(const BiasedArgs& given, const AttnBiasedDesc& b, hipStream_t st) {
   const AttnFusedDesc& d = b.base;
   BiasedArgs a = given;
-  a.ntiles = wide_form(d) ? (d.s + 127) / 128 : (d.s + BLK - 1) / BLK;
+  a.ntiles = wide_form(b) ? (d.s + 127) / 128 : (d.s + BLK - 1) / BLK;
   a.table_parts = b.d_table ? b.table_parts : nullptr;
   const int kind = (b.cap > 0 ? 3 : 0) + (b.table ? 2 : b.slopes ? 1 : 0);
   auto run = [&](auto width) {
     constexpr int D = decltype(width)::value;
     switch (kind) {
-      case 0: bwd_launch<D, false, 0>(a, d, st); break;
-      case 1: bwd_launch<D, false, 1>(a, d, st); break;
-      case 2: bwd_launch<D, false, 2>(a, d, st); break;
-      case 3: bwd_launch<D, true, 0>(a, d, st); break;
-      case 4: bwd_launch<D, true, 1>(a, d, st); break;
-      default: bwd_launch<D, true, 2>(a, d, st);
+      case 0: bwd_launch<D, false, 0>(a, b, st); break;
+      case 1: bwd_launch<D, false, 1>(a, b, st); break;
+      case 2: bwd_launch<D, false, 2>(a, b, st); break;
+      case 3: bwd_launch<D, true, 0>(a, b, st); break;
+      case 4: bwd_launch<D, true, 1>(a, b, st); break;
+      default: bwd_launch<D, true, 2>(a, b, st);
     }
   };
   if (d.d == 64) run(std::integral_constant<int, 64>());

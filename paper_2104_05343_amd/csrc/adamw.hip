@@ -222,7 +222,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
     const float gk = a.grad_scale ? g[k] * gs : g[k];
     m[k] = a.b1 * m[k] + a.c1 * gk;
     v[k] = a.b2 * v[k] + a.c2 * (gk * gk);
-    w[k] = w[k] - (step_size * (m[k] / (sqrtf(v[k]) * root + a.eps)) + shrink * w[k]);
+    // root and reciprocal of one unit in the last place: a 4e-7th of the update, which w's own rounding hides (exactly rounded ones are
+    // 25 operations more, and with 8-bit moments and two hashes an element the arithmetic is what counts)
+    w[k] = w[k] - (step_size * (m[k] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[k]) * root + a.eps)) + shrink * w[k]);
   }
 
   unsigned hash[8];

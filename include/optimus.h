@@ -251,7 +251,8 @@ int optimus_attention_fused_bwd_static(const void* qkv, const void* attn, const 
  *   with documents where documents[t] != documents[u], or either is negative: a token of a negative document is padding;
  *   where the table's number is -1e30 or less (-infinity included).
  * A row without a pair has attn 0, lse -infinity and gradients 0.  What qkv, attn and d_attn hold in rows of padding is not looked at,
- * NaN included; their rows of attn and d_qkv are written as zeros.
+ * NaN included; their rows of attn and d_qkv are written as zeros.  (Other pairs that are left out have weight zero, and zero times
+ * an infinity or NaN is NaN: as without changes, the values of tokens that are not padding are taken to be finite.)
  * bucket(n) of the distance n = t - u: a side has `side` buckets: buckets, or buckets / 2 with two_sided; near = side / 2.  Distances
  * 0 .. near - 1 have a bucket each; bucket near + k begins at the first whole number not below near * (max_distance / near)^(k / (side -
  * near)); the last has no end.  n < 0 (a later key): bucket 0, or with two_sided side + bucket(-n).  2 <= side, even `buckets` with

@@ -282,3 +282,43 @@ def test_captured_and_on_another_stream():
     opt.attention_biased_bwd(r.dQKV, r.O, r.L, r.dO, r.G, r.T, r.b, r.s, r.h, r.n, r.q, 0, 0, True, opt.BF16, r.bias, r.ws, stream=st)
     st.synchronize()
     assert not torch.isnan(r.G).any()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_packed_sequence(d):
+    """A sequence of 70001 tokens: documents of about 80 are attentions of their own, whose oracle is small."""
+    s, lengths, rng = 70001, [], np.random.default_rng(9)
+    while sum(lengths) < s:
+        lengths.append(int(rng.integers(1, 160)))
+    lengths[-1] -= sum(lengths) - s
+    docs = np.repeat(np.arange(len(lengths)), lengths).astype(np.int32)[None, :]
+    ends = np.cumsum(lengths)
+    for k in (100, 500):   # two documents are padding
+        docs[0, ends[k] - lengths[k]:ends[k]] = -1
+    r = Run(1, s, d, 1, 1, True, docs=docs, slopes=True).go()
+    O, G, L = (to_host(x).reshape(s, -1).astype(np.float64) for x in (r.O, r.G, r.L))
+    assert not np.isnan(O).any() and not np.isnan(G).any()
+    for k in list(range(0, len(lengths), 7)) + [100, 500, len(lengths) - 1]:
+        rows = slice(ends[k] - lengths[k], ends[k])
+        Q, K, V = (r.qkv[rows, c * d:(c + 1) * d].astype(np.float64) for c in range(3))
+        if docs[0, rows.start] < 0:
+            assert not O[rows].any() and not G[rows].any() and np.all(np.isneginf(L[rows]))
+            continue
+        want, lse, P = oab.forward(Q, K, V, causal=True, slope=float(r.slopes[0]))
+        dO = r.d_attn[rows].astype(np.float64)
+        assert np.all(np.abs(L[rows, 0] - lse) <= 1e-5 * np.maximum(1, np.abs(lse)))
+        assert np.all(np.abs(O[rows] - want) <= HALF * (1.01 * np.abs(want) + P @ np.abs(V)) + FP32 * (P @ np.abs(V)))
+        dQ, dK, dV, _, P, dS = oab.backward(Q, K, V, dO, O[rows], L[rows, 0], causal=True, slope=float(r.slopes[0]))
+        for c, (w, size) in enumerate(((dQ, np.abs(dS) @ np.abs(K) / np.sqrt(d)), (dK, np.abs(dS).T @ np.abs(Q) / np.sqrt(d)), (dV, P.T @ np.abs(dO)))):
+            # (dS is a difference: its fp32 error is one of the two terms', which are of the size of sqrt(d) values)
+            assert np.all(np.abs(G[rows, c * d:(c + 1) * d] - w) <= HALF * (1.01 * np.abs(w) + size) + 100 * FP32)
+
+
+def test_bits_do_not_depend_on_the_launch():
+    """Few and many matrices take kernels of 64 and of 128 rows: the forward's bits are the same."""
+    one = Run(1, 1100, 128, 1, 1, True, **KINDS["cap+slopes"])
+    many = Run(64, 1100, 128, 1, 1, True, **KINDS["cap+slopes"])
+    many.dQKV[:one.dQKV.numel()].copy_(one.dQKV)
+    one.forward(), many.forward()
+    torch.cuda.synchronize()
+    assert torch.equal(one.O, many.O[:one.O.numel()]) and torch.equal(one.L, many.L[:one.L.numel()])

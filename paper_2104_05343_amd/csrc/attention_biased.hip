@@ -255,7 +255,7 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
   f.s = d.s; f.nh = d.nh; f.ld = d.ld; f.ldo = d.ldo;
   f.dev_qkv = d.dev_qkv; f.dev_attn = d.dev_attn; f.dev_vec = (long long)d.nb * d.nh * d.s;
   f.scale = 1.0f / sqrtf((float)d.d);
-  f.scale_log2 = f.scale * LOG2E;
+  f.scale_log2 = (float)(1.4426950408889634 / sqrt((double)d.d));
   a.nb = d.nb; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal; a.nblk = (d.s + BLK - 1) / BLK;
   if (b.cap > 0) {
     const double in = 1.0 / (sqrt((double)d.d) * b.cap);
@@ -265,6 +265,9 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
     for (int k = 0; k < 5; ++k, power *= in * in) a.tanh_of[k] = (float)(of[k] * power);
     a.cap_exp = (float)(2.0 * in * 1.4426950408889634);
     a.cap_small = (float)(0.25 / in);
+    a.weight_lo = (float)(b.cap * 1.4426950408889634 * (in / (double)a.tanh_of[0]) - (double)a.cap_log2);
+  } else {
+    a.weight_lo = (float)(1.4426950408889634 / sqrt((double)d.d) - (double)f.scale_log2);
   }
   a.slopes = b.slopes; a.table = b.table; a.documents = b.documents; a.prefix = b.prefix;
   a.blocks = (const i32x4_t*)b.blocks; a.table_parts = b.table_parts;

@@ -13,7 +13,7 @@ namespace {
 constexpr int kSkew = 41;   // places of a key: 39 diagonals, zeros behind them; of the halves' rows, four apart, in different banks
 constexpr int kSkewed = 8 * kSkew;
 struct BucketSums {
-  float own[2], far_pos, far_neg;
+  double own[2], far_pos, far_neg;   // (a few additions a tile, each tile a tree of fp32 ones)
   int lo[2], hi[2];      // distances of the lane's buckets
   int far, back;
   float* skewed;         // LDS of the wavefront: [8][kSkew], and [64] behind it
@@ -21,7 +21,7 @@ struct BucketSums {
   __device__ __forceinline__ void init(const BiasedArgs& a, float* lds, const int* first_, int lane) {
     skewed = lds;
     line = lds + kSkewed;
-    own[0] = own[1] = far_pos = far_neg = 0.f;
+    own[0] = own[1] = far_pos = far_neg = 0.0;
     far = a.far; back = a.two_sided ? a.far : 0;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -182,6 +182,9 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   const bool table_grad = BIAS == 2 && a.table_parts;
   if (BIAS == 2) sums.init(a, lds.sums[wave], lds.bias.first, lane);
   const float lse2 = query < s && qdoc >= 0 ? lse2_of(lse) : INFINITY;
+  // The table's gradient is an fp32 sum: there the part of lse * log2(e) that its rounding loses is kept, in terms of the last place of
+  // a number around 20 a relative error of P.  (lse2 infinite: its row has no P.)
+  const float lse2_lo = BIAS == 2 && lse2 < 1e30f ? fmaf(lse, LOG2E, -lse2) + lse * 1.92596299e-8f : 0.f;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     qf[ks] = zero_if(qdoc < 0, qf[ks]);
@@ -218,7 +221,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
         const int k0 = kbase + t2 * 32, dist0 = query - k0 - 4 * g;
         // the table's gradient wants dS before the tanh's part: that waits in `part` then; else it goes into dP first
         f32x16 part;
-        if (CAP) tanh16(sacc, a);
+        if (CAP) tanh16<BIAS == 2>(sacc, a);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           pacc[r] -= delta;
@@ -227,16 +230,17 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
         }
         const int lo = q0 - k0 - 31;
         if (masked || !plain_tile<BIAS>(bias, lo, lo + 62)) {
-          any16<CAP, BIAS, -1>(sacc, a, bias, dist0, k0 + 4 * g, limit, &lds.key_docs[wave][t2 * 32 + 4 * g], qdoc);
+          any16<CAP, BIAS, -1, BIAS == 2>(sacc, a, bias, dist0, k0 + 4 * g, limit, &lds.key_docs[wave][t2 * 32 + 4 * g], qdoc, lse2, lse2_lo);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(sacc[r] - lse2) * pacc[r];  // dS^T
+          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(BIAS == 2 ? sacc[r] : sacc[r] - lse2) * pacc[r];  // dS^T
         } else {
           float w, c;
           plain_weights<CAP, BIAS>(a, bias, lo, w, c);
           plain16<CAP, BIAS, -1>(sacc, a, bias, dist0, lo);
-          c -= lse2;
+          c -= BIAS == 2 ? lse2_lo : lse2;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], w, c)) * pacc[r];
+          for (int r = 0; r < 16; ++r)
+            sacc[r] = __builtin_amdgcn_exp2f(BIAS == 2 ? fmaf(sacc[r], w, -lse2) + fmaf(sacc[r], a.weight_lo, c) : fmaf(sacc[r], w, c)) * pacc[r];
         }
         if (BIAS == 2 && table_grad) sums.add(sacc, lo, g, lane, a.buckets > 64);
         if (CAP && BIAS == 2) {
@@ -265,8 +269,8 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   }
   if (BIAS == 2 && table_grad) {   // (in the wavefront's own place)
     sums.finish(a, lane);
-    lds.sums[wave][lane] = sums.own[0];
-    lds.sums[wave][64 + lane] = sums.own[1];
+    lds.sums[wave][lane] = (float)sums.own[0];
+    lds.sums[wave][64 + lane] = (float)sums.own[1];
   }
   __syncthreads();
   if (BIAS == 2 && table_grad && tid < a.buckets) {
@@ -680,13 +684,13 @@ __global__ __launch_bounds__(512, 2) void attn_biased_bwd_wide_kernel(BiasedArgs
   }
 }
 
-// d_table[device][head][bucket]: the parts of the head's matrices and tiles, added in that order by 1024 / 128 threads a bucket, then
-// theirs.
+// d_table[device][head][bucket]: the parts of the head's matrices and tiles, eight threads a bucket in that order, then theirs, in 64
+// bits: thousands of parts of either sign.
 __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, float* d_table) {
-  __shared__ float sums[1024];
+  __shared__ double sums[1024];
   const int head = blockIdx.x, dev = blockIdx.y, b = threadIdx.x & 127, slice = threadIdx.x >> 7;
   const int n = a.nb * a.ntiles;
-  float sum = 0.f;
+  double sum = 0.0;
   if (b < a.buckets)
     for (int p = slice; p < n; p += 8) {
       const int seq = p / a.ntiles, tile = p % a.ntiles;
@@ -697,7 +701,7 @@ __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, f
   if (slice == 0 && b < a.buckets) {
 #pragma unroll
     for (int k = 1; k < 8; ++k) sum += sums[k * 128 + b];
-    d_table[((long long)dev * a.f.nh + head) * a.buckets + b] = sum;
+    d_table[((long long)dev * a.f.nh + head) * a.buckets + b] = (float)sum;
   }
 }
 

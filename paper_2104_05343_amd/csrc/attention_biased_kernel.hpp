@@ -28,6 +28,7 @@ struct BiasedArgs {
   int nb, q, dev0;           // sequences of a device, grid, first device of the launch
   int causal, nblk;          // nblk: blocks of 64 tokens of a sequence
   float cap_log2;            // cap * log2(e)
+  float weight_lo;           // what the rounding of the scores' weight (and of the tanh's first coefficient) loses
   float cap_exp;             // 2 log2(e) / (sqrt(d) cap)
   float tanh_of[5];          // coefficients of tanh(v / (sqrt(d) cap)) at v, v^3, .. v^9
   float cap_small;           // Q K^T below which the polynomial is taken: cap sqrt(d) / 4
@@ -166,6 +167,9 @@ __device__ constexpr int slot(int r) { return 8 * (r >> 2) + (r & 3); }
 
 // v = Q K^T -> tanh(v / (sqrt(d) cap)).  Below a quarter the odd polynomial up to the ninth power, in v itself (relative error 1e-8);
 // above, 1 - 2 / (exp(2x) + 1), whose absolute error of a unit in the last place of 1 is a relative one of 5e-7 of such a score.
+// FINE (where sums of dS are an fp32 result): the polynomial for each score below a quarter, and the reciprocal refined by a Newton step,
+// so that the scores' error is that of their own last place.
+template <bool FINE = false>
 __device__ __forceinline__ void tanh16(f32x16& v, const BiasedArgs& a) {
   float mx = 0.f;
 #pragma unroll
@@ -178,7 +182,18 @@ __device__ __forceinline__ void tanh16(f32x16& v, const BiasedArgs& a) {
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = fmaf(-2.0f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v[r] * a.cap_exp) + 1.0f), 1.0f);
+    for (int r = 0; r < 16; ++r) {
+      const float e1 = __builtin_amdgcn_exp2f(v[r] * a.cap_exp) + 1.0f;
+      float q = __builtin_amdgcn_rcpf(e1);
+      if (FINE) {
+        q = e1 < 1e30f ? fmaf(fmaf(-e1, q, 1.0f), q, q) : q;   // (infinity times zero)
+        const float y = v[r] * v[r];
+        const float near = v[r] * fmaf(y, fmaf(y, fmaf(y, fmaf(y, a.tanh_of[4], a.tanh_of[3]), a.tanh_of[2]), a.tanh_of[1]), a.tanh_of[0]);
+        v[r] = fabsf(v[r]) < a.cap_small ? near : fmaf(-2.0f, q, 1.0f);
+      } else {
+        v[r] = fmaf(-2.0f, q, 1.0f);
+      }
+    }
   }
 }
 
@@ -249,9 +264,11 @@ __device__ __forceinline__ void plain16(f32x16& v, const BiasedArgs& a, const Bi
   }
 }
 // Any tile: log2(e) times the score, -infinity where the pair is left out: the other token's place (at + slot(r)) behind `bound`
-// (SIGN < 0) or ahead of it, or of another document than `doc`.  docs: LDS, the other tokens' from the lane's slot 0 on.
-template <bool CAP, int BIAS, int SIGN>
-__device__ __forceinline__ void any16(f32x16& v, const BiasedArgs& a, const Bias& b, int dist0, int at, int bound, const int* docs, int doc) {
+// (SIGN < 0) or ahead of it, or of another document than `doc`.  docs: LDS, the other tokens' from the lane's slot 0 on.  FINE: hi + lo
+// is taken off the score, hi before the bias: with a row's log-sum-exp what is rounded then is small where it counts.
+template <bool CAP, int BIAS, int SIGN, bool FINE = false>
+__device__ __forceinline__ void any16(f32x16& v, const BiasedArgs& a, const Bias& b, int dist0, int at, int bound, const int* docs, int doc,
+                                      float hi = 0.f, float lo = 0.f) {
   asm volatile("");   // a branch, not selects: taken by few tiles, and seven operations a score
   const float w = CAP ? a.cap_log2 : a.f.scale_log2;
   const int reach = bound - at;
@@ -262,9 +279,12 @@ __device__ __forceinline__ void any16(f32x16& v, const BiasedArgs& a, const Bias
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 4 * c + e, dist = dist0 + SIGN * slot(r);
-      float x = v[r] * w;
+      float x = FINE ? fmaf(v[r], w, -hi) : v[r] * w;
       if (BIAS == 1) x = fmaf(-b.slope2, fabsf((float)dist), x);
-      if (BIAS == 2) x += b.at0[min(max(dist, -b.far), b.far)];
+      if (BIAS == 2) {
+        const float bias = b.at0[min(max(dist, -b.far), b.far)];
+        x += FINE ? fmaf(v[r], a.weight_lo, bias - lo) : bias;
+      }
       const bool out = (SIGN < 0 ? slot(r) > reach : slot(r) < reach) | (other[e] != doc) | (doc < 0);
       v[r] = out ? -INFINITY : x;
     }

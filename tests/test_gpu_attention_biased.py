@@ -205,6 +205,13 @@ def test_masking_tables():
         assert np.all(np.isneginf(to_host(r.L).reshape(2, 2, 150)[:, 1])) and np.all(np.isneginf(to_host(r.L).reshape(2, 2, 150)[:, 0, :3]))
 
 
+@pytest.mark.parametrize("cap", [1e-3, 0.02, 1e30])
+def test_caps_at_the_ends_of_their_range(cap):
+    """Scores all at the cap, and a cap that changes nothing."""
+    Run(2, 150, 256, 2, 1, True, cap=cap, stretch=4.0).go().check()
+    Run(2, 150, 128, 2, 1, False, cap=cap, stretch=4.0, **dict(BUCKETS, buckets=16)).go().check()
+
+
 def test_without_changes_it_is_the_fused_attention():
     """No cap, no bias, no mask: what the attention without changes computes, to its own accuracy."""
     r = Run(4, 300, 256, 4, 2, True).go().check()

@@ -446,7 +446,7 @@ int optimus_cross_entropy2d_bwd(const void* logits, const int32_t* labels, const
  *   up or down at random in proportion to the place between the two neighbours (to nearest, updates below half a step would be lost).
  * Moments: fp32 m, v [n]; or, with m_scale and v_scale, 8 bits: e4m3 numbers (OCP: 1 sign, 4 exponent, 3 mantissa bits), element k
  *   standing for number * 2^(scale[k / 128] - 127) (scale 255: NaN), rounded at random like the weights; a v above zero stays above zero.
- *   Zeroed memory is a valid state of either kind.  A group with a gradient that is not finite turns NaN as a whole.
+ *   Zeroed memory is a valid state of either kind.  A group with a gradient whose square is not finite in fp32 turns NaN as a whole.
  * The random bits are a hash of (seed, step, index in `tensors`, element): the same call gives the same bits.
  * grad_scale, lr_on_device, step_on_device: NULL, or device memory that is read when the step runs, in place of 1, lr and step: what
  *   a captured step changes between its replays.
@@ -464,7 +464,7 @@ typedef struct {
   float weight_decay;
 } optimus_adamw_tensor;
 typedef struct {
-  double lr, beta1, beta2, eps;         /* 0 <= beta < 1, eps > 0 */
+  double lr, beta1, beta2, eps;         /* 0 <= beta < 1, eps > 0 (in fp32) */
   int64_t step;                         /* 1 in the first step */
   uint64_t seed;
   const float* grad_scale; const float* lr_on_device; const int64_t* step_on_device;

@@ -172,6 +172,11 @@ __device__ __forceinline__ u32x2u pack8(const float x[8], const unsigned dither[
   return w;
 }
 
+// EXACT: root and division are rounded exactly.  Otherwise root and reciprocal are of one unit in the last place, a 4e-7th of the update,
+// which w's own rounding hides (25 operations less, and with 8-bit moments and two hashes an element the arithmetic is what counts).  They
+// take numbers below 2^-126 for 0, so that a root below 2^-63 is lost: nothing beside an eps from 1e-15 on, a division by eps alone
+// beside a smaller one.
+template <bool EXACT>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
 #pragma clang fp contract(off)
   // the tensor of this workgroup: the last one that does not start behind it
@@ -222,9 +227,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
     const float gk = a.grad_scale ? g[k] * gs : g[k];
     m[k] = a.b1 * m[k] + a.c1 * gk;
     v[k] = a.b2 * v[k] + a.c2 * (gk * gk);
-    // root and reciprocal of one unit in the last place: a 4e-7th of the update, which w's own rounding hides (exactly rounded ones are
-    // 25 operations more, and with 8-bit moments and two hashes an element the arithmetic is what counts)
-    w[k] = w[k] - (step_size * (m[k] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[k]) * root + a.eps)) + shrink * w[k]);
+    const float move = EXACT ? m[k] / (sqrtf(v[k]) * root + a.eps) : m[k] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[k]) * root + a.eps);
+    w[k] = w[k] - (step_size * move + shrink * w[k]);
   }
 
   unsigned hash[8];
@@ -296,7 +300,7 @@ int check_tensor(const optimus_adamw_tensor& t) {
 int adamw_check(const optimus_adamw_cfg* cfg, const optimus_adamw_tensor* tensors, int count) {
   if (!cfg || !tensors) return OPTIMUS_EINVAL;
   if (count < 1 || count > (1 << 20)) return OPTIMUS_ESHAPE;
-  if (!isfinite(cfg->lr) || !(cfg->beta1 >= 0 && cfg->beta1 < 1) || !(cfg->beta2 >= 0 && cfg->beta2 < 1) || !(cfg->eps > 0) || !isfinite(cfg->eps) ||
+  if (!isfinite(cfg->lr) || !(cfg->beta1 >= 0 && cfg->beta1 < 1) || !(cfg->beta2 >= 0 && cfg->beta2 < 1) || !((float)cfg->eps > 0) || !isfinite(cfg->eps) ||
       (cfg->step < 1 && !cfg->step_on_device))
     return OPTIMUS_EINVAL;
   for (int k = 0; k < count; ++k)
@@ -344,7 +348,8 @@ int adamw_launch(const optimus_adamw_cfg* cfg, unsigned long long seed, const op
       groups += (unsigned)own;
       ++k;
     }
-    adamw_kernel<<<groups, kThreads, 0, st>>>(a);
+    if (a.eps < 1e-15f) adamw_kernel<true><<<groups, kThreads, 0, st>>>(a);   // (a kernel of its own: one that chose took 520 us for 486)
+    else adamw_kernel<false><<<groups, kThreads, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }
   return OPTIMUS_OK;

@@ -86,7 +86,7 @@ def test_refuses_tensors(change, code):
 
 
 @pytest.mark.parametrize("change", [dict(lr=float("inf")), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=float("nan")), dict(eps=0.0),
-                                    dict(eps=float("inf")), dict(step=0)])
+                                    dict(eps=float("inf")), dict(eps=1e-50), dict(step=0)])
 def test_refuses_settings(change):
     cfg = opt.AdamwCfg(1e-3, 0.9, 0.99, 1e-8, 1, 0)
     for k, v in change.items():

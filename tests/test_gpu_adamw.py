@@ -167,6 +167,24 @@ def test_zeroed_state_and_zero_gradients():
         assert torch.equal(c.param, before) and not c.m.any() and not c.v.any()
 
 
+@pytest.mark.parametrize("eps", [1e-30, 1e-42])
+def test_an_eps_next_to_zero(eps):
+    """Gradients whose v is below the smallest normal number, 2^-126: the first step is still lr * sign(g), as long as g^2 keeps its digits.
+    From 10^-19.5 on v is at least 1e-41; its two roundings of at most half of 2^-149 are 7e-5 of that, half as much of its root.  The
+    decay and w take four roundings more.  A gradient of zero leaves its weight alone."""
+    n = 1000
+    g = np.logspace(-19.5, -16.5, n).astype(np.float32) * np.where(np.arange(n) % 3, 1, -1).astype(np.float32)
+    g[::10] = 0
+    w = torch.linspace(-1, 1, n, device=DEV)
+    old, m, v = to_host(w).astype(np.float64), torch.zeros_like(w), torch.zeros_like(w)
+    cfg = opt.AdamwCfg(H["lr"], H["beta1"], H["beta2"], eps, 1, 0)
+    opt.adamw_step(cfg, opt.make_adamw_tensors([dict(param=w, grad=torch.from_numpy(g).to(DEV), m=m, v=v)]))
+    torch.cuda.synchronize()
+    want = oad.step(old, np.zeros(n), np.zeros(n), g[None].astype(np.float64), **dict(H, eps=eps), t=1, decay=0.0)[0]
+    assert np.all(np.abs(to_host(w) - want) <= H["lr"] * 4e-5 + 2.0 ** -22 * (np.abs(old) + H["lr"]))
+    assert np.array_equal(to_host(w)[::10], old[::10].astype(np.float32))
+
+
 def test_gradient_that_is_not_finite():
     """fp32: its own element turns NaN or infinite.  8 bits: its group of 128; every other weight, moment and scale keeps its value."""
     for bad in (float("nan"), float("inf"), -float("inf")):

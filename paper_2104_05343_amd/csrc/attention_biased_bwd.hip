@@ -707,10 +707,10 @@ __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, f
 
 // 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64).  Width 64 keeps them where there
 // are documents, a cap or a table's gradient: two workgroups a compute unit, each with barriers of its own, overlap one's arithmetic
-// with the other's products.  64 rows / 128 rows, us: width 128, causal, 16 matrices of 512 (256 workgroups of 64 rows) 25.3 / 25.3, 10 of 1000 without
-// a mask (320) 66.5 / 37.1, 16 of 4096 457 / 256; width 64, causal, 16 of 1024 (512) 23.4 / 25.2, 16 of 2048 (1024) 52.6 / 49.4, 16 of
-// 4096 157 / 153, with cap and slopes 212 / 233, with documents of 700 67 / 73; with the
-// table's gradient 64 of 2048 without a mask 379 / 394, with it 236 / 249.
+// with the other's products.  64 rows / 128 rows, us: width 128, causal, 16 matrices of 512 (256 workgroups of 64 rows) 25.3 / 25.3, 10
+// of 1000 without a mask (320) 66.5 / 37.1, 16 of 4096 457 / 256; width 64, causal, 16 of 1024 (512) 23.4 / 25.2, 16 of 2048 (1024)
+// 52.6 / 49.4, 16 of 4096 157 / 153, with cap and slopes 212 / 233, with documents of 700 67 / 73; with the table's gradient 64 of 2048
+// without a mask 379 / 394, with it 236 / 249.
 // The two forms add dK and dV (width 128) and the table's gradient up in different orders, so the choice follows one device's matrices,
 // whatever the launch covers.
 bool wide_form(const AttnBiasedDesc& b) {

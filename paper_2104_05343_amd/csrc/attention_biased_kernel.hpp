@@ -8,10 +8,11 @@
 // Backward: P = exp(S - lse), dS = P (dO V^T - rowsum(dO * O)); the table's gradient is the sum of dS over a bucket's pairs; from
 // there on dS (1 - tanh^2).
 //
-// What the additions cost beside the 32 to 64 clk a matrix instruction takes: the tanh 7 operations a score (the largest of the tile among them) while a tile's scores stay
-// below a quarter of the cap (odd polynomial), else an exponential and a reciprocal; slopes 2; the table nothing but one fused
-// multiply-add where a whole tile lies in the last bucket, one LDS read where it does not.  Blocks of keys that share no document with
-// the workgroup's rows are not loaded: documents packed one after the other cost the sum of their squares.
+// What the additions cost beside the 32 to 64 clk a matrix instruction takes: the tanh 7 operations a score (the largest of the tile
+// among them) while a tile's scores stay below a quarter of the cap (odd polynomial), else an exponential and a reciprocal; slopes 2;
+// the table nothing but one fused multiply-add where a whole tile lies in the last bucket, one LDS read where it does not.  Blocks of
+// keys that share no document with the workgroup's rows are not loaded: documents packed one after the other cost the sum of their
+// squares.
 #pragma once
 #include "attention_fused_kernel.hpp"
 

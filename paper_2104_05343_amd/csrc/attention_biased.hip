@@ -7,9 +7,9 @@ namespace {
 
 // Forward.  NRG: row groups of 32 queries per workgroup, as in the attention without changes.  Two workgroups of 128 rows a compute unit
 // of width 64, where 128 registers a lane are enough: with slopes a dozen would be spilled (16 matrices of 4096, causal, 76 us; one
-// workgroup 63).
-template <int D, int NRG, bool CAP, int BIAS>
-__global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 && BIAS != 1 ? 4 : NRG == 4 || D == 64 ? 2 : 1) void attn_biased_fwd_kernel(BiasedArgs a) {
+// workgroup 63), with a cap beyond 64 eight.  (With a smaller one and a table eight are.)
+template <int D, int NRG, int CAP, int BIAS>
+__global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 && BIAS != 1 && CAP != 2 ? 4 : NRG == 4 || D == 64 ? 2 : 1) void attn_biased_fwd_kernel(BiasedArgs a) {
   constexpr int KS = D / 16, DT = D / 32, BQ = NRG * 32, AHEAD = D == 64 ? 1 : 2;
   __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][PAIR * D];  // [stage][K, V][pair tile]
   __shared__ BiasLds<BIAS> bias_lds;
@@ -101,8 +101,8 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 && BIAS != 1 ? 4 : N
                                  sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
                                });
       if (CAP) {
-        tanh16(sacc[0], a);
-        tanh16(sacc[1], a);
+        tanh16<CAP>(sacc[0], a);
+        tanh16<CAP>(sacc[1], a);
       }
       const int dist0 = query - kbase - 4 * g, lo = q0 - kbase - (BLK - 1), hi = q0 + 31 - kbase;
       float w = 1.0f, c = 0.f;
@@ -258,7 +258,11 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
   f.scale_log2 = (float)(1.4426950408889634 / sqrt((double)d.d));
   a.nb = d.nb; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal; a.nblk = (d.s + BLK - 1) / BLK;
   if (b.cap > 0) {
-    const double in = 1.0 / (sqrt((double)d.d) * b.cap);
+    const double inverse = 1.0 / (sqrt((double)d.d) * b.cap);
+    int shift = 0;
+    if (cap_form(b) == 2) frexp(inverse, &shift);
+    const double in = ldexp(inverse, -shift);   // u / x
+    a.cap_pre = (float)ldexp(1.0, shift);
     a.cap_log2 = (float)(b.cap * 1.4426950408889634);
     const double of[5] = {1.0, -1.0 / 3, 2.0 / 15, -17.0 / 315, 62.0 / 2835};
     double power = in;
@@ -280,7 +284,7 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
   return a;
 }
 
-template <int D, bool CAP, int BIAS>
+template <int D, int CAP, int BIAS>
 void fwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
   // 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64): a wavefront has the same loop
   // either way and a SIMD to itself.  64 rows / 128 rows, us: width 128, causal with a cap, 16 matrices of 1024 (256 workgroups of 64
@@ -308,20 +312,9 @@ int launch_attn_biased_fwd(const AttnBiasedDesc& b, hipStream_t st) {
   if (!desc_ok(b) || !d.qkv || !d.attn || !d.lse) return OPTIMUS_ESHAPE;
   const BiasedArgs a = make_args(b);
   launch_attn_biased_prepare(a, d.d, false, d.nb * d.nh, d.ndev, st);
-  const int kind = (b.cap > 0 ? 3 : 0) + (b.table ? 2 : b.slopes ? 1 : 0);
-  auto run = [&](auto width) {
-    constexpr int D = decltype(width)::value;
-    switch (kind) {
-      case 0: fwd_launch<D, false, 0>(a, d, st); break;
-      case 1: fwd_launch<D, false, 1>(a, d, st); break;
-      case 2: fwd_launch<D, false, 2>(a, d, st); break;
-      case 3: fwd_launch<D, true, 0>(a, d, st); break;
-      case 4: fwd_launch<D, true, 1>(a, d, st); break;
-      default: fwd_launch<D, true, 2>(a, d, st);
-    }
-  };
-  if (d.d == 64) run(std::integral_constant<int, 64>());
-  else run(std::integral_constant<int, 128>());
+  with_kind(b, [&](auto width, auto cap, auto bias) {
+    fwd_launch<decltype(width)::value, decltype(cap)::value, decltype(bias)::value>(a, d, st);
+  });
   return hip_launch_status();
 }
 

@@ -116,7 +116,7 @@ struct DkvLds {
 // log-sum-exp of a row -> what is subtracted from its scores.  Of a row without pairs +infinity, which makes every P of it zero.
 __device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
 
-template <int D, int NRG, bool CAP, int BIAS>
+template <int D, int NRG, int CAP, int BIAS>
 __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG, BIAS>& lds, int tile, int mat, int dev) {
   constexpr int KS = D / 16, DT = D / 32, BQ = NRG * 32;
   const FusedArgs& f = a.f;
@@ -221,7 +221,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
         const int k0 = kbase + t2 * 32, dist0 = query - k0 - 4 * g;
         // the table's gradient wants dS before the tanh's part: that waits in `part` then; else it goes into dP first
         f32x16 part;
-        if (CAP) tanh16<BIAS == 2>(sacc, a);
+        if (CAP) tanh16<CAP, BIAS == 2>(sacc, a);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           pacc[r] -= delta;
@@ -297,10 +297,10 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
 // 32 x 32 scores S (rows: queries q0 .., columns: keys) and dP = dO V^T in accumulators -> P and dS (the gradient of Q K^T) in their place.
 // l, d, docs: of the 32 queries.  (dP - rowsum) (1 - tanh^2) comes before the scores, so that the tanh needs no place of its own.
 // first: query from which on the key is seen.
-template <bool CAP, int BIAS>
+template <int CAP, int BIAS>
 __device__ __forceinline__ void biased_dkv_scores(f32x16& sacc, f32x16& pacc, const float* l, const float* d, const int* docs, int q0, int k0, int key,
                                                   int first, int kdoc, bool masked, const BiasedArgs& a, const Bias& bias, int g) {
-  if (CAP) tanh16(sacc, a);
+  if (CAP) tanh16<CAP>(sacc, a);
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const float4 d4 = *(const float4*)(d + 8 * c + 4 * g);
@@ -334,7 +334,7 @@ __device__ __forceinline__ void biased_dkv_scores(f32x16& sacc, f32x16& pacc, co
   }
 }
 
-template <int D, int NRG, bool CAP, int BIAS>
+template <int D, int NRG, int CAP, int BIAS>
 __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, NRG, BIAS>& lds, int tile, int mat, int dev) {
   constexpr int KS = D / 16, DT = D / 32, BKW = NRG * 32;
   const FusedArgs& f = a.f;
@@ -507,7 +507,7 @@ struct WideDkvLds {
   alignas(16) float d[2][BLK];
   alignas(16) int docs[2][BLK];
 };
-template <bool CAP, int BIAS>
+template <int CAP, int BIAS>
 __device__ __forceinline__ void biased_dkv_wide_body(const BiasedArgs& a, WideDkvLds<BIAS>& lds, int tile, int mat, int dev) {
   constexpr int D = 128, KS = D / 16, DT = D / 32, BKW = 128, KREG = KS / 2;   // KREG: K fragments kept in registers
   const FusedArgs& f = a.f;
@@ -658,7 +658,7 @@ template <size_t A, size_t B>
 constexpr size_t larger() { return A > B ? A : B; }
 
 // Both kinds in one grid ordered by loop length, longest first, the kinds alternating: x = (rank, matrix, kind), y = device.
-template <int D, bool CAP, int BIAS>
+template <int D, int CAP, int BIAS>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_biased_bwd_kernel(BiasedArgs a, int ntiles, int nmat) {
   constexpr size_t DQ = sizeof(DqLds<D, 2, BIAS>), DKV = sizeof(DkvLds<D, 2, BIAS>);
   __shared__ __attribute__((aligned(1024))) char lds[DQ > DKV ? DQ : DKV];
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_biased_bwd_kernel(B
 }
 
 // The same in workgroups of eight wavefronts and 128 rows: x = (matrix, kind), y = rank, z = device.
-template <int D, bool CAP, int BIAS>
+template <int D, int CAP, int BIAS>
 __global__ __launch_bounds__(512, 2) void attn_biased_bwd_wide_kernel(BiasedArgs a) {
   const int rank = blockIdx.y, mat = blockIdx.x >> 1, kind = blockIdx.x & 1, ntiles = gridDim.y, dev = blockIdx.z;
   if constexpr (D == 128) {
@@ -720,7 +720,7 @@ bool wide_form(const AttnBiasedDesc& b) {
   return groups > num_cus();
 }
 
-template <int D, bool CAP, int BIAS>
+template <int D, int CAP, int BIAS>
 void bwd_launch(const BiasedArgs& a, const AttnBiasedDesc& b, hipStream_t st) {
   const AttnFusedDesc& d = b.base;
   const int nmat = d.nb * d.nh;
@@ -735,20 +735,9 @@ int launch_attn_biased_bwd_kernels(const BiasedArgs& given, const AttnBiasedDesc
   BiasedArgs a = given;
   a.ntiles = wide_form(b) ? (d.s + 127) / 128 : (d.s + BLK - 1) / BLK;
   a.table_parts = b.d_table ? b.table_parts : nullptr;
-  const int kind = (b.cap > 0 ? 3 : 0) + (b.table ? 2 : b.slopes ? 1 : 0);
-  auto run = [&](auto width) {
-    constexpr int D = decltype(width)::value;
-    switch (kind) {
-      case 0: bwd_launch<D, false, 0>(a, b, st); break;
-      case 1: bwd_launch<D, false, 1>(a, b, st); break;
-      case 2: bwd_launch<D, false, 2>(a, b, st); break;
-      case 3: bwd_launch<D, true, 0>(a, b, st); break;
-      case 4: bwd_launch<D, true, 1>(a, b, st); break;
-      default: bwd_launch<D, true, 2>(a, b, st);
-    }
-  };
-  if (d.d == 64) run(std::integral_constant<int, 64>());
-  else run(std::integral_constant<int, 128>());
+  with_kind(b, [&](auto width, auto cap, auto bias) {
+    bwd_launch<decltype(width)::value, decltype(cap)::value, decltype(bias)::value>(a, b, st);
+  });
   if (a.table_parts) attn_biased_table_kernel<<<dim3(d.nh, d.ndev), 1024, 0, st>>>(a, b.d_table);
   return hip_launch_status();
 }

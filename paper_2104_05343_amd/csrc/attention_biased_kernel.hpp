@@ -30,9 +30,10 @@ struct BiasedArgs {
   int causal, nblk;          // nblk: blocks of 64 tokens of a sequence
   float cap_log2;            // cap * log2(e)
   float weight_lo;           // what the rounding of the scores' weight (and of the tanh's first coefficient) loses
-  float cap_exp;             // 2 log2(e) / (sqrt(d) cap)
-  float tanh_of[5];          // coefficients of tanh(v / (sqrt(d) cap)) at v, v^3, .. v^9
-  float cap_small;           // Q K^T below which the polynomial is taken: cap sqrt(d) / 4
+  float cap_pre;             // a power of two that Q K^T is scaled by beside a large cap: x; 1 otherwise
+  float cap_exp;             // 2 u log2(e) / x
+  float tanh_of[5];          // coefficients of tanh u at x, x^3, .. x^9
+  float cap_small;           // x below which the polynomial is taken: u = 1/4
   int buckets, side, two_sided, far;   // side: buckets of one side; far: first distance of its last one
   int ntiles;                // row tiles of a matrix in the parts of the table's gradient
   const float* slopes;       // [heads]
@@ -49,6 +50,28 @@ void launch_attn_biased_prepare(const BiasedArgs& a, int d, bool delta, int nmat
 int launch_attn_biased_bwd_kernels(const BiasedArgs& a, const AttnBiasedDesc& d, hipStream_t st);
 
 namespace {
+
+// The kernels' CAP: 0 none, 1 up to 64, 2 beyond (tanh16).
+inline int cap_form(const AttnBiasedDesc& b) { return b.cap > 64 ? 2 : b.cap > 0 ? 1 : 0; }
+// Calls run(width, cap, bias), constants of the kernels' D, CAP and BIAS.
+template <class F>
+void with_kind(const AttnBiasedDesc& b, F run) {
+  using std::integral_constant;
+  auto with_cap = [&](auto width, auto cap) {
+    if (b.table) run(width, cap, integral_constant<int, 2>());
+    else if (b.slopes) run(width, cap, integral_constant<int, 1>());
+    else run(width, cap, integral_constant<int, 0>());
+  };
+  auto with_width = [&](auto width) {
+    switch (cap_form(b)) {
+      case 0: with_cap(width, integral_constant<int, 0>()); break;
+      case 1: with_cap(width, integral_constant<int, 1>()); break;
+      default: with_cap(width, integral_constant<int, 2>());
+    }
+  };
+  if (b.base.d == 64) with_width(integral_constant<int, 64>());
+  else with_width(integral_constant<int, 128>());
+}
 
 // What a wavefront knows about its matrix.
 struct Matrix {
@@ -166,30 +189,38 @@ __device__ __forceinline__ bf16x8 cols_at(unsigned at, int row0, int dt) {
 // place of accumulator slot r in its 32 x 32 tile, without the lane's 4 * (lane / 32)
 __device__ constexpr int slot(int r) { return 8 * (r >> 2) + (r & 3); }
 
-// v = Q K^T -> tanh(v / (sqrt(d) cap)).  Below a quarter the odd polynomial up to the ninth power, in v itself (relative error 1e-8);
-// above, 1 - 2 / (exp(2x) + 1), whose absolute error of a unit in the last place of 1 is a relative one of 5e-7 of such a score.
-// FINE (where sums of dS are an fp32 result): the polynomial for each score below a quarter, and the reciprocal refined by a Newton step,
-// so that the scores' error is that of their own last place.
-template <bool FINE = false>
+// v = Q K^T -> tanh(u), u = v / (sqrt(d) cap).  Below a quarter the odd polynomial up to the ninth power, in v itself (relative error
+// 1e-8); above, 1 - 2 / (exp(2u) + 1), whose absolute error of a unit or two in the last place of 1 is a relative one of 1e-6 of such a
+// score.  A tile with a score beyond a quarter takes the second form for all of them where that error, of the cap whatever the score, is
+// small beside the rounding of P to bf16: up to a cap of 64 1.8e-5 of a score at most, 6e-6 as a rule.
+// CAP 2 (a larger cap) and FINE (where sums of dS are an fp32 result): the polynomial for each score below a quarter, and the reciprocal
+// refined by a Newton step.  (16 matrices of 4096 of width 128, causal, every tile beyond a quarter: forward 110 us, with CAP 2 153;
+// width 64 93 and 137.)
+// CAP 2 scales v by a power of two first: its powers, and those of 1 / (sqrt(d) cap), leave fp32's range else.
+template <int CAP, bool FINE = false>
 __device__ __forceinline__ void tanh16(f32x16& v, const BiasedArgs& a) {
+  if (CAP == 2) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] *= a.cap_pre;
+  }
+  auto polynomial = [&](float x) {
+    const float y = x * x;
+    return x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, a.tanh_of[4], a.tanh_of[3]), a.tanh_of[2]), a.tanh_of[1]), a.tanh_of[0]);
+  };
   float mx = 0.f;
 #pragma unroll
   for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fabsf(v[r]));
   if (__builtin_amdgcn_ballot_w64(mx < a.cap_small) == ~0ull) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float y = v[r] * v[r];
-      v[r] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, a.tanh_of[4], a.tanh_of[3]), a.tanh_of[2]), a.tanh_of[1]), a.tanh_of[0]);
-    }
+    for (int r = 0; r < 16; ++r) v[r] = polynomial(v[r]);
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float e1 = __builtin_amdgcn_exp2f(v[r] * a.cap_exp) + 1.0f;
       float q = __builtin_amdgcn_rcpf(e1);
-      if (FINE) {
+      if (FINE || CAP == 2) {
         q = e1 < 1e30f ? fmaf(fmaf(-e1, q, 1.0f), q, q) : q;   // (infinity times zero)
-        const float y = v[r] * v[r];
-        const float near = v[r] * fmaf(y, fmaf(y, fmaf(y, fmaf(y, a.tanh_of[4], a.tanh_of[3]), a.tanh_of[2]), a.tanh_of[1]), a.tanh_of[0]);
+        const float near = polynomial(v[r]);
         v[r] = fabsf(v[r]) < a.cap_small ? near : fmaf(-2.0f, q, 1.0f);
       } else {
         v[r] = fmaf(-2.0f, q, 1.0f);
@@ -251,12 +282,12 @@ template <int BIAS>
 __device__ __forceinline__ bool plain_tile(const Bias& b, int lo, int hi) {
   return BIAS == 1 ? lo >= 0 || hi <= 0 : BIAS == 2 ? lo >= b.far || hi <= -b.back : true;
 }
-template <bool CAP, int BIAS>
+template <int CAP, int BIAS>
 __device__ __forceinline__ void plain_weights(const BiasedArgs& a, const Bias& b, int lo, float& w, float& c) {
   w = BIAS == 1 ? 1.0f : CAP ? a.cap_log2 : a.f.scale_log2;
   c = BIAS == 2 ? (lo >= b.far ? b.far_pos : b.far_neg) : 0.f;
 }
-template <bool CAP, int BIAS, int SIGN>
+template <int CAP, int BIAS, int SIGN>
 __device__ __forceinline__ void plain16(f32x16& v, const BiasedArgs& a, const Bias& b, int dist0, int lo) {
   if (BIAS == 1) {
     const float sg = lo >= 0 ? -b.slope2 : b.slope2, base = sg * (float)dist0, w = CAP ? a.cap_log2 : a.f.scale_log2;
@@ -267,7 +298,7 @@ __device__ __forceinline__ void plain16(f32x16& v, const BiasedArgs& a, const Bi
 // Any tile: log2(e) times the score, -infinity where the pair is left out: the other token's place (at + slot(r)) behind `bound`
 // (SIGN < 0) or ahead of it, or of another document than `doc`.  docs: LDS, the other tokens' from the lane's slot 0 on.  FINE: hi + lo
 // is taken off the score, hi before the bias: with a row's log-sum-exp what is rounded then is small where it counts.
-template <bool CAP, int BIAS, int SIGN, bool FINE = false>
+template <int CAP, int BIAS, int SIGN, bool FINE = false>
 __device__ __forceinline__ void any16(f32x16& v, const BiasedArgs& a, const Bias& b, int dist0, int at, int bound, const int* docs, int doc,
                                       float hi = 0.f, float lo = 0.f) {
   asm volatile("");   // a branch, not selects: taken by few tiles, and seven operations a score

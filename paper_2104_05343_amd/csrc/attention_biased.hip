@@ -107,7 +107,9 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 && BIAS != 1 && CAP 
       const int dist0 = query - kbase - 4 * g, lo = q0 - kbase - (BLK - 1), hi = q0 + 31 - kbase;
       float w = 1.0f, c = 0.f;
       // pairs to leave out exist only in the last blocks and where documents meet (wave-uniform tests)
-      if ((a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) || (m.docs && !one_document(blk, own)) || !plain_tile<BIAS>(bias, lo, hi)) {
+      const bool masked = (a.causal ? kbase + BLK - 1 > max(q0, m.prefix - 1) : kbase + BLK > s) || (m.docs && !one_document(blk, own));
+      const bool plain = !masked && plain_tile<BIAS>(bias, lo, hi);
+      if (!plain) {
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2)
           any16<CAP, BIAS, -1>(sacc[t2], a, bias, dist0 - 32 * t2, kbase + 32 * t2 + 4 * g, limit, &key_docs[wave][32 * t2 + 4 * g], qdoc);
@@ -121,7 +123,19 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 && BIAS != 1 && CAP 
       for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
+      // The exponents below are v w + c less the maximum without a rounding in between, and the rounded maximum is up to 2^-24 of itself
+      // too small: an exponent above zero, which overflows from 2^31 on.  From 2^28 on the scores are rounded first, like the maximum.
+      // (With slopes they are; a cap up to 64 has no such scores.)
+      const bool large = BIAS != 1 && CAP != 1 && plain && __builtin_amdgcn_ballot_w64(fabsf(fmaf(mx, w, c)) > 0x1p28f) != 0;
       mx = fmaf(halfwave_max(mx), w, c);   // (w is positive: it commutes with the maximum)
+      if (large) {
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sacc[t2][r] = fmaf(sacc[t2][r], w, c);
+        w = 1.0f;
+        c = 0.f;
+      }
       // The running maximum follows the block's only when that is more than 2^8 above it (see the attention without changes).  A row
       // that has met no key yet keeps -infinity, and 0 in its place where it is subtracted: its terms are exp2(-infinity) = 0.
       const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;

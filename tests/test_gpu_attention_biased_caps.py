@@ -119,6 +119,29 @@ def test_rows_beside_one_that_reaches_the_cap(cap, kind, d):
         _compare(x, long_rows, cap, causal, slopes, table, _device(x, cap, causal, slopes, table, d_attn), d_attn, None)
 
 
+@pytest.mark.parametrize("share", [0.05, 0.2, 0.24, 0.5, 3.0])
+@pytest.mark.parametrize("cap", [1e5, 1e7, 1e10, 1e16, 1e20, 1e25, 1e30])
+def test_scores_around_a_very_large_cap(cap, share):
+    """Forward: scores in every part of the cap's range, products beyond 1e19 (whose squares fp32 does not hold) among them."""
+    for kind in ("none", "table"):
+        slopes, table = _bias(kind, 1, np.random.default_rng(3))
+        x, long_rows = _inputs(1, 100, 1, 64, cap, (share,), 7)
+        print("cap", cap, kind, share, flush=True)
+        _compare(x, long_rows, cap, False, slopes, table, _device(x, cap, False, slopes, table), None, None)
+
+
+@pytest.mark.parametrize("size", [1e6, 1e8, 1e9, 1e12, 1e20, 1e30])
+def test_very_large_scores_without_a_cap(size):
+    """Forward: rows of scores of every finite size beside ordinary ones, one key winning them by far, or all of them below zero."""
+    for kind in ("none", "slopes", "table"):
+        slopes, table = _bias(kind, 1, np.random.default_rng(3))
+        x, long_rows = _inputs(1, 200, 1, 64, size, (1.0,), 8)
+        x[:, 64:128, :, 1, 3] = -np.abs(x[:, 64:128, :, 1, 3])   # a block of keys that long rows see below zero
+        print("size", size, kind, flush=True)
+        for causal in (False, True):
+            _compare(x, long_rows, 0.0, causal, slopes, table, _device(x, 0.0, causal, slopes, table), None, None)
+
+
 @pytest.mark.parametrize("b,s,n,d", [(8, 700, 16, 128), (16, 700, 8, 64)])
 @pytest.mark.parametrize("kind", ["none", "slopes", "table"])
 def test_larger_launches(b, s, n, d, kind):

@@ -174,8 +174,8 @@ __device__ __forceinline__ u32x2u pack8(const float x[8], const unsigned dither[
 
 // EXACT: root and division are rounded exactly.  Otherwise root and reciprocal are of one unit in the last place, a 4e-7th of the update,
 // which w's own rounding hides (25 operations less, and with 8-bit moments and two hashes an element the arithmetic is what counts).  They
-// take numbers below 2^-126 for 0, so that a root below 2^-63 is lost: nothing beside an eps from 1e-15 on, a division by eps alone
-// beside a smaller one.
+// take numbers below 2^-126 for 0, so that a root below 2^-63 is lost, up to 2^-63 / sqrt(1 - beta2) of what eps is added to: as small a
+// part of the update where eps is 2^-42 / sqrt(1 - beta2) or more (beta2 = 0.999: 7e-12), all of it beside a tiny eps.
 template <bool EXACT>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
 #pragma clang fp contract(off)
@@ -330,6 +330,7 @@ int adamw_launch(const optimus_adamw_cfg* cfg, unsigned long long seed, const op
     a.root = (float)(1.0 / sqrt(-expm1((double)cfg->step * a.log_b2)));
   }
   a.grad_scale = cfg->grad_scale; a.lr_dev = cfg->lr_on_device; a.step_dev = (const long long*)cfg->step_on_device;
+  const bool exact = cfg->eps * sqrt(1.0 - cfg->beta2) < 0x1p-42;
   for (int k = 0; k < count;) {
     unsigned groups = 0;
     a.count = 0;
@@ -348,7 +349,7 @@ int adamw_launch(const optimus_adamw_cfg* cfg, unsigned long long seed, const op
       groups += (unsigned)own;
       ++k;
     }
-    if (a.eps < 1e-15f) adamw_kernel<true><<<groups, kThreads, 0, st>>>(a);   // (a kernel of its own: one that chose took 520 us for 486)
+    if (exact) adamw_kernel<true><<<groups, kThreads, 0, st>>>(a);   // (a kernel of its own: one that chose took 520 us for 486)
     else adamw_kernel<false><<<groups, kThreads, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }

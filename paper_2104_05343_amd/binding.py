@@ -338,8 +338,24 @@ def attention_fused_bwd(qkv, attn, lse, d_attn, d_qkv, b, s, h, n, q, i, j, caus
                                              int(causal), dtype, p, nb, _stream(stream)), "optimus_attention_fused_bwd")
 
 
+_INT32, _FP32_ONLY = (torch.int32,), (torch.float32,)
+
+
+def _plain_tensor(t, dtypes, where):
+    """What a struct of addresses cannot say of a tensor: its type and that its elements lie one after the other.  None and addresses pass."""
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype not in dtypes:
+        raise OptimusError(EDTYPE, where)
+    if not t.is_contiguous():
+        raise OptimusError(EINVAL, where)
+
+
 def make_attention_bias(cap=0.0, slopes=None, table=None, buckets=0, max_distance=0, two_sided=False, documents=None, prefix=None) -> AttentionBias:
-    """What changes the scores (optimus_attention_bias).  Holds addresses: keep the tensors alive."""
+    """What changes the scores (optimus_attention_bias): slopes and table fp32, documents and prefix int32, all contiguous (EDTYPE, EINVAL).
+    Holds addresses: keep the tensors alive."""
+    for name, t, dtypes in (("slopes", slopes, _FP32_ONLY), ("table", table, _FP32_ONLY), ("documents", documents, _INT32), ("prefix", prefix, _INT32)):
+        _plain_tensor(t, dtypes, "make_attention_bias: " + name)
     return AttentionBias(float(cap), _ptr(slopes), _ptr(table), buckets, max_distance, int(two_sided), _ptr(documents), _ptr(prefix))
 
 
@@ -457,16 +473,45 @@ def stack_bwd(cfg: LayerCfg, params, grads, d_out, buf: StackBuffers, d_x, done=
                                    _stream(stream)), "optimus_stack_bwd")
 
 
+_EIGHT_BITS = (torch.uint8, torch.int8, torch.float8_e4m3fn)
+_POWERS = (torch.uint8, torch.int8, torch.float8_e8m0fnu)
+
+
+def _check_adamw_tensors(t):
+    """Types, sizes and places of one entry's tensors: what the struct of addresses cannot say of them."""
+    param, parts = t["param"], t.get("grad_parts", 1)
+    n, eight = t.get("n", param.numel()), t.get("m_scale") is not None or t.get("v_scale") is not None
+    weights, moments = (torch.float32, torch.bfloat16), _EIGHT_BITS if eight else _FP32_ONLY
+    groups = -(-n // 128)
+    dense = param.permute(sorted(range(param.dim()), key=param.stride, reverse=True)).is_contiguous()   # its elements without gaps, in any order
+    for name, dtypes, least in (("param", weights, n), ("master", _FP32_ONLY, n), ("grad", weights, n * parts), ("m", moments, n), ("v", moments, n),
+                                ("m_scale", _POWERS, groups), ("v_scale", _POWERS, groups)):
+        x, where = t.get(name), "make_adamw_tensors: " + name
+        if x is None or isinstance(x, int):
+            continue
+        if x.dtype not in dtypes:
+            raise OptimusError(EDTYPE, where)
+        if x.numel() < least:
+            raise OptimusError(ESHAPE, where)
+        # one order in memory: contiguous, or a transposed param with the others laid out like it (or flat)
+        plain = x.is_contiguous() and (param.is_contiguous() or x.dim() == 1)
+        if not plain and not (dense and x.shape == param.shape and x.stride() == param.stride()) or x.device != param.device:
+            raise OptimusError(EINVAL, where)
+
+
 def make_adamw_tensors(tensors):
     """tensors: list of dicts param, grad, m, v (torch tensors) and, where they differ from these defaults, master=None, m_scale=None,
-    v_scale=None, n=param.numel(), grad_parts=1, weight_decay=0.0.  The array holds addresses: keep the tensors alive."""
+    v_scale=None, n=param.numel(), grad_parts=1, weight_decay=0.0.  Refused: types other than optimus_adamw_tensor's (EDTYPE), fewer than n
+    elements (ESHAPE), elements not one after the other or not on param's device (EINVAL).  The array holds addresses: keep the tensors
+    alive."""
     codes = {torch.float32: FP32, torch.bfloat16: BF16}
     out = (AdamwTensor * len(tensors))()
     for a, t in zip(out, tensors):
+        _check_adamw_tensors(t)
         for name in ("param", "master", "grad", "m", "v", "m_scale", "v_scale"):
             setattr(a, name, _ptr(t.get(name)))
         a.n = t.get("n", t["param"].numel())
-        a.param_dtype, a.grad_dtype = (codes.get(t[k].dtype, -1) for k in ("param", "grad"))
+        a.param_dtype, a.grad_dtype = (codes[t[k].dtype] for k in ("param", "grad"))
         a.grad_parts, a.weight_decay = t.get("grad_parts", 1), t.get("weight_decay", 0.0)
     return out
 
@@ -477,7 +522,11 @@ def adamw_step(cfg: AdamwCfg, tensors, stream=None):
 
 
 def make_adamw_state(m, v, m_scale=None, v_scale=None, master=None) -> AdamwState:
-    """One layer's moments (stack_adamw_elements of them) and masters.  Holds addresses: keep the tensors alive."""
+    """One layer's moments (stack_adamw_elements of them) and masters, types as in optimus_adamw_tensor, contiguous (EDTYPE, EINVAL).
+    Holds addresses: keep the tensors alive."""
+    moments = _FP32_ONLY if m_scale is None and v_scale is None else _EIGHT_BITS
+    for name, t, dtypes in (("m", m, moments), ("v", v, moments), ("m_scale", m_scale, _POWERS), ("v_scale", v_scale, _POWERS), ("master", master, _FP32_ONLY)):
+        _plain_tensor(t, dtypes, "make_adamw_state: " + name)
     return AdamwState(_ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), _ptr(master))
 
 

@@ -155,6 +155,7 @@ SIGNATURES = {
     "optimus_debug_set_corun_variants": (None, [_INT, _INT]),
     "optimus_debug_last_gemm_plan": (_INT, []),
     "optimus_debug_layer_bwd_streams": (_INT, [C.POINTER(LayerCfg), _INT, _INT]),
+    "optimus_debug_attention_biased_rows": (_INT, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias), _INT]),
     "optimus_debug_plan_summa": (_INT, [_INT, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _INT, C.POINTER(C.c_int)]),
     "optimus_debug_plan_pair": (_INT, [_I64, _I64, _I64, _INT, _INT, _INT]),
     "optimus_debug_mfma_rate": (_INT, [_P, _INT, _INT, _INT, _P]),
@@ -603,6 +604,10 @@ def debug_last_gemm_pair() -> bool:
     """Whether that product shared its launch with another one."""
     p = lib().optimus_debug_last_gemm_plan()
     return p >= 0 and bool(p >> 18 & 1)
+
+
+def debug_attention_biased_rows(backward, b, s, h, n, q, i, j, bias: AttentionBias, table_gradient=False) -> int:
+    return lib().optimus_debug_attention_biased_rows(int(backward), b, s, h, n, q, i, j, C.byref(bias), int(table_gradient))
 
 
 def debug_layer_bwd_streams(cfg: LayerCfg, i, j) -> int:

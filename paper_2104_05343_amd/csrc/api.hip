@@ -1248,5 +1248,15 @@ int optimus_debug_layer_bwd_streams(const optimus_layer_cfg* c, int i, int j) {
   if (layer_check(c, i, j, &a)) return -1;
   return two_streams_pay(c, is_grid(i, j)) ? 2 : 1;
 }
+int optimus_debug_attention_biased_rows(int backward, int b, int s, int h, int n, int q, int i, int j, const optimus_attention_bias* bias,
+                                        int table_gradient) {
+  AttnDims a;
+  AttnBiasedDesc d = {};
+  if (attn_biased_dims(b, s, h, n, q, &a) || check_coords(q, i, j) || bias_desc(bias, 1, &d) || (table_gradient && !d.table)) return -1;
+  d.base.s = s; d.base.d = a.d; d.base.nb = a.nb; d.base.nh = a.nh;
+  d.base.ndev = is_grid(i, j) ? q * q : 1;
+  d.d_table = table_gradient ? (float*)(uintptr_t)4096 : nullptr;   // (whether there is one counts)
+  return (backward ? attn_biased_bwd_wide(d) : attn_biased_fwd_wide(d)) ? 128 : 64;
+}
 
 }  // extern "C"

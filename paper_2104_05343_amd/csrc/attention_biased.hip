@@ -299,12 +299,7 @@ BiasedArgs make_args(const AttnBiasedDesc& b) {
 }
 
 template <int D, int CAP, int BIAS>
-void fwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, hipStream_t st) {
-  // 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64): a wavefront has the same loop
-  // either way and a SIMD to itself.  64 rows / 128 rows, us: width 128, causal with a cap, 16 matrices of 1024 (256 workgroups of 64
-  // rows) 23.7 / 26.8, 32 of them 31.3 / 27.5; width 64, 16 of 2048 (512) 29.7 / 37.7, 64 of 1024 (1024) 27.9 / 27.1, without a mask
-  // 40.1 / 34.2.  The bits are the same.
-  const bool big = (long long)((d.s + BLK - 1) / BLK) * d.nb * d.nh * d.ndev > num_cus() * (D == 64 ? 2 : 1);
+void fwd_launch(const BiasedArgs& a, const AttnFusedDesc& d, bool big, hipStream_t st) {
   const int rows = big ? 128 : BLK;
   const dim3 grid(d.nb * d.nh, (d.s + rows - 1) / rows, d.ndev);
   if (big) attn_biased_fwd_kernel<D, 4, CAP, BIAS><<<grid, 512, 0, st>>>(a);
@@ -321,13 +316,22 @@ void launch_attn_biased_prepare(const BiasedArgs& a, int d, bool delta, int nmat
   else attn_biased_prepare_kernel<128><<<grid, 256, 0, st>>>(a, mats);
 }
 
+// 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64): a wavefront has the same loop
+// either way and a SIMD to itself.  64 rows / 128 rows, us: width 128, causal with a cap, 16 matrices of 1024 (256 workgroups of 64
+// rows) 23.7 / 26.8, 32 of them 31.3 / 27.5; width 64, 16 of 2048 (512) 29.7 / 37.7, 64 of 1024 (1024) 27.9 / 27.1, without a mask
+// 40.1 / 34.2.  The bits are the same.
+bool attn_biased_fwd_wide(const AttnBiasedDesc& b) {
+  const AttnFusedDesc& d = b.base;
+  return (long long)((d.s + BLK - 1) / BLK) * d.nb * d.nh * d.ndev > num_cus() * (d.d == 64 ? 2 : 1);
+}
+
 int launch_attn_biased_fwd(const AttnBiasedDesc& b, hipStream_t st) {
   const AttnFusedDesc& d = b.base;
   if (!desc_ok(b) || !d.qkv || !d.attn || !d.lse) return OPTIMUS_ESHAPE;
   const BiasedArgs a = make_args(b);
   launch_attn_biased_prepare(a, d.d, false, d.nb * d.nh, d.ndev, st);
   with_kind(b, [&](auto width, auto cap, auto bias) {
-    fwd_launch<decltype(width)::value, decltype(cap)::value, decltype(bias)::value>(a, d, st);
+    fwd_launch<decltype(width)::value, decltype(cap)::value, decltype(bias)::value>(a, d, attn_biased_fwd_wide(b), st);
   });
   return hip_launch_status();
 }

@@ -705,6 +705,16 @@ __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, f
   }
 }
 
+template <int D, int CAP, int BIAS>
+void bwd_launch(const BiasedArgs& a, const AttnBiasedDesc& b, hipStream_t st) {
+  const AttnFusedDesc& d = b.base;
+  const int nmat = d.nb * d.nh;
+  if (attn_biased_bwd_wide(b)) attn_biased_bwd_wide_kernel<D, CAP, BIAS><<<dim3(2 * nmat, a.ntiles, d.ndev), 512, 0, st>>>(a);
+  else attn_biased_bwd_kernel<D, CAP, BIAS><<<dim3((unsigned)(2ll * a.ntiles * nmat), d.ndev), 256, 0, st>>>(a, a.ntiles, nmat);
+}
+
+}  // namespace
+
 // 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64).  Width 64 keeps them where there
 // are documents, a cap or a table's gradient: two workgroups a compute unit, each with barriers of its own, overlap one's arithmetic
 // with the other's products.  64 rows / 128 rows, us: width 128, causal, 16 matrices of 512 (256 workgroups of 64 rows) 25.3 / 25.3, 10
@@ -713,27 +723,17 @@ __global__ __launch_bounds__(1024) void attn_biased_table_kernel(BiasedArgs a, f
 // without a mask 379 / 394, with it 236 / 249.
 // The two forms add dK and dV (width 128) and the table's gradient up in different orders, so the choice follows one device's matrices,
 // whatever the launch covers.
-bool wide_form(const AttnBiasedDesc& b) {
+bool attn_biased_bwd_wide(const AttnBiasedDesc& b) {
   const AttnFusedDesc& d = b.base;
   const long long groups = 2ll * ((d.s + BLK - 1) / BLK) * d.nb * d.nh;
   if (d.d == 64) return groups > 2 * num_cus() && !b.documents && !(b.cap > 0) && !b.d_table;
   return groups > num_cus();
 }
 
-template <int D, int CAP, int BIAS>
-void bwd_launch(const BiasedArgs& a, const AttnBiasedDesc& b, hipStream_t st) {
-  const AttnFusedDesc& d = b.base;
-  const int nmat = d.nb * d.nh;
-  if (wide_form(b)) attn_biased_bwd_wide_kernel<D, CAP, BIAS><<<dim3(2 * nmat, a.ntiles, d.ndev), 512, 0, st>>>(a);
-  else attn_biased_bwd_kernel<D, CAP, BIAS><<<dim3((unsigned)(2ll * a.ntiles * nmat), d.ndev), 256, 0, st>>>(a, a.ntiles, nmat);
-}
-
-}  // namespace
-
 int launch_attn_biased_bwd_kernels(const BiasedArgs& given, const AttnBiasedDesc& b, hipStream_t st) {
   const AttnFusedDesc& d = b.base;
   BiasedArgs a = given;
-  a.ntiles = wide_form(b) ? (d.s + 127) / 128 : (d.s + BLK - 1) / BLK;
+  a.ntiles = attn_biased_bwd_wide(b) ? (d.s + 127) / 128 : (d.s + BLK - 1) / BLK;
   a.table_parts = b.d_table ? b.table_parts : nullptr;
   with_kind(b, [&](auto width, auto cap, auto bias) {
     bwd_launch<decltype(width)::value, decltype(cap)::value, decltype(bias)::value>(a, b, st);

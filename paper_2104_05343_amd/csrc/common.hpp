@@ -206,6 +206,8 @@ struct AttnBiasedDesc {
 };
 int launch_attn_biased_fwd(const AttnBiasedDesc& d, hipStream_t stream);
 int launch_attn_biased_bwd(const AttnBiasedDesc& d, hipStream_t stream);
+bool attn_biased_fwd_wide(const AttnBiasedDesc& d);   // whether workgroups have 128 rows, not 64
+bool attn_biased_bwd_wide(const AttnBiasedDesc& d);
 
 // Attention that keeps the probabilities, head widths 64 and 128 (attention_probs.hip): nmat matrices of consecutive sequences,
 // nh heads each.

@@ -97,6 +97,11 @@ struct BucketSums {
   }
 };
 
+// 128-row workgroups of width 64 are for sequences without documents (attn_biased_bwd_wide) and compiled without them: 16 matrices of
+// 4096, causal, 149 us; with the branches for documents 158.
+template <int D, int NRG>
+constexpr bool no_documents() { return D == 64 && NRG == 4; }
+
 template <int D, int NRG, int BIAS>
 struct DqLds {
   bf16_t tile[2][2][PAIR * D];   // [stage][K, V]
@@ -124,7 +129,8 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % NRG, par = wave / NRG;
   const int s = f.s;
-  const Matrix m = matrix_of<D>(a, mat, dev);
+  Matrix m = matrix_of<D>(a, mat, dev);
+  if (no_documents<D, NRG>()) m.docs = nullptr;
   const bf16_t* Qp = f.qkv + m.qkv;
   const bf16_t* Kp = Qp + D;
   const bf16_t* Vp = Qp + 2 * D;
@@ -342,7 +348,8 @@ __device__ __forceinline__ void biased_dkv_body(const BiasedArgs& a, DkvLds<D, N
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % NRG, par = wave / NRG;
   const int s = f.s;
-  const Matrix m = matrix_of<D>(a, mat, dev);
+  Matrix m = matrix_of<D>(a, mat, dev);
+  if (no_documents<D, NRG>()) m.docs = nullptr;
   const bf16_t* Qp = f.qkv + m.qkv;
   const bf16_t* Kp = Qp + D;
   const bf16_t* Vp = Qp + 2 * D;
@@ -715,18 +722,20 @@ void bwd_launch(const BiasedArgs& a, const AttnBiasedDesc& b, hipStream_t st) {
 
 }  // namespace
 
-// 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64).  Width 64 keeps them where there
-// are documents, a cap or a table's gradient: two workgroups a compute unit, each with barriers of its own, overlap one's arithmetic
-// with the other's products.  64 rows / 128 rows, us: width 128, causal, 16 matrices of 512 (256 workgroups of 64 rows) 25.3 / 25.3, 10
-// of 1000 without a mask (320) 66.5 / 37.1, 16 of 4096 457 / 256; width 64, causal, 16 of 1024 (512) 23.4 / 25.2, 16 of 2048 (1024)
-// 52.6 / 49.4, 16 of 4096 157 / 153, with cap and slopes 212 / 233, with documents of 700 67 / 73; with the table's gradient 64 of 2048
-// without a mask 379 / 394, with it 236 / 249.
+// 64-row workgroups as long as all of them run at once (one a compute unit of width 128, two of 64), and at width 64 with documents.
+// 64 rows / 128 rows, us: width 128, causal, 16 matrices of 512 (256 workgroups of 64 rows) 25.3 / 25.3, 10 of 1000 without a mask (320)
+// 66.5 / 37.1, 16 of 4096 457 / 256; width 64, causal, 16 of 1024 (512) 23.4 / 25.2, 16 of 2048 (1024) 60.7 / 52.0, 16 of 4096 164 / 149, 64
+// of 1024 64.9 / 62.7, 64 of 2048 without a mask 312 / 287.  With a cap of 50, with the table's gradient: 16 of 2048 74.9 / 65.8, 79.8 /
+// 68.5; 128 of 512 57.4 / 58.0, 72.7 / 68.6; 64 of 4096 830 / 767, 752 / 698; without a mask 64 of 2048 401 / 377, 382 / 360, 24 of 1400 97.1 /
+// 103.7, 102.2 / 105.2: ahead in 86 of 100 launches of 8 to 128 matrices, by up to 15 %, and up to 7 % behind where the last round is
+// short.  With documents of 700 the other way: causal, 16 of 2048 38.2 / 41.7, 16 of 4096 99 / 108, 64 of 2048 135 / 151, 64 of 4096 392 / 407,
+// without a mask 673 / 677.
 // The two forms add dK and dV (width 128) and the table's gradient up in different orders, so the choice follows one device's matrices,
 // whatever the launch covers.
 bool attn_biased_bwd_wide(const AttnBiasedDesc& b) {
   const AttnFusedDesc& d = b.base;
   const long long groups = 2ll * ((d.s + BLK - 1) / BLK) * d.nb * d.nh;
-  if (d.d == 64) return groups > 2 * num_cus() && !b.documents && !(b.cap > 0) && !b.d_table;
+  if (d.d == 64) return groups > 2 * num_cus() && !b.documents;
   return groups > num_cus();
 }
 

@@ -30,15 +30,14 @@ CASES = [c for c in itertools.product((64, 128), ("few", "many"), CAPS, BIASES, 
 
 
 def test_the_cases_take_every_kernel():
-    """On 256 compute units.  128-row backward kernels of width 64 exist for no cap, no documents and no table's gradient."""
+    """On 256 compute units.  128-row backward kernels of width 64 are for sequences without documents."""
     assert opt.debug_attention_biased_rows(False, 1, 64, 64, 1, 1, 0, 0, opt.make_attention_bias(slopes=4096, table=4096)) == -1   # refused
     forward = {(c[0], _rows(False, *c), c[2], c[3]) for c in CASES}
     assert forward == set(itertools.product((64, 128), (64, 128), CAPS, BIASES))
     backward = {(c[0], _rows(True, *c), c[2], c[3], "documents" in c[4], c[5]) for c in CASES}
     want = {(d, rows, cap, bias, docs, gradient) for d, rows, cap, bias, docs, gradient in
             itertools.product((64, 128), (64, 128), CAPS, BIASES, (False, True), (False, True))
-            if (bias == "table" or not gradient) and not (d == 64 and rows == 128 and (cap or docs or gradient))}
-    # (64 rows at width 64 without any of these: few matrices)
+            if (bias == "table" or not gradient) and not (d == 64 and rows == 128 and docs)}
     assert backward == want
 
 

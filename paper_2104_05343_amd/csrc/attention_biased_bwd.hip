@@ -118,6 +118,10 @@ struct DkvLds {
   alignas(16) int docs[2][PAIR];
 };
 
+// P = 2^x is at most 1: beyond it (the instruction's own clamp, which costs nothing) lies what the rounding of a log-sum-exp beyond some
+// millions makes of it, in the end an infinity that would turn gradients of zero into NaN.
+__device__ __forceinline__ float weight_of(float x) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f); }
+
 // log-sum-exp of a row -> what is subtracted from its scores.  Of a row without pairs +infinity, which makes every P of it zero.
 __device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
 
@@ -238,7 +242,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
         if (masked || !plain_tile<BIAS>(bias, lo, lo + 62)) {
           any16<CAP, BIAS, -1, BIAS == 2>(sacc, a, bias, dist0, k0 + 4 * g, limit, &lds.key_docs[wave][t2 * 32 + 4 * g], qdoc, lse2, lse2_lo);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(BIAS == 2 ? sacc[r] : sacc[r] - lse2) * pacc[r];  // dS^T
+          for (int r = 0; r < 16; ++r) sacc[r] = weight_of(BIAS == 2 ? sacc[r] : sacc[r] - lse2) * pacc[r];  // dS^T
         } else {
           float w, c;
           plain_weights<CAP, BIAS>(a, bias, lo, w, c);
@@ -246,7 +250,7 @@ __device__ __forceinline__ void biased_dq_body(const BiasedArgs& a, DqLds<D, NRG
           c -= BIAS == 2 ? lse2_lo : lse2;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            sacc[r] = __builtin_amdgcn_exp2f(BIAS == 2 ? fmaf(sacc[r], w, -lse2) + fmaf(sacc[r], a.weight_lo, c) : fmaf(sacc[r], w, c)) * pacc[r];
+            sacc[r] = weight_of(BIAS == 2 ? fmaf(sacc[r], w, -lse2) + fmaf(sacc[r], a.weight_lo, c) : fmaf(sacc[r], w, c)) * pacc[r];
         }
         if (BIAS == 2 && table_grad) sums.add(sacc, lo, g, lane, a.buckets > 64);
         if (CAP && BIAS == 2) {
@@ -333,7 +337,7 @@ __device__ __forceinline__ void biased_dkv_scores(f32x16& sacc, f32x16& pacc, co
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 4 * c + e;
-      const float p = __builtin_amdgcn_exp2f(fmaf(sacc[r], w, BIAS == 2 ? c0 - lv[e] : -lv[e]));   // (of a row without pairs, and past the end: 0)
+      const float p = weight_of(fmaf(sacc[r], w, BIAS == 2 ? c0 - lv[e] : -lv[e]));   // (of a row without pairs, and past the end: 0)
       sacc[r] = p;
       pacc[r] *= p;
     }

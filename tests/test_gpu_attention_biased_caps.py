@@ -142,6 +142,50 @@ def test_very_large_scores_without_a_cap(size):
             _compare(x, long_rows, 0.0, causal, slopes, table, _device(x, 0.0, causal, slopes, table), None, None)
 
 
+@pytest.mark.parametrize("b,n", [(1, 1), (8, 16)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size,cap", [(1e6, 0.0), (1e9, 0.0), (1e12, 0.0), (1e30, 0.0), (1e9, 1e9), (1e30, 1e30)])
+def test_gradients_beside_rows_of_very_large_scores(size, cap, d, b, n):
+    """Backward: rows whose fp32 log-sum-exp holds nothing of their P, with gradients of zero, leave the others theirs.  (b, n: workgroups of
+    64 rows and of 128.)"""
+    for kind in ("none", "slopes", "table"):
+        rng = np.random.default_rng(4)
+        slopes, table = _bias(kind, n, rng)
+        x, long_rows = _inputs(b, 300, n, d, size, (0.2, 1.0), 9)
+        d_attn = round_to_bf16(rng.standard_normal((b, 300, n, d)).astype(np.float32))
+        d_attn[:, long_rows] = 0
+        print("gradients", size, cap, kind, d, b, n, flush=True)
+        got = _device(x, cap, True, slopes, table, d_attn)
+        assert all(np.all(np.isfinite(got[k])) for k in ("G", "T") if k in got)
+        with np.errstate(over="ignore", invalid="ignore"):   # (the oracle's P of the long rows, which meets zeros)
+            _gradients_of_ordinary_rows(x, long_rows, cap, slopes, table, got, d_attn, {(0, 0), (b - 1, n - 1)})
+
+
+def _gradients_of_ordinary_rows(x, long_rows, cap, slopes, table, got, d_attn, which):
+    """dQ of the ordinary rows, dK and dV summed over them: the oracle with the long rows taken out of the sums (their dS and dO are zero)."""
+    s, d = x.shape[1], x.shape[4]
+    for seq, head in which:
+        Q, K, V = (x[seq, :, head, k].astype(np.float64) for k in range(3))
+        kw = dict(causal=True, cap=cap)
+        if slopes is not None:
+            kw["slope"] = float(slopes[head])
+        if table is not None:
+            kw.update(table=table[head], max_distance=TABLE["max_distance"])
+        go, gl, dO = got["O"][seq, :, head], got["L"][seq, head], d_attn[seq, :, head].astype(np.float64)
+        S, grad = oab.scores(Q, K, **kw)
+        P = np.where(long_rows[:, None] | np.isneginf(S), 0, np.exp(np.where(np.isneginf(S), 0, S) - gl[:, None]))
+        dS = P * (dO @ V.T - (dO * go).sum(1, keepdims=True)) * grad
+        spread = P * (np.abs(dO) @ np.abs(V).T + (np.abs(dO) * np.abs(go)).sum(1, keepdims=True))
+        Q = np.where(long_rows[:, None], 0, Q)   # (times dS of zero)
+        raw, fine = np.abs(dS), FP32 * spread
+        for k, (w, size, small) in enumerate(((dS @ K / np.sqrt(d), raw @ np.abs(K) / np.sqrt(d), fine @ np.abs(K) / np.sqrt(d)),
+                                              (dS.T @ Q / np.sqrt(d), raw.T @ np.abs(Q) / np.sqrt(d), fine.T @ np.abs(Q) / np.sqrt(d)),
+                                              (P.T @ dO, P.T @ np.abs(dO), FP32 * P.T @ np.abs(dO)))):
+            g = got["G"][seq, :, head, k]
+            bad = ~(np.abs(g - w) <= HALF * (1.01 * np.abs(w) + size) + 2 * small + 1e-30)
+            assert not np.any(bad), (seq, head, "QKV"[k], np.argwhere(bad)[:4])
+
+
 @pytest.mark.parametrize("b,s,n,d", [(8, 700, 16, 128), (16, 700, 8, 64)])
 @pytest.mark.parametrize("kind", ["none", "slopes", "table"])
 def test_larger_launches(b, s, n, d, kind):

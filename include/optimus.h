@@ -253,6 +253,11 @@ int optimus_attention_fused_bwd_static(const void* qkv, const void* attn, const 
  * A row without a pair has attn 0, lse -infinity and gradients 0.  What qkv, attn and d_attn hold in rows of padding is not looked at,
  * NaN included; their rows of attn and d_qkv are written as zeros.  (Other pairs that are left out have weight zero, and zero times
  * an infinity or NaN is NaN: as without changes, the values of tokens that are not padding are taken to be finite.)
+ * Accuracy: P, and dS in the backward, are rounded to bf16 before their products with V, dO, Q and K, as the operands are; sums, soft-max
+ * statistics and scores are fp32.  The tanh is off by at most 3e-7 (a cap of 50: 1.4e-5 of a score), with a cap beyond 64 only from a
+ * quarter of the cap on, below it by a few roundings of itself.  The forward takes finite scores of any size.  In the backward
+ * P = exp(S - lse), at most 1, is off by some 2e-7 |S| of itself, the rounding of an fp32 lse: little up to scores of 1e4; from 1e7 on the
+ * gradients of such a row mean nothing, those of others are not touched.
  * bucket(n) of the distance n = t - u: a side has `side` buckets: buckets, or buckets / 2 with two_sided; near = side / 2.  Distances
  * 0 .. near - 1 have a bucket each; bucket near + k begins at the first whole number not below near * (max_distance / near)^(k / (side -
  * near)); the last has no end.  n < 0 (a later key): bucket 0, or with two_sided side + bucket(-n).  2 <= side, even `buckets` with
@@ -439,7 +444,8 @@ int optimus_cross_entropy2d_bwd(const void* logits, const int32_t* labels, const
                                 float scale, int64_t M, int64_t v, int q, int i, int j, int dtype, void* stream);
 
 /* ---- one AdamW step over many tensors (the update of Section 3.2.3, which lets the layers share one parameter-gradient buffer) ----
- * Per element, in fp32 whatever the types:  g = grad_scale * sum over the parts of grad;  m = beta1 m + (1 - beta1) g;
+ * Per element, in fp32 whatever the types (root and reciprocal to a unit in the last place each, 4e-7 of the update; rounded exactly where
+ * eps is below 2^-42 / sqrt(1 - beta2)):  g = grad_scale * sum over the parts of grad;  m = beta1 m + (1 - beta1) g;
  *   v = beta2 v + (1 - beta2) g^2;  w = w - (lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps) + lr * weight_decay * w).
  * A vector's partial gradients [q][q][N/q] of optimus_layer_bwd are q parts of N elements: they are added in order here.
  * Weights: fp32; or bf16 with an fp32 `master` (which is updated; param receives it rounded to nearest even); or bf16 alone, rounded

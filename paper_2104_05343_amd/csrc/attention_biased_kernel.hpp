@@ -1,6 +1,6 @@
 // Fused local attention whose scores are changed before the soft-max (attention_fused_kernel.hpp has the layout of the work, which is
 // the same here):
-//   S = Q K^T / sqrt(d);  S = cap tanh(S / cap);  S -= slope[head] |t - u|, or S += table[head][bucket(u - t)];
+//   S = Q K^T / sqrt(d);  S = cap tanh(S / cap);  S -= slope[head] |t - u|, or S += table[head][bucket(t - u)];
 //   pair (t, u) is left out where the documents of t and u differ or t is padding (document < 0), where the mask is causal and u is
 //   behind both t and the prefix, and where the table's number is -1e30 or less.
 // A row that is left without a pair has output 0, log-sum-exp -infinity and no gradients.
@@ -9,7 +9,8 @@
 // there on dS (1 - tanh^2).
 //
 // What the additions cost beside the 32 to 64 clk a matrix instruction takes: the tanh 7 operations a score (the largest of the tile
-// among them) while a tile's scores stay below a quarter of the cap (odd polynomial), else an exponential and a reciprocal; slopes 2;
+// among them) while a tile's scores stay below a quarter of the cap (odd polynomial), else an exponential and a reciprocal, beside a cap
+// beyond 64 both; slopes 2;
 // the table nothing but one fused multiply-add where a whole tile lies in the last bucket, one LDS read where it does not.  Blocks of
 // keys that share no document with the workgroup's rows are not loaded: documents packed one after the other cost the sum of their
 // squares.

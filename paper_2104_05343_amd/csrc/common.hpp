@@ -201,7 +201,7 @@ struct AttnBiasedDesc {
   const int* documents;     // [sequences of the grid][s], or nullptr
   const int* prefix;        // [sequences of the grid], or nullptr
   void* blocks;             // scratch with documents: 16 bytes per 64 tokens of every sequence of the grid
-  float* table_parts;       // scratch with d_table: attn_biased_parts(...) floats
+  float* table_parts;       // scratch with d_table: devices * matrices * ceil(s / 64) * buckets floats
   float* d_table;           // backward: [device][heads of a device][buckets] of the launch's devices, or nullptr
 };
 int launch_attn_biased_fwd(const AttnBiasedDesc& d, hipStream_t stream);

@@ -283,6 +283,33 @@ int optimus_attention_biased_bwd(const void* qkv, const void* attn, const float*
                                  const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream);
 size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int q, const optimus_attention_bias* bias);
 
+/* ---- rotary positions of one to four axes, between the 3h projection and the attention ----
+ * The attention above knows the order of its tokens by masks and biases only; rotary positions turn queries and keys by angles, so that
+ * their products depend on differences of positions.  Layouts, coordinates as in optimus_attention_*; dtype FP32 or BF16, any head width up
+ * to 4096.  With P the sum of pairs[0 .. axes), pair p < P of every head's query and key are its elements p and P + p, or with interleaved
+ * 2p and 2p + 1; further elements, and values, are not changed.  A pair belongs to an axis: the first pairs[0] to axis 0, the next to axis 1
+ * and so on, or with in_turn the axes take turns, one pair each, those that have all of theirs passed over.  Its frequency is
+ * base^(-k / pairs[axis]) for the k-th pair of its axis, or with shared_ladder base^(-p / P).
+ *   angle = positions[axis][token] * scale[axis] * frequency;  (x, y) -> (x cos - y sin, x sin + y cos)
+ * The angle is a product of 64 bits, its whole turns are taken off before it is rounded to fp32.  positions: int32 device memory [axes][b*s]
+ * (rows sequence-major, every device of a grid row reads the same ones), of any sign; host: scale and base > 0 (finite, EINVAL).
+ * optimus_rotary writes the blocks of `out` whole, values too; out == qkv turns them in place; blocks that overlap otherwise: EINVAL.
+ * optimus_rotary_bwd is the gradient, the turn by -angle: of d_out with respect to qkv, in place with d_qkv == d_out.
+ * axes 1 .. 4, pairs[] >= 1, P <= 128, 2P <= h/n, even h/n with interleaved, 3h/q <= 2^18 (ESHAPE).  Pointers need the alignment of their elements
+ * only.  The struct is read before the call returns; one row (s = 1) is a call like any other. */
+typedef struct {
+  const int32_t* positions;
+  int axes;
+  int pairs[4];
+  double scale[4];
+  double base;
+  int interleaved, in_turn, shared_ladder;
+} optimus_rotary_axes;
+int optimus_rotary(const void* qkv, void* out, int b, int s, int h, int n, int q, int i, int j, int dtype, const optimus_rotary_axes* axes,
+                   void* stream);
+int optimus_rotary_bwd(const void* d_out, void* d_qkv, int b, int s, int h, int n, int q, int i, int j, int dtype,
+                       const optimus_rotary_axes* axes, void* stream);
+
 /* ---- one transformer layer on device (i, j) (Section 3.2; Eq. 1) ----
  * Wiring: a1 = LN1(x); qkv = a1 Wqkv + b; attn = local attention;
  * h_mid = x + attn Wo + b; a2 = LN2(h_mid); pre = a2 W1 + b; g = GeLU(pre);
@@ -442,6 +469,29 @@ int optimus_cross_entropy2d(const void* logits, const int32_t* labels, float* lo
                             int64_t M, int64_t v, int q, int i, int j, int dtype, void* stream);
 int optimus_cross_entropy2d_bwd(const void* logits, const int32_t* labels, const float* lse, void* d_logits,
                                 float scale, int64_t M, int64_t v, int q, int i, int j, int dtype, void* stream);
+
+/* ---- the norm of all gradients, and clipping by it, between the backward pass and the update ----
+ * norm = sqrt(sum over tensors and elements of g^2), g the sum of an element's parts (partial gradients [q][q][N/q] of optimus_layer_bwd
+ * are q parts of N elements); squares and sums in 64 bits.  scale = max_norm / norm where norm is above max_norm, else 1: what
+ * optimus_adamw_cfg.grad_scale takes, so that an update clips without a pass of its own.  A gradient that holds an infinity or NaN: scale
+ * is NaN.  norm: 1 float; scale: 1 float or NULL; norms: [count], each tensor's own, or NULL: device memory, written.  max_norm > 0, infinity
+ * included (EINVAL).  ws: optimus_gradient_norm_workspace_bytes(...) bytes (0 for a list that is refused), 8-byte aligned.
+ * optimus_gradient_clip: clipped = *scale * g, in the gradient's dtype, the parts added (in fp32, in order): clipped[n] may be grad
+ * itself (in place, with parts its first n elements; a scale of 1 then leaves a gradient without parts as it is), else it meets no
+ * other clipped and no gradient (EINVAL).  The norm does not look at clipped.
+ * gradients: host array, read before the call returns.  Pointers need the alignment of their elements only.  n from 1 to 2^34, parts to 65536,
+ * count to 65536 (ESHAPE).  A captured call reads the addresses it was captured with. */
+typedef struct {
+  const void* grad;    /* [parts][n] */
+  void* clipped;       /* [n]; optimus_gradient_clip only */
+  int64_t n;
+  int dtype;           /* OPTIMUS_FP32 / OPTIMUS_BF16 */
+  int parts;
+} optimus_gradient;
+int optimus_gradient_norm(const optimus_gradient* gradients, int count, float max_norm, float* norm, float* scale, float* norms, void* ws,
+                          size_t ws_bytes, void* stream);
+size_t optimus_gradient_norm_workspace_bytes(const optimus_gradient* gradients, int count);
+int optimus_gradient_clip(const optimus_gradient* gradients, int count, const float* scale, void* stream);
 
 /* ---- one AdamW step over many tensors (the update of Section 3.2.3, which lets the layers share one parameter-gradient buffer) ----
  * Per element, in fp32 whatever the types (root and reciprocal to a unit in the last place each, 4e-7 of the update; rounded exactly where

@@ -78,6 +78,15 @@ class AttentionBias(C.Structure):
                 ("two_sided", C.c_int), ("documents", C.c_void_p), ("prefix", C.c_void_p)]
 
 
+class RotaryAxes(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("axes", C.c_int), ("pairs", C.c_int * 4), ("scale", C.c_double * 4), ("base", C.c_double),
+                ("interleaved", C.c_int), ("in_turn", C.c_int), ("shared_ladder", C.c_int)]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("clipped", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int), ("parts", C.c_int)]
+
+
 class AdamwTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int), ("grad_dtype", C.c_int),
@@ -131,6 +140,8 @@ SIGNATURES = {
     "optimus_attention_biased_bwd": (_INT, [_P, _P, _P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT,
                                             C.POINTER(AttentionBias), _P, _SZ, _P]),
     "optimus_attention_biased_workspace_bytes": (_SZ, [_INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias)]),
+    "optimus_rotary": (_INT, [_P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(RotaryAxes), _P]),
+    "optimus_rotary_bwd": (_INT, [_P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(RotaryAxes), _P]),
     "optimus_embedding_fwd": (_INT, [_P, _P, _P, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
     "optimus_embedding_bwd": (_INT, [_P, _P, _P, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
     "optimus_cross_entropy2d_stats": (_INT, [_P, _P, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
@@ -145,6 +156,9 @@ SIGNATURES = {
     "optimus_layer_workspace_bytes_grid": (_SZ, [C.POINTER(LayerCfg)]),
     "optimus_layer_fwd": (_INT, [C.POINTER(LayerCfg), C.POINTER(LayerTensors), _INT, _INT, _P, _SZ, _P]),
     "optimus_layer_bwd": (_INT, [C.POINTER(LayerCfg), C.POINTER(LayerTensors), _INT, _INT, _P, _SZ, _P]),
+    "optimus_gradient_norm": (_INT, [C.POINTER(Gradient), _INT, _F, _P, _P, _P, _P, _SZ, _P]),
+    "optimus_gradient_norm_workspace_bytes": (_SZ, [C.POINTER(Gradient), _INT]),
+    "optimus_gradient_clip": (_INT, [C.POINTER(Gradient), _INT, _P, _P]),
     "optimus_adamw_step": (_INT, [C.POINTER(AdamwCfg), C.POINTER(AdamwTensor), _INT, _P]),
     "optimus_stack_adamw_elements": (_I64, [C.POINTER(LayerCfg)]),
     "optimus_stack_bwd_adamw": (_INT, [C.POINTER(LayerCfg), _INT, C.POINTER(LayerParams), C.POINTER(AdamwState), C.POINTER(AdamwCfg), _F, _P, _P,
@@ -376,6 +390,25 @@ def attention_biased_bwd(qkv, attn, lse, d_attn, d_qkv, d_table, b, s, h, n, q, 
                                               int(causal), dtype, C.byref(bias), p, nb, _stream(stream)), "optimus_attention_biased_bwd")
 
 
+def make_rotary(positions, pairs, base=10000.0, scale=None, interleaved=False, in_turn=False, shared=False) -> RotaryAxes:
+    """Rotary positions (optimus_rotary_axes): positions int32 [len(pairs)][b*s], contiguous (EDTYPE, EINVAL); pairs of each axis; scale of
+    each axis' positions, 1 by default.  Holds the positions' address: keep the tensor alive."""
+    _plain_tensor(positions, _INT32, "make_rotary: positions")
+    scale = [1.0] * len(pairs) if scale is None else list(scale)
+    if not 1 <= len(pairs) <= 4 or len(scale) != len(pairs):
+        raise OptimusError(EINVAL, "make_rotary: axes")
+    return RotaryAxes(_ptr(positions), len(pairs), (C.c_int * 4)(*pairs), (C.c_double * 4)(*scale), float(base), int(interleaved), int(in_turn),
+                      int(shared))
+
+
+def rotary(qkv, out, b, s, h, n, q, i, j, dtype, axes: RotaryAxes, stream=None):
+    _check(lib().optimus_rotary(_ptr(qkv), _ptr(out), b, s, h, n, q, i, j, dtype, C.byref(axes), _stream(stream)), "optimus_rotary")
+
+
+def rotary_bwd(d_out, d_qkv, b, s, h, n, q, i, j, dtype, axes: RotaryAxes, stream=None):
+    _check(lib().optimus_rotary_bwd(_ptr(d_out), _ptr(d_qkv), b, s, h, n, q, i, j, dtype, C.byref(axes), _stream(stream)), "optimus_rotary_bwd")
+
+
 def layer_workspace_bytes(cfg: LayerCfg) -> int:
     return lib().optimus_layer_workspace_bytes(C.byref(cfg))
 
@@ -515,6 +548,46 @@ def make_adamw_tensors(tensors):
         a.param_dtype, a.grad_dtype = (codes[t[k].dtype] for k in ("param", "grad"))
         a.grad_parts, a.weight_decay = t.get("grad_parts", 1), t.get("weight_decay", 0.0)
     return out
+
+
+def make_gradients(tensors):
+    """tensors: list of dicts grad (a torch tensor) and, where they differ from these defaults, n=grad.numel() // parts, parts=1,
+    clipped=grad.  Refused: types other than optimus_gradient's (EDTYPE), fewer than n * parts elements, or n of clipped (ESHAPE), elements
+    not one after the other or not on one device (EINVAL).  The array holds addresses: keep the tensors alive."""
+    codes = {torch.float32: FP32, torch.bfloat16: BF16}
+    out = (Gradient * len(tensors))()
+    for a, t in zip(out, tensors):
+        grad, parts = t["grad"], t.get("parts", 1)
+        clipped = t["clipped"] if t.get("clipped") is not None else grad
+        n = t.get("n", grad.numel() // max(1, parts))
+        for name, x, least in (("grad", grad, n * parts), ("clipped", clipped, n)):
+            _plain_tensor(x, (grad.dtype,) if grad.dtype in codes else tuple(codes), "make_gradients: " + name)
+            if x.numel() < least:
+                raise OptimusError(ESHAPE, "make_gradients: " + name)
+            if x.device != tensors[0]["grad"].device:
+                raise OptimusError(EINVAL, "make_gradients: " + name)
+        a.grad, a.clipped, a.n, a.dtype, a.parts = _ptr(grad), _ptr(clipped), n, codes[grad.dtype], parts
+    return out
+
+
+def gradient_norm_workspace_bytes(gradients) -> int:
+    return lib().optimus_gradient_norm_workspace_bytes(gradients, len(gradients))
+
+
+def gradient_norm(gradients, max_norm, norm, scale=None, norms=None, ws=None, stream=None):
+    """gradients: what make_gradients returned; norm, scale (1 element) and norms (one a tensor): fp32, contiguous (EDTYPE, EINVAL, ESHAPE)."""
+    for name, t, least in (("norm", norm, 1), ("scale", scale, 1), ("norms", norms, len(gradients))):
+        _plain_tensor(t, _FP32_ONLY, "gradient_norm: " + name)
+        if t is not None and not isinstance(t, int) and t.numel() < least:
+            raise OptimusError(ESHAPE, "gradient_norm: " + name)
+    p, nb = _ws(ws)
+    _check(lib().optimus_gradient_norm(gradients, len(gradients), max_norm, _ptr(norm), _ptr(scale), _ptr(norms), p, nb, _stream(stream)),
+           "optimus_gradient_norm")
+
+
+def gradient_clip(gradients, scale, stream=None):
+    _plain_tensor(scale, _FP32_ONLY, "gradient_clip: scale")
+    _check(lib().optimus_gradient_clip(gradients, len(gradients), _ptr(scale), _stream(stream)), "optimus_gradient_clip")
 
 
 def adamw_step(cfg: AdamwCfg, tensors, stream=None):

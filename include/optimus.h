@@ -283,6 +283,39 @@ int optimus_attention_biased_bwd(const void* qkv, const void* attn, const float*
                                  const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream);
 size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int q, const optimus_attention_bias* bias);
 
+/* ---- attention over chosen blocks of keys ----
+ * For sequences too long for all pairs: keys come in blocks of `block` (a multiple of 64, up to 4096; at most 1024 blocks in a sequence), and
+ * a query attends to `count` blocks (1 .. 64) at most.  Two steps, of which the second takes any choice:
+ * optimus_attention_select(qkv): mean[v] = mean of block v's keys (sum in 64 bits, rounded to fp32 and then to bf16); a query t chooses its
+ *   own block, t / block, and the count - 1 others with the largest products q_t . mean[v]: with causal != 0 among the blocks in front of
+ *   its own, else among all.  The order is that of the exact products (fp32 ones decide where they leave no doubt, 64-bit ones else); of
+ *   equal ones the lower block is chosen, a product that is NaN is below all others.  selected int32 [q][q][(b/q)*(n/q)][s][count] in device
+ *   order: ascending, -1 behind them.  No gradient goes through the choice.
+ * optimus_attention_selected_fwd: S = Q K^T / sqrt(d) over the keys of the blocks in `selected` (causal != 0: and u <= t), P = softmax, O = P V,
+ *   lse as in optimus_attention_fused_*.  Entries in any order; those below 0, beyond the sequence, repeated, or of blocks that a causal query
+ *   does not see count as not there.  A query without a key has attn 0, lse -infinity and gradients 0.
+ * optimus_attention_selected_bwd: from the same `selected` and the forward's attn and lse: P = exp(S - lse), dS = P (dO V^T - rowsum(dO attn)).
+ * lengths: int32 [b] device memory or NULL (all s): tokens of a sequence that count (clamped to 0 .. s).  What qkv and d_attn hold behind them
+ * is not looked at, NaN included; there selected is -1, attn 0, lse -infinity and d_qkv 0.
+ * P and dS are rounded to bf16 before their products, as the operands are; scores, sums and a query's partial results are fp32; lse enters as
+ * in optimus_attention_biased_bwd.  qkv, attn, lse, d_attn, d_qkv, coordinates and limits as in optimus_attention_fused_*; bf16 only;
+ * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
+ * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
+ * from call to call: calls that may overlap need one each.  It holds up to 128 MiB of partial results, or one (sequence, head)'s:
+ * s * count * (d + 2) * 4 bytes. */
+typedef struct {
+  int block, count;
+  const int32_t* lengths;
+} optimus_selection;
+int optimus_attention_select(const void* qkv, int32_t* selected, int b, int s, int h, int n, int q, int i, int j, int causal, int dtype,
+                             const optimus_selection* selection, void* ws, size_t ws_bytes, void* stream);
+int optimus_attention_selected_fwd(const void* qkv, const int32_t* selected, void* attn, float* lse, int b, int s, int h, int n, int q, int i, int j,
+                                   int causal, int dtype, const optimus_selection* selection, void* ws, size_t ws_bytes, void* stream);
+int optimus_attention_selected_bwd(const void* qkv, const int32_t* selected, const void* attn, const float* lse, const void* d_attn, void* d_qkv,
+                                   int b, int s, int h, int n, int q, int i, int j, int causal, int dtype, const optimus_selection* selection,
+                                   void* ws, size_t ws_bytes, void* stream);
+size_t optimus_attention_selected_workspace_bytes(int b, int s, int h, int n, int q, int i, int j, const optimus_selection* selection);
+
 /* ---- rotary positions of one to four axes, between the 3h projection and the attention ----
  * The attention above knows the order of its tokens by masks and biases only; rotary positions turn queries and keys by angles, so that
  * their products depend on differences of positions.  Layouts, coordinates as in optimus_attention_*; dtype FP32 or BF16, any head width up

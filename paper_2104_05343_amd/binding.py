@@ -78,6 +78,10 @@ class AttentionBias(C.Structure):
                 ("two_sided", C.c_int), ("documents", C.c_void_p), ("prefix", C.c_void_p)]
 
 
+class Selection(C.Structure):
+    _fields_ = [("block", C.c_int), ("count", C.c_int), ("lengths", C.c_void_p)]
+
+
 class RotaryAxes(C.Structure):
     _fields_ = [("positions", C.c_void_p), ("axes", C.c_int), ("pairs", C.c_int * 4), ("scale", C.c_double * 4), ("base", C.c_double),
                 ("interleaved", C.c_int), ("in_turn", C.c_int), ("shared_ladder", C.c_int)]
@@ -140,6 +144,12 @@ SIGNATURES = {
     "optimus_attention_biased_bwd": (_INT, [_P, _P, _P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT,
                                             C.POINTER(AttentionBias), _P, _SZ, _P]),
     "optimus_attention_biased_workspace_bytes": (_SZ, [_INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias)]),
+    "optimus_attention_select": (_INT, [_P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection), _P, _SZ, _P]),
+    "optimus_attention_selected_fwd": (_INT, [_P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection), _P, _SZ,
+                                              _P]),
+    "optimus_attention_selected_bwd": (_INT, [_P, _P, _P, _P, _P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection), _P,
+                                              _SZ, _P]),
+    "optimus_attention_selected_workspace_bytes": (_SZ, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection)]),
     "optimus_rotary": (_INT, [_P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(RotaryAxes), _P]),
     "optimus_rotary_bwd": (_INT, [_P, _P, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(RotaryAxes), _P]),
     "optimus_embedding_fwd": (_INT, [_P, _P, _P, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _P]),
@@ -388,6 +398,38 @@ def attention_biased_bwd(qkv, attn, lse, d_attn, d_qkv, d_table, b, s, h, n, q, 
     p, nb = _ws(ws)
     _check(lib().optimus_attention_biased_bwd(_ptr(qkv), _ptr(attn), _ptr(lse), _ptr(d_attn), _ptr(d_qkv), _ptr(d_table), b, s, h, n, q, i, j,
                                               int(causal), dtype, C.byref(bias), p, nb, _stream(stream)), "optimus_attention_biased_bwd")
+
+
+def make_selection(block, count, lengths=None) -> Selection:
+    """Which blocks a query attends to (optimus_selection): lengths int32 [b], contiguous, or None (EDTYPE, EINVAL).  Holds its address: keep the
+    tensor alive."""
+    _plain_tensor(lengths, _INT32, "make_selection: lengths")
+    return Selection(block, count, _ptr(lengths))
+
+
+def attention_selected_workspace_bytes(b, s, h, n, q, i, j, selection: Selection) -> int:
+    return lib().optimus_attention_selected_workspace_bytes(b, s, h, n, q, i, j, C.byref(selection))
+
+
+def attention_select(qkv, selected, b, s, h, n, q, i, j, causal, dtype, selection: Selection, ws, stream=None):
+    _plain_tensor(selected, _INT32, "attention_select: selected")
+    p, nb = _ws(ws)
+    _check(lib().optimus_attention_select(_ptr(qkv), _ptr(selected), b, s, h, n, q, i, j, int(causal), dtype, C.byref(selection), p, nb,
+                                          _stream(stream)), "optimus_attention_select")
+
+
+def attention_selected_fwd(qkv, selected, attn, lse, b, s, h, n, q, i, j, causal, dtype, selection: Selection, ws, stream=None):
+    _plain_tensor(selected, _INT32, "attention_selected_fwd: selected")
+    p, nb = _ws(ws)
+    _check(lib().optimus_attention_selected_fwd(_ptr(qkv), _ptr(selected), _ptr(attn), _ptr(lse), b, s, h, n, q, i, j, int(causal), dtype,
+                                                C.byref(selection), p, nb, _stream(stream)), "optimus_attention_selected_fwd")
+
+
+def attention_selected_bwd(qkv, selected, attn, lse, d_attn, d_qkv, b, s, h, n, q, i, j, causal, dtype, selection: Selection, ws, stream=None):
+    _plain_tensor(selected, _INT32, "attention_selected_bwd: selected")
+    p, nb = _ws(ws)
+    _check(lib().optimus_attention_selected_bwd(_ptr(qkv), _ptr(selected), _ptr(attn), _ptr(lse), _ptr(d_attn), _ptr(d_qkv), b, s, h, n, q, i, j,
+                                                int(causal), dtype, C.byref(selection), p, nb, _stream(stream)), "optimus_attention_selected_bwd")
 
 
 def make_rotary(positions, pairs, base=10000.0, scale=None, interleaved=False, in_turn=False, shared=False) -> RotaryAxes:

@@ -412,6 +412,48 @@ int run_attention_biased(bool bwd, const void* qkv, void* attn, float* lse, cons
   return bwd ? launch_attn_biased_bwd(d, as_stream(stream)) : launch_attn_biased_fwd(d, as_stream(stream));
 }
 
+// ---- attention over chosen blocks ----
+int selected_desc(int b, int s, int h, int n, int q, int i, int j, const optimus_selection* sel, AttnDims* a, AttnSelectedDesc* d) {
+  if (const int rc = attn_fused_dims(b, s, h, n, q, a)) return rc;
+  if (const int rc = check_coords(q, i, j)) return rc;
+  if (!sel) return OPTIMUS_EINVAL;
+  if (sel->block < 64 || sel->block % 64 || sel->block > 4096 || (s - 1) / sel->block >= 1024 || sel->count < 1 || sel->count > 64) return OPTIMUS_ESHAPE;
+  if ((uintptr_t)sel->lengths & 3) return OPTIMUS_EINVAL;
+  AttnFusedDesc& f = d->base;
+  f.s = s; f.d = a->d; f.nb = a->nb; f.nh = a->nh; f.ld = a->ld; f.ldo = a->ldo;
+  f.ndev = is_grid(i, j) ? q * q : 1;
+  if (f.ndev * a->nmat > 65535 || 512ll * a->ld >= (1ll << 31)) return OPTIMUS_ESHAPE;
+  f.dev_qkv = a->blk_qkv; f.dev_attn = a->blk_attn;
+  d->q = q; d->dev0 = is_grid(i, j) ? 0 : i * q + j;
+  d->block = sel->block; d->count = sel->count; d->lengths = sel->lengths;
+  return OPTIMUS_OK;
+}
+size_t selected_ws_bytes(const AttnSelectedDesc& d) {
+  const size_t choice = attn_select_ws_bytes(d), both = attn_selected_ws_bytes(d);
+  return choice > both ? choice : both;
+}
+enum { kChoose, kForward, kBackward };
+int run_attention_selected(int what, const void* qkv, int32_t* selected, void* attn, float* lse, const void* d_attn, void* d_qkv, int b, int s, int h,
+                           int n, int q, int i, int j, int causal, int dtype, const optimus_selection* sel, void* ws, size_t ws_bytes, void* stream) {
+  if (!qkv || !selected || (what != kChoose && (!attn || !lse)) || (what == kBackward && (!d_attn || !d_qkv))) return OPTIMUS_EINVAL;
+  if (dtype != OPTIMUS_BF16) return OPTIMUS_EDTYPE;
+  AttnDims a;
+  AttnSelectedDesc d = {};
+  if (const int rc = selected_desc(b, s, h, n, q, i, j, sel, &a, &d)) return rc;
+  if (!ws || ws_bytes < selected_ws_bytes(d) || (uintptr_t)ws & 255) return OPTIMUS_EWORKSPACE;
+  AttnFusedDesc& f = d.base;
+  f.qkv = (const bf16_t*)qkv + d.dev0 * a.blk_qkv;
+  f.attn = attn ? (bf16_t*)attn + d.dev0 * a.blk_attn : nullptr;
+  f.lse = lse ? lse + d.dev0 * a.nmat * s : nullptr;
+  f.d_attn = d_attn ? (const bf16_t*)d_attn + d.dev0 * a.blk_attn : nullptr;
+  f.d_qkv = d_qkv ? (bf16_t*)d_qkv + d.dev0 * a.blk_qkv : nullptr;
+  f.causal = causal ? 1 : 0;
+  d.selected = d.chosen = selected + d.dev0 * a.nmat * s * sel->count;
+  d.ws = ws;
+  if (what == kChoose) return launch_attn_select(d, as_stream(stream));
+  return what == kForward ? launch_attn_selected_fwd(d, as_stream(stream)) : launch_attn_selected_bwd(d, as_stream(stream));
+}
+
 int end_desc(int64_t M, int64_t v, int64_t h, int q, int i, int j, int dtype, EndDesc* d) {
   if (dtype != OPTIMUS_FP32 && dtype != OPTIMUS_BF16) return OPTIMUS_EDTYPE;
   if (q <= 0 || M <= 0 || v <= 0 || h <= 0 || M % q || v % q || h % q) return OPTIMUS_ESHAPE;
@@ -885,6 +927,27 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
   AttnBiasedDesc d = {};
   if (attn_biased_dims(b, s, h, n, q, &a) || bias_desc(bias, 1, &d)) return 0;
   return biased_ws(a, b, q, d).total;
+}
+size_t optimus_attention_selected_workspace_bytes(int b, int s, int h, int n, int q, int i, int j, const optimus_selection* selection) {
+  AttnDims a;
+  AttnSelectedDesc d = {};
+  return selected_desc(b, s, h, n, q, i, j, selection, &a, &d) ? 0 : selected_ws_bytes(d);
+}
+int optimus_attention_select(const void* qkv, int32_t* selected, int b, int s, int h, int n, int q, int i, int j, int causal, int dtype,
+                             const optimus_selection* selection, void* ws, size_t ws_bytes, void* stream) {
+  return run_attention_selected(kChoose, qkv, selected, nullptr, nullptr, nullptr, nullptr, b, s, h, n, q, i, j, causal, dtype, selection, ws, ws_bytes,
+                                stream);
+}
+int optimus_attention_selected_fwd(const void* qkv, const int32_t* selected, void* attn, float* lse, int b, int s, int h, int n, int q, int i, int j,
+                                   int causal, int dtype, const optimus_selection* selection, void* ws, size_t ws_bytes, void* stream) {
+  return run_attention_selected(kForward, qkv, const_cast<int32_t*>(selected), attn, lse, nullptr, nullptr, b, s, h, n, q, i, j, causal, dtype, selection,
+                                ws, ws_bytes, stream);
+}
+int optimus_attention_selected_bwd(const void* qkv, const int32_t* selected, const void* attn, const float* lse, const void* d_attn, void* d_qkv,
+                                   int b, int s, int h, int n, int q, int i, int j, int causal, int dtype, const optimus_selection* selection,
+                                   void* ws, size_t ws_bytes, void* stream) {
+  return run_attention_selected(kBackward, qkv, const_cast<int32_t*>(selected), const_cast<void*>(attn), const_cast<float*>(lse), d_attn, d_qkv, b, s, h,
+                                n, q, i, j, causal, dtype, selection, ws, ws_bytes, stream);
 }
 int optimus_attention_biased_fwd(const void* qkv, void* attn, float* lse, int b, int s, int h, int n, int q, int i, int j, int causal,
                                  int dtype, const optimus_attention_bias* bias, void* ws, size_t ws_bytes, void* stream) {

@@ -1,0 +1,339 @@
+// The choice of blocks for the attention over chosen blocks (attention_selected_kernel.hpp): mean keys, scores, the best of a row.
+//
+// The choice is that of exact scores, q . mean with both as the bf16 numbers they are; equal scores: the lower block.  The matrix cores give
+// scores that are off by at most E = d 2^-23 |q| |mean| (a rounding of the running sum per product), which decides all but a few
+// rows in a thousand: with x the K-th largest such score, what is above x + 2E is chosen, what is below x - 2E is not, and where more than
+// the places left lie between, their scores are computed again in 64 bits (products of bf16 numbers and their sums are exact there,
+// unless they span more than 2^37).
+//
+// A workgroup has 32 queries of one block: its wavefronts share the blocks' scores out among them, 32 at a time, into LDS, then eight lanes
+// have a query each, an eighth of its scores in registers, and find a threshold with K scores above it by halving.
+// Bound: the arithmetic of that search, some 12 rounds of two operations a score; the means are a pass over the keys.
+#include "attention_selected_kernel.hpp"
+
+namespace optimus {
+namespace {
+
+// Mean keys: a wavefront has a block, a lane 8 of its columns in every (64 / (d / 8))-th row.  Sums in 64 bits: their bf16 rounding does not
+// depend on the order then.
+template <int D>
+__global__ __launch_bounds__(256) void block_means_kernel(SelectedArgs a) {
+  constexpr int CH = D / 8, ROWS = 64 / CH;
+  const FusedArgs& f = a.f;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int v = blockIdx.x * 4 + wave, mm = blockIdx.y;
+  if (v >= a.blocks) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int row0 = v * a.block, rows = min(a.block, m.len - row0);
+  if (rows <= 0) return;
+  const bf16_t* p = f.qkv + m.qkv + D + (long long)row0 * f.ld + lane % CH * 8;
+  double sum[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum[k] = 0.0;
+#pragma unroll 4
+  for (int r = lane / CH; r < rows; r += ROWS) {
+    const bf16x8 x = *(const bf16x8*)(p + (long long)r * f.ld);
+    const u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      sum[2 * k] += (double)__uint_as_float(w[k] << 16);
+      sum[2 * k + 1] += (double)__uint_as_float(w[k] & 0xffff0000u);
+    }
+  }
+  float mean[8], size = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+#pragma unroll
+    for (int step = CH; step < 64; step <<= 1) sum[k] += __shfl_xor(sum[k], step);
+    mean[k] = bf16_to_f32(f32_to_bf16((float)(sum[k] / rows)));
+    size = fmaf(mean[k], mean[k], size);
+  }
+#pragma unroll
+  for (int step = 1; step < CH; step <<= 1) size += __shfl_xor(size, step);
+  const long long at = (long long)mm * a.blocks + v;
+  if (lane < CH) {
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = pack2_bf16(mean[2 * k], mean[2 * k + 1]);
+    *(u32x4*)(a.means + at * D + lane * 8) = w;
+  }
+  if (lane == 0) a.mean_sizes[at] = sqrtf(size) * 1.0001f;
+}
+
+// sums and the like over the eight lanes of a query
+template <class T, class F>
+__device__ __forceinline__ T eight(T x, F f) {
+#pragma unroll
+  for (int step = 1; step < 8; step <<= 1) x = f(x, __shfl_xor(x, step));
+  return x;
+}
+__device__ __forceinline__ int sum8(int x) { return eight(x, [](int p, int q) { return p + q; }); }
+__device__ __forceinline__ float min8(float x) { return eight(x, [](float p, float q) { return fminf(p, q); }); }
+__device__ __forceinline__ float max8(float x) { return eight(x, [](float p, float q) { return fmaxf(p, q); }); }
+
+constexpr int kRows = 32;             // queries of a workgroup
+constexpr int kKept = kMostCount;     // best exact scores kept of a query
+
+// LDS: scores [kRows][stride], kept scores, kept blocks, chosen bits
+__host__ __device__ inline int score_stride(int blocks) { return (blocks + 31) / 32 * 32 + 4; }
+__host__ __device__ inline int bit_words(int blocks) { return (blocks + 31) / 32; }
+inline size_t select_lds(int blocks) {
+  return (size_t)kRows * (score_stride(blocks) * 4 + bit_words(blocks) * 4 + kKept * 10);
+}
+
+// NV: scores of a lane; 8 NV blocks at most.
+template <int D, int NV>
+__global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
+  constexpr int KS = D / 16;
+  extern __shared__ __attribute__((aligned(16))) char dynamic[];
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int mm = blockIdx.y, q0 = blockIdx.x * kRows;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int own = q0 / a.block;                       // (blocks are multiples of 64 keys)
+  const int have = (m.len + a.block - 1) / a.block;   // blocks with keys
+  const int others = a.causal ? min(own, have) : have;   // candidates, the own block among them without a mask
+  const int K = a.count - 1;
+  const int stride = score_stride(a.blocks), words = bit_words(a.blocks);
+  double* kept = (double*)dynamic;                                     // [kRows][kKept]
+  float* scores = (float*)(kept + kRows * kKept);                      // [kRows][stride]
+  unsigned* bits = (unsigned*)(scores + kRows * stride);               // [kRows][words]
+  unsigned short* kept_block = (unsigned short*)(bits + kRows * words);   // [kRows][kKept]
+  const int row = tid >> 3, e = tid & 7, t = q0 + row;   // eight lanes a query
+  int* out = a.chosen + (m.vec + t) * a.count;
+  const bool query = t < m.len;
+  const int eligible = a.causal ? others : others - 1;
+  if (K == 0 || eligible <= K || q0 >= m.len) {   // (a workgroup's queries are of one block) the own one, or all of them
+    if (t < f.s) {
+      const int n = !query ? 0 : K == 0 ? 1 : eligible + 1, first = K == 0 ? own : 0;
+      for (int k = e; k < a.count; k += 8) out[k] = k < n ? first + k : -1;
+    }
+    return;
+  }
+  // scores: 32 blocks a wavefront at a time
+  {
+    const int qrow = min(q0 + (lane & 31), m.len - 1);
+    const bf16_t* Q = f.qkv + m.qkv + (long long)qrow * f.ld + g * 8;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(Q + ks * 16);
+    const bf16_t* means = a.means + (long long)mm * a.blocks * D;
+    for (int v0 = wave * 32; v0 < others; v0 += 128) {
+      const bf16_t* p = means + (long long)min(v0 + (lane & 31), others - 1) * D + g * 8;
+      f32x16 acc = zero16();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(p + ks * 16), qf[ks], acc, 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *(float4*)(scores + (lane & 31) * stride + v0 + 8 * c + 4 * g) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+    }
+  }
+  for (int k = tid; k < kRows * words; k += 256) bits[k] = 0;
+  // E of the row
+  float mean_size = 0.f, q_size = 0.f;
+  for (int v = e; v < others; v += 8) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
+  mean_size = max8(mean_size);
+  const bf16_t* Q = f.qkv + m.qkv + (long long)min(t, m.len - 1) * f.ld + e * (D / 8);
+#pragma unroll
+  for (int k = 0; k < D / 8; ++k) q_size = fmaf(bf16_to_f32(Q[k]), bf16_to_f32(Q[k]), q_size);
+  q_size = sqrtf(eight(q_size, [](float p, float q) { return p + q; })) * 1.0001f;
+  float error = q_size * mean_size * (D * 1.1920929e-7f);
+  __syncthreads();
+  const float* mine = scores + row * stride;
+  // a lane's scores: of blocks e, e + 8, ..; -infinity: no candidate.  wild: a score or the bound is not finite, or too small for the bound
+  float x[NV];
+  float lo = INFINITY, hi = -INFINITY;
+  bool wild = !(error < 1e30f) || error < 1e-30f || q_size < 1e-25f || mean_size < 1e-25f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = e + 8 * k;
+    const bool candidate = v < others && v != own;
+    x[k] = candidate ? mine[v] : -INFINITY;
+    wild = wild || (candidate && !(fabsf(x[k]) < 1e30f));
+    lo = candidate ? fminf(lo, x[k]) : lo;
+    hi = fmaxf(hi, x[k]);
+  }
+  lo = min8(lo);
+  hi = max8(hi);
+  wild = sum8(wild) != 0;
+  // a threshold with K scores from it on: halving [lo, hi), at lo at least K are (all), at hi fewer (a step above the largest)
+  float cut = lo;
+  bool found = wild || !query;
+  hi += fabsf(hi) * 1e-6f + 1e-37f;
+  for (int round = 0; round < 40 && __builtin_amdgcn_ballot_w64(!found) != 0; ++round) {
+    const float middle = 0.5f * lo + 0.5f * hi;
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) n += x[k] >= middle ? 1 : 0;
+    n = sum8(n);
+    if (!found) {
+      if (n >= K) lo = middle;
+      else hi = middle;
+      cut = lo;
+      found = n == K;
+    }
+  }
+  // scores certainly chosen are above the K-th, which is the least from `cut` on (or in [lo, hi) where no threshold divides them)
+  float least = INFINITY;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) least = x[k] >= cut ? fminf(least, x[k]) : least;
+  least = min8(least);
+  int n_cut = 0;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) n_cut += x[k] >= cut ? 1 : 0;
+  n_cut = sum8(n_cut);
+  float above = (n_cut == K ? least : hi) + 2.0f * error, below = least - 2.0f * error;
+  if (wild) {
+    above = INFINITY;
+    below = -INFINITY;
+  }
+  int n_above = 0, n_below = 0;   // scores from `below` on
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = e + 8 * k;
+    const bool candidate = v < others && v != own;
+    n_above += candidate && x[k] > above ? 1 : 0;
+    n_below += candidate && !(x[k] < below) ? 1 : 0;
+  }
+  n_above = wild ? 0 : sum8(n_above);
+  n_below = sum8(n_below);
+  const bool decided = n_below == K;
+  // the bits of what is chosen; what is contested otherwise stays for the exact scores
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = e + 8 * k;
+    const bool candidate = v < others && v != own;
+    if (query && candidate && (decided ? !(x[k] < below) : !wild && x[k] > above)) atomicOr(&bits[row * words + (v >> 5)], 1u << (v & 31));
+  }
+  if (query && e == 0) atomicOr(&bits[row * words + (own >> 5)], 1u << (own & 31));
+  __builtin_amdgcn_wave_barrier();
+  if (__builtin_amdgcn_ballot_w64(query && !decided) != 0) {
+    // exact scores, in the order of the blocks, the best ones kept: one that is not above the worst kept is out (equal: the lower block stays)
+    const int places = query && !decided ? K - n_above : 0;
+    double* best = kept + row * kKept;
+    unsigned short* block_of = kept_block + row * kKept;
+    int n = 0, worst_at = 0;
+    double worst = 0.0;
+    const bf16_t* means = a.means + (long long)mm * a.blocks * D + e * (D / 8);
+    for (int v = 0; v < others; ++v) {
+      const float approximate = mine[v];
+      const bool contested = places > 0 && v != own && !(approximate < below) && (wild || !(approximate > above));
+      if (__builtin_amdgcn_ballot_w64(contested) == 0) continue;
+      double score = 0.0;
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) score += (double)bf16_to_f32(Q[k]) * (double)bf16_to_f32(means[(long long)v * D + k]);
+      score = eight(score, [](double p, double q) { return p + q; });
+      if (score != score) score = -INFINITY;   // (a score that is no number is below all)
+      if (contested && n < places) {
+        if (e == 0) {
+          best[n] = score;
+          block_of[n] = (unsigned short)v;
+        }
+        ++n;
+      } else if (contested && score > worst) {
+        if (e == 0) {
+          best[worst_at] = score;
+          block_of[worst_at] = (unsigned short)v;
+        }
+      } else {
+        continue;
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (n == places) {   // the worst kept: the lowest score, of equal ones the last block
+        double w = INFINITY;
+        int at = -1, of = -1;
+        for (int k = e; k < n; k += 8) {
+          const double y = best[k];
+          const int b = block_of[k];
+          if (at < 0 || y < w || (y == w && b > of)) {
+            w = y;
+            at = k;
+            of = b;
+          }
+        }
+#pragma unroll
+        for (int step = 1; step < 8; step <<= 1) {
+          const double y = __shfl_xor(w, step);
+          const int other = __shfl_xor(at, step), b = __shfl_xor(of, step);
+          if (other >= 0 && (at < 0 || y < w || (y == w && b > of))) {
+            w = y;
+            at = other;
+            of = b;
+          }
+        }
+        worst = w;
+        worst_at = at;
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    for (int k = e; k < n; k += 8) {
+      const int v = block_of[k];
+      atomicOr(&bits[row * words + (v >> 5)], 1u << (v & 31));
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  // the row's blocks in order: a lane has a run of words, those of lower lanes come first
+  if (t >= f.s) return;
+  const int each = (words + 7) / 8, from = min(e * each, words), to = min(from + each, words);
+  int n = 0;
+  for (int w = from; w < to; ++w) n += __popc(bits[row * words + w]);
+  int before = n;
+#pragma unroll
+  for (int step = 1; step < 8; step <<= 1) {
+    const int y = __shfl_up(before, step, 8);
+    if (e >= step) before += y;
+  }
+  const int all = __shfl(before, 7, 8);
+  int k = before - n;
+  for (int w = from; w < to; ++w)
+    for (unsigned left = bits[row * words + w]; left; left &= left - 1) out[k++] = w * 32 + __builtin_ctz(left);
+  for (int r = all + e; r < a.count; r += 8) out[r] = -1;
+}
+
+template <int D, int NV>
+void select_launch(const SelectedArgs& a, int mats, hipStream_t st) {
+  const size_t lds = select_lds(a.blocks);
+  if (lds > 65536) (void)hipFuncSetAttribute((const void*)select_kernel<D, NV>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  select_kernel<D, NV><<<dim3((a.f.s + kRows - 1) / kRows, mats), 256, lds, st>>>(a);
+}
+template <int D>
+void choose(const SelectedArgs& a, int mats, hipStream_t st) {
+  block_means_kernel<D><<<dim3((a.blocks + 3) / 4, mats), 256, 0, st>>>(a);
+  if (a.blocks <= 32) select_launch<D, 4>(a, mats, st);
+  else if (a.blocks <= 64) select_launch<D, 8>(a, mats, st);
+  else if (a.blocks <= 128) select_launch<D, 16>(a, mats, st);
+  else if (a.blocks <= 256) select_launch<D, 32>(a, mats, st);
+  else if (a.blocks <= 512) select_launch<D, 64>(a, mats, st);
+  else select_launch<D, 128>(a, mats, st);
+}
+
+size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+size_t attn_select_ws_bytes(const AttnSelectedDesc& b) {
+  const AttnFusedDesc& d = b.base;
+  const size_t means = (size_t)d.ndev * d.nb * d.nh * ((d.s + b.block - 1) / b.block);
+  return round256(means * d.d * 2) + round256(means * 4);
+}
+
+int launch_attn_select(const AttnSelectedDesc& b, hipStream_t st) {
+  const AttnFusedDesc& d = b.base;
+  SelectedArgs a = {};
+  a.f.qkv = (const bf16_t*)d.qkv;
+  a.f.s = d.s; a.f.nh = d.nh; a.f.ld = d.ld; a.f.ldo = d.ldo;
+  a.f.dev_qkv = d.dev_qkv; a.f.dev_attn = d.dev_attn;
+  a.chosen = b.chosen; a.lengths = b.lengths;
+  a.nb = d.nb; a.nmat = d.nb * d.nh; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal;
+  a.block = b.block; a.count = b.count; a.blocks = (d.s + b.block - 1) / b.block;
+  const int mats = d.ndev * a.nmat;
+  if (mats > 65535 || a.blocks > kMostBlocks) return OPTIMUS_ESHAPE;
+  a.means = (bf16_t*)b.ws;
+  a.mean_sizes = (float*)((char*)b.ws + round256((size_t)mats * a.blocks * d.d * 2));
+  if (d.d == 64) choose<64>(a, mats, st);
+  else choose<128>(a, mats, st);
+  return hip_launch_status();
+}
+
+}  // namespace optimus

@@ -1,0 +1,535 @@
+// Attention over chosen blocks (attention_selected_kernel.hpp): the lists, the forward pass, the sums over a query's blocks, what the
+// host decides.
+#include "attention_selected_kernel.hpp"
+
+namespace optimus {
+namespace {
+
+// ---------------------------------------------------------------- lists
+// Pairs of 512 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
+// make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
+constexpr int kWords = kListChunk / 32;
+
+__device__ __forceinline__ bool sees(const SelectedArgs& a, int len, int t, int v) {
+  return v >= 0 && v < a.blocks && v * a.block < len && (!a.causal || v * a.block <= t);
+}
+// The thread's query's entries into `bits` (zeroed); of the same block the first counts: entry(e, block, counts).
+template <class F>
+__device__ __forceinline__ void chunk_pairs(const SelectedArgs& a, int mm, int len, int t, unsigned* bits, F entry) {
+  const int tid = threadIdx.x;
+  if (t >= len) return;
+  const int* own = a.selected + ((long long)mm * a.f.s + t) * a.count;
+  for (int e = 0; e < a.count; ++e) {
+    const int v = own[e];
+    bool counts = false;
+    if (sees(a, len, t, v)) {
+      const unsigned bit = 1u << (tid & 31);
+      counts = !(atomicOr(&bits[(tid >> 5) * a.blocks + v], bit) & bit);   // (a query's bits are one thread's: no race for the first)
+    }
+    entry(e, v, counts);
+  }
+}
+__device__ __forceinline__ int chunk_query(const SelectedArgs& a, int unit_in_matrix, int chunk) {
+  const int in_unit = chunk * kListChunk + threadIdx.x;
+  return in_unit < a.unit_rows ? unit_in_matrix * a.unit_rows + in_unit : a.f.s;   // s: none
+}
+
+__global__ __launch_bounds__(kListChunk) void list_count_kernel(SelectedArgs a) {
+  extern __shared__ unsigned bits[];
+  const int chunk = blockIdx.x, unit = blockIdx.y, mm = unit / a.units;
+  const int len = selected_matrix<64>(a, mm).len;
+  for (int k = threadIdx.x; k < kWords * a.blocks; k += kListChunk) bits[k] = 0;
+  __syncthreads();
+  chunk_pairs(a, mm, len, chunk_query(a, unit % a.units, chunk), bits, [](int, int, bool) {});
+  __syncthreads();
+  for (int v = threadIdx.x; v < a.blocks; v += kListChunk) {
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) n += __popc(bits[w * a.blocks + v]);
+    a.counts[((long long)unit * a.chunks + chunk) * a.blocks + v] = n;
+  }
+}
+
+// exclusive sums of x over the 1024 threads, the sum of all in *total
+__device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int in = x;
+#pragma unroll
+  for (int step = 1; step < 64; step <<= 1) {
+    const int y = __shfl_up(in, step);
+    if (lane >= step) in += y;
+  }
+  if (lane == 63) lds[wave] = in;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    const int y = lds[w];
+    before += w < wave ? y : 0;
+    all += y;
+  }
+  __syncthreads();
+  *total = all;
+  return before + in - x;
+}
+
+__global__ __launch_bounds__(1024) void list_places_kernel(SelectedArgs a) {
+  __shared__ int lds[16];
+  const int unit = blockIdx.x, v = threadIdx.x;
+  int n = 0;
+  if (v < a.blocks) {
+    int* c = a.counts + (long long)unit * a.chunks * a.blocks + v;
+    for (int k = 0; k < a.chunks; ++k) {
+      const int x = c[(long long)k * a.blocks];
+      c[(long long)k * a.blocks] = n;
+      n += x;
+    }
+  }
+  int all;
+  const int at = exclusive_sum(n, lds, &all);
+  int* offsets = a.offsets + (long long)unit * (a.blocks + 1);
+  if (v < a.blocks) offsets[v] = at;
+  if (v == 0) offsets[a.blocks] = all;
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    if (!a.items[kind]) continue;
+    const int items = (n + a.seg[kind] - 1) / a.seg[kind], first = exclusive_sum(items, lds, &all);
+    int* firsts = a.first_item + ((long long)kind * a.all_units + unit) * (a.blocks + 1);
+    if (v < a.blocks) firsts[v] = first;
+    if (v == 0) firsts[a.blocks] = all;
+    for (int k = 0; k < items; ++k)
+      a.items[kind][(long long)unit * a.most[kind] + first + k] = i32x4_t{v, at + k * a.seg[kind], min(a.seg[kind], n - k * a.seg[kind]), 0};
+  }
+}
+
+__global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
+  extern __shared__ unsigned bits[];
+  const int chunk = blockIdx.x, unit = blockIdx.y, mm = unit / a.units, tid = threadIdx.x;
+  const int len = selected_matrix<64>(a, mm).len;
+  const int t = chunk_query(a, unit % a.units, chunk);
+  for (int k = tid; k < kWords * a.blocks; k += kListChunk) bits[k] = 0;
+  __syncthreads();
+  unsigned long long counted = 0;   // (at most 64 entries)
+  chunk_pairs(a, mm, len, t, bits, [&](int e, int, bool counts) { counted |= counts ? 1ull << e : 0; });
+  __syncthreads();
+  if (t >= a.f.s) return;
+  const long long first = (long long)unit * a.unit_rows * a.count;
+  int* places = a.places + first + (long long)(t - unit % a.units * a.unit_rows) * a.count;
+  const int* own = a.selected + ((long long)mm * a.f.s + t) * a.count;
+  const int* offsets = a.offsets + (long long)unit * (a.blocks + 1);
+  const int* before = a.counts + ((long long)unit * a.chunks + chunk) * a.blocks;
+  for (int e = 0; e < a.count; ++e) {
+    int place = -1;
+    if (counted >> e & 1) {
+      const int v = own[e];
+      place = offsets[v] + before[v] + __popc(bits[(tid >> 5) * a.blocks + v] & ((1u << (tid & 31)) - 1));
+      for (int w = 0; w < tid >> 5; ++w) place += __popc(bits[w * a.blocks + v]);
+      a.list[first + place] = t;
+    }
+    places[e] = place;
+  }
+}
+
+// ---------------------------------------------------------------- forward
+// A wavefront has 32 queries of a tile of 128.  KT > 0: the block is at most 32 KT = 64 or 128 keys, stays in LDS for all of the workgroup's
+// queries, and a row's scores are all there before the maximum is taken: no barrier behind the loads, no rescaling.  The next tile's
+// queries are requested as soon as the products of this one have read theirs.
+template <int D, int KT>
+__global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, STEPS = KT / 2, AHEAD = 2;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[STEPS][2][BLK * D];   // [64 keys][K, V]
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  ListItem it;
+  if (!list_item(a, 0, unit, blockIdx.x, &it)) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const int key0 = it.block * a.block, last = m.len - 1;
+  TileLoader<D, 4, BLK, true> ldr;
+  ldr.init(f.ld, wave, lane);
+#pragma unroll
+  for (int st = 0; st < STEPS; ++st) {   // (keys past the end of the sequence: zeros)
+    ldr.issue(Qp + D, key0 + st * BLK, m.len, lds[st][0]);
+    ldr.issue(Qp + 2 * D, key0 + st * BLK, m.len, lds[st][1]);
+  }
+  const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
+  const long long first = (long long)unit * a.unit_rows * a.count + it.start;
+  const long long out = (long long)blockIdx.y * a.unit_rows * a.count + it.start;
+  const int* list = a.list + first;
+  int row = wave * 32 + (lane & 31);
+  int t = list[min(row, it.pairs - 1)];
+  bf16x8 qf[KS];
+  auto load_queries = [&](int q) {
+    const bf16_t* p = Qp + (long long)q * f.ld + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(p + ks * 16);
+  };
+  load_queries(t);
+  wait_loads_and_barrier();
+  for (int base = 0; base + wave * 32 < it.pairs; base += kQueries) {
+    f32x16 sacc[KT];
+#pragma unroll
+    for (int t2 = 0; t2 < KT; ++t2) sacc[t2] = zero16();
+    pipelined<KT * KS, AHEAD>([&](int n) { return rows_at<D>(in_rows, n / KS / 2 * (2 * BLK) + n / KS % 2 * 32, n % KS); },
+                              [&](int n, const bf16x8& x) {
+                                sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
+                              });
+    const int limit = a.causal ? min(t, last) : last;
+    const bool mine = base + row < it.pairs;
+    if (base + kQueries + wave * 32 < it.pairs) {
+      t = list[min(base + kQueries + row, it.pairs - 1)];
+      load_queries(t);
+    }
+    if (__builtin_amdgcn_ballot_w64(limit < key0 + 32 * KT - 1) != 0) {
+      const int reach = limit - key0 - 4 * g;
+#pragma unroll
+      for (int t2 = 0; t2 < KT; ++t2)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[t2][r] = 32 * t2 + slot(r) > reach ? -INFINITY : sacc[t2][r];
+    }
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int t2 = 0; t2 < KT; ++t2)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
+    mx = halfwave_max(mx);   // (a listed query sees the block's first key)
+#pragma unroll
+    for (int t2 = 0; t2 < KT; ++t2)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f((sacc[t2][r] - mx) * f.scale_log2);
+        sacc[t2][r] = p;
+        sum += p;
+      }
+    sum = halfwave_sum(sum);
+    bf16x8 pf[KT][2];
+#pragma unroll
+    for (int t2 = 0; t2 < KT; ++t2) {
+      pf[t2][0] = pack_acc<0>(sacc[t2]);
+      pf[t2][1] = pack_acc<1>(sacc[t2]);
+    }
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+    pipelined<2 * KT * DT, AHEAD>([&](int n) { return cols_at<D>(in_cols, n / DT / 4 * (2 * BLK) + n / DT % 4 * 16, n % DT); },
+                                  [&](int n, const bf16x8& x) {
+                                    const int k = n / DT;
+                                    oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf[k / 2][k & 1], x, oacc[n % DT], 0, 0, 0);
+                                  });
+    const long long at = out + base + wave * 32;
+    store_rows<DT>(a.rows + at * D, oacc, it.pairs - base - wave * 32, g, lane);
+    if (mine && g == 0) a.ml[at + (lane & 31)] = make_float2(mx, sum);
+  }
+}
+
+// Blocks of more than 128 keys: 64 at a time through two stages, running maximum and sum.
+template <int D>
+__global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, AHEAD = 2;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][BLK * D];   // [stage][K, V]
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  ListItem it;
+  if (!list_item(a, 0, unit, blockIdx.x, &it)) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const int key0 = it.block * a.block, last = m.len - 1;
+  const int steps = (min(a.block, m.len - key0) + BLK - 1) / BLK;
+  const int rounds = (it.pairs + kQueries - 1) / kQueries;
+  TileLoader<D, 4, BLK, true> ldr;
+  ldr.init(f.ld, wave, lane);
+  auto issue = [&](int step, int st) {
+    ldr.issue(Qp + D, key0 + step * BLK, m.len, lds[st][0]);
+    ldr.issue(Qp + 2 * D, key0 + step * BLK, m.len, lds[st][1]);
+  };
+  issue(0, 0);
+  const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
+  const long long first = (long long)unit * a.unit_rows * a.count + it.start;
+  const long long out = (long long)blockIdx.y * a.unit_rows * a.count + it.start;
+  const int* list = a.list + first;
+  const int row = wave * 32 + (lane & 31);
+  wait_loads_and_barrier();
+  int stage = 0;
+  for (int round = 0; round < rounds; ++round) {
+    const int base = round * kQueries, left = it.pairs - base - wave * 32;   // (at most 0: the wavefront only keeps the barriers)
+    const int t = list[min(base + row, it.pairs - 1)];
+    const int limit = a.causal ? min(t, last) : last;
+    bf16x8 qf[KS];
+    const bf16_t* p = Qp + (long long)t * f.ld + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(p + ks * 16);
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+    for (int step = 0; step < steps; ++step, stage ^= 1) {
+      const int next = step + 1 < steps ? step + 1 : 0;
+      if (step + 1 < steps || round + 1 < rounds) issue(next, stage ^ 1);
+      const int kbase = key0 + step * BLK;
+      if (left > 0 && __builtin_amdgcn_ballot_w64(limit >= kbase) != 0) {
+        const unsigned kt = in_rows + stage * (2 * BLK * D * 2), vt = in_cols + stage * (2 * BLK * D * 2);
+        f32x16 sacc[2];
+        sacc[0] = zero16();
+        sacc[1] = zero16();
+        pipelined<2 * KS, AHEAD>([&](int n) { return rows_at<D>(kt, n / KS * 32, n % KS); },
+                                 [&](int n, const bf16x8& x) {
+                                   sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
+                                 });
+        if (__builtin_amdgcn_ballot_w64(limit < kbase + BLK - 1) != 0) {
+          const int reach = limit - kbase - 4 * g;
+#pragma unroll
+          for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[t2][r] = 32 * t2 + slot(r) > reach ? -INFINITY : sacc[t2][r];
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
+        mx = halfwave_max(mx);
+        // The maximum follows the step's when that is above it by more than 2^8 after scaling: a step's largest term is at most 2^8 then.
+        const bool move = __builtin_amdgcn_ballot_w64((mx - m_run) * f.scale_log2 > 8.0f) != 0;
+        const float m_new = move ? fmaxf(m_run, mx) : m_run;
+        float sum = 0.f;
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float e = __builtin_amdgcn_exp2f((sacc[t2][r] - m_new) * f.scale_log2);
+            sacc[t2][r] = e;
+            sum += e;
+          }
+        sum = halfwave_sum(sum);
+        if (move) {
+          const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * f.scale_log2);   // (m_new is a score: the first step holds a key of every row)
+          l_run *= alpha;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float of_row = __shfl(alpha, slot(r) + 4 * g);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) oacc[dt][r] *= of_row;
+          }
+          m_run = m_new;
+        }
+        l_run += sum;
+        bf16x8 pf[2][2];
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2) {
+          pf[t2][0] = pack_acc<0>(sacc[t2]);
+          pf[t2][1] = pack_acc<1>(sacc[t2]);
+        }
+        pipelined<4 * DT, AHEAD>([&](int n) { return cols_at<D>(vt, n / DT * 16, n % DT); },
+                                 [&](int n, const bf16x8& x) {
+                                   const int k = n / DT;
+                                   oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf[k / 2][k & 1], x, oacc[n % DT], 0, 0, 0);
+                                 });
+      }
+      wait_loads_and_barrier();
+    }
+    if (left > 0) {
+      const long long at = out + base + wave * 32;
+      store_rows<DT>(a.rows + at * D, oacc, left, g, lane);
+      if ((lane & 31) < left && g == 0) a.ml[at + (lane & 31)] = make_float2(m_run, l_run);
+    }
+  }
+}
+
+// A query's rows to its output, a half-wavefront each.  FORWARD: weighted by their maxima, divided by the sum; the others: added, times
+// 1 / sqrt(d), to dQ.
+template <int D, bool FORWARD>
+__global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
+  constexpr int DT = D / 32;
+  typedef typename RowPart<DT>::V V;
+  __shared__ __attribute__((aligned(16))) float lds[8][D];
+  const FusedArgs& f = a.f;
+  const int half = threadIdx.x >> 5, n = threadIdx.x & 31;
+  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  const int in_unit = blockIdx.x * 8 + half, t = unit % a.units * a.unit_rows + in_unit;
+  const bool inside = in_unit < a.unit_rows && t < f.s;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const long long rows = (long long)blockIdx.y * a.unit_rows * a.count;
+  const int* places = a.places + (long long)unit * a.unit_rows * a.count + (long long)in_unit * a.count;
+  // entries n and n + 32
+  int place[2];
+  float2 ml[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    place[k] = inside && n + 32 * k < a.count ? places[n + 32 * k] : -1;
+    if (FORWARD) ml[k] = place[k] >= 0 ? a.ml[rows + place[k]] : make_float2(-INFINITY, 0.f);
+  }
+  float weight[2] = {1.0f, 1.0f}, total = 0.f, top = -INFINITY;
+  if (FORWARD) {
+    top = fmaxf(ml[0].x, ml[1].x);
+#pragma unroll
+    for (int step = 1; step < 32; step <<= 1) top = fmaxf(top, __shfl_xor(top, step));
+    const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      weight[k] = __builtin_amdgcn_exp2f((ml[k].x - from) * f.scale_log2);   // (of no pair: 0)
+      total += weight[k] * ml[k].y;
+    }
+#pragma unroll
+    for (int step = 1; step < 32; step <<= 1) total += __shfl_xor(total, step);
+    const float inverse = total > 0.f ? 1.0f / total : 0.f;
+    weight[0] *= inverse;
+    weight[1] *= inverse;
+  }
+  V sum;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) sum[dt] = 0.f;
+#pragma unroll 4
+  for (int e = 0; e < a.count; ++e) {
+    const int p = __shfl(e < 32 ? place[0] : place[1], e & 31, 32);
+    const float w = __shfl(e < 32 ? weight[0] : weight[1], e & 31, 32);
+    if (p >= 0) {
+      const V x = *(const V*)(a.rows + (rows + p) * D + n * DT);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) sum[dt] = FORWARD ? fmaf(w, x[dt], sum[dt]) : sum[dt] + x[dt];
+    }
+  }
+  if (FORWARD) {
+    write_row<DT>(f.attn + m.attn + (long long)t * f.ldo, sum, lds[half], n, inside);
+    if (inside && n == 0) f.lse[m.vec + t] = total > 0.f ? top * f.scale + __logf(total) : -INFINITY;
+  } else {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) sum[dt] *= f.scale;
+    write_row<DT>(f.d_qkv + m.qkv + (long long)t * f.ld, sum, lds[half], n, inside);
+  }
+}
+
+SelectedArgs make_args(const AttnSelectedDesc& b) {
+  const AttnFusedDesc& d = b.base;
+  SelectedArgs a = {};
+  FusedArgs& f = a.f;
+  f.qkv = (const bf16_t*)d.qkv; f.attn = (bf16_t*)d.attn; f.lse = d.lse;
+  f.d_attn = (const bf16_t*)d.d_attn; f.d_qkv = (bf16_t*)d.d_qkv;
+  f.s = d.s; f.nh = d.nh; f.ld = d.ld; f.ldo = d.ldo;
+  f.dev_qkv = d.dev_qkv; f.dev_attn = d.dev_attn; f.dev_vec = (long long)d.nb * d.nh * d.s;
+  f.scale = 1.0f / sqrtf((float)d.d);
+  f.scale_log2 = (float)(1.4426950408889634 / sqrt((double)d.d));
+  a.selected = b.selected; a.lengths = b.lengths;
+  a.nb = d.nb; a.nmat = d.nb * d.nh; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal;
+  a.block = b.block; a.count = b.count; a.blocks = (d.s + b.block - 1) / b.block;
+  return a;
+}
+
+size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// the workspace's parts into the arguments
+SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bool bwd) {
+  SelectedArgs a = make_args(b);
+  a.unit_rows = p.unit_rows; a.units = p.units; a.all_units = p.mats * p.units; a.chunks = p.chunks;
+  char* at = (char*)b.ws;
+  auto take = [&](size_t bytes) {
+    char* r = at;
+    at += bytes;
+    return r;
+  };
+  a.counts = (int*)take(p.counts);
+  a.offsets = (int*)take(p.offsets);
+  a.first_item = (int*)take(p.first_item);
+  for (int k = 0; k < 2; ++k) {
+    a.seg[k] = p.seg[k];
+    a.most[k] = p.most[k];
+    a.items[k] = (i32x4_t*)take(p.items[k]);
+  }
+  if (!bwd) a.items[1] = nullptr;
+  a.list = (int*)take(p.list);
+  a.places = (int*)take(p.places);
+  a.f.delta = (float*)take(p.delta);
+  a.rows = (float*)take(p.rows);
+  a.ml = (float2*)take(p.ml);
+  a.key_rows = (float*)a.rows;   // (dK and dV come when the rows of dQ are done with)
+  return a;
+}
+
+template <int D>
+void fwd_launch(const SelectedArgs& a, int portion, hipStream_t st) {
+  const dim3 grid(a.most[0], portion);
+  if (a.block == 64) selected_fwd_kernel<D, 2><<<grid, 256, 0, st>>>(a);
+  else if (a.block == 128) selected_fwd_kernel<D, 4><<<grid, 256, 0, st>>>(a);
+  else selected_fwd_long_kernel<D><<<grid, 256, 0, st>>>(a);
+  selected_combine_kernel<D, true><<<dim3((a.unit_rows + 7) / 8, portion), 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipStream_t st) {
+  const dim3 grid((a.unit_rows + 7) / 8, portion);
+  if (d == 64) selected_combine_kernel<64, false><<<grid, 256, 0, st>>>(a);
+  else selected_combine_kernel<128, false><<<grid, 256, 0, st>>>(a);
+}
+
+void launch_selected_lists(const SelectedArgs& a, hipStream_t st) {
+  const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 64 KiB
+  list_count_kernel<<<dim3(a.chunks, a.all_units), kListChunk, bits, st>>>(a);
+  list_places_kernel<<<a.all_units, 1024, 0, st>>>(a);
+  list_fill_kernel<<<dim3(a.chunks, a.all_units), kListChunk, bits, st>>>(a);
+}
+
+// Portions: partial results of 128 MiB at a time, half of the Infinity Cache.
+bool attn_selected_plan(const AttnSelectedDesc& b, int ndev, SelectedPlan* out) {
+  SelectedPlan p = {};
+  const AttnFusedDesc& d = b.base;
+  const long long blocks = (d.s + b.block - 1) / b.block;
+  p.mats = ndev * d.nb * d.nh;
+  const long long row_bytes = d.d * 4 + 8, budget = 128ll << 20;
+  p.unit_rows = d.s;
+  p.units = (d.s + p.unit_rows - 1) / p.unit_rows;
+  p.chunks = (p.unit_rows + kListChunk - 1) / kListChunk;
+  const long long units = (long long)p.mats * p.units, pairs = (long long)p.unit_rows * b.count;
+  if (units > 65535) return false;
+  const long long fit = budget / (pairs * row_bytes);
+  p.unit_portion = (int)(fit < 1 ? 1 : fit > units ? units : fit);
+  p.seg[0] = 512;
+  p.seg[1] = 1024;
+  for (int k = 0; k < 2; ++k) p.most[k] = (int)(blocks + pairs / p.seg[k]);
+  const long long key_bytes = (long long)p.most[1] * p.units * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
+  const long long key_fit = budget / key_bytes;
+  p.mat_portion = (int)(key_fit < 1 ? 1 : key_fit > p.mats ? p.mats : key_fit);
+  p.counts = round256((size_t)units * p.chunks * blocks * 4);
+  p.offsets = round256((size_t)units * (blocks + 1) * 4);
+  p.first_item = round256((size_t)2 * units * (blocks + 1) * 4);
+  for (int k = 0; k < 2; ++k) p.items[k] = round256((size_t)units * p.most[k] * 16);
+  p.list = p.places = round256((size_t)units * pairs * 4);
+  p.delta = round256((size_t)p.mats * d.s * 4);
+  const size_t rows = (size_t)p.unit_portion * pairs * d.d * 4, keys = (size_t)p.mat_portion * key_bytes;
+  p.rows = round256(rows > keys ? rows : keys);
+  p.ml = round256((size_t)p.unit_portion * pairs * 8);
+  p.total = p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.delta + p.rows + p.ml;
+  *out = p;
+  return true;
+}
+size_t attn_selected_ws_bytes(const AttnSelectedDesc& b) {
+  SelectedPlan p;
+  return attn_selected_plan(b, b.base.ndev, &p) ? p.total : 0;
+}
+
+int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
+  SelectedPlan p;
+  if (!attn_selected_plan(b, b.base.ndev, &p)) return OPTIMUS_ESHAPE;
+  SelectedArgs a = with_workspace(b, p, false);
+  launch_selected_lists(a, st);
+  for (a.unit0 = 0; a.unit0 < a.all_units; a.unit0 += p.unit_portion) {
+    const int portion = min(p.unit_portion, a.all_units - a.unit0);
+    if (b.base.d == 64) fwd_launch<64>(a, portion, st);
+    else fwd_launch<128>(a, portion, st);
+    if (const int rc = hip_launch_status()) return rc;
+  }
+  return OPTIMUS_OK;
+}
+
+int launch_attn_selected_bwd(const AttnSelectedDesc& b, hipStream_t st) {
+  SelectedPlan p;
+  if (!attn_selected_plan(b, b.base.ndev, &p)) return OPTIMUS_ESHAPE;
+  const SelectedArgs a = with_workspace(b, p, true);
+  launch_selected_lists(a, st);
+  return launch_selected_bwd_kernels(a, p, b.base.d, st);
+}
+
+}  // namespace optimus

@@ -1,0 +1,363 @@
+// Backward of the attention over chosen blocks (attention_selected_kernel.hpp): dQ as the forward makes its output, a row a pair, added
+// up by the query; dK and dV by workgroups that own 64 keys and walk a piece of their block's list, added up by the key.
+#include "attention_selected_kernel.hpp"
+
+namespace optimus {
+namespace {
+
+// P = 2^x, at most 1 (see the attention with changed scores)
+__device__ __forceinline__ float weight_of(float x) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f); }
+// what is subtracted from a row's scores; a row that saw nothing: +infinity, which makes every P of it zero
+__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
+
+// rowsum(dO * O) of every query, 0 past the end of a sequence
+template <int D>
+__global__ __launch_bounds__(256) void selected_delta_kernel(SelectedArgs a) {
+  const FusedArgs& f = a.f;
+  const int lane = threadIdx.x & 63, g = lane >> 5, wave = threadIdx.x >> 6, mm = blockIdx.y;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int t = blockIdx.x * 128 + wave * 32 + (lane & 31), row = min(t, f.s - 1);
+  float delta = 0.f;
+  if (t < m.len) {
+    const bf16_t* G = f.d_attn + m.attn + (long long)row * f.ldo + g * 8;
+    const bf16_t* O = f.attn + m.attn + (long long)row * f.ldo + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) delta += delta_piece(*(const bf16x8*)(G + ks * 16), *(const bf16x8*)(O + ks * 16));
+  }
+  delta = halfwave_sum(delta);
+  if (g == 0 && t < f.s) f.delta[m.vec + t] = delta;
+}
+
+// dS^T of 32 keys in LDS (rows_at from kt; V 64 rows behind) against the wavefront's queries, packed as fragments
+template <int D>
+__device__ __forceinline__ void dq_scores(bf16x8 (&dsf)[2], unsigned kt, const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16], float lse2, float delta,
+                                          float scale_log2, bool masked, int reach) {
+  constexpr int KS = D / 16;
+  f32x16 sacc = zero16(), pacc = zero16();
+  pipelined<2 * KS, 2>([&](int n) { return rows_at<D>(kt, n & 1 ? BLK : 0, n / 2); },
+                       [&](int n, const bf16x8& x) {
+                         f32x16& acc = n & 1 ? pacc : sacc;
+                         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dof[n / 2] : qf[n / 2], acc, 0, 0, 0);
+                       });
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    float p = weight_of(fmaf(sacc[r], scale_log2, -lse2));
+    if (masked && slot(r) > reach) p = 0.f;
+    sacc[r] = p * (pacc[r] - delta);
+  }
+  dsf[0] = pack_acc<0>(sacc);
+  dsf[1] = pack_acc<1>(sacc);
+}
+
+// dQ rows.  KT > 0: the block's K and V stay in LDS (64 or 128 keys); 0: 64 keys at a time through two stages.
+template <int D, int KT>
+__global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, STAGES = KT == 2 ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[STAGES][2][BLK * D];   // [stage][K, V]
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  ListItem it;
+  if (!list_item(a, 0, unit, blockIdx.x, &it)) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const bf16_t* Gp = f.d_attn + m.attn;
+  const int key0 = it.block * a.block, last = m.len - 1;
+  const int steps = KT ? KT / 2 : (min(a.block, m.len - key0) + BLK - 1) / BLK;
+  const int rounds = (it.pairs + kQueries - 1) / kQueries;
+  TileLoader<D, 4, BLK, true> ldr;
+  ldr.init(f.ld, wave, lane);
+  auto issue = [&](int step, int st) {
+    ldr.issue(Qp + D, key0 + step * BLK, m.len, lds[st][0]);
+    ldr.issue(Qp + 2 * D, key0 + step * BLK, m.len, lds[st][1]);
+  };
+#pragma unroll
+  for (int st = 0; st < (KT ? STAGES : 1); ++st) issue(st, st);
+  const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane);
+  const long long first = (long long)unit * a.unit_rows * a.count + it.start;
+  const long long out = (long long)blockIdx.y * a.unit_rows * a.count + it.start;
+  const int* list = a.list + first;
+  const int row = wave * 32 + (lane & 31);
+  bf16x8 qf[KS], dof[KS];
+  int t = 0;
+  float lse2 = 0.f, delta = 0.f;
+  auto load_queries = [&](int base) {
+    t = list[min(base + row, it.pairs - 1)];
+    const bf16_t* q = Qp + (long long)t * f.ld + g * 8;
+    const bf16_t* o = Gp + (long long)t * f.ldo + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = *(const bf16x8*)(q + ks * 16);
+      dof[ks] = *(const bf16x8*)(o + ks * 16);
+    }
+    lse2 = lse2_of(f.lse[m.vec + t]);
+    delta = f.delta[m.vec + t];
+  };
+  load_queries(0);
+  wait_loads_and_barrier();
+  int stage = 0;
+  for (int round = 0; round < rounds; ++round) {
+    const int base = round * kQueries, left = it.pairs - base - wave * 32;
+    if (KT && left <= 0) break;
+    if (round > 0) load_queries(base);
+    const int limit = a.causal ? min(t, last) : last;
+    f32x16 acc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
+    for (int step = 0; step < steps; ++step, stage ^= 1) {
+      if (!KT && (step + 1 < steps || round + 1 < rounds)) issue(step + 1 < steps ? step + 1 : 0, stage ^ 1);
+      const int kbase = key0 + step * BLK;
+      if (KT || (left > 0 && __builtin_amdgcn_ballot_w64(limit >= kbase) != 0)) {
+        const unsigned at = (unsigned)((KT ? step : stage) * (2 * BLK * D * 2));
+        const bool masked = __builtin_amdgcn_ballot_w64(limit < kbase + BLK - 1) != 0;
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2) {
+          bf16x8 dsf[2];
+          dq_scores<D>(dsf, in_rows + at + t2 * (32 * D * 2), qf, dof, lse2, delta, f.scale_log2, masked, limit - kbase - 32 * t2 - 4 * g);
+          pipelined<2 * DT, 2>([&](int n) { return cols_at<D>(in_cols + at, t2 * 32 + n / DT * 16, n % DT); },
+                               [&](int n, const bf16x8& x) {
+                                 acc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dsf[n / DT], x, acc[n % DT], 0, 0, 0);
+                               });
+        }
+      }
+      if (!KT) wait_loads_and_barrier();
+    }
+    if (left > 0) store_rows<DT>(a.rows + (out + base + wave * 32) * D, acc, left, g, lane);
+  }
+}
+
+// A tile of gathered rows, global -> LDS directly: rows of [.][ld] matrices by their numbers, in the layout of TileLoader.  64-bit addresses:
+// a list's rows lie anywhere in the sequence.
+template <int D, int NW, int ROWS>
+struct GatherLoader {
+  static constexpr int CH = D / 8, ROWS_PER_KIB = 64 / CH, PIECES = ROWS * D * 2 / 1024, PER = PIECES / NW;
+  static_assert(PIECES % NW == 0, "tile must divide over the wavefronts");
+  int number[PER], wave, lane;
+  // the numbers of the tile's rows: list entries row0 .., the last one again past the end
+  __device__ __forceinline__ void fetch(const int* list, int row0, int pairs) {
+#pragma unroll
+    for (int it = 0; it < PER; ++it) number[it] = list[min(row0 + (wave * PER + it) * ROWS_PER_KIB + lane / CH, pairs - 1)];
+  }
+  __device__ __forceinline__ void issue(const bf16_t* mat, int ld, bf16_t* tile) const {
+    const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) bf16_t*)tile;
+#pragma unroll
+    for (int it = 0; it < PER; ++it) {
+      const int row = (wave * PER + it) * ROWS_PER_KIB + lane / CH;
+      const bf16_t* p = mat + (long long)number[it] * ld + (((lane % CH) ^ swz<D>(row)) << 3);
+      const unsigned m0v = __builtin_amdgcn_readfirstlane(lds_base + (unsigned)(wave * PER + it) * 1024u);
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(m0v) : "memory", "m0");
+    }
+  }
+};
+
+template <int D>
+struct SelDkvLds {
+  bf16_t tile[2][2][PAIR * D];   // [stage][Q, dO]
+  alignas(16) float l[2][PAIR];
+  alignas(16) float d[2][PAIR];
+  alignas(16) int t[2][PAIR];
+};
+// dK and dV of 64 keys from a piece of their block's list.  Wavefronts: 32 keys, every second 64 queries, as in the fused attention.
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(SelectedArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, NRG = 2;
+  __shared__ __attribute__((aligned(1024))) SelDkvLds<D> lds;
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave % NRG, par = wave / NRG;
+  const int tiles = a.block / BLK, item = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+  const int unit = blockIdx.y + a.mat0 * a.units, mm = unit / a.units;
+  ListItem it;
+  if (!list_item(a, 1, unit, item, &it)) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int kt0 = it.block * a.block + tile * BLK;
+  if (kt0 >= m.len) return;
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const bf16_t* Gp = f.d_attn + m.attn;
+  const int k0 = kt0 + rg * 32, key = k0 + (lane & 31), krow = min(key, m.len - 1);
+  bf16x8 kf[KS], vf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = *(const bf16x8*)(Qp + D + (long long)krow * f.ld + ks * 16 + g * 8);
+    vf[ks] = *(const bf16x8*)(Qp + 2 * D + (long long)krow * f.ld + ks * 16 + g * 8);
+  }
+  const int* list = a.list + (long long)unit * a.unit_rows * a.count + it.start;
+  const int n_it = (it.pairs + PAIR - 1) / PAIR;
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    dkacc[dt] = zero16();
+    dvacc[dt] = zero16();
+  }
+  const unsigned in_rows = lds_address(lds.tile) + lane_rows<D>(lane), in_cols = lds_address(lds.tile) + lane_cols<D>(lane);
+  GatherLoader<D, 4, PAIR> ldr;
+  ldr.wave = wave;
+  ldr.lane = lane;
+  // a row's numbers go through registers and reach LDS at the end of an iteration
+  int next_t = 0, row_t = 0;
+  float next_l = 0.f, next_d = 0.f;
+  auto load_numbers = [&](int n) {   // of iteration n
+    ldr.fetch(list, n * PAIR, it.pairs);
+    if (tid < PAIR) row_t = list[min(n * PAIR + tid, it.pairs - 1)];
+  };
+  auto issue = [&](int st) {
+    if (tid < PAIR) {
+      next_t = row_t;
+      next_l = f.lse[m.vec + row_t];
+      next_d = f.delta[m.vec + row_t];
+    }
+    ldr.issue(Qp, f.ld, lds.tile[st][0]);
+    ldr.issue(Gp, f.ldo, lds.tile[st][1]);
+  };
+  auto store_numbers = [&](int n, int st) {   // (past the end of the list: no P)
+    if (tid < PAIR) {
+      lds.l[st][tid] = n * PAIR + tid < it.pairs ? lse2_of(next_l) : INFINITY;
+      lds.d[st][tid] = next_d;
+      lds.t[st][tid] = next_t;
+    }
+  };
+  load_numbers(0);
+  issue(0);
+  if (n_it > 1) load_numbers(1);
+  store_numbers(0, 0);
+  wait_loads_and_barrier();
+  for (int n = 0; n < n_it; ++n) {
+    const int st = n & 1;
+    if (n + 1 < n_it) {
+      issue(st ^ 1);
+      if (n + 2 < n_it) load_numbers(n + 2);
+    }
+    const int base = n * PAIR + par * BLK;
+    // (the block's own queries come first: where the first of 64 is behind the keys, all are)
+    const int first_t = __builtin_amdgcn_readfirstlane(lds.t[st][par * BLK]);
+    if (base < it.pairs && k0 < m.len) {
+      const unsigned stage = (unsigned)((st * 2 * PAIR + par * BLK) * D * 2);
+      const unsigned qt = in_rows + stage, qc = in_cols + stage;
+      const bool masked = a.causal && first_t < k0 + 31;
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        f32x16 sacc = zero16(), pacc = zero16();
+        pipelined<2 * KS, 2>([&](int k) { return rows_at<D>(qt, (k & 1 ? PAIR : 0) + t2 * 32, k / 2); },
+                             [&](int k, const bf16x8& x) {
+                               f32x16& acc = k & 1 ? pacc : sacc;
+                               acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, k & 1 ? vf[k / 2] : kf[k / 2], acc, 0, 0, 0);
+                             });
+        const int at = par * BLK + t2 * 32 + 4 * g;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float4 l4 = *(const float4*)(lds.l[st] + at + 8 * c), d4 = *(const float4*)(lds.d[st] + at + 8 * c);
+          const int4 t4 = *(const int4*)(lds.t[st] + at + 8 * c);
+          const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+          const int tv[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * c + e;
+            float p = weight_of(fmaf(sacc[r], f.scale_log2, -lv[e]));
+            if (masked && tv[e] < key) p = 0.f;
+            sacc[r] = p;
+            pacc[r] = p * (pacc[r] - dv[e]);
+          }
+        }
+        const bf16x8 pf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)}, dsf[2] = {pack_acc<0>(pacc), pack_acc<1>(pacc)};
+        pipelined<4 * DT, 2>([&](int k) { return cols_at<D>(qc, (k & 1 ? 0 : PAIR) + t2 * 32 + k / (2 * DT) * 16, k / 2 % DT); },
+                             [&](int k, const bf16x8& x) {
+                               const int dt = k / 2 % DT, u = k / (2 * DT);
+                               f32x16& acc = k & 1 ? dkacc[dt] : dvacc[dt];
+                               acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k & 1 ? dsf[u] : pf[u], x, acc, 0, 0, 0);
+                             });
+      }
+    }
+    if (n + 1 < n_it) store_numbers(n + 1, st ^ 1);
+    wait_loads_and_barrier();
+  }
+  float* xch = (float*)&lds.tile[0][0][0] + rg * (2 * DT * 16) * 64;
+  if (par == 1) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        xch[(dt * 16 + r) * 64 + lane] = dkacc[dt][r];
+        xch[((DT + dt) * 16 + r) * 64 + lane] = dvacc[dt][r];
+      }
+  }
+  __syncthreads();
+  if (par == 1) return;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dkacc[dt][r] += xch[(dt * 16 + r) * 64 + lane];
+      dvacc[dt][r] += xch[((DT + dt) * 16 + r) * 64 + lane];
+    }
+  float* to = a.key_rows + (((long long)blockIdx.y * a.most[1] + item) * tiles + tile) * (2 * BLK * D) + rg * 32 * D;
+  store_rows<DT>(to, dkacc, m.len - k0, g, lane);
+  store_rows<DT>(to + BLK * D, dvacc, m.len - k0, g, lane);
+}
+
+// Sums over a key's pieces, in the order of the lists, to dK and dV; zeros where there is none.
+template <int D>
+__global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs a) {
+  constexpr int DT = D / 32;
+  typedef typename RowPart<DT>::V V;
+  __shared__ __attribute__((aligned(16))) float lds[8][D];
+  const FusedArgs& f = a.f;
+  const int half = threadIdx.x >> 5, n = threadIdx.x & 31;
+  const int mm = a.mat0 + blockIdx.y;
+  const int key = blockIdx.x * 8 + half;
+  const bool inside = key < f.s;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int v = min(key, f.s - 1) / a.block, in_block = key - v * a.block, tiles = a.block / BLK;
+  V dk, dv;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = 0.f;
+  if (key < m.len) {
+    for (int u = 0; u < a.units; ++u) {
+      const int* first = a.first_item + ((long long)a.all_units + (long long)mm * a.units + u) * (a.blocks + 1);
+      const int from = first[v], to = first[v + 1];
+      const long long of_unit = ((long long)blockIdx.y * a.units + u) * a.most[1];
+#pragma unroll 2
+      for (int k = from; k < to; ++k) {
+        const float* p = a.key_rows + ((of_unit + k) * tiles + in_block / BLK) * (2 * BLK * D) + in_block % BLK * D + n * DT;
+        dk += *(const V*)p;
+        dv += *(const V*)(p + BLK * D);
+      }
+    }
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dk[dt] *= f.scale;
+  bf16_t* to = f.d_qkv + m.qkv + (long long)key * f.ld + D;
+  write_row<DT>(to, dk, lds[half], n, inside);
+  write_row<DT>(to + D, dv, lds[half], n, inside);
+}
+
+template <int D>
+int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
+  const int s = a.f.s;
+  selected_delta_kernel<D><<<dim3((s + 127) / 128, p.mats), 256, 0, st>>>(a);
+  for (a.unit0 = 0; a.unit0 < a.all_units; a.unit0 += p.unit_portion) {
+    const int portion = min(p.unit_portion, a.all_units - a.unit0);
+    const dim3 grid(a.most[0], portion);
+    if (a.block == 64) selected_dq_kernel<D, 2><<<grid, 256, 0, st>>>(a);
+    else if (a.block == 128) selected_dq_kernel<D, 4><<<grid, 256, 0, st>>>(a);
+    else selected_dq_kernel<D, 0><<<grid, 256, 0, st>>>(a);
+    launch_selected_dq_combine(a, D, portion, st);
+    if (const int rc = hip_launch_status()) return rc;
+  }
+  for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.mat_portion) {
+    const int portion = min(p.mat_portion, p.mats - a.mat0);
+    selected_dkv_kernel<D><<<dim3(a.most[1] * (a.block / BLK), portion * a.units), 256, 0, st>>>(a);
+    selected_dkv_combine_kernel<D><<<dim3((s + 7) / 8, portion), 256, 0, st>>>(a);
+    if (const int rc = hip_launch_status()) return rc;
+  }
+  return OPTIMUS_OK;
+}
+
+}  // namespace
+
+int launch_selected_bwd_kernels(const SelectedArgs& a, const SelectedPlan& p, int d, hipStream_t st) {
+  return d == 64 ? bwd_launch<64>(a, p, st) : bwd_launch<128>(a, p, st);
+}
+
+}  // namespace optimus

@@ -1,0 +1,131 @@
+// Attention in which a query sees some blocks of keys only: its own and those that a cheap score ranks highest.
+//   mean[v] = mean of block v's keys, rounded to bf16;  score(t, v) = q_t . mean[v]
+//   a query attends to its own block and to the count - 1 others of highest score (causal: among those in front of its own)
+// The choice is one step (attention_select.hip), the attention over any chosen blocks another (attention_selected.hip forward,
+// attention_selected_bwd.hip backward); tiles, fragments and layouts are those of the fused attention (attention_fused_kernel.hpp).
+//
+// How the work is cut.  Neighbouring queries choose different blocks, so a tile of queries has no common keys to load and a tile of the dense
+// attention would be mostly masked.  The other way round a block of keys has a list of the queries that chose it.  A workgroup takes a
+// block and a piece of its list: the block's K and V are loaded once, queries come 128 at a time, gathered by their numbers, and every
+// product is dense.  What a query gets from one block is a partial result, a row of fp32 numbers with its maximum and sum (forward)
+// or a row of dQ (backward): it goes to memory at the pair's place in the list, and a second kernel adds up each query's rows, at the places
+// that the step which makes the lists has noted.  dK and dV need no such rows: their workgroups walk a block's list.
+// The rows are count * s * d * 4 bytes a matrix: written and read once they cost as much as the products do, so that they are made in
+// portions (units of queries, a few at a time) that stay in the Infinity Cache.
+#pragma once
+#include "attention_biased_kernel.hpp"
+
+namespace optimus {
+
+constexpr int kListChunk = 512;        // queries of a workgroup that makes the lists
+constexpr int kMostBlocks = 1024, kMostCount = 64;
+constexpr int kQueries = 128;          // list rows of a tile
+
+struct SelectedArgs {
+  FusedArgs f;                         // f.attn, f.lse, f.d_attn, f.d_qkv, f.delta: first device of the launch
+  const int* selected;                 // [matrix][s][count], first device of the launch
+  int* chosen;                         // the same, written (attention_select)
+  const int* lengths;                  // [sequences of the grid], or nullptr
+  bf16_t* means;                       // [matrix][blocks][d]
+  float* mean_sizes;                   // [matrix][blocks]: Euclidean norms, rounded up
+  int nb, nmat, q, dev0, causal;       // sequences and matrices of a device
+  int block, blocks, count;            // keys of a block, blocks of a sequence, blocks of a query
+  // lists: a unit is a range of a matrix' queries
+  int unit_rows, units, all_units;     // queries of a unit, units of a matrix, of the whole call
+  int chunks;                          // kListChunk pieces of a unit
+  int unit0;                           // first unit of this launch
+  int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, most items of a unit
+  int* counts;                         // [unit][chunk][block]: pairs; then pairs of earlier chunks of the block
+  int* offsets;                        // [unit][blocks + 1]: place of a block's first pair
+  int* first_item;                     // [kind][unit][blocks + 1]
+  i32x4_t* items[2];                   // [unit][most]: block, place of the first pair, pairs, -
+  int* list;                           // [unit][unit_rows * count]: query of every pair
+  int* places;                         // [unit][unit_rows][count]: place of the pair in list, -1: none
+  float* rows;                         // [unit - unit0][unit_rows * count][d]: partial results, see store_rows
+  float2* ml;                          // [unit - unit0][unit_rows * count]: maximum of Q K^T, sum of exponentials
+  float* key_rows;                     // [matrix of the launch][unit][item][block / 64][dK, dV][64][d]
+  int mat0;                            // dK and dV: first matrix of this launch
+};
+
+// What the host decides; bytes of the workspace, in this order
+struct SelectedPlan {
+  int mats;                            // of the launch
+  int unit_rows, units, chunks;
+  int unit_portion, mat_portion;       // units and matrices whose partial results are in memory at a time
+  int seg[2], most[2];
+  size_t counts, offsets, first_item, items[2], list, places, delta, rows, ml, total;
+};
+
+// csrc/attention_selected*.hip
+int launch_selected_bwd_kernels(const SelectedArgs& a, const SelectedPlan& p, int d, hipStream_t st);
+void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipStream_t st);
+
+namespace {
+
+// What a wavefront knows about its matrix, mm counted over the devices of the launch.
+struct SelMatrix {
+  int len;
+  long long qkv, attn, vec;   // element offsets of the matrix' first row
+};
+template <int D>
+__device__ __forceinline__ SelMatrix selected_matrix(const SelectedArgs& a, int mm) {
+  SelMatrix m;
+  const FusedArgs& f = a.f;
+  const int dev = mm / a.nmat, mat = mm % a.nmat, seq = mat / f.nh, head = mat % f.nh;
+  m.len = a.lengths ? min(max(a.lengths[(a.dev0 + dev) / a.q * a.nb + seq], 0), f.s) : f.s;
+  m.qkv = dev * f.dev_qkv + (long long)seq * f.s * f.ld + head * 3 * D;
+  m.attn = dev * f.dev_attn + (long long)seq * f.s * f.ldo + head * D;
+  m.vec = (long long)mm * f.s;
+  return m;
+}
+
+// A tile's accumulators, products with the rows' operand in the A slot: lane n = lane % 32 holds column 32 dt + n of the rows
+// slot(r) + 4 (lane / 32).  A row goes to memory as [n][dt], so that 32 lanes write it whole with 4 (or 2) numbers each; what reads it
+// undoes the order.
+template <int DT> struct RowPart;
+template <> struct RowPart<4> { typedef __attribute__((ext_vector_type(4))) float V; };
+template <> struct RowPart<2> { typedef __attribute__((ext_vector_type(2))) float V; };
+template <int DT>
+__device__ __forceinline__ void store_rows(float* to, const f32x16 (&acc)[DT], int left, int g, int lane) {
+  typedef typename RowPart<DT>::V V;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int row = slot(r) + 4 * g;
+    V v;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v[dt] = acc[dt][r];
+    if (row < left) *(V*)(to + row * (32 * DT) + (lane & 31) * DT) = v;
+  }
+}
+// A half-wavefront's row of D numbers [n][dt] -> bf16 at `to`, columns in order, through LDS of its own.
+template <int DT>
+__device__ __forceinline__ void write_row(bf16_t* to, const typename RowPart<DT>::V v, float* lds, int n, bool write) {
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) lds[dt * 32 + n] = v[dt];
+  __builtin_amdgcn_wave_barrier();
+  if (DT == 4) {
+    const float4 x = *(const float4*)(lds + 4 * n);
+    if (write) *(u32x2*)(to + 4 * n) = u32x2{pack2_bf16(x.x, x.y), pack2_bf16(x.z, x.w)};
+  } else {
+    const float2 x = *(const float2*)(lds + 2 * n);
+    if (write) *(unsigned*)(to + 2 * n) = pack2_bf16(x.x, x.y);
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Work of a workgroup: a block and a piece of its list.
+struct ListItem {
+  int block, start, pairs;
+};
+__device__ __forceinline__ bool list_item(const SelectedArgs& a, int kind, int unit, int k, ListItem* it) {
+  const int* first = a.first_item + ((long long)kind * a.all_units + unit) * (a.blocks + 1);
+  if (k >= first[a.blocks]) return false;
+  const i32x4_t x = a.items[kind][(long long)unit * a.most[kind] + k];
+  it->block = __builtin_amdgcn_readfirstlane(x.x);
+  it->start = __builtin_amdgcn_readfirstlane(x.y);
+  it->pairs = __builtin_amdgcn_readfirstlane(x.z);
+  return true;
+}
+
+}  // namespace
+}  // namespace optimus

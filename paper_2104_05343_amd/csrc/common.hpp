@@ -209,6 +209,22 @@ int launch_attn_biased_bwd(const AttnBiasedDesc& d, hipStream_t stream);
 bool attn_biased_fwd_wide(const AttnBiasedDesc& d);   // whether workgroups have 128 rows, not 64
 bool attn_biased_bwd_wide(const AttnBiasedDesc& d);
 
+// Attention over chosen blocks of keys (attention_selected_kernel.hpp).
+struct AttnSelectedDesc {
+  AttnFusedDesc base;       // lse, selected: first device of the launch; delta: not used
+  int q, dev0;              // grid, first device of the launch
+  int block, count;         // keys of a block, blocks of a query
+  const int* selected;      // [device][matrix][s][count]
+  int* chosen;              // the same, written by the choice
+  const int* lengths;       // [sequences of the grid], or nullptr
+  void* ws;
+};
+size_t attn_select_ws_bytes(const AttnSelectedDesc& d);     // of the choice
+size_t attn_selected_ws_bytes(const AttnSelectedDesc& d);   // of both directions; 0 for a launch that is refused
+int launch_attn_select(const AttnSelectedDesc& d, hipStream_t stream);
+int launch_attn_selected_fwd(const AttnSelectedDesc& d, hipStream_t stream);
+int launch_attn_selected_bwd(const AttnSelectedDesc& d, hipStream_t stream);
+
 // Attention that keeps the probabilities, head widths 64 and 128 (attention_probs.hip): nmat matrices of consecutive sequences,
 // nh heads each.
 struct AttnProbsDesc {

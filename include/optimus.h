@@ -301,7 +301,7 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * in optimus_attention_biased_bwd.  qkv, attn, lse, d_attn, d_qkv, coordinates and limits as in optimus_attention_fused_*; bf16 only;
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
- * from call to call: calls that may overlap need one each.  It holds up to 128 MiB of partial results, or one (sequence, head)'s:
+ * from call to call: calls that may overlap need one each.  It holds up to 384 MiB of partial results, or one (sequence, head)'s:
  * s * count * (d + 2) * 4 bytes. */
 typedef struct {
   int block, count;
@@ -618,6 +618,9 @@ int optimus_debug_last_gemm_plan(void);
 /* The streams an optimus_layer_bwd of this size runs on when it is not captured (a captured one: two, once the library
  * has its stream): 1 or 2, or -1 for arguments that optimus_layer_bwd refuses.  Host arithmetic only. */
 int optimus_debug_layer_bwd_streams(const optimus_layer_cfg* cfg, int i, int j);
+/* Whether an optimus_attention_selected_fwd / _bwd of this size computes all blocks with a mask (1), or lists of the queries of each block (0);
+ * -1 for arguments that these refuse.  Host arithmetic only. */
+int optimus_debug_attention_selected_masked(int b, int s, int h, int n, int q, int i, int j, int causal, const optimus_selection* selection);
 /* Rows of a workgroup, 64 or 128, in which an optimus_attention_biased_fwd, or with backward != 0 _bwd (table_gradient: with d_table), of
  * this size would run; -1 for arguments that these refuse.  Host arithmetic only. */
 int optimus_debug_attention_biased_rows(int backward, int b, int s, int h, int n, int q, int i, int j, const optimus_attention_bias* bias,

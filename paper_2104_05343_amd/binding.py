@@ -180,6 +180,7 @@ SIGNATURES = {
     "optimus_debug_last_gemm_plan": (_INT, []),
     "optimus_debug_layer_bwd_streams": (_INT, [C.POINTER(LayerCfg), _INT, _INT]),
     "optimus_debug_attention_biased_rows": (_INT, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias), _INT]),
+    "optimus_debug_attention_selected_masked": (_INT, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection)]),
     "optimus_debug_plan_summa": (_INT, [_INT, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _INT, C.POINTER(C.c_int)]),
     "optimus_debug_plan_pair": (_INT, [_I64, _I64, _I64, _INT, _INT, _INT]),
     "optimus_debug_mfma_rate": (_INT, [_P, _INT, _INT, _INT, _P]),
@@ -719,6 +720,13 @@ def debug_last_gemm_pair() -> bool:
     """Whether that product shared its launch with another one."""
     p = lib().optimus_debug_last_gemm_plan()
     return p >= 0 and bool(p >> 18 & 1)
+
+
+def debug_attention_selected_masked(b, s, h, n, q, i, j, causal, selection: Selection) -> bool:
+    rc = lib().optimus_debug_attention_selected_masked(b, s, h, n, q, i, j, int(causal), C.byref(selection))
+    if rc < 0:
+        raise OptimusError(ESHAPE, "optimus_debug_attention_selected_masked")
+    return bool(rc)
 
 
 def debug_attention_biased_rows(backward, b, s, h, n, q, i, j, bias: AttentionBias, table_gradient=False) -> int:

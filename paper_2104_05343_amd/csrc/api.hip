@@ -428,9 +428,13 @@ int selected_desc(int b, int s, int h, int n, int q, int i, int j, const optimus
   d->block = sel->block; d->count = sel->count; d->lengths = sel->lengths;
   return OPTIMUS_OK;
 }
-size_t selected_ws_bytes(const AttnSelectedDesc& d) {
-  const size_t choice = attn_select_ws_bytes(d), both = attn_selected_ws_bytes(d);
-  return choice > both ? choice : both;
+size_t selected_ws_bytes(AttnSelectedDesc d) {   // (whether there is a mask is not known when it is asked for)
+  size_t most = attn_select_ws_bytes(d);
+  for (d.base.causal = 0; d.base.causal < 2; ++d.base.causal) {
+    const size_t bytes = attn_selected_ws_bytes(d);
+    if (bytes > most) most = bytes;
+  }
+  return most;
 }
 enum { kChoose, kForward, kBackward };
 int run_attention_selected(int what, const void* qkv, int32_t* selected, void* attn, float* lse, const void* d_attn, void* d_qkv, int b, int s, int h,
@@ -1310,6 +1314,13 @@ int optimus_debug_layer_bwd_streams(const optimus_layer_cfg* c, int i, int j) {
   AttnDims a;
   if (layer_check(c, i, j, &a)) return -1;
   return two_streams_pay(c, is_grid(i, j)) ? 2 : 1;
+}
+int optimus_debug_attention_selected_masked(int b, int s, int h, int n, int q, int i, int j, int causal, const optimus_selection* selection) {
+  AttnDims a;
+  AttnSelectedDesc d = {};
+  if (selected_desc(b, s, h, n, q, i, j, selection, &a, &d)) return -1;
+  d.base.causal = causal ? 1 : 0;
+  return attn_selected_masked(d) ? 1 : 0;
 }
 int optimus_debug_attention_biased_rows(int backward, int b, int s, int h, int n, int q, int i, int j, const optimus_attention_bias* bias,
                                         int table_gradient) {

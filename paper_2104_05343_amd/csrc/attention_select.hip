@@ -60,25 +60,35 @@ __global__ __launch_bounds__(256) void block_means_kernel(SelectedArgs a) {
   if (lane == 0) a.mean_sizes[at] = sqrtf(size) * 1.0001f;
 }
 
-// sums and the like over the eight lanes of a query
+// sums and the like over the eight lanes of a query, in all of them: neighbours, pairs, then the other four mirrored (data-parallel moves, no
+// trips to LDS)
+template <int CTRL>
+__device__ __forceinline__ int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, false); }
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) { return __uint_as_float((unsigned)moved<CTRL>((int)__float_as_uint(x))); }
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+  const long long b = __double_as_longlong(x);
+  const unsigned lo = (unsigned)moved<CTRL>((int)b), hi = (unsigned)moved<CTRL>((int)(b >> 32));
+  return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
 template <class T, class F>
 __device__ __forceinline__ T eight(T x, F f) {
-#pragma unroll
-  for (int step = 1; step < 8; step <<= 1) x = f(x, __shfl_xor(x, step));
-  return x;
+  x = f(x, moved<0xB1>(x));
+  x = f(x, moved<0x4E>(x));
+  return f(x, moved<0x141>(x));
 }
 __device__ __forceinline__ int sum8(int x) { return eight(x, [](int p, int q) { return p + q; }); }
 __device__ __forceinline__ float min8(float x) { return eight(x, [](float p, float q) { return fminf(p, q); }); }
 __device__ __forceinline__ float max8(float x) { return eight(x, [](float p, float q) { return fmaxf(p, q); }); }
 
 constexpr int kRows = 32;             // queries of a workgroup
-constexpr int kKept = kMostCount;     // best exact scores kept of a query
 
-// LDS: scores [kRows][stride], kept scores, kept blocks, chosen bits
+// LDS: kept scores [kRows][kept], scores [kRows][stride], bits of chosen and of contested blocks [kRows][words], kept blocks [kRows][kept]
 __host__ __device__ inline int score_stride(int blocks) { return (blocks + 31) / 32 * 32 + 4; }
 __host__ __device__ inline int bit_words(int blocks) { return (blocks + 31) / 32; }
-inline size_t select_lds(int blocks) {
-  return (size_t)kRows * (score_stride(blocks) * 4 + bit_words(blocks) * 4 + kKept * 10);
+inline size_t select_lds(int blocks, int count) {
+  return (size_t)kRows * (score_stride(blocks) * 4 + bit_words(blocks) * 8 + count * 10) + 16;
 }
 
 // NV: scores of a lane; 8 NV blocks at most.
@@ -96,10 +106,12 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
   const int others = a.causal ? min(own, have) : have;   // candidates, the own block among them without a mask
   const int K = a.count - 1;
   const int stride = score_stride(a.blocks), words = bit_words(a.blocks);
-  double* kept = (double*)dynamic;                                     // [kRows][kKept]
-  float* scores = (float*)(kept + kRows * kKept);                      // [kRows][stride]
-  unsigned* bits = (unsigned*)(scores + kRows * stride);               // [kRows][words]
-  unsigned short* kept_block = (unsigned short*)(bits + kRows * words);   // [kRows][kKept]
+  double* kept = (double*)dynamic;
+  float* scores = (float*)(kept + kRows * a.count);
+  unsigned* bits = (unsigned*)(scores + kRows * stride);
+  unsigned* contested = bits + kRows * words;
+  float* sizes = (float*)(contested + kRows * words);                  // largest mean of each wavefront's blocks
+  unsigned short* kept_block = (unsigned short*)(sizes + 4);
   const int row = tid >> 3, e = tid & 7, t = q0 + row;   // eight lanes a query
   int* out = a.chosen + (m.vec + t) * a.count;
   const bool query = t < m.len;
@@ -129,31 +141,64 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
         *(float4*)(scores + (lane & 31) * stride + v0 + 8 * c + 4 * g) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
     }
   }
-  for (int k = tid; k < kRows * words; k += 256) bits[k] = 0;
-  // E of the row
+  for (int k = tid; k < 2 * kRows * words; k += 256) bits[k] = 0;
+  // E of the row: a query's size by its eight lanes, the largest mean by the workgroup
   float mean_size = 0.f, q_size = 0.f;
-  for (int v = e; v < others; v += 8) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
-  mean_size = max8(mean_size);
-  const bf16_t* Q = f.qkv + m.qkv + (long long)min(t, m.len - 1) * f.ld + e * (D / 8);
+  for (int v = tid; v < others; v += 256) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
 #pragma unroll
-  for (int k = 0; k < D / 8; ++k) q_size = fmaf(bf16_to_f32(Q[k]), bf16_to_f32(Q[k]), q_size);
+  for (int step = 1; step < 64; step <<= 1) mean_size = fmaxf(mean_size, __shfl_xor(mean_size, step));
+  if (lane == 0) sizes[wave] = mean_size;
+  const bf16_t* Q = f.qkv + m.qkv + (long long)min(t, m.len - 1) * f.ld + e * (D / 8);
+  float q[D / 8];
+#pragma unroll
+  for (int k = 0; k < D / 64; ++k) {
+    const u32x4 w = *(const u32x4*)(Q + 8 * k);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      q[8 * k + 2 * j] = __uint_as_float(w[j] << 16);
+      q[8 * k + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < D / 8; ++k) q_size = fmaf(q[k], q[k], q_size);
   q_size = sqrtf(eight(q_size, [](float p, float q) { return p + q; })) * 1.0001f;
-  float error = q_size * mean_size * (D * 1.1920929e-7f);
   __syncthreads();
+  mean_size = fmaxf(fmaxf(sizes[0], sizes[1]), fmaxf(sizes[2], sizes[3]));
+  float error = q_size * mean_size * (D * 1.1920929e-7f);
   const float* mine = scores + row * stride;
   // a lane's scores: of blocks e, e + 8, ..; -infinity: no candidate.  wild: a score or the bound is not finite, or too small for the bound
   float x[NV];
   float lo = INFINITY, hi = -INFINITY;
   bool wild = !(error < 1e30f) || error < 1e-30f || q_size < 1e-25f || mean_size < 1e-25f;
+  // (the loops over them in parts of 64 blocks, of which a workgroup in the front of its sequence has few)
+  constexpr int PART = NV < 8 ? NV : 8;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = e + 8 * k;
-    const bool candidate = v < others && v != own;
-    x[k] = candidate ? mine[v] : -INFINITY;
-    wild = wild || (candidate && !(fabsf(x[k]) < 1e30f));
-    lo = candidate ? fminf(lo, x[k]) : lo;
-    hi = fmaxf(hi, x[k]);
+  for (int p = 0; p < NV; p += PART) {
+    const bool some = 8 * p < others;
+#pragma unroll
+    for (int k = p; k < p + PART; ++k) x[k] = -INFINITY;
+    if (some) {
+#pragma unroll
+      for (int k = p; k < p + PART; ++k) {
+        const int v = e + 8 * k;
+        const bool candidate = v < others && v != own;
+        x[k] = candidate ? mine[v] : -INFINITY;
+        wild = wild || (candidate && !(fabsf(x[k]) < 1e30f));
+        lo = candidate ? fminf(lo, x[k]) : lo;
+        hi = fmaxf(hi, x[k]);
+      }
+    }
   }
+  auto at_least = [&](float from) {   // scores from `from` on, of the row
+    int n = 0;
+#pragma unroll
+    for (int p = 0; p < NV; p += PART)
+      if (8 * p < others) {
+#pragma unroll
+        for (int k = p; k < p + PART; ++k) n += x[k] >= from ? 1 : 0;
+      }
+    return sum8(n);
+  };
   lo = min8(lo);
   hi = max8(hi);
   wild = sum8(wild) != 0;
@@ -163,10 +208,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
   hi += fabsf(hi) * 1e-6f + 1e-37f;
   for (int round = 0; round < 40 && __builtin_amdgcn_ballot_w64(!found) != 0; ++round) {
     const float middle = 0.5f * lo + 0.5f * hi;
-    int n = 0;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) n += x[k] >= middle ? 1 : 0;
-    n = sum8(n);
+    const int n = at_least(middle);
     if (!found) {
       if (n >= K) lo = middle;
       else hi = middle;
@@ -179,10 +221,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) least = x[k] >= cut ? fminf(least, x[k]) : least;
   least = min8(least);
-  int n_cut = 0;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) n_cut += x[k] >= cut ? 1 : 0;
-  n_cut = sum8(n_cut);
+  const int n_cut = at_least(cut);
   float above = (n_cut == K ? least : hi) + 2.0f * error, below = least - 2.0f * error;
   if (wild) {
     above = INFINITY;
@@ -199,39 +238,49 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
   n_above = wild ? 0 : sum8(n_above);
   n_below = sum8(n_below);
   const bool decided = n_below == K;
-  // the bits of what is chosen; what is contested otherwise stays for the exact scores
+  // the bits of what is chosen, and of what is left to the exact scores
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int v = e + 8 * k;
-    const bool candidate = v < others && v != own;
-    if (query && candidate && (decided ? !(x[k] < below) : !wild && x[k] > above)) atomicOr(&bits[row * words + (v >> 5)], 1u << (v & 31));
+    if (query && v < others && v != own && !(x[k] < below))
+      atomicOr(&(decided || (!wild && x[k] > above) ? bits : contested)[row * words + (v >> 5)], 1u << (v & 31));
   }
   if (query && e == 0) atomicOr(&bits[row * words + (own >> 5)], 1u << (own & 31));
   __builtin_amdgcn_wave_barrier();
   if (__builtin_amdgcn_ballot_w64(query && !decided) != 0) {
     // exact scores, in the order of the blocks, the best ones kept: one that is not above the worst kept is out (equal: the lower block stays)
     const int places = query && !decided ? K - n_above : 0;
-    double* best = kept + row * kKept;
-    unsigned short* block_of = kept_block + row * kKept;
-    int n = 0, worst_at = 0;
+    double* best = kept + row * a.count;
+    unsigned short* block_of = kept_block + row * a.count;
+    int n = 0, worst_at = 0, word = -1;
     double worst = 0.0;
+    unsigned left = 0;
     const bf16_t* means = a.means + (long long)mm * a.blocks * D + e * (D / 8);
-    for (int v = 0; v < others; ++v) {
-      const float approximate = mine[v];
-      const bool contested = places > 0 && v != own && !(approximate < below) && (wild || !(approximate > above));
-      if (__builtin_amdgcn_ballot_w64(contested) == 0) continue;
+    while (true) {   // a query's next block each, until none has one
+      while (left == 0 && word + 1 < words) left = contested[row * words + ++word];
+      const bool contest = left != 0;
+      if (__builtin_amdgcn_ballot_w64(contest) == 0) break;
+      const int v = contest ? word * 32 + __builtin_ctz(left) : 0;
+      left &= left - 1;
       double score = 0.0;
 #pragma unroll
-      for (int k = 0; k < D / 8; ++k) score += (double)bf16_to_f32(Q[k]) * (double)bf16_to_f32(means[(long long)v * D + k]);
+      for (int k = 0; k < D / 64; ++k) {
+        const u32x4 w = *(const u32x4*)(means + (long long)v * D + 8 * k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          score += (double)q[8 * k + 2 * j] * (double)__uint_as_float(w[j] << 16);
+          score += (double)q[8 * k + 2 * j + 1] * (double)__uint_as_float(w[j] & 0xffff0000u);
+        }
+      }
       score = eight(score, [](double p, double q) { return p + q; });
       if (score != score) score = -INFINITY;   // (a score that is no number is below all)
-      if (contested && n < places) {
+      if (contest && n < places) {
         if (e == 0) {
           best[n] = score;
           block_of[n] = (unsigned short)v;
         }
         ++n;
-      } else if (contested && score > worst) {
+      } else if (contest && score > worst) {
         if (e == 0) {
           best[worst_at] = score;
           block_of[worst_at] = (unsigned short)v;
@@ -293,7 +342,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
 
 template <int D, int NV>
 void select_launch(const SelectedArgs& a, int mats, hipStream_t st) {
-  const size_t lds = select_lds(a.blocks);
+  const size_t lds = select_lds(a.blocks, a.count);
   if (lds > 65536) (void)hipFuncSetAttribute((const void*)select_kernel<D, NV>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   select_kernel<D, NV><<<dim3((a.f.s + kRows - 1) / kRows, mats), 256, lds, st>>>(a);
 }

@@ -9,6 +9,8 @@ namespace {
 // Pairs of 512 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
 // make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
 constexpr int kWords = kListChunk / 32;
+constexpr long long kMaskedCost = 3;              // of a chosen pair with lists, in pairs of the masked form
+constexpr size_t kPortion = (size_t)384 << 20;    // bytes of partial results in memory at a time
 
 __device__ __forceinline__ bool sees(const SelectedArgs& a, int len, int t, int v) {
   return v >= 0 && v < a.blocks && v * a.block < len && (!a.causal || v * a.block <= t);
@@ -19,34 +21,34 @@ __device__ __forceinline__ void chunk_pairs(const SelectedArgs& a, int mm, int l
   const int tid = threadIdx.x;
   if (t >= len) return;
   const int* own = a.selected + ((long long)mm * a.f.s + t) * a.count;
-  for (int e = 0; e < a.count; ++e) {
-    const int v = own[e];
-    bool counts = false;
-    if (sees(a, len, t, v)) {
-      const unsigned bit = 1u << (tid & 31);
-      counts = !(atomicOr(&bits[(tid >> 5) * a.blocks + v], bit) & bit);   // (a query's bits are one thread's: no race for the first)
+  for (int e0 = 0; e0 < a.count; e0 += 8) {   // eight loads in flight
+    int v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = e0 + u < a.count ? own[e0 + u] : -1;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      bool counts = false;
+      if (sees(a, len, t, v[u])) {
+        const unsigned bit = 1u << (tid & 31);
+        counts = !(atomicOr(&bits[(tid >> 5) * a.blocks + v[u]], bit) & bit);   // (a query's bits are one thread's: no race for the first)
+      }
+      entry(e0 + u, v[u], counts);
     }
-    entry(e, v, counts);
   }
 }
-__device__ __forceinline__ int chunk_query(const SelectedArgs& a, int unit_in_matrix, int chunk) {
-  const int in_unit = chunk * kListChunk + threadIdx.x;
-  return in_unit < a.unit_rows ? unit_in_matrix * a.unit_rows + in_unit : a.f.s;   // s: none
-}
-
 __global__ __launch_bounds__(kListChunk) void list_count_kernel(SelectedArgs a) {
   extern __shared__ unsigned bits[];
-  const int chunk = blockIdx.x, unit = blockIdx.y, mm = unit / a.units;
+  const int chunk = blockIdx.x, mm = blockIdx.y;
   const int len = selected_matrix<64>(a, mm).len;
   for (int k = threadIdx.x; k < kWords * a.blocks; k += kListChunk) bits[k] = 0;
   __syncthreads();
-  chunk_pairs(a, mm, len, chunk_query(a, unit % a.units, chunk), bits, [](int, int, bool) {});
+  chunk_pairs(a, mm, len, chunk * kListChunk + threadIdx.x, bits, [](int, int, bool) {});
   __syncthreads();
   for (int v = threadIdx.x; v < a.blocks; v += kListChunk) {
     int n = 0;
 #pragma unroll
     for (int w = 0; w < kWords; ++w) n += __popc(bits[w * a.blocks + v]);
-    a.counts[((long long)unit * a.chunks + chunk) * a.blocks + v] = n;
+    a.counts[((long long)mm * a.chunks + chunk) * a.blocks + v] = n;
   }
 }
 
@@ -75,58 +77,78 @@ __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
 
 __global__ __launch_bounds__(1024) void list_places_kernel(SelectedArgs a) {
   __shared__ int lds[16];
-  const int unit = blockIdx.x, v = threadIdx.x;
+  const int mm = blockIdx.x, v = threadIdx.x;
   int n = 0;
   if (v < a.blocks) {
-    int* c = a.counts + (long long)unit * a.chunks * a.blocks + v;
-    for (int k = 0; k < a.chunks; ++k) {
-      const int x = c[(long long)k * a.blocks];
-      c[(long long)k * a.blocks] = n;
-      n += x;
+    int* c = a.counts + (long long)mm * a.chunks * a.blocks + v;
+    for (int k = 0; k < a.chunks; k += 8) {   // eight loads in flight
+      int x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = k + u < a.chunks ? c[(long long)(k + u) * a.blocks] : 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (k + u < a.chunks) c[(long long)(k + u) * a.blocks] = n;
+        n += x[u];
+      }
     }
   }
   int all;
   const int at = exclusive_sum(n, lds, &all);
-  int* offsets = a.offsets + (long long)unit * (a.blocks + 1);
+  int* offsets = a.offsets + (long long)mm * (a.blocks + 1);
   if (v < a.blocks) offsets[v] = at;
   if (v == 0) offsets[a.blocks] = all;
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
     if (!a.items[kind]) continue;
     const int items = (n + a.seg[kind] - 1) / a.seg[kind], first = exclusive_sum(items, lds, &all);
-    int* firsts = a.first_item + ((long long)kind * a.all_units + unit) * (a.blocks + 1);
+    int* firsts = a.first_item + ((long long)kind * a.mats + mm) * (a.blocks + 1);
     if (v < a.blocks) firsts[v] = first;
     if (v == 0) firsts[a.blocks] = all;
     for (int k = 0; k < items; ++k)
-      a.items[kind][(long long)unit * a.most[kind] + first + k] = i32x4_t{v, at + k * a.seg[kind], min(a.seg[kind], n - k * a.seg[kind]), 0};
+      a.items[kind][(long long)mm * a.most[kind] + first + k] = i32x4_t{v, at + k * a.seg[kind], min(a.seg[kind], n - k * a.seg[kind]), 0};
   }
 }
 
 __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
   extern __shared__ unsigned bits[];
-  const int chunk = blockIdx.x, unit = blockIdx.y, mm = unit / a.units, tid = threadIdx.x;
+  int* place_of = (int*)(bits + kWords * a.blocks);   // [word][block]: place of a word's first pair
+  const int chunk = blockIdx.x, mm = blockIdx.y, tid = threadIdx.x;
   const int len = selected_matrix<64>(a, mm).len;
-  const int t = chunk_query(a, unit % a.units, chunk);
+  const int t = chunk * kListChunk + tid;
   for (int k = tid; k < kWords * a.blocks; k += kListChunk) bits[k] = 0;
   __syncthreads();
   unsigned long long counted = 0;   // (at most 64 entries)
   chunk_pairs(a, mm, len, t, bits, [&](int e, int, bool counts) { counted |= counts ? 1ull << e : 0; });
   __syncthreads();
-  if (t >= a.f.s) return;
-  const long long first = (long long)unit * a.unit_rows * a.count;
-  int* places = a.places + first + (long long)(t - unit % a.units * a.unit_rows) * a.count;
-  const int* own = a.selected + ((long long)mm * a.f.s + t) * a.count;
-  const int* offsets = a.offsets + (long long)unit * (a.blocks + 1);
-  const int* before = a.counts + ((long long)unit * a.chunks + chunk) * a.blocks;
-  for (int e = 0; e < a.count; ++e) {
-    int place = -1;
-    if (counted >> e & 1) {
-      const int v = own[e];
-      place = offsets[v] + before[v] + __popc(bits[(tid >> 5) * a.blocks + v] & ((1u << (tid & 31)) - 1));
-      for (int w = 0; w < tid >> 5; ++w) place += __popc(bits[w * a.blocks + v]);
-      a.list[first + place] = t;
+  const int* offsets = a.offsets + (long long)mm * (a.blocks + 1);
+  const int* before = a.counts + ((long long)mm * a.chunks + chunk) * a.blocks;
+  for (int v = tid; v < a.blocks; v += kListChunk) {
+    int n = offsets[v] + before[v];
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+      place_of[w * a.blocks + v] = n;
+      n += __popc(bits[w * a.blocks + v]);
     }
-    places[e] = place;
+  }
+  __syncthreads();
+  if (t >= a.f.s) return;
+  const long long first = (long long)mm * a.f.s * a.count;
+  int* places = a.places + first + (long long)t * a.count;
+  const int* own = a.selected + first + (long long)t * a.count;
+  const int word = (tid >> 5) * a.blocks;
+  for (int e0 = 0; e0 < a.count; e0 += 8) {
+    int v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = e0 + u < a.count ? own[e0 + u] : -1;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      int place = -1;
+      if (counted >> (e0 + u) & 1) {
+        place = place_of[word + v[u]] + __popc(bits[word + v[u]] & ((1u << (tid & 31)) - 1));
+        a.list[first + place] = t;
+      }
+      if (e0 + u < a.count) places[e0 + u] = place;
+    }
   }
 }
 
@@ -141,9 +163,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  const int mm = a.mat0 + blockIdx.y;
   ListItem it;
-  if (!list_item(a, 0, unit, blockIdx.x, &it)) return;
+  if (!list_item(a, 0, mm, blockIdx.x, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const bf16_t* Qp = f.qkv + m.qkv;
   const int key0 = it.block * a.block, last = m.len - 1;
@@ -155,8 +177,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
     ldr.issue(Qp + 2 * D, key0 + st * BLK, m.len, lds[st][1]);
   }
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
-  const long long first = (long long)unit * a.unit_rows * a.count + it.start;
-  const long long out = (long long)blockIdx.y * a.unit_rows * a.count + it.start;
+  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
   const int* list = a.list + first;
   int row = wave * 32 + (lane & 31);
   int t = list[min(row, it.pairs - 1)];
@@ -232,9 +253,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  const int mm = a.mat0 + blockIdx.y;
   ListItem it;
-  if (!list_item(a, 0, unit, blockIdx.x, &it)) return;
+  if (!list_item(a, 0, mm, blockIdx.x, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const bf16_t* Qp = f.qkv + m.qkv;
   const int key0 = it.block * a.block, last = m.len - 1;
@@ -248,8 +269,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
   };
   issue(0, 0);
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
-  const long long first = (long long)unit * a.unit_rows * a.count + it.start;
-  const long long out = (long long)blockIdx.y * a.unit_rows * a.count + it.start;
+  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
   const int* list = a.list + first;
   const int row = wave * 32 + (lane & 31);
   wait_loads_and_barrier();
@@ -348,12 +368,12 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[8][D];
   const FusedArgs& f = a.f;
   const int half = threadIdx.x >> 5, n = threadIdx.x & 31;
-  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
-  const int in_unit = blockIdx.x * 8 + half, t = unit % a.units * a.unit_rows + in_unit;
-  const bool inside = in_unit < a.unit_rows && t < f.s;
+  const int mm = a.mat0 + blockIdx.y;
+  const int t = blockIdx.x * 8 + half;
+  const bool inside = t < f.s;
   const SelMatrix m = selected_matrix<D>(a, mm);
-  const long long rows = (long long)blockIdx.y * a.unit_rows * a.count;
-  const int* places = a.places + (long long)unit * a.unit_rows * a.count + (long long)in_unit * a.count;
+  const long long rows = (long long)blockIdx.y * f.s * a.count;
+  const int* places = a.places + (m.vec + t) * a.count;
   // entries n and n + 32
   int place[2];
   float2 ml[2];
@@ -415,6 +435,7 @@ SelectedArgs make_args(const AttnSelectedDesc& b) {
   a.selected = b.selected; a.lengths = b.lengths;
   a.nb = d.nb; a.nmat = d.nb * d.nh; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal;
   a.block = b.block; a.count = b.count; a.blocks = (d.s + b.block - 1) / b.block;
+  a.by_steps = b.block == 64 ? 0u : (unsigned)(((1ull << 32) + b.block / 64 - 1) / (b.block / 64));
   return a;
 }
 
@@ -423,13 +444,15 @@ size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 // the workspace's parts into the arguments
 SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bool bwd) {
   SelectedArgs a = make_args(b);
-  a.unit_rows = p.unit_rows; a.units = p.units; a.all_units = p.mats * p.units; a.chunks = p.chunks;
+  a.mats = p.mats; a.chunks = p.chunks; a.mask_words = p.mask_words;
   char* at = (char*)b.ws;
   auto take = [&](size_t bytes) {
     char* r = at;
     at += bytes;
     return r;
   };
+  a.f.delta = (float*)take(p.delta);
+  a.mask = (unsigned*)take(p.mask);
   a.counts = (int*)take(p.counts);
   a.offsets = (int*)take(p.offsets);
   a.first_item = (int*)take(p.first_item);
@@ -441,11 +464,18 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
   if (!bwd) a.items[1] = nullptr;
   a.list = (int*)take(p.list);
   a.places = (int*)take(p.places);
-  a.f.delta = (float*)take(p.delta);
   a.rows = (float*)take(p.rows);
   a.ml = (float2*)take(p.ml);
   a.key_rows = (float*)a.rows;   // (dK and dV come when the rows of dQ are done with)
   return a;
+}
+
+void launch_lists(const SelectedArgs& a, hipStream_t st) {
+  const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 64 KiB
+  if (2 * bits > 65536) (void)hipFuncSetAttribute((const void*)list_fill_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(2 * bits));
+  list_count_kernel<<<dim3(a.chunks, a.mats), kListChunk, bits, st>>>(a);
+  list_places_kernel<<<a.mats, 1024, 0, st>>>(a);
+  list_fill_kernel<<<dim3(a.chunks, a.mats), kListChunk, 2 * bits, st>>>(a);
 }
 
 template <int D>
@@ -454,69 +484,77 @@ void fwd_launch(const SelectedArgs& a, int portion, hipStream_t st) {
   if (a.block == 64) selected_fwd_kernel<D, 2><<<grid, 256, 0, st>>>(a);
   else if (a.block == 128) selected_fwd_kernel<D, 4><<<grid, 256, 0, st>>>(a);
   else selected_fwd_long_kernel<D><<<grid, 256, 0, st>>>(a);
-  selected_combine_kernel<D, true><<<dim3((a.unit_rows + 7) / 8, portion), 256, 0, st>>>(a);
+  selected_combine_kernel<D, true><<<dim3((a.f.s + 7) / 8, portion), 256, 0, st>>>(a);
 }
 
 }  // namespace
 
 void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipStream_t st) {
-  const dim3 grid((a.unit_rows + 7) / 8, portion);
+  const dim3 grid((a.f.s + 7) / 8, portion);
   if (d == 64) selected_combine_kernel<64, false><<<grid, 256, 0, st>>>(a);
   else selected_combine_kernel<128, false><<<grid, 256, 0, st>>>(a);
 }
 
-void launch_selected_lists(const SelectedArgs& a, hipStream_t st) {
-  const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 64 KiB
-  list_count_kernel<<<dim3(a.chunks, a.all_units), kListChunk, bits, st>>>(a);
-  list_places_kernel<<<a.all_units, 1024, 0, st>>>(a);
-  list_fill_kernel<<<dim3(a.chunks, a.all_units), kListChunk, bits, st>>>(a);
+// The masked form where the pairs of queries and blocks that it computes are at most kMaskedCost times the chosen ones.
+bool attn_selected_masked(const AttnSelectedDesc& b) {
+  const long long blocks = (b.base.s + b.block - 1) / b.block, k = b.count < blocks ? b.count : blocks;
+  if (blocks > kMaskedBlocks) return false;
+  const long long all = b.base.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
+  const long long chosen = b.base.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
+  return all <= kMaskedCost * chosen;
 }
 
-// Portions: partial results of 128 MiB at a time, half of the Infinity Cache.
-bool attn_selected_plan(const AttnSelectedDesc& b, int ndev, SelectedPlan* out) {
+void attn_selected_plan(const AttnSelectedDesc& b, SelectedPlan* out) {
   SelectedPlan p = {};
   const AttnFusedDesc& d = b.base;
-  const long long blocks = (d.s + b.block - 1) / b.block;
-  p.mats = ndev * d.nb * d.nh;
-  const long long row_bytes = d.d * 4 + 8, budget = 128ll << 20;
-  p.unit_rows = d.s;
-  p.units = (d.s + p.unit_rows - 1) / p.unit_rows;
-  p.chunks = (p.unit_rows + kListChunk - 1) / kListChunk;
-  const long long units = (long long)p.mats * p.units, pairs = (long long)p.unit_rows * b.count;
-  if (units > 65535) return false;
-  const long long fit = budget / (pairs * row_bytes);
-  p.unit_portion = (int)(fit < 1 ? 1 : fit > units ? units : fit);
-  p.seg[0] = 512;
+  const size_t blocks = (d.s + b.block - 1) / b.block, pairs = (size_t)d.s * b.count;
+  p.mats = d.ndev * d.nb * d.nh;
+  const size_t mats = p.mats;
+  p.masked = attn_selected_masked(b);
+  p.delta = round256(mats * d.s * 4);
+  if (p.masked) {
+    p.mask_words = (d.s + 31) / 32;
+    p.mask = round256(mats * blocks * p.mask_words * 4);
+    p.total = p.delta + p.mask;
+    *out = p;
+    return;
+  }
+  p.chunks = (d.s + kListChunk - 1) / kListChunk;
+  p.seg[0] = 256;
   p.seg[1] = 1024;
   for (int k = 0; k < 2; ++k) p.most[k] = (int)(blocks + pairs / p.seg[k]);
-  const long long key_bytes = (long long)p.most[1] * p.units * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
-  const long long key_fit = budget / key_bytes;
-  p.mat_portion = (int)(key_fit < 1 ? 1 : key_fit > p.mats ? p.mats : key_fit);
-  p.counts = round256((size_t)units * p.chunks * blocks * 4);
-  p.offsets = round256((size_t)units * (blocks + 1) * 4);
-  p.first_item = round256((size_t)2 * units * (blocks + 1) * 4);
-  for (int k = 0; k < 2; ++k) p.items[k] = round256((size_t)units * p.most[k] * 16);
-  p.list = p.places = round256((size_t)units * pairs * 4);
-  p.delta = round256((size_t)p.mats * d.s * 4);
-  const size_t rows = (size_t)p.unit_portion * pairs * d.d * 4, keys = (size_t)p.mat_portion * key_bytes;
+  const size_t row_bytes = pairs * (d.d * 4 + 8), key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
+  auto fit = [&](size_t bytes) { return (int)(kPortion / bytes < 1 ? 1 : kPortion / bytes > mats ? mats : kPortion / bytes); };
+  p.portion = fit(row_bytes);
+  p.key_portion = fit(key_bytes);
+  p.counts = round256(mats * p.chunks * blocks * 4);
+  p.offsets = round256(mats * (blocks + 1) * 4);
+  p.first_item = round256(2 * mats * (blocks + 1) * 4);
+  for (int k = 0; k < 2; ++k) p.items[k] = round256(mats * p.most[k] * 16);
+  p.list = p.places = round256(mats * pairs * 4);
+  const size_t rows = p.portion * pairs * d.d * 4, keys = p.key_portion * key_bytes;
   p.rows = round256(rows > keys ? rows : keys);
-  p.ml = round256((size_t)p.unit_portion * pairs * 8);
-  p.total = p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.delta + p.rows + p.ml;
+  p.ml = round256(p.portion * pairs * 8);
+  p.total = p.delta + p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.ml;
   *out = p;
-  return true;
 }
 size_t attn_selected_ws_bytes(const AttnSelectedDesc& b) {
   SelectedPlan p;
-  return attn_selected_plan(b, b.base.ndev, &p) ? p.total : 0;
+  attn_selected_plan(b, &p);
+  return p.total;
 }
 
 int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
   SelectedPlan p;
-  if (!attn_selected_plan(b, b.base.ndev, &p)) return OPTIMUS_ESHAPE;
+  attn_selected_plan(b, &p);
   SelectedArgs a = with_workspace(b, p, false);
-  launch_selected_lists(a, st);
-  for (a.unit0 = 0; a.unit0 < a.all_units; a.unit0 += p.unit_portion) {
-    const int portion = min(p.unit_portion, a.all_units - a.unit0);
+  if (p.masked) {
+    launch_selected_masked(a, p.mats, b.base.d, false, st);
+    return hip_launch_status();
+  }
+  launch_lists(a, st);
+  for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
+    const int portion = min(p.portion, p.mats - a.mat0);
     if (b.base.d == 64) fwd_launch<64>(a, portion, st);
     else fwd_launch<128>(a, portion, st);
     if (const int rc = hip_launch_status()) return rc;
@@ -526,9 +564,13 @@ int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
 
 int launch_attn_selected_bwd(const AttnSelectedDesc& b, hipStream_t st) {
   SelectedPlan p;
-  if (!attn_selected_plan(b, b.base.ndev, &p)) return OPTIMUS_ESHAPE;
+  attn_selected_plan(b, &p);
   const SelectedArgs a = with_workspace(b, p, true);
-  launch_selected_lists(a, st);
+  if (p.masked) {
+    launch_selected_masked(a, p.mats, b.base.d, true, st);
+    return hip_launch_status();
+  }
+  launch_lists(a, st);
   return launch_selected_bwd_kernels(a, p, b.base.d, st);
 }
 

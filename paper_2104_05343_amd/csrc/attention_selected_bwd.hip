@@ -57,9 +57,9 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int unit = a.unit0 + blockIdx.y, mm = unit / a.units;
+  const int mm = a.mat0 + blockIdx.y;
   ListItem it;
-  if (!list_item(a, 0, unit, blockIdx.x, &it)) return;
+  if (!list_item(a, 0, mm, blockIdx.x, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const bf16_t* Qp = f.qkv + m.qkv;
   const bf16_t* Gp = f.d_attn + m.attn;
@@ -75,8 +75,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
 #pragma unroll
   for (int st = 0; st < (KT ? STAGES : 1); ++st) issue(st, st);
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane);
-  const long long first = (long long)unit * a.unit_rows * a.count + it.start;
-  const long long out = (long long)blockIdx.y * a.unit_rows * a.count + it.start;
+  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
   const int* list = a.list + first;
   const int row = wave * 32 + (lane & 31);
   bf16x8 qf[KS], dof[KS];
@@ -168,9 +167,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % NRG, par = wave / NRG;
   const int tiles = a.block / BLK, item = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-  const int unit = blockIdx.y + a.mat0 * a.units, mm = unit / a.units;
+  const int mm = a.mat0 + blockIdx.y;
   ListItem it;
-  if (!list_item(a, 1, unit, item, &it)) return;
+  if (!list_item(a, 1, mm, item, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const int kt0 = it.block * a.block + tile * BLK;
   if (kt0 >= m.len) return;
@@ -183,7 +182,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
     kf[ks] = *(const bf16x8*)(Qp + D + (long long)krow * f.ld + ks * 16 + g * 8);
     vf[ks] = *(const bf16x8*)(Qp + 2 * D + (long long)krow * f.ld + ks * 16 + g * 8);
   }
-  const int* list = a.list + (long long)unit * a.unit_rows * a.count + it.start;
+  const int* list = a.list + m.vec * a.count + it.start;
   const int n_it = (it.pairs + PAIR - 1) / PAIR;
   f32x16 dkacc[DT], dvacc[DT];
 #pragma unroll
@@ -313,16 +312,13 @@ __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs 
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = 0.f;
   if (key < m.len) {
-    for (int u = 0; u < a.units; ++u) {
-      const int* first = a.first_item + ((long long)a.all_units + (long long)mm * a.units + u) * (a.blocks + 1);
-      const int from = first[v], to = first[v + 1];
-      const long long of_unit = ((long long)blockIdx.y * a.units + u) * a.most[1];
+    const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1);
+    const int from = first[v], to = first[v + 1];
 #pragma unroll 2
-      for (int k = from; k < to; ++k) {
-        const float* p = a.key_rows + ((of_unit + k) * tiles + in_block / BLK) * (2 * BLK * D) + in_block % BLK * D + n * DT;
-        dk += *(const V*)p;
-        dv += *(const V*)(p + BLK * D);
-      }
+    for (int k = from; k < to; ++k) {
+      const float* p = a.key_rows + (((long long)blockIdx.y * a.most[1] + k) * tiles + in_block / BLK) * (2 * BLK * D) + in_block % BLK * D + n * DT;
+      dk += *(const V*)p;
+      dv += *(const V*)(p + BLK * D);
     }
   }
 #pragma unroll
@@ -336,8 +332,8 @@ template <int D>
 int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
   const int s = a.f.s;
   selected_delta_kernel<D><<<dim3((s + 127) / 128, p.mats), 256, 0, st>>>(a);
-  for (a.unit0 = 0; a.unit0 < a.all_units; a.unit0 += p.unit_portion) {
-    const int portion = min(p.unit_portion, a.all_units - a.unit0);
+  for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
+    const int portion = min(p.portion, p.mats - a.mat0);
     const dim3 grid(a.most[0], portion);
     if (a.block == 64) selected_dq_kernel<D, 2><<<grid, 256, 0, st>>>(a);
     else if (a.block == 128) selected_dq_kernel<D, 4><<<grid, 256, 0, st>>>(a);
@@ -345,9 +341,9 @@ int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
     launch_selected_dq_combine(a, D, portion, st);
     if (const int rc = hip_launch_status()) return rc;
   }
-  for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.mat_portion) {
-    const int portion = min(p.mat_portion, p.mats - a.mat0);
-    selected_dkv_kernel<D><<<dim3(a.most[1] * (a.block / BLK), portion * a.units), 256, 0, st>>>(a);
+  for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.key_portion) {
+    const int portion = min(p.key_portion, p.mats - a.mat0);
+    selected_dkv_kernel<D><<<dim3(a.most[1] * (a.block / BLK), portion), 256, 0, st>>>(a);
     selected_dkv_combine_kernel<D><<<dim3((s + 7) / 8, portion), 256, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }

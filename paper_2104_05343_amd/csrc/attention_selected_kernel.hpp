@@ -4,14 +4,15 @@
 // The choice is one step (attention_select.hip), the attention over any chosen blocks another (attention_selected.hip forward,
 // attention_selected_bwd.hip backward); tiles, fragments and layouts are those of the fused attention (attention_fused_kernel.hpp).
 //
-// How the work is cut.  Neighbouring queries choose different blocks, so a tile of queries has no common keys to load and a tile of the dense
+// Where queries choose a third and more of the blocks that they could, it is the fused attention with a mask (attention_selected_masked.hip).
+//
+// How the work is cut otherwise.  Neighbouring queries choose different blocks, so a tile of queries has no common keys to load and a tile of the dense
 // attention would be mostly masked.  The other way round a block of keys has a list of the queries that chose it.  A workgroup takes a
 // block and a piece of its list: the block's K and V are loaded once, queries come 128 at a time, gathered by their numbers, and every
 // product is dense.  What a query gets from one block is a partial result, a row of fp32 numbers with its maximum and sum (forward)
 // or a row of dQ (backward): it goes to memory at the pair's place in the list, and a second kernel adds up each query's rows, at the places
 // that the step which makes the lists has noted.  dK and dV need no such rows: their workgroups walk a block's list.
-// The rows are count * s * d * 4 bytes a matrix: written and read once they cost as much as the products do, so that they are made in
-// portions (units of queries, a few at a time) that stay in the Infinity Cache.
+// The rows are count * s * d * 4 bytes a matrix, which bounds this form: they are made for some matrices at a time.
 #pragma once
 #include "attention_biased_kernel.hpp"
 
@@ -19,6 +20,7 @@ namespace optimus {
 
 constexpr int kListChunk = 512;        // queries of a workgroup that makes the lists
 constexpr int kMostBlocks = 1024, kMostCount = 64;
+constexpr int kMaskedBlocks = 256;     // most blocks of a sequence in the masked form
 constexpr int kQueries = 128;          // list rows of a tile
 
 struct SelectedArgs {
@@ -30,37 +32,43 @@ struct SelectedArgs {
   float* mean_sizes;                   // [matrix][blocks]: Euclidean norms, rounded up
   int nb, nmat, q, dev0, causal;       // sequences and matrices of a device
   int block, blocks, count;            // keys of a block, blocks of a sequence, blocks of a query
-  // lists: a unit is a range of a matrix' queries
-  int unit_rows, units, all_units;     // queries of a unit, units of a matrix, of the whole call
-  int chunks;                          // kListChunk pieces of a unit
-  int unit0;                           // first unit of this launch
-  int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, most items of a unit
-  int* counts;                         // [unit][chunk][block]: pairs; then pairs of earlier chunks of the block
-  int* offsets;                        // [unit][blocks + 1]: place of a block's first pair
-  int* first_item;                     // [kind][unit][blocks + 1]
-  i32x4_t* items[2];                   // [unit][most]: block, place of the first pair, pairs, -
-  int* list;                           // [unit][unit_rows * count]: query of every pair
-  int* places;                         // [unit][unit_rows][count]: place of the pair in list, -1: none
-  float* rows;                         // [unit - unit0][unit_rows * count][d]: partial results, see store_rows
-  float2* ml;                          // [unit - unit0][unit_rows * count]: maximum of Q K^T, sum of exponentials
-  float* key_rows;                     // [matrix of the launch][unit][item][block / 64][dK, dV][64][d]
-  int mat0;                            // dK and dV: first matrix of this launch
+  // the masked form
+  unsigned by_steps;                   // ceil(2^32 / (block / 64)), see divide
+  int mask_words;                      // of a block's queries, 32 a word
+  unsigned* mask;                      // [matrix][block][mask_words]: whether a query has chosen the block
+  // lists
+  int mats, mat0;                      // matrices of the call, first one of this launch
+  int chunks;                          // kListChunk pieces of a sequence
+  int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, most items of a matrix
+  int* counts;                         // [matrix][chunk][block]: pairs; then pairs of earlier chunks of the block
+  int* offsets;                        // [matrix][blocks + 1]: place of a block's first pair
+  int* first_item;                     // [kind][matrix][blocks + 1]
+  i32x4_t* items[2];                   // [matrix][most]: block, place of the first pair, pairs, -
+  int* list;                           // [matrix][s * count]: query of every pair
+  int* places;                         // [matrix][s][count]: place of the pair in list, -1: none
+  float* rows;                         // [matrix - mat0][s * count][d]: partial results, see store_rows
+  float2* ml;                          // [matrix - mat0][s * count]: maximum of Q K^T, sum of exponentials
+  float* key_rows;                     // [matrix - mat0][item][block / 64][dK, dV][64][d]
 };
 
 // What the host decides; bytes of the workspace, in this order
 struct SelectedPlan {
-  int mats;                            // of the launch
-  int unit_rows, units, chunks;
-  int unit_portion, mat_portion;       // units and matrices whose partial results are in memory at a time
+  bool masked;
+  int mats, chunks, mask_words;
+  int portion, key_portion;            // matrices whose partial results are in memory at a time: of queries, of keys
   int seg[2], most[2];
-  size_t counts, offsets, first_item, items[2], list, places, delta, rows, ml, total;
+  size_t delta, mask, counts, offsets, first_item, items[2], list, places, rows, ml, total;
 };
 
 // csrc/attention_selected*.hip
 int launch_selected_bwd_kernels(const SelectedArgs& a, const SelectedPlan& p, int d, hipStream_t st);
 void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipStream_t st);
+void launch_selected_masked(const SelectedArgs& a, int mats, int d, bool bwd, hipStream_t st);
 
 namespace {
+
+// u / n for m = ceil(2^32 / n): exact while u * n <= 2^32; n = 1 has m = 0
+__device__ __forceinline__ unsigned divide(unsigned u, unsigned m) { return m ? __umulhi(u, m) : u; }
 
 // What a wavefront knows about its matrix, mm counted over the devices of the launch.
 struct SelMatrix {
@@ -72,7 +80,8 @@ __device__ __forceinline__ SelMatrix selected_matrix(const SelectedArgs& a, int 
   SelMatrix m;
   const FusedArgs& f = a.f;
   const int dev = mm / a.nmat, mat = mm % a.nmat, seq = mat / f.nh, head = mat % f.nh;
-  m.len = a.lengths ? min(max(a.lengths[(a.dev0 + dev) / a.q * a.nb + seq], 0), f.s) : f.s;
+  // (the same in every lane: loads through buffer resources want it in a scalar register)
+  m.len = __builtin_amdgcn_readfirstlane(a.lengths ? min(max(a.lengths[(a.dev0 + dev) / a.q * a.nb + seq], 0), f.s) : f.s);
   m.qkv = dev * f.dev_qkv + (long long)seq * f.s * f.ld + head * 3 * D;
   m.attn = dev * f.dev_attn + (long long)seq * f.s * f.ldo + head * D;
   m.vec = (long long)mm * f.s;
@@ -117,10 +126,10 @@ __device__ __forceinline__ void write_row(bf16_t* to, const typename RowPart<DT>
 struct ListItem {
   int block, start, pairs;
 };
-__device__ __forceinline__ bool list_item(const SelectedArgs& a, int kind, int unit, int k, ListItem* it) {
-  const int* first = a.first_item + ((long long)kind * a.all_units + unit) * (a.blocks + 1);
+__device__ __forceinline__ bool list_item(const SelectedArgs& a, int kind, int mm, int k, ListItem* it) {
+  const int* first = a.first_item + ((long long)kind * a.mats + mm) * (a.blocks + 1);
   if (k >= first[a.blocks]) return false;
-  const i32x4_t x = a.items[kind][(long long)unit * a.most[kind] + k];
+  const i32x4_t x = a.items[kind][(long long)mm * a.most[kind] + k];
   it->block = __builtin_amdgcn_readfirstlane(x.x);
   it->start = __builtin_amdgcn_readfirstlane(x.y);
   it->pairs = __builtin_amdgcn_readfirstlane(x.z);

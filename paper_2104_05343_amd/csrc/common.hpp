@@ -220,7 +220,8 @@ struct AttnSelectedDesc {
   void* ws;
 };
 size_t attn_select_ws_bytes(const AttnSelectedDesc& d);     // of the choice
-size_t attn_selected_ws_bytes(const AttnSelectedDesc& d);   // of both directions; 0 for a launch that is refused
+size_t attn_selected_ws_bytes(const AttnSelectedDesc& d);   // of both directions
+bool attn_selected_masked(const AttnSelectedDesc& d);       // whether they are the fused attention with a mask, not lists
 int launch_attn_select(const AttnSelectedDesc& d, hipStream_t stream);
 int launch_attn_selected_fwd(const AttnSelectedDesc& d, hipStream_t stream);
 int launch_attn_selected_bwd(const AttnSelectedDesc& d, hipStream_t stream);

@@ -110,12 +110,23 @@ def test_refuses_more():
 def test_workspace():
     size = lambda *a, sel=opt.make_selection(64, 3): opt.attention_selected_workspace_bytes(*a, sel)   # noqa: E731
     one, all_of = size(4, 200, 256, 4, 2, 0, 1), size(4, 200, 256, 4, 2, -1, -1)
-    assert 4 * 200 * 3 * (64 + 2) * 4 <= one < all_of
+    assert 4 * 200 * 4 <= one < all_of
     assert size(3, 200, 256, 4, 2, 0, 1) == size(4, 200, 320, 4, 2, 0, 1) == size(4, 200, 256, 4, 2, 0, 2) == 0
     assert size(4, 200, 256, 4, 2, 0, 1, sel=opt.make_selection(63, 3)) == 0
-    # partial results of one (sequence, head) where 128 MiB do not hold them, not of all of them
+    assert size(4, 5000, 256, 4, 2, 0, 1) >= 4 * 5000 * 3 * (64 + 2) * 4                # lists: partial results of all pairs
+    # of one (sequence, head) where 384 MiB do not hold them, not of all of them
     long = size(1, 1 << 18, 1024, 8, 1, 0, 0, sel=opt.make_selection(256, 16))
     assert long < 2 * (1 << 18) * 16 * (128 + 2) * 4
+
+
+def test_form():
+    """Every block with a mask where queries choose a third of what they could, at most 256 blocks; else lists."""
+    masked = lambda s, block, count, causal: opt.debug_attention_selected_masked(4, s, 256, 4, 2, 0, 1, causal, opt.make_selection(block, count))   # noqa: E731
+    assert masked(1, 64, 1, True) and masked(200, 64, 3, False) and masked(4096, 128, 8, True) and masked(1152, 64, 6, False)
+    assert not masked(5000, 64, 3, True) and not masked(1216, 64, 6, False) and not masked(32768, 128, 16, True)
+    assert masked(16384, 64, 64, True) and not masked(16385, 64, 64, True)              # 256 and 257 blocks
+    with pytest.raises(opt.OptimusError):
+        masked(200, 65, 3, True)
 
 
 def test_refuses_tensors():

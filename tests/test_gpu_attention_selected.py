@@ -328,3 +328,66 @@ def test_a_long_sequence():
         ds = p * (dO[rows] @ V[u] - (dO[rows] * O[rows]).sum(1))
         for got, w, size in ((G[u, d:2 * d], ds @ Q[rows] / 8, np.abs(ds) @ np.abs(Q[rows]) / 8), (G[u, 2 * d:], p @ dO[rows], p @ np.abs(dO[rows]))):
             assert np.all(np.abs(got - w) <= HALF * (1.01 * np.abs(w) + size) + 100 * FP32)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("s", [1025, 1087, 1088, 1089, 1119, 1120, 1121, 1151, 1152, 1153])
+def test_block_boundaries_with_lists(s, d):
+    """Few of many blocks: lists of queries, around the tiles of 32, 64 and 128 rows and keys."""
+    for block, count, causal in ((64, 2, True), (64, 4, False), (128, 1, True), (128, 2, False), (192, 1, True), (192, 1, False)):
+        r = Run(2, s, 2 * d, 2, 1, causal, block=block, count=count, lengths=[s, 700])
+        assert not opt.debug_attention_selected_masked(2, s, 2 * d, 2, 1, -1, -1, causal, r.sel)
+        r.go().check(which={(0, 0), (1, 1)})
+
+
+def test_all_forms_are_tested():
+    """Which of these tests' sizes take lists, which the mask: both, of every kind of block, in the boundary tests and in the grids."""
+    for block, count, s, want in ((64, 3, 400, True), (128, 2, 400, True), (192, 2, 400, True), (64, 2, 1089, False), (128, 1, 1089, False), (192, 1, 1089, False)):
+        assert opt.debug_attention_selected_masked(1, s, 128, 2, 1, 0, 0, True, opt.make_selection(block, count)) == want
+
+
+@pytest.mark.parametrize("block", [64, 128, 256])
+def test_choices_of_the_callers_own_with_lists(block):
+    """More blocks than a third of them named: repeated, unsorted, out of range, none, all queries the same one."""
+    b, n, s, count = 2, 2, 26 * block + 17, 2
+    for causal in (True, False):
+        for low, high in ((-3, 29), (0, 2), (-1, 0), (-2 ** 31, 2 ** 31 - 1)):
+            r = Run(b, s, n * 64, n, 1, causal, block=block, count=count, selected=_given(b, n, s, count, low, high))
+            assert not opt.debug_attention_selected_masked(b, s, n * 64, n, 1, -1, -1, causal, r.sel)
+            r.go().check(which={(0, 0), (1, 1)} if block == 64 else {(1, 0)})
+
+
+def test_grids_and_lengths_with_lists():
+    full = Run(4, 1300, 256, 4, 2, True, block=64, count=2, lengths=[1300, 700, 0, 1299], dirty=True).go().check(which={(0, 0), (1, 3), (2, 1), (3, 2)})
+    assert not opt.debug_attention_selected_masked(4, 1300, 256, 4, 2, -1, -1, True, full.sel)
+    for dev in ((0, 1), (1, 0)):
+        one = Run(4, 1300, 256, 4, 2, True, block=64, count=2, lengths=[1300, 700, 0, 1299], dirty=True, at=dev).go()
+        k = dev[0] * 2 + dev[1]
+        for name in "SOLG":
+            x, y = getattr(full, name).view(4, -1), getattr(one, name).view(4, -1)
+            assert torch.equal(x[k].view(torch.uint8), y[k].view(torch.uint8)), name
+            rest = y[[e for e in range(4) if e != k]]
+            assert (rest == -123).all() if name == "S" else torch.isnan(rest).all(), name
+
+
+def test_captured_with_lists():
+    r = Run(2, 1300, 256, 4, 1, True, block=64, count=2, lengths=[1300, 1100]).go()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.choose()
+        r.forward()
+        r.backward()
+    saved, other = r.dQKV.clone(), torch.roll(r.dQKV, 8 * 64)
+    for k in range(4):
+        r.dQKV.copy_(saved if k % 2 == 0 else other)
+        r.keep.copy_(torch.tensor([1300, 1100] if k % 2 == 0 else [333, 1300], dtype=torch.int32))
+        for x in (r.O, r.L, r.G):
+            x.fill_(float("nan"))
+        r.S.fill_(-9)
+        r.ws.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (r.S, r.O, r.L, r.G)]
+        r.ws.fill_(0x55)
+        r.go()
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(got, (r.S, r.O, r.L, r.G)))

@@ -297,12 +297,12 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * optimus_attention_selected_bwd: from the same `selected` and the forward's attn and lse: P = exp(S - lse), dS = P (dO V^T - rowsum(dO attn)).
  * lengths: int32 [b] device memory or NULL (all s): tokens of a sequence that count (clamped to 0 .. s).  What qkv and d_attn hold behind them
  * is not looked at, NaN included; there selected is -1, attn 0, lse -infinity and d_qkv 0.
- * P and dS are rounded to bf16 before their products, as the operands are; scores, sums and a query's partial results are fp32; lse enters as
- * in optimus_attention_biased_bwd.  qkv, attn, lse, d_attn, d_qkv, coordinates and limits as in optimus_attention_fused_*; bf16 only;
+ * P and dS are rounded to bf16 before their products, as the operands are, and what a query gets from one block may be rounded to 11 bits (fp16,
+ * scaled) before the blocks' parts are added; scores and sums are fp32; lse enters as in optimus_attention_biased_bwd.  qkv, attn, lse, d_attn, d_qkv, coordinates and limits as in optimus_attention_fused_*; bf16 only;
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
  * from call to call: calls that may overlap need one each.  It holds up to 384 MiB of partial results, or one (sequence, head)'s:
- * s * count * (d + 2) * 4 bytes. */
+ * s * count * (2 d + 12) bytes. */
 typedef struct {
   int block, count;
   const int32_t* lengths;

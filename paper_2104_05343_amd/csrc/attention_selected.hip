@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
                                     oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf[k / 2][k & 1], x, oacc[n % DT], 0, 0, 0);
                                   });
     const long long at = out + base + wave * 32;
-    store_rows<DT>(a.rows + at * D, oacc, it.pairs - base - wave * 32, g, lane);
+    store_parts<DT>(a.rows + at * D, a.units + at, oacc, it.pairs - base - wave * 32, g, lane);
     if (mine && g == 0) a.ml[at + (lane & 31)] = make_float2(mx, sum);
   }
 }
@@ -353,21 +353,21 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
     }
     if (left > 0) {
       const long long at = out + base + wave * 32;
-      store_rows<DT>(a.rows + at * D, oacc, left, g, lane);
+      store_parts<DT>(a.rows + at * D, a.units + at, oacc, left, g, lane);
       if ((lane & 31) < left && g == 0) a.ml[at + (lane & 31)] = make_float2(m_run, l_run);
     }
   }
 }
 
 // A query's rows to its output, a half-wavefront each.  FORWARD: weighted by their maxima, divided by the sum; the others: added, times
-// 1 / sqrt(d), to dQ.
+// 1 / sqrt(d), to dQ.  A row is 16 bytes of 16 lanes (8 of width 64), so that two or four come at a time, and four times as many are in flight.
 template <int D, bool FORWARD>
 __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
-  constexpr int DT = D / 32;
-  typedef typename RowPart<DT>::V V;
+  constexpr int DT = D / 32, LANES = D / 8, PARTS = 32 / LANES;
+  typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
   __shared__ __attribute__((aligned(16))) float lds[8][D];
   const FusedArgs& f = a.f;
-  const int half = threadIdx.x >> 5, n = threadIdx.x & 31;
+  const int half = threadIdx.x >> 5, n = threadIdx.x & 31, part = n / LANES, c = n % LANES;
   const int mm = a.mat0 + blockIdx.y;
   const int t = blockIdx.x * 8 + half;
   const bool inside = t < f.s;
@@ -376,13 +376,15 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   const int* places = a.places + (m.vec + t) * a.count;
   // entries n and n + 32
   int place[2];
+  float weight[2];
   float2 ml[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     place[k] = inside && n + 32 * k < a.count ? places[n + 32 * k] : -1;
+    weight[k] = place[k] >= 0 ? a.units[rows + place[k]] : 0.f;
     if (FORWARD) ml[k] = place[k] >= 0 ? a.ml[rows + place[k]] : make_float2(-INFINITY, 0.f);
   }
-  float weight[2] = {1.0f, 1.0f}, total = 0.f, top = -INFINITY;
+  float total = 0.f, top = -INFINITY;
   if (FORWARD) {
     top = fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
@@ -390,8 +392,9 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
     const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      weight[k] = __builtin_amdgcn_exp2f((ml[k].x - from) * f.scale_log2);   // (of no pair: 0)
-      total += weight[k] * ml[k].y;
+      const float w = __builtin_amdgcn_exp2f((ml[k].x - from) * f.scale_log2);   // (of no pair: 0)
+      total += w * ml[k].y;
+      weight[k] *= w;
     }
 #pragma unroll
     for (int step = 1; step < 32; step <<= 1) total += __shfl_xor(total, step);
@@ -399,27 +402,40 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
     weight[0] *= inverse;
     weight[1] *= inverse;
   }
-  V sum;
+  float sum[8];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) sum[dt] = 0.f;
-#pragma unroll 4
-  for (int e = 0; e < a.count; ++e) {
-    const int p = __shfl(e < 32 ? place[0] : place[1], e & 31, 32);
-    const float w = __shfl(e < 32 ? weight[0] : weight[1], e & 31, 32);
-    if (p >= 0) {
-      const V x = *(const V*)(a.rows + (rows + p) * D + n * DT);
+  for (int k = 0; k < 8; ++k) sum[k] = 0.f;
+  for (int e0 = 0; e0 < a.count; e0 += 4 * PARTS) {
+    f16x8 x[4];
+    float w[4];
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) sum[dt] = FORWARD ? fmaf(w, x[dt], sum[dt]) : sum[dt] + x[dt];
+    for (int u = 0; u < 4; ++u) {
+      const int e = e0 + u * PARTS + part;
+      const int p0 = __shfl(place[0], e & 31, 32), p1 = __shfl(place[1], e & 31, 32);
+      const float w0 = __shfl(weight[0], e & 31, 32), w1 = __shfl(weight[1], e & 31, 32);
+      const int p = e < 32 ? p0 : e < 64 ? p1 : -1;
+      w[u] = e < 32 ? w0 : w1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[u][k] = 0;
+      if (p >= 0) x[u] = *(const f16x8*)(a.rows + (rows + p) * D + c * 8);
     }
-  }
-  if (FORWARD) {
-    write_row<DT>(f.attn + m.attn + (long long)t * f.ldo, sum, lds[half], n, inside);
-    if (inside && n == 0) f.lse[m.vec + t] = total > 0.f ? top * f.scale + __logf(total) : -INFINITY;
-  } else {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) sum[dt] *= f.scale;
-    write_row<DT>(f.d_qkv + m.qkv + (long long)t * f.ld, sum, lds[half], n, inside);
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum[k] = fmaf(w[u], (float)x[u][k], sum[k]);
   }
+#pragma unroll
+  for (int step = LANES; step < 32; step <<= 1)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] += __shfl_xor(sum[k], step);
+  if (part == 0) {   // numbers 8c .. of a row are [column % 32][column / 32]
+#pragma unroll
+    for (int k = 0; k < 8; ++k) lds[half][(8 * c + k) % DT * 32 + (8 * c + k) / DT] = FORWARD ? sum[k] : sum[k] * f.scale;
+  }
+  __builtin_amdgcn_wave_barrier();
+  bf16_t* to = FORWARD ? f.attn + m.attn + (long long)t * f.ldo : f.d_qkv + m.qkv + (long long)t * f.ld;
+  write_ordered<DT>(to, lds[half], n, inside);
+  if (FORWARD && inside && n == 0) f.lse[m.vec + t] = total > 0.f ? top * f.scale + __logf(total) : -INFINITY;
 }
 
 SelectedArgs make_args(const AttnSelectedDesc& b) {
@@ -464,7 +480,8 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
   if (!bwd) a.items[1] = nullptr;
   a.list = (int*)take(p.list);
   a.places = (int*)take(p.places);
-  a.rows = (float*)take(p.rows);
+  a.rows = (f16_t*)take(p.rows);
+  a.units = (float*)take(p.units);
   a.ml = (float2*)take(p.ml);
   a.key_rows = (float*)a.rows;   // (dK and dV come when the rows of dQ are done with)
   return a;
@@ -523,7 +540,7 @@ void attn_selected_plan(const AttnSelectedDesc& b, SelectedPlan* out) {
   p.seg[0] = 256;
   p.seg[1] = 1024;
   for (int k = 0; k < 2; ++k) p.most[k] = (int)(blocks + pairs / p.seg[k]);
-  const size_t row_bytes = pairs * (d.d * 4 + 8), key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
+  const size_t row_bytes = pairs * (d.d * 2 + 12), key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
   auto fit = [&](size_t bytes) { return (int)(kPortion / bytes < 1 ? 1 : kPortion / bytes > mats ? mats : kPortion / bytes); };
   p.portion = fit(row_bytes);
   p.key_portion = fit(key_bytes);
@@ -532,10 +549,11 @@ void attn_selected_plan(const AttnSelectedDesc& b, SelectedPlan* out) {
   p.first_item = round256(2 * mats * (blocks + 1) * 4);
   for (int k = 0; k < 2; ++k) p.items[k] = round256(mats * p.most[k] * 16);
   p.list = p.places = round256(mats * pairs * 4);
-  const size_t rows = p.portion * pairs * d.d * 4, keys = p.key_portion * key_bytes;
+  const size_t rows = p.portion * pairs * d.d * 2, keys = p.key_portion * key_bytes;
   p.rows = round256(rows > keys ? rows : keys);
+  p.units = round256(p.portion * pairs * 4);
   p.ml = round256(p.portion * pairs * 8);
-  p.total = p.delta + p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.ml;
+  p.total = p.delta + p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.units + p.ml;
   *out = p;
 }
 size_t attn_selected_ws_bytes(const AttnSelectedDesc& b) {

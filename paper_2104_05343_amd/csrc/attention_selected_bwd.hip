@@ -122,7 +122,10 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
       }
       if (!KT) wait_loads_and_barrier();
     }
-    if (left > 0) store_rows<DT>(a.rows + (out + base + wave * 32) * D, acc, left, g, lane);
+    if (left > 0) {
+      const long long at = out + base + wave * 32;
+      store_parts<DT>(a.rows + at * D, a.units + at, acc, left, g, lane);
+    }
   }
 }
 

@@ -23,6 +23,8 @@ constexpr int kMostBlocks = 1024, kMostCount = 64;
 constexpr int kMaskedBlocks = 256;     // most blocks of a sequence in the masked form
 constexpr int kQueries = 128;          // list rows of a tile
 
+typedef _Float16 f16_t;
+
 struct SelectedArgs {
   FusedArgs f;                         // f.attn, f.lse, f.d_attn, f.d_qkv, f.delta: first device of the launch
   const int* selected;                 // [matrix][s][count], first device of the launch
@@ -46,7 +48,8 @@ struct SelectedArgs {
   i32x4_t* items[2];                   // [matrix][most]: block, place of the first pair, pairs, -
   int* list;                           // [matrix][s * count]: query of every pair
   int* places;                         // [matrix][s][count]: place of the pair in list, -1: none
-  float* rows;                         // [matrix - mat0][s * count][d]: partial results, see store_rows
+  f16_t* rows;                         // [matrix - mat0][s * count][d]: partial results, see store_parts
+  float* units;                        // [matrix - mat0][s * count]: what a row's numbers are to be multiplied by
   float2* ml;                          // [matrix - mat0][s * count]: maximum of Q K^T, sum of exponentials
   float* key_rows;                     // [matrix - mat0][item][block / 64][dK, dV][64][d]
 };
@@ -57,7 +60,7 @@ struct SelectedPlan {
   int mats, chunks, mask_words;
   int portion, key_portion;            // matrices whose partial results are in memory at a time: of queries, of keys
   int seg[2], most[2];
-  size_t delta, mask, counts, offsets, first_item, items[2], list, places, rows, ml, total;
+  size_t delta, mask, counts, offsets, first_item, items[2], list, places, rows, units, ml, total;
 };
 
 // csrc/attention_selected*.hip
@@ -106,12 +109,88 @@ __device__ __forceinline__ void store_rows(float* to, const f32x16 (&acc)[DT], i
     if (row < left) *(V*)(to + row * (32 * DT) + (lane & 31) * DT) = v;
   }
 }
-// A half-wavefront's row of D numbers [n][dt] -> bf16 at `to`, columns in order, through LDS of its own.
+// A pair's partial result, rounded to fp16: a block's part of a query's output, or of its dQ, off by 2^-12 of itself, where the rounding of P
+// and dS to bf16 has left it off by some 2^-9; the sums over a block's keys and over the blocks stay fp32.  (8 (sequence, head)s of 32768 x 128,
+// 16 of 256 blocks: 2.2 GB of fp32 rows cost 300 us to write beside the products' 417, and 389 to read.)  Each row is scaled by a power of
+// two that brings its largest number to 2^14, so that nothing is lost to fp16's range but what is below 2^-28 of that.
+template <int DT> struct RowHalves;
+template <> struct RowHalves<4> { typedef __attribute__((ext_vector_type(4))) _Float16 V; };
+template <> struct RowHalves<2> { typedef __attribute__((ext_vector_type(2))) _Float16 V; };
+
+template <int CTRL>
+__device__ __forceinline__ float lane_moved(float x) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
+}
+// first: [a's row of 16 lanes 0, b's 0, a's 2, b's 2]; second: [a's 1, b's 1, a's 3, b's 3]
+__device__ __forceinline__ void swap_rows(float& a, float& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
 template <int DT>
-__device__ __forceinline__ void write_row(bf16_t* to, const typename RowPart<DT>::V v, float* lds, int n, bool write) {
+__device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x16 (&acc)[DT], int left, int g, int lane) {
+  typedef typename RowHalves<DT>::V V;
+  // largest of row r over 32 lanes, 16 rows at once: with every step a lane keeps half as many of them
+  float most[16];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) lds[dt * 32 + n] = v[dt];
-  __builtin_amdgcn_wave_barrier();
+  for (int r = 0; r < 16; ++r) {
+    most[r] = fabsf(acc[0][r]);
+#pragma unroll
+    for (int dt = 1; dt < DT; ++dt) most[r] = fmaxf(most[r], fabsf(acc[dt][r]));
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {   // rows r and r + 8: lanes 0 .. 15 keep the first
+    swap_rows(most[r], most[r + 8]);
+    most[r] = fmaxf(most[r], most[r + 8]);
+  }
+  const bool upper = lane & 8;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {   // rows r and r + 4: every other eight lanes
+    const float keep = upper ? most[r + 4] : most[r], give = upper ? most[r] : most[r + 4];
+    most[r] = fmaxf(keep, lane_moved<0x128>(give));
+    most[r] = fmaxf(most[r], lane_moved<0xB1>(most[r]));
+    most[r] = fmaxf(most[r], lane_moved<0x4E>(most[r]));
+    most[r] = fmaxf(most[r], lane_moved<0x141>(most[r]));
+  }
+  // a lane's four rows are r + 4 (lane / 8 % 4).  2^(141 - e) for a largest number of biased exponent e
+  float scale[16];
+  float4 unit;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int e = min(max((int)(__float_as_uint(most[r]) >> 23), 16), 254);
+    scale[r] = __uint_as_float((unsigned)(268 - e) << 23);
+    (&unit.x)[r] = __uint_as_float((unsigned)(e - 14) << 23);
+  }
+  const int first_row = 8 * (lane >> 3 & 3) + 4 * g;   // slot(r) + 4 g of them
+  if ((lane & 7) == 0) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (first_row + r < left) units[first_row + r] = (&unit.x)[r];
+  }
+  // and back to all lanes
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float other = lane_moved<0x128>(scale[r]);
+    scale[r + 4] = upper ? scale[r] : other;
+    scale[r] = upper ? other : scale[r];
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    scale[r + 8] = scale[r];
+    swap_rows(scale[r], scale[r + 8]);
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int row = slot(r) + 4 * g;
+    V v;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v[dt] = (f16_t)(acc[dt][r] * scale[r]);
+    if (row < left) *(V*)(to + row * (32 * DT) + (lane & 31) * DT) = v;
+  }
+}
+// A half-wavefront's row of D numbers in LDS, columns in order -> bf16 at `to`.
+template <int DT>
+__device__ __forceinline__ void write_ordered(bf16_t* to, const float* lds, int n, bool write) {
   if (DT == 4) {
     const float4 x = *(const float4*)(lds + 4 * n);
     if (write) *(u32x2*)(to + 4 * n) = u32x2{pack2_bf16(x.x, x.y), pack2_bf16(x.z, x.w)};
@@ -119,6 +198,14 @@ __device__ __forceinline__ void write_row(bf16_t* to, const typename RowPart<DT>
     const float2 x = *(const float2*)(lds + 2 * n);
     if (write) *(unsigned*)(to + 2 * n) = pack2_bf16(x.x, x.y);
   }
+}
+// The same from [n][dt] in registers, through LDS of its own.
+template <int DT>
+__device__ __forceinline__ void write_row(bf16_t* to, const typename RowPart<DT>::V v, float* lds, int n, bool write) {
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) lds[dt * 32 + n] = v[dt];
+  __builtin_amdgcn_wave_barrier();
+  write_ordered<DT>(to, lds, n, write);
   __builtin_amdgcn_wave_barrier();
 }
 

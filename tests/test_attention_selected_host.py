@@ -113,10 +113,10 @@ def test_workspace():
     assert 4 * 200 * 4 <= one < all_of
     assert size(3, 200, 256, 4, 2, 0, 1) == size(4, 200, 320, 4, 2, 0, 1) == size(4, 200, 256, 4, 2, 0, 2) == 0
     assert size(4, 200, 256, 4, 2, 0, 1, sel=opt.make_selection(63, 3)) == 0
-    assert size(4, 5000, 256, 4, 2, 0, 1) >= 4 * 5000 * 3 * (64 + 2) * 4                # lists: partial results of all pairs
+    assert size(4, 5000, 256, 4, 2, 0, 1) >= 4 * 5000 * 3 * (64 * 2 + 12)                # lists: partial results of all pairs
     # of one (sequence, head) where 384 MiB do not hold them, not of all of them
     long = size(1, 1 << 18, 1024, 8, 1, 0, 0, sel=opt.make_selection(256, 16))
-    assert long < 2 * (1 << 18) * 16 * (128 + 2) * 4
+    assert (1 << 18) * 16 * (128 * 2 + 12) <= long < 2 * (1 << 18) * 16 * (128 * 2 + 12)
 
 
 def test_form():

@@ -12,6 +12,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 HALF = 2.0 ** -8     # a rounding to bf16, relative
 FP32 = 2e-5          # relative error of P: fp32 sums of 64 to 128 products, scores below 30 in units of log2
+PART = 2.0 ** -12    # with lists, a block's part of an output or of dQ is rounded to fp16
 
 
 class Run:
@@ -95,11 +96,11 @@ class Run:
                 some = ~empty_rows
                 assert np.all(np.abs(gl[some] - lse[some]) <= 1e-5 * np.maximum(1, np.abs(lse[some])))
                 # P rounded, V exact, the output rounded
-                assert np.all(np.abs(got - want) <= HALF * (1.01 * np.abs(want) + P @ np.abs(V)) + FP32 * (P @ np.abs(V)) + 1e-30), (seq, head)
+                assert np.all(np.abs(got - want) <= HALF * (1.01 * np.abs(want) + P @ np.abs(V)) + (FP32 + PART) * (P @ np.abs(V)) + 1e-30), (seq, head)
                 dQ, dK, dV, P, dS = oas.backward(Q, K, V, dO, got, gl.astype(np.float64), see)
                 spread = P * (np.abs(dO) @ np.abs(V).T + (np.abs(dO) * np.abs(got)).sum(1, keepdims=True))   # what dS is a difference of
                 raw, fine = np.abs(dS), FP32 * spread
-                for k, (w, size, small) in enumerate(((dQ, raw @ np.abs(K) / np.sqrt(d), fine @ np.abs(K) / np.sqrt(d)),
+                for k, (w, size, small) in enumerate(((dQ, raw @ np.abs(K) / np.sqrt(d), (fine + PART * raw) @ np.abs(K) / np.sqrt(d)),
                                                       (dK, raw.T @ np.abs(Q) / np.sqrt(d), fine.T @ np.abs(Q) / np.sqrt(d)),
                                                       (dV, P.T @ np.abs(dO), FP32 * P.T @ np.abs(dO)))):
                     g = G[rows, (3 * head + k) * d:(3 * head + k + 1) * d]
@@ -221,7 +222,7 @@ def test_scores_of_any_size(scale):
     off = 128 * 2.0 ** -24 * (np.abs(Q) @ np.abs(K).T / np.sqrt(128)).max(1, keepdims=True)
     L = to_host(r.L).astype(np.float64)
     assert np.all(np.abs(L - lse) <= 1e-5 * np.maximum(1, np.abs(lse)) + off[:, 0])
-    bound = HALF * (1.01 * np.abs(want) + P @ np.abs(V)) + (FP32 + 2 * np.expm1(np.minimum(2 * off, 1))) * np.abs(V).max()
+    bound = HALF * (1.01 * np.abs(want) + P @ np.abs(V)) + (FP32 + PART + 2 * np.expm1(np.minimum(2 * off, 1))) * np.abs(V).max()
     assert np.all(np.abs(mat_to_host(r.O, 600, 128, 1) - want) <= bound)
 
 
@@ -317,11 +318,11 @@ def test_a_long_sequence():
         p = np.exp(x - x.max())
         lse, p = x.max() + np.log(p.sum()), p / p.sum()
         assert abs(L[t] - lse) <= 1e-5 * max(1, abs(lse))
-        assert np.all(np.abs(O[t] - p @ V[keys]) <= HALF * (1.01 * np.abs(p @ V[keys]) + p @ np.abs(V[keys])) + FP32 * (p @ np.abs(V[keys])))
+        assert np.all(np.abs(O[t] - p @ V[keys]) <= HALF * (1.01 * np.abs(p @ V[keys]) + p @ np.abs(V[keys])) + (FP32 + PART) * (p @ np.abs(V[keys])))
         ds = p * (V[keys] @ dO[t] - (dO[t] * O[t]).sum())
         want, size = ds @ K[keys] / 8, np.abs(ds) @ np.abs(K[keys]) / 8
         # (dS is a difference: its fp32 error is one of the two terms', which are of the size of sqrt(d) values)
-        assert np.all(np.abs(G[t, :d] - want) <= HALF * (1.01 * np.abs(want) + size) + 100 * FP32)
+        assert np.all(np.abs(G[t, :d] - want) <= HALF * (1.01 * np.abs(want) + size) + PART * size + 100 * FP32)
     for u in [0, 200, 40000, s - 1]:
         rows = np.nonzero((chosen == u // 128).any(1) & (np.arange(s) >= u))[0]
         p = np.exp(Q[rows] @ K[u] / 8 - L[rows])

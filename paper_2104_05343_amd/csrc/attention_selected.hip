@@ -153,6 +153,12 @@ __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
 }
 
 // ---------------------------------------------------------------- forward
+// maxima and sums of a wavefront's 32 rows, `rows` of them (see store_parts)
+__device__ __forceinline__ void store_ml(float2* to, float m, float l, int rows, int g, int lane) {
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(to, 0, __builtin_amdgcn_readfirstlane(rows) * 8, 0x00020000);
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(l)}, rsrc, g == 0 ? lane * 8 : 0x7fffffff, 0, 0);
+}
+
 // A wavefront has 32 queries of a tile of 128.  KT > 0: the block is at most 32 KT = 64 or 128 keys, stays in LDS for all of the workgroup's
 // queries, and a row's scores are all there before the maximum is taken: no barrier behind the loads, no rescaling.  The next tile's
 // queries are requested as soon as the products of this one have read theirs.
@@ -198,7 +204,6 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
                                 sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
                               });
     const int limit = a.causal ? min(t, last) : last;
-    const bool mine = base + row < it.pairs;
     if (base + kQueries + wave * 32 < it.pairs) {
       t = list[min(base + kQueries + row, it.pairs - 1)];
       load_queries(t);
@@ -240,8 +245,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
                                     oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf[k / 2][k & 1], x, oacc[n % DT], 0, 0, 0);
                                   });
     const long long at = out + base + wave * 32;
-    store_parts<DT>(a.rows + at * D, a.units + at, oacc, it.pairs - base - wave * 32, g, lane);
-    if (mine && g == 0) a.ml[at + (lane & 31)] = make_float2(mx, sum);
+    const int left = min(it.pairs - base - wave * 32, 32);
+    store_parts<DT>(a.rows + at * D, a.units + at, oacc, left, g, lane);
+    store_ml(a.ml + at, mx, sum, left, g, lane);
   }
 }
 
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
   wait_loads_and_barrier();
   int stage = 0;
   for (int round = 0; round < rounds; ++round) {
-    const int base = round * kQueries, left = it.pairs - base - wave * 32;   // (at most 0: the wavefront only keeps the barriers)
+    const int base = round * kQueries, left = min(it.pairs - base - wave * 32, 32);   // (at most 0: the wavefront only keeps the barriers)
     const int t = list[min(base + row, it.pairs - 1)];
     const int limit = a.causal ? min(t, last) : last;
     bf16x8 qf[KS];
@@ -354,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
     if (left > 0) {
       const long long at = out + base + wave * 32;
       store_parts<DT>(a.rows + at * D, a.units + at, oacc, left, g, lane);
-      if ((lane & 31) < left && g == 0) a.ml[at + (lane & 31)] = make_float2(m_run, l_run);
+      store_ml(a.ml + at, m_run, l_run, left, g, lane);
     }
   }
 }
@@ -379,8 +385,23 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   float weight[2];
   float2 ml[2];
 #pragma unroll
+  for (int k = 0; k < 2; ++k) place[k] = inside && n + 32 * k < a.count ? places[n + 32 * k] : -1;
+  // rows of entries e0 .. e0 + 4 PARTS - 1; the first ones are on their way while the weights are computed
+  f16x8 x[4];
+  auto load_rows = [&](int e0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int e = e0 + u * PARTS + part;
+      const int p0 = __shfl(place[0], e & 31, 32), p1 = __shfl(place[1], e & 31, 32);
+      const int p = e < 32 ? p0 : e < 64 ? p1 : -1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[u][k] = 0;
+      if (p >= 0) x[u] = *(const f16x8*)(a.rows + (rows + p) * D + c * 8);
+    }
+  };
+  load_rows(0);
+#pragma unroll
   for (int k = 0; k < 2; ++k) {
-    place[k] = inside && n + 32 * k < a.count ? places[n + 32 * k] : -1;
     weight[k] = place[k] >= 0 ? a.units[rows + place[k]] : 0.f;
     if (FORWARD) ml[k] = place[k] >= 0 ? a.ml[rows + place[k]] : make_float2(-INFINITY, 0.f);
   }
@@ -406,23 +427,15 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) sum[k] = 0.f;
   for (int e0 = 0; e0 < a.count; e0 += 4 * PARTS) {
-    f16x8 x[4];
-    float w[4];
+    if (e0 > 0) load_rows(e0);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int e = e0 + u * PARTS + part;
-      const int p0 = __shfl(place[0], e & 31, 32), p1 = __shfl(place[1], e & 31, 32);
       const float w0 = __shfl(weight[0], e & 31, 32), w1 = __shfl(weight[1], e & 31, 32);
-      const int p = e < 32 ? p0 : e < 64 ? p1 : -1;
-      w[u] = e < 32 ? w0 : w1;
+      const float w = e < 32 ? w0 : w1;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[u][k] = 0;
-      if (p >= 0) x[u] = *(const f16x8*)(a.rows + (rows + p) * D + c * 8);
+      for (int k = 0; k < 8; ++k) sum[k] = fmaf(w, (float)x[u][k], sum[k]);
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sum[k] = fmaf(w[u], (float)x[u][k], sum[k]);
   }
 #pragma unroll
   for (int step = LANES; step < 32; step <<= 1)

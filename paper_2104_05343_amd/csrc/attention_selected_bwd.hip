@@ -99,7 +99,6 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
   for (int round = 0; round < rounds; ++round) {
     const int base = round * kQueries, left = it.pairs - base - wave * 32;
     if (KT && left <= 0) break;
-    if (round > 0) load_queries(base);
     const int limit = a.causal ? min(t, last) : last;
     f32x16 acc[DT];
 #pragma unroll
@@ -122,9 +121,10 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
       }
       if (!KT) wait_loads_and_barrier();
     }
+    if (base + kQueries + (KT ? wave * 32 : 0) < it.pairs) load_queries(base + kQueries);
     if (left > 0) {
       const long long at = out + base + wave * 32;
-      store_parts<DT>(a.rows + at * D, a.units + at, acc, left, g, lane);
+      store_parts<DT>(a.rows + at * D, a.units + at, acc, min(left, 32), g, lane);
     }
   }
 }

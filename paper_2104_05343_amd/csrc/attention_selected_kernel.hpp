@@ -128,7 +128,8 @@ __device__ __forceinline__ void swap_rows(float& a, float& b) {
   b = __uint_as_float(r[1]);
 }
 template <int DT>
-__device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x16 (&acc)[DT], int left, int g, int lane) {
+__device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x16 (&acc)[DT], int rows, int g, int lane) {
+  const int left = __builtin_amdgcn_readfirstlane(rows);
   typedef typename RowHalves<DT>::V V;
   // largest of row r over 32 lanes, 16 rows at once: with every step a lane keeps half as many of them
   float most[16];
@@ -162,11 +163,13 @@ __device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x1
     (&unit.x)[r] = __uint_as_float((unsigned)(e - 14) << 23);
   }
   const int first_row = 8 * (lane >> 3 & 3) + 4 * g;   // slot(r) + 4 g of them
-  if ((lane & 7) == 0) {
+  // Through buffer resources that end behind the last row: a store under a condition would have the wait for the next tile's queries, which are
+  // requested ahead of it, wait for the stores too.
+  const auto to_units = __builtin_amdgcn_make_buffer_rsrc(units, 0, left * 4, 0x00020000);
+  const auto to_rows = __builtin_amdgcn_make_buffer_rsrc(to, 0, left * (64 * DT), 0x00020000);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (first_row + r < left) units[first_row + r] = (&unit.x)[r];
-  }
+  for (int r = 0; r < 4; ++r)
+    __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint((&unit.x)[r]), to_units, (lane & 7) == 0 ? (first_row + r) * 4 : 0x7fffffff, 0, 0);
   // and back to all lanes
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -185,7 +188,9 @@ __device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x1
     V v;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) v[dt] = (f16_t)(acc[dt][r] * scale[r]);
-    if (row < left) *(V*)(to + row * (32 * DT) + (lane & 31) * DT) = v;
+    const int at = row * (64 * DT) + (lane & 31) * (2 * DT);
+    if constexpr (DT == 4) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), to_rows, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, v), to_rows, at, 0, 0);
   }
 }
 // A half-wavefront's row of D numbers in LDS, columns in order -> bf16 at `to`.

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
         *(float4*)(scores + (lane & 31) * stride + v0 + 8 * c + 4 * g) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
     }
   }
-  for (int k = tid; k < 2 * kRows * words; k += 256) bits[k] = 0;
+  for (int k = tid; k < kRows * words; k += 256) contested[k] = 0;
   // E of the row: a query's size by its eight lanes, the largest mean by the workgroup
   float mean_size = 0.f, q_size = 0.f;
   for (int v = tid; v < others; v += 256) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
@@ -216,36 +216,70 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
       found = n == K;
     }
   }
-  // scores certainly chosen are above the K-th, which is the least from `cut` on (or in [lo, hi) where no threshold divides them)
-  float least = INFINITY;
+  // The K-th score is the least from `cut` on.  Where K are from there on, and the next one is further away than both can be off together,
+  // they are the choice.
+  float least = INFINITY, next = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) least = x[k] >= cut ? fminf(least, x[k]) : least;
+  for (int p = 0; p < NV; p += PART)
+    if (8 * p < others) {
+#pragma unroll
+      for (int k = p; k < p + PART; ++k) {
+        least = x[k] >= cut ? fminf(least, x[k]) : least;
+        next = x[k] >= cut ? next : fmaxf(next, x[k]);
+      }
+    }
   least = min8(least);
-  const int n_cut = at_least(cut);
-  float above = (n_cut == K ? least : hi) + 2.0f * error, below = least - 2.0f * error;
-  if (wild) {
-    above = INFINITY;
-    below = -INFINITY;
-  }
-  int n_above = 0, n_below = 0;   // scores from `below` on
+  next = max8(next);
+  const bool separated = found && !wild;
+  bool decided = separated && least - next > 2.0f * error;
+  float above = (separated ? least : hi) + 2.0f * error, below = least - 2.0f * error;
+  int n_above = 0;
+  if (__builtin_amdgcn_ballot_w64(query && !decided) != 0) {
+    // Else what is above the K-th (or `hi`, where no threshold divides the scores) by twice the error is chosen, what is as far below the least
+    // is not, and as many of the scores between as there are places left.
+    if (wild) {
+      above = INFINITY;
+      below = -INFINITY;
+    }
+    int n_below = 0;   // scores from `below` on
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = e + 8 * k;
-    const bool candidate = v < others && v != own;
-    n_above += candidate && x[k] > above ? 1 : 0;
-    n_below += candidate && !(x[k] < below) ? 1 : 0;
-  }
-  n_above = wild ? 0 : sum8(n_above);
-  n_below = sum8(n_below);
-  const bool decided = n_below == K;
-  // the bits of what is chosen, and of what is left to the exact scores
+    for (int k = 0; k < NV; ++k) {
+      const int v = e + 8 * k;
+      const bool candidate = v < others && v != own;
+      n_above += candidate && x[k] > above ? 1 : 0;
+      n_below += candidate && !(x[k] < below) ? 1 : 0;
+    }
+    n_above = wild ? 0 : sum8(n_above);
+    n_below = sum8(n_below);
+    if (!decided && n_below == K) {
+      decided = true;
+      cut = below;
+    }
+    const bool open = query && !decided;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = e + 8 * k;
-    if (query && v < others && v != own && !(x[k] < below))
-      atomicOr(&(decided || (!wild && x[k] > above) ? bits : contested)[row * words + (v >> 5)], 1u << (v & 31));
+    for (int k = 0; k < NV; ++k) {   // the bits of what is left to the exact scores
+      const int v = e + 8 * k;
+      if (open && v < others && v != own && !(x[k] < below) && (wild || !(x[k] > above))) atomicOr(&contested[row * words + (v >> 5)], 1u << (v & 31));
+    }
   }
-  if (query && e == 0) atomicOr(&bits[row * words + (own >> 5)], 1u << (own & 31));
+  // The bits of what is chosen so far: a comparison's 64 lanes are eight blocks of each of eight queries.
+  {
+    const float from = !query ? INFINITY : decided ? cut : above;   // (scores are finite here, or none is taken)
+    const bool over = !decided || wild;                             // beyond `above`, not from it on
+    unsigned word = 0;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      if (8 * (k & ~7) < others) {
+        const unsigned long long take = __builtin_amdgcn_ballot_w64(over ? x[k] > from : x[k] >= from);
+        word |= ((unsigned)(take >> (lane & 56)) & 0xffu) << (8 * (k & 3));
+      }
+      if ((k & 3) == 3) {
+        if (own >> 5 == k >> 2 && query) word |= 1u << (own & 31);
+        if (e == 0 && (k >> 2) < words) bits[row * words + (k >> 2)] = word;
+        word = 0;
+      }
+    }
+  }
   __builtin_amdgcn_wave_barrier();
   if (__builtin_amdgcn_ballot_w64(query && !decided) != 0) {
     // exact scores, in the order of the blocks, the best ones kept: one that is not above the worst kept is out (equal: the lower block stays)
@@ -348,7 +382,8 @@ void select_launch(const SelectedArgs& a, int mats, hipStream_t st) {
 }
 template <int D>
 void choose(const SelectedArgs& a, int mats, hipStream_t st) {
-  block_means_kernel<D><<<dim3((a.blocks + 3) / 4, mats), 256, 0, st>>>(a);
+  // (every block is chosen, or the own one alone: no scores)
+  if (a.count > 1 && a.count < a.blocks) block_means_kernel<D><<<dim3((a.blocks + 3) / 4, mats), 256, 0, st>>>(a);
   if (a.blocks <= 32) select_launch<D, 4>(a, mats, st);
   else if (a.blocks <= 64) select_launch<D, 8>(a, mats, st);
   else if (a.blocks <= 128) select_launch<D, 16>(a, mats, st);

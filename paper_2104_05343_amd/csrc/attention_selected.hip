@@ -161,7 +161,7 @@ __device__ __forceinline__ void store_ml(float2* to, float m, float l, int rows,
 
 // A wavefront has 32 queries of a tile of 128.  KT > 0: the block is at most 32 KT = 64 or 128 keys, stays in LDS for all of the workgroup's
 // queries, and a row's scores are all there before the maximum is taken: no barrier behind the loads, no rescaling.  The next tile's
-// queries are requested as soon as the products of this one have read theirs.
+// queries are requested as soon as the products of this one have read theirs, and ahead of its stores: the wait for them is no wait for stores.
 template <int D, int KT>
 __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
   constexpr int KS = D / 16, DT = D / 32, STEPS = KT / 2, AHEAD = 2;
@@ -185,8 +185,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
   const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
   const int* list = a.list + first;
-  int row = wave * 32 + (lane & 31);
-  int t = list[min(row, it.pairs - 1)];
+  // a tile's queries are requested a tile ahead, their numbers two, and past the end too: the last one again
+  const int row = wave * 32 + (lane & 31);
+  int t = list[min(row, it.pairs - 1)], t_next = list[min(row + kQueries, it.pairs - 1)];
   bf16x8 qf[KS];
   auto load_queries = [&](int q) {
     const bf16_t* p = Qp + (long long)q * f.ld + g * 8;
@@ -204,10 +205,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
                                 sacc[n / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n % KS], sacc[n / KS], 0, 0, 0);
                               });
     const int limit = a.causal ? min(t, last) : last;
-    if (base + kQueries + wave * 32 < it.pairs) {
-      t = list[min(base + kQueries + row, it.pairs - 1)];
-      load_queries(t);
-    }
+    t = t_next;
+    load_queries(t);
+    t_next = list[min(base + 2 * kQueries + row, it.pairs - 1)];
     if (__builtin_amdgcn_ballot_w64(limit < key0 + 32 * KT - 1) != 0) {
       const int reach = limit - key0 - 4 * g;
 #pragma unroll

@@ -79,10 +79,11 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
   const int* list = a.list + first;
   const int row = wave * 32 + (lane & 31);
   bf16x8 qf[KS], dof[KS];
-  int t = 0;
-  float lse2 = 0.f, delta = 0.f;
+  // a tile's queries are requested a tile ahead, their numbers two, and past the end too: the last one again
+  int t = 0, t_next = list[min(row, it.pairs - 1)];
+  float lse = 0.f, delta = 0.f;
   auto load_queries = [&](int base) {
-    t = list[min(base + row, it.pairs - 1)];
+    t = t_next;
     const bf16_t* q = Qp + (long long)t * f.ld + g * 8;
     const bf16_t* o = Gp + (long long)t * f.ldo + g * 8;
 #pragma unroll
@@ -90,8 +91,9 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
       qf[ks] = *(const bf16x8*)(q + ks * 16);
       dof[ks] = *(const bf16x8*)(o + ks * 16);
     }
-    lse2 = lse2_of(f.lse[m.vec + t]);
+    lse = f.lse[m.vec + t];
     delta = f.delta[m.vec + t];
+    t_next = list[min(base + kQueries + row, it.pairs - 1)];
   };
   load_queries(0);
   wait_loads_and_barrier();
@@ -100,6 +102,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
     const int base = round * kQueries, left = it.pairs - base - wave * 32;
     if (KT && left <= 0) break;
     const int limit = a.causal ? min(t, last) : last;
+    const float lse2 = lse2_of(lse);
     f32x16 acc[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
       }
       if (!KT) wait_loads_and_barrier();
     }
-    if (base + kQueries + (KT ? wave * 32 : 0) < it.pairs) load_queries(base + kQueries);
+    load_queries(base + kQueries);
     if (left > 0) {
       const long long at = out + base + wave * 32;
       store_parts<DT>(a.rows + at * D, a.units + at, acc, min(left, 32), g, lane);

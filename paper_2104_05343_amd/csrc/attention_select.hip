@@ -72,6 +72,8 @@ __device__ __forceinline__ double moved(double x) {
   const unsigned lo = (unsigned)moved<CTRL>((int)b), hi = (unsigned)moved<CTRL>((int)(b >> 32));
   return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
+template <int CTRL>
+__device__ __forceinline__ unsigned moved(unsigned x) { return (unsigned)moved<CTRL>((int)x); }
 template <class T, class F>
 __device__ __forceinline__ T eight(T x, F f) {
   x = f(x, moved<0xB1>(x));
@@ -84,17 +86,18 @@ __device__ __forceinline__ float max8(float x) { return eight(x, [](float p, flo
 
 constexpr int kRows = 32;             // queries of a workgroup
 
-// LDS: kept scores [kRows][kept], scores [kRows][stride], bits of chosen and of contested blocks [kRows][words], kept blocks [kRows][kept]
-__host__ __device__ inline int score_stride(int blocks) { return (blocks + 31) / 32 * 32 + 4; }
+// LDS: kept scores [kRows][kept], scores [kRows][stride], bits of chosen and of contested blocks [kRows][words], largest mean of each
+// wavefront's blocks [4], rows with scores that are not finite, kept blocks [kRows][kept]
+__host__ __device__ inline int score_stride(int blocks) { return (blocks + 63) / 64 * 64 + 4; }
 __host__ __device__ inline int bit_words(int blocks) { return (blocks + 31) / 32; }
 inline size_t select_lds(int blocks, int count) {
-  return (size_t)kRows * (score_stride(blocks) * 4 + bit_words(blocks) * 8 + count * 10) + 16;
+  return (size_t)kRows * (score_stride(blocks) * 4 + bit_words(blocks) * 8 + count * 10) + 32;
 }
 
-// NV: scores of a lane; 8 NV blocks at most.
+// NV: scores of a lane, 4 of every 32 blocks; 8 NV blocks at most.
 template <int D, int NV>
 __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
-  constexpr int KS = D / 16;
+  constexpr int KS = D / 16, PART = NV < 8 ? NV : 8;   // (loops over the scores go in parts of 64 blocks, of which the front of a sequence has few)
   extern __shared__ __attribute__((aligned(16))) char dynamic[];
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
@@ -110,8 +113,9 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
   float* scores = (float*)(kept + kRows * a.count);
   unsigned* bits = (unsigned*)(scores + kRows * stride);
   unsigned* contested = bits + kRows * words;
-  float* sizes = (float*)(contested + kRows * words);                  // largest mean of each wavefront's blocks
-  unsigned short* kept_block = (unsigned short*)(sizes + 4);
+  float* sizes = (float*)(contested + kRows * words);
+  unsigned* wild_rows = (unsigned*)(sizes + 4);
+  unsigned short* kept_block = (unsigned short*)(wild_rows + 4);
   const int row = tid >> 3, e = tid & 7, t = q0 + row;   // eight lanes a query
   int* out = a.chosen + (m.vec + t) * a.count;
   const bool query = t < m.len;
@@ -123,98 +127,107 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
     }
     return;
   }
-  // scores: 32 blocks a wavefront at a time
+  for (int k = tid; k < kRows * words; k += 256) contested[k] = 0;
+  if (tid == 0) *wild_rows = 0;
+  const bf16_t* Q = f.qkv + m.qkv + (long long)min(t, m.len - 1) * f.ld + e * (D / 8);
+  u32x4 qw[D / 64];
+#pragma unroll
+  for (int k = 0; k < D / 64; ++k) qw[k] = *(const u32x4*)(Q + 8 * k);
+  __syncthreads();
+  // Scores, 32 blocks a wavefront at a time; of no candidate: NaN, which is neither above nor below a threshold, largest nor least.
   {
     const int qrow = min(q0 + (lane & 31), m.len - 1);
-    const bf16_t* Q = f.qkv + m.qkv + (long long)qrow * f.ld + g * 8;
+    const bf16_t* P = f.qkv + m.qkv + (long long)qrow * f.ld + g * 8;
     bf16x8 qf[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(Q + ks * 16);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(P + ks * 16);
     const bf16_t* means = a.means + (long long)mm * a.blocks * D;
-    for (int v0 = wave * 32; v0 < others; v0 += 128) {
+    const int end = (others + 8 * PART - 1) / (8 * PART) * (8 * PART);
+    for (int v0 = wave * 32; v0 < end; v0 += 128) {
       const bf16_t* p = means + (long long)min(v0 + (lane & 31), others - 1) * D + g * 8;
       f32x16 acc = zero16();
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(p + ks * 16), qf[ks], acc, 0, 0, 0);
+      float zero = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) zero = fmaf(acc[r], 0.f, zero);   // (an infinity or NaN: NaN)
+      if (!(zero == 0.f)) atomicOr(wild_rows, 1u << (lane & 31));
+      if (v0 + 32 > others || (own >= v0 && own < v0 + 32)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int v = v0 + slot(r) + 4 * g;
+          acc[r] = v < others && v != own ? acc[r] : NAN;
+        }
+      }
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         *(float4*)(scores + (lane & 31) * stride + v0 + 8 * c + 4 * g) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
     }
   }
-  for (int k = tid; k < kRows * words; k += 256) contested[k] = 0;
   // E of the row: a query's size by its eight lanes, the largest mean by the workgroup
   float mean_size = 0.f, q_size = 0.f;
   for (int v = tid; v < others; v += 256) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
 #pragma unroll
   for (int step = 1; step < 64; step <<= 1) mean_size = fmaxf(mean_size, __shfl_xor(mean_size, step));
   if (lane == 0) sizes[wave] = mean_size;
-  const bf16_t* Q = f.qkv + m.qkv + (long long)min(t, m.len - 1) * f.ld + e * (D / 8);
   float q[D / 8];
 #pragma unroll
-  for (int k = 0; k < D / 64; ++k) {
-    const u32x4 w = *(const u32x4*)(Q + 8 * k);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      q[8 * k + 2 * j] = __uint_as_float(w[j] << 16);
-      q[8 * k + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    }
+  for (int k = 0; k < D / 8; ++k) {
+    const unsigned w = qw[k / 8][k / 2 % 4];
+    q[k] = __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16);
+    q_size = fmaf(q[k], q[k], q_size);
   }
-#pragma unroll
-  for (int k = 0; k < D / 8; ++k) q_size = fmaf(q[k], q[k], q_size);
   q_size = sqrtf(eight(q_size, [](float p, float q) { return p + q; })) * 1.0001f;
   __syncthreads();
   mean_size = fmaxf(fmaxf(sizes[0], sizes[1]), fmaxf(sizes[2], sizes[3]));
-  float error = q_size * mean_size * (D * 1.1920929e-7f);
-  const float* mine = scores + row * stride;
-  // a lane's scores: of blocks e, e + 8, ..; -infinity: no candidate.  wild: a score or the bound is not finite, or too small for the bound
+  const float error = q_size * mean_size * (D * 1.1920929e-7f);
+  // wild: a score or the bound is not finite, or too small for the bound: all scores are computed again
+  const bool wild = !(error < 1e30f) || error < 1e-30f || q_size < 1e-25f || mean_size < 1e-25f || (*wild_rows >> row & 1);
+  // a lane's scores: of blocks 4 e + j of every 32
+  const float* mine = scores + row * stride + 4 * e;
   float x[NV];
   float lo = INFINITY, hi = -INFINITY;
-  bool wild = !(error < 1e30f) || error < 1e-30f || q_size < 1e-25f || mean_size < 1e-25f;
-  // (the loops over them in parts of 64 blocks, of which a workgroup in the front of its sequence has few)
-  constexpr int PART = NV < 8 ? NV : 8;
 #pragma unroll
   for (int p = 0; p < NV; p += PART) {
-    const bool some = 8 * p < others;
+    if (8 * p < others) {
 #pragma unroll
-    for (int k = p; k < p + PART; ++k) x[k] = -INFINITY;
-    if (some) {
+      for (int k = p; k < p + PART; k += 4) {
+        const float4 y = *(const float4*)(mine + 8 * k);
+        x[k] = y.x;
+        x[k + 1] = y.y;
+        x[k + 2] = y.z;
+        x[k + 3] = y.w;
+      }
 #pragma unroll
       for (int k = p; k < p + PART; ++k) {
-        const int v = e + 8 * k;
-        const bool candidate = v < others && v != own;
-        x[k] = candidate ? mine[v] : -INFINITY;
-        wild = wild || (candidate && !(fabsf(x[k]) < 1e30f));
-        lo = candidate ? fminf(lo, x[k]) : lo;
+        lo = fminf(lo, x[k]);
         hi = fmaxf(hi, x[k]);
       }
+    } else {
+#pragma unroll
+      for (int k = p; k < p + PART; ++k) x[k] = NAN;
     }
   }
-  auto at_least = [&](float from) {   // scores from `from` on, of the row
-    int n = 0;
-#pragma unroll
-    for (int p = 0; p < NV; p += PART)
-      if (8 * p < others) {
-#pragma unroll
-        for (int k = p; k < p + PART; ++k) n += x[k] >= from ? 1 : 0;
-      }
-    return sum8(n);
-  };
   lo = min8(lo);
   hi = max8(hi);
-  wild = sum8(wild) != 0;
-  // a threshold with K scores from it on: halving [lo, hi), at lo at least K are (all), at hi fewer (a step above the largest)
+  // a threshold with K scores from it on: halving [lo, hi), from lo on at least K are (all), from hi fewer (a step above the largest)
   float cut = lo;
   bool found = wild || !query;
   hi += fabsf(hi) * 1e-6f + 1e-37f;
   for (int round = 0; round < 40 && __builtin_amdgcn_ballot_w64(!found) != 0; ++round) {
     const float middle = 0.5f * lo + 0.5f * hi;
-    const int n = at_least(middle);
-    if (!found) {
-      if (n >= K) lo = middle;
-      else hi = middle;
-      cut = lo;
-      found = n == K;
-    }
+    int n = 0;
+#pragma unroll
+    for (int p = 0; p < NV; p += PART)
+      if (8 * p < others) {
+#pragma unroll
+        for (int k = p; k < p + PART; ++k) n += x[k] >= middle ? 1 : 0;
+      }
+    n = sum8(n);
+    lo = !found && n >= K ? middle : lo;
+    hi = !found && n < K ? middle : hi;
+    cut = found ? cut : lo;
+    found = found || n == K;
   }
   // The K-th score is the least from `cut` on.  Where K are from there on, and the next one is further away than both can be off together,
   // they are the choice.
@@ -224,8 +237,8 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
     if (8 * p < others) {
 #pragma unroll
       for (int k = p; k < p + PART; ++k) {
-        least = x[k] >= cut ? fminf(least, x[k]) : least;
-        next = x[k] >= cut ? next : fmaxf(next, x[k]);
+        least = fminf(least, x[k] >= cut ? x[k] : INFINITY);
+        next = fmaxf(next, x[k] >= cut ? -INFINITY : x[k]);
       }
     }
   least = min8(least);
@@ -244,7 +257,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
     int n_below = 0;   // scores from `below` on
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int v = e + 8 * k;
+      const int v = 32 * (k >> 2) + 4 * e + (k & 3);
       const bool candidate = v < others && v != own;
       n_above += candidate && x[k] > above ? 1 : 0;
       n_below += candidate && !(x[k] < below) ? 1 : 0;
@@ -258,26 +271,29 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
     const bool open = query && !decided;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {   // the bits of what is left to the exact scores
-      const int v = e + 8 * k;
+      const int v = 32 * (k >> 2) + 4 * e + (k & 3);
       if (open && v < others && v != own && !(x[k] < below) && (wild || !(x[k] > above))) atomicOr(&contested[row * words + (v >> 5)], 1u << (v & 31));
     }
   }
-  // The bits of what is chosen so far: a comparison's 64 lanes are eight blocks of each of eight queries.
+  // The bits of what is chosen so far, from a threshold on (decided) or above one: four of a word each lane.
   {
-    const float from = !query ? INFINITY : decided ? cut : above;   // (scores are finite here, or none is taken)
-    const bool over = !decided || wild;                             // beyond `above`, not from it on
-    unsigned word = 0;
+    const float from = !query || wild ? NAN : decided ? cut : above;   // (NaN: none)
+    const bool over = !decided;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (8 * (k & ~7) < others) {
-        const unsigned long long take = __builtin_amdgcn_ballot_w64(over ? x[k] > from : x[k] >= from);
-        word |= ((unsigned)(take >> (lane & 56)) & 0xffu) << (8 * (k & 3));
+    for (int w = 0; w < NV / 4; ++w) {
+      unsigned word = 0;
+      if (32 * w < others) {
+#pragma unroll
+        for (int j = 3; j >= 0; --j) word = 2 * word + (x[4 * w + j] >= from ? 1 : 0);
+        if (over) {   // (what equals the threshold is contested)
+          word = 0;
+#pragma unroll
+          for (int j = 3; j >= 0; --j) word = 2 * word + (x[4 * w + j] > from ? 1 : 0);
+        }
+        word = eight(word << (4 * e), [](unsigned p, unsigned q) { return p | q; });
       }
-      if ((k & 3) == 3) {
-        if (own >> 5 == k >> 2 && query) word |= 1u << (own & 31);
-        if (e == 0 && (k >> 2) < words) bits[row * words + (k >> 2)] = word;
-        word = 0;
-      }
+      if (own >> 5 == w && query) word |= 1u << (own & 31);
+      if (e == 0 && w < words) bits[row * words + w] = word;
     }
   }
   __builtin_amdgcn_wave_barrier();

@@ -6,7 +6,7 @@ namespace optimus {
 namespace {
 
 // ---------------------------------------------------------------- lists
-// Pairs of 512 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
+// Pairs of 256 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
 // make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
 constexpr int kWords = kListChunk / 32;
 constexpr long long kMaskedCost = 3;              // of a chosen pair with lists, in pairs of the masked form
@@ -217,15 +217,13 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
     }
     float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int t2 = 0; t2 < KT; ++t2)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
+    for (int t2 = 0; t2 < KT; ++t2) mx = scale_scores(sacc[t2], f.scale_log2, mx);
     mx = halfwave_max(mx);   // (a listed query sees the block's first key)
 #pragma unroll
     for (int t2 = 0; t2 < KT; ++t2)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f((sacc[t2][r] - mx) * f.scale_log2);
+        const float p = __builtin_amdgcn_exp2f(sacc[t2][r] - mx);
         sacc[t2][r] = p;
         sum += p;
       }
@@ -312,27 +310,22 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
 #pragma unroll
             for (int r = 0; r < 16; ++r) sacc[t2][r] = 32 * t2 + slot(r) > reach ? -INFINITY : sacc[t2][r];
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
-        mx = halfwave_max(mx);
-        // The maximum follows the step's when that is above it by more than 2^8 after scaling: a step's largest term is at most 2^8 then.
-        const bool move = __builtin_amdgcn_ballot_w64((mx - m_run) * f.scale_log2 > 8.0f) != 0;
+        const float mx = halfwave_max(scale_scores(sacc[1], f.scale_log2, scale_scores(sacc[0], f.scale_log2, -INFINITY)));
+        // The maximum follows the step's when that is above it by more than 8: a step's largest term is at most 2^8 then.
+        const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
         const float m_new = move ? fmaxf(m_run, mx) : m_run;
         float sum = 0.f;
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f((sacc[t2][r] - m_new) * f.scale_log2);
+            const float e = __builtin_amdgcn_exp2f(sacc[t2][r] - m_new);
             sacc[t2][r] = e;
             sum += e;
           }
         sum = halfwave_sum(sum);
         if (move) {
-          const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * f.scale_log2);   // (m_new is a score: the first step holds a key of every row)
+          const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);   // (m_new is a score: the first step holds a key of every row)
           l_run *= alpha;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -413,7 +406,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
     const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const float w = __builtin_amdgcn_exp2f((ml[k].x - from) * f.scale_log2);   // (of no pair: 0)
+      const float w = __builtin_amdgcn_exp2f(ml[k].x - from);   // (of no pair: 0)
       total += w * ml[k].y;
       weight[k] *= w;
     }
@@ -448,7 +441,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   __builtin_amdgcn_wave_barrier();
   bf16_t* to = FORWARD ? f.attn + m.attn + (long long)t * f.ldo : f.d_qkv + m.qkv + (long long)t * f.ld;
   write_ordered<DT>(to, lds[half], n, inside);
-  if (FORWARD && inside && n == 0) f.lse[m.vec + t] = total > 0.f ? top * f.scale + __logf(total) : -INFINITY;
+  if (FORWARD && inside && n == 0) f.lse[m.vec + t] = total > 0.f ? (top + __log2f(total)) * LN2 : -INFINITY;
 }
 
 SelectedArgs make_args(const AttnSelectedDesc& b) {
@@ -501,8 +494,7 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
 }
 
 void launch_lists(const SelectedArgs& a, hipStream_t st) {
-  const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 64 KiB
-  if (2 * bits > 65536) (void)hipFuncSetAttribute((const void*)list_fill_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(2 * bits));
+  const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 32 KiB
   list_count_kernel<<<dim3(a.chunks, a.mats), kListChunk, bits, st>>>(a);
   list_places_kernel<<<a.mats, 1024, 0, st>>>(a);
   list_fill_kernel<<<dim3(a.chunks, a.mats), kListChunk, 2 * bits, st>>>(a);
@@ -550,12 +542,16 @@ void attn_selected_plan(const AttnSelectedDesc& b, SelectedPlan* out) {
     return;
   }
   p.chunks = (d.s + kListChunk - 1) / kListChunk;
-  p.seg[0] = 256;
   p.seg[1] = 1024;
-  for (int k = 0; k < 2; ++k) p.most[k] = (int)(blocks + pairs / p.seg[k]);
-  const size_t row_bytes = pairs * (d.d * 2 + 12), key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
+  const size_t row_bytes = pairs * (d.d * 2 + 12);   // of a matrix
   auto fit = [&](size_t bytes) { return (int)(kPortion / bytes < 1 ? 1 : kPortion / bytes > mats ? mats : kPortion / bytes); };
   p.portion = fit(row_bytes);
+  // Pieces of a list as long as some 2000 of them leave no compute unit without work, 256 to 1024 rows (no bits depend on it): a launch of 10^6
+  // pairs (two matrices of 32768 queries, 16 blocks each) 1006 us with 256 in all, 932 with 1024; 2.4 * 10^6 of width 64 395 with 256, 376 with 512.
+  p.seg[0] = 256;
+  while (p.seg[0] < 1024 && p.portion * pairs / p.seg[0] >= 4096) p.seg[0] *= 2;
+  for (int k = 0; k < 2; ++k) p.most[k] = (int)(blocks + pairs / p.seg[k]);
+  const size_t key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
   p.key_portion = fit(key_bytes);
   p.counts = round256(mats * p.chunks * blocks * 4);
   p.offsets = round256(mats * (blocks + 1) * 4);

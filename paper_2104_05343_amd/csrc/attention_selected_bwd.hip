@@ -296,12 +296,30 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
       dkacc[dt][r] += xch[(dt * 16 + r) * 64 + lane];
       dvacc[dt][r] += xch[((DT + dt) * 16 + r) * 64 + lane];
     }
+  const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1) + it.block;
+  if (first[1] - first[0] == 1) {   // the block's only piece: dK and dV themselves, a row of 32 keys after the other through LDS
+    float* row = xch;               // (the wavefront's own part of it, which it has read)
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const f32x16 (&acc)[DT] = which == 0 ? dkacc : dvacc;
+      const float w = which == 0 ? f.scale : 1.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) row[(slot(r) + 4 * g) * D + dt * 32 + (lane & 31)] = acc[dt][r] * w;
+      __builtin_amdgcn_wave_barrier();
+      for (int k = g; k < 32; k += 2)
+        write_ordered<DT>(f.d_qkv + m.qkv + (long long)(k0 + k) * f.ld + (which == 0 ? D : 2 * D), row + k * D, lane & 31, k0 + k < m.len);
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
   float* to = a.key_rows + (((long long)blockIdx.y * a.most[1] + item) * tiles + tile) * (2 * BLK * D) + rg * 32 * D;
   store_rows<DT>(to, dkacc, m.len - k0, g, lane);
   store_rows<DT>(to + BLK * D, dvacc, m.len - k0, g, lane);
 }
 
-// Sums over a key's pieces, in the order of the lists, to dK and dV; zeros where there is none.
+// Sums over a key's pieces, in the order of the lists, to dK and dV; zeros where there is none.  (A single piece is written by its workgroup.)
 template <int D>
 __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs a) {
   constexpr int DT = D / 32;
@@ -317,9 +335,10 @@ __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs 
   V dk, dv;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = 0.f;
-  if (key < m.len) {
-    const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1);
-    const int from = first[v], to = first[v + 1];
+  const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1);
+  const int from = first[v], to = first[v + 1];
+  const bool write = inside && (key >= m.len || to - from != 1);
+  if (key < m.len && write) {
 #pragma unroll 2
     for (int k = from; k < to; ++k) {
       const float* p = a.key_rows + (((long long)blockIdx.y * a.most[1] + k) * tiles + in_block / BLK) * (2 * BLK * D) + in_block % BLK * D + n * DT;
@@ -329,9 +348,9 @@ __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs 
   }
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dk[dt] *= f.scale;
-  bf16_t* to = f.d_qkv + m.qkv + (long long)key * f.ld + D;
-  write_row<DT>(to, dk, lds[half], n, inside);
-  write_row<DT>(to + D, dv, lds[half], n, inside);
+  bf16_t* out = f.d_qkv + m.qkv + (long long)key * f.ld + D;
+  write_row<DT>(out, dk, lds[half], n, write);
+  write_row<DT>(out + D, dv, lds[half], n, write);
 }
 
 template <int D>

@@ -18,7 +18,7 @@
 
 namespace optimus {
 
-constexpr int kListChunk = 512;        // queries of a workgroup that makes the lists
+constexpr int kListChunk = 256;        // queries of a workgroup that makes the lists
 constexpr int kMostBlocks = 1024, kMostCount = 64;
 constexpr int kMaskedBlocks = 256;     // most blocks of a sequence in the masked form
 constexpr int kQueries = 128;          // list rows of a tile
@@ -50,7 +50,7 @@ struct SelectedArgs {
   int* places;                         // [matrix][s][count]: place of the pair in list, -1: none
   f16_t* rows;                         // [matrix - mat0][s * count][d]: partial results, see store_parts
   float* units;                        // [matrix - mat0][s * count]: what a row's numbers are to be multiplied by
-  float2* ml;                          // [matrix - mat0][s * count]: maximum of Q K^T, sum of exponentials
+  float2* ml;                          // [matrix - mat0][s * count]: maximum of log2(e) Q K^T / sqrt(d), sum of exponentials
   float* key_rows;                     // [matrix - mat0][item][block / 64][dK, dV][64][d]
 };
 
@@ -126,6 +126,16 @@ __device__ __forceinline__ void swap_rows(float& a, float& b) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
   a = __uint_as_float(r[0]);
   b = __uint_as_float(r[1]);
+}
+// scores times w, and the largest of them and m: products are known to be no signalling NaN, of which every maximum of a matrix instruction's
+// results would be cleared by an instruction of its own, and rounded before the maximum is subtracted scores of any size have exponents up to zero
+__device__ __forceinline__ float scale_scores(f32x16& v, float w, float m) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    v[r] *= w;
+    m = fmaxf(m, v[r]);
+  }
+  return m;
 }
 template <int DT>
 __device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x16 (&acc)[DT], int rows, int g, int lane) {

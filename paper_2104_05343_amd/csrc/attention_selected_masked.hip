@@ -97,24 +97,8 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
 #pragma unroll
           for (int r = 0; r < 16; ++r) sacc[t2][r] = 32 * t2 + slot(r) > reach ? -INFINITY : sacc[t2][r];
       }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[t2][r]);
-      mx = halfwave_max(mx);
+      float mx = halfwave_max(scale_scores(sacc[1], f.scale_log2, scale_scores(sacc[0], f.scale_log2, -INFINITY)));
       mx = chosen ? mx : -INFINITY;
-      // (scores beyond 2^28 are rounded before the maximum is subtracted, as it is: see the attention with changed scores)
-      float w = f.scale_log2;
-      const bool large = __builtin_amdgcn_ballot_w64(fabsf(mx) * w > 0x1p28f && chosen) != 0;
-      mx *= w;
-      if (large) {
-#pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[t2][r] *= w;
-        w = 1.0f;
-      }
       const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
       const float m_new = move ? fmaxf(m_run, mx) : m_run;
       const float m_sub = m_new == -INFINITY ? 0.f : m_new;
@@ -124,7 +108,7 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
       for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], w, off));
+          const float p = __builtin_amdgcn_exp2f(sacc[t2][r] + off);
           sacc[t2][r] = p;
           sum += p;
         }
@@ -186,16 +170,17 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
 }
 
 // ---------------------------------------------------------------- backward
-// Ahead of the others, 512 queries a workgroup: rowsum(dO * O), 0 past the end of a sequence, and the choices by blocks, a bit a query.
+// Ahead of the others, 128 queries a workgroup: rowsum(dO * O), 0 past the end of a sequence, and the choices by blocks, a bit a query.
+constexpr int kPrepared = 128;
 template <int D>
-__global__ __launch_bounds__(kListChunk) void masked_prepare_kernel(SelectedArgs a) {
-  __shared__ unsigned bits[kMaskedBlocks][kListChunk / 32 + 1];
+__global__ __launch_bounds__(256) void masked_prepare_kernel(SelectedArgs a) {
+  __shared__ unsigned bits[kMaskedBlocks][kPrepared / 32];
   const FusedArgs& f = a.f;
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = tid >> 6, mm = blockIdx.y, t0 = blockIdx.x * kListChunk;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = tid >> 6, mm = blockIdx.y, t0 = blockIdx.x * kPrepared;
   const SelMatrix m = selected_matrix<D>(a, mm);
-  for (int k = tid; k < a.blocks * (kListChunk / 32 + 1); k += kListChunk) (&bits[0][0])[k] = 0;
+  for (int k = tid; k < a.blocks * (kPrepared / 32); k += 256) (&bits[0][0])[k] = 0;
   __syncthreads();
-  if (t0 + tid < m.len) {
+  if (tid < kPrepared && t0 + tid < m.len) {
     const int* own = a.selected + (m.vec + t0 + tid) * a.count;
 #pragma unroll 4
     for (int e = 0; e < a.count; ++e) {
@@ -203,9 +188,8 @@ __global__ __launch_bounds__(kListChunk) void masked_prepare_kernel(SelectedArgs
       if (v >= 0 && v < a.blocks) atomicOr(&bits[v][tid >> 5], 1u << (tid & 31));
     }
   }
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int t = t0 + half * 256 + wave * 32 + (lane & 31), row = min(t, f.s - 1);
+  {
+    const int t = t0 + wave * 32 + (lane & 31), row = min(t, f.s - 1);
     float delta = 0.f;
     if (t < m.len) {
       const bf16_t* G = f.d_attn + m.attn + (long long)row * f.ldo + g * 8;
@@ -217,8 +201,8 @@ __global__ __launch_bounds__(kListChunk) void masked_prepare_kernel(SelectedArgs
     if (g == 0 && t < f.s) f.delta[m.vec + t] = delta;
   }
   __syncthreads();
-  for (int k = tid; k < a.blocks * (kListChunk / 32); k += kListChunk) {
-    const int v = k / (kListChunk / 32), w = k % (kListChunk / 32), at = blockIdx.x * (kListChunk / 32) + w;
+  for (int k = tid; k < a.blocks * (kPrepared / 32); k += 256) {
+    const int v = k / (kPrepared / 32), w = k % (kPrepared / 32), at = blockIdx.x * (kPrepared / 32) + w;
     if (at < a.mask_words) a.mask[((long long)mm * a.blocks + v) * a.mask_words + at] = bits[v][w];
   }
 }
@@ -633,7 +617,7 @@ void fwd_launch(const SelectedArgs& a, int mats, hipStream_t st) {
 }
 template <int D>
 void bwd_launch(const SelectedArgs& a, int mats, hipStream_t st) {
-  masked_prepare_kernel<D><<<dim3((a.f.s + kListChunk - 1) / kListChunk, mats), kListChunk, 0, st>>>(a);
+  masked_prepare_kernel<D><<<dim3((a.f.s + kPrepared - 1) / kPrepared, mats), 256, 0, st>>>(a);
   if constexpr (D == 128) {
     // the two forms add dK and dV up in different orders: the choice follows one device's matrices, whatever the launch covers
     if (2ll * ((a.f.s + BLK - 1) / BLK) * a.nmat > num_cus()) {

@@ -618,9 +618,12 @@ int optimus_debug_last_gemm_plan(void);
 /* The streams an optimus_layer_bwd of this size runs on when it is not captured (a captured one: two, once the library
  * has its stream): 1 or 2, or -1 for arguments that optimus_layer_bwd refuses.  Host arithmetic only. */
 int optimus_debug_layer_bwd_streams(const optimus_layer_cfg* cfg, int i, int j);
-/* Whether an optimus_attention_selected_fwd / _bwd of this size computes all blocks with a mask (1), or lists of the queries of each block (0);
+/* Force how optimus_attention_selected_fwd / _bwd run: 1 = all blocks with a mask (up to 256 blocks in a sequence), 0 = lists of the queries of
+ * each block, -1 = automatic.  The workspace that is asked for follows. */
+void optimus_debug_set_attention_selected_form(int form);
+/* Whether an optimus_attention_selected_fwd, or with backward != 0 _bwd, of this size computes all blocks with a mask (1), or lists (0);
  * -1 for arguments that these refuse.  Host arithmetic only. */
-int optimus_debug_attention_selected_masked(int b, int s, int h, int n, int q, int i, int j, int causal, const optimus_selection* selection);
+int optimus_debug_attention_selected_masked(int backward, int b, int s, int h, int n, int q, int i, int j, int causal, const optimus_selection* selection);
 /* Rows of a workgroup, 64 or 128, in which an optimus_attention_biased_fwd, or with backward != 0 _bwd (table_gradient: with d_table), of
  * this size would run; -1 for arguments that these refuse.  Host arithmetic only. */
 int optimus_debug_attention_biased_rows(int backward, int b, int s, int h, int n, int q, int i, int j, const optimus_attention_bias* bias,

@@ -180,7 +180,8 @@ SIGNATURES = {
     "optimus_debug_last_gemm_plan": (_INT, []),
     "optimus_debug_layer_bwd_streams": (_INT, [C.POINTER(LayerCfg), _INT, _INT]),
     "optimus_debug_attention_biased_rows": (_INT, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(AttentionBias), _INT]),
-    "optimus_debug_attention_selected_masked": (_INT, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection)]),
+    "optimus_debug_set_attention_selected_form": (None, [_INT]),
+    "optimus_debug_attention_selected_masked": (_INT, [_INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, _INT, C.POINTER(Selection)]),
     "optimus_debug_plan_summa": (_INT, [_INT, _I64, _I64, _I64, _INT, _INT, _INT, _INT, _INT, C.POINTER(C.c_int)]),
     "optimus_debug_plan_pair": (_INT, [_I64, _I64, _I64, _INT, _INT, _INT]),
     "optimus_debug_mfma_rate": (_INT, [_P, _INT, _INT, _INT, _P]),
@@ -722,8 +723,12 @@ def debug_last_gemm_pair() -> bool:
     return p >= 0 and bool(p >> 18 & 1)
 
 
-def debug_attention_selected_masked(b, s, h, n, q, i, j, causal, selection: Selection) -> bool:
-    rc = lib().optimus_debug_attention_selected_masked(b, s, h, n, q, i, j, int(causal), C.byref(selection))
+def debug_set_attention_selected_form(form: int):
+    lib().optimus_debug_set_attention_selected_form(form)
+
+
+def debug_attention_selected_masked(backward, b, s, h, n, q, i, j, causal, selection: Selection) -> bool:
+    rc = lib().optimus_debug_attention_selected_masked(int(backward), b, s, h, n, q, i, j, int(causal), C.byref(selection))
     if rc < 0:
         raise OptimusError(ESHAPE, "optimus_debug_attention_selected_masked")
     return bool(rc)

@@ -1315,12 +1315,13 @@ int optimus_debug_layer_bwd_streams(const optimus_layer_cfg* c, int i, int j) {
   if (layer_check(c, i, j, &a)) return -1;
   return two_streams_pay(c, is_grid(i, j)) ? 2 : 1;
 }
-int optimus_debug_attention_selected_masked(int b, int s, int h, int n, int q, int i, int j, int causal, const optimus_selection* selection) {
+void optimus_debug_set_attention_selected_form(int form) { attn_selected_set_form(form); }
+int optimus_debug_attention_selected_masked(int backward, int b, int s, int h, int n, int q, int i, int j, int causal, const optimus_selection* selection) {
   AttnDims a;
   AttnSelectedDesc d = {};
   if (selected_desc(b, s, h, n, q, i, j, selection, &a, &d)) return -1;
   d.base.causal = causal ? 1 : 0;
-  return attn_selected_masked(d) ? 1 : 0;
+  return attn_selected_masked(d, backward != 0) ? 1 : 0;
 }
 int optimus_debug_attention_biased_rows(int backward, int b, int s, int h, int n, int q, int i, int j, const optimus_attention_bias* bias,
                                         int table_gradient) {

@@ -1,5 +1,7 @@
 // Attention over chosen blocks (attention_selected_kernel.hpp): the lists, the forward pass, the sums over a query's blocks, what the
 // host decides.
+#include <atomic>
+
 #include "attention_selected_kernel.hpp"
 
 namespace optimus {
@@ -9,7 +11,7 @@ namespace {
 // Pairs of 256 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
 // make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
 constexpr int kWords = kListChunk / 32;
-constexpr long long kMaskedCost = 3;              // of a chosen pair with lists, in pairs of the masked form
+std::atomic<int> g_form{-1};                      // forced by a tuning hook: 1 masked, 0 lists
 constexpr size_t kPortion = (size_t)384 << 20;    // bytes of partial results in memory at a time
 
 __device__ __forceinline__ bool sees(const SelectedArgs& a, int len, int t, int v) {
@@ -517,22 +519,39 @@ void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipSt
   else selected_combine_kernel<128, false><<<grid, 256, 0, st>>>(a);
 }
 
-// The masked form where the pairs of queries and blocks that it computes are at most kMaskedCost times the chosen ones.
-bool attn_selected_masked(const AttnSelectedDesc& b) {
-  const long long blocks = (b.base.s + b.block - 1) / b.block, k = b.count < blocks ? b.count : blocks;
+// Which form.  The masked one computes all pairs of queries and keys (causal: half of them), lists the chosen ones, each of which costs as much
+// as some of the others: its part of a row goes through memory once for every block, and there are the lists to make.  Measured, us, masked /
+// lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
+//   width 128: 8192 queries, blocks of 128, 4 chosen 355 / 134, 1049 / 449; 8 302 / 222, 1056 / 653; 12 299 / 310, 1051 / 909; 16 296 / 377, 1060 / 1116;
+//   16384, 256, 8 1112 / 631, 4311 / 2079; 4096, 64, 4 80 / 67, 276 / 190; 8 82 / 99, 288 / 292; 4096, 512, 2 76 / 105, 288 / 332;
+//   8 of 2048, 64, 3 36 / 33, 70 / 72
+//   width 64: 8192, 128, 8 164 / 128, 610 / 306; 16 169 / 219, 618 / 497; 16384, 256, 8 604 / 390, 2394 / 933; 4096, 64, 8 57 / 71, 175 / 153; 4096, 512, 2
+//   54 / 66, 173 / 162; 8 of 2048, 64, 3 22 / 30, 42 / 56
+// so a chosen pair costs (forward) 1.6 + 180 / block of the others, backward 1.5 + 150 / block, of width 64 1.2 + 120 / block, and lists some 20 us
+// more, in which one pair of a device's matrices takes the time given below.  (One device's, whatever the launch covers: the forms add up in
+// different orders.)
+bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
+  const AttnFusedDesc& d = b.base;
+  const double blocks = (d.s + b.block - 1) / b.block, k = b.count < blocks ? b.count : blocks, B = b.block;
   if (blocks > kMaskedBlocks) return false;
-  const long long all = b.base.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
-  const long long chosen = b.base.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
-  return all <= kMaskedCost * chosen;
+  const int forced = g_form.load(std::memory_order_relaxed);
+  if (forced >= 0) return forced != 0;
+  const double all = d.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
+  const double chosen = d.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
+  const double factor = !bwd ? 1.6 + 180 / B : d.d == 128 ? 1.5 + 150 / B : 1.2 + 120 / B;
+  const double pair_us = !bwd ? (d.d == 128 ? 5.5e-7 : 3.0e-7) : (d.d == 128 ? 1.9e-6 : 1.1e-6);
+  const double pairs = (double)d.nb * d.nh * B * (d.s < b.block ? d.s : B);   // of queries and keys, of a pair of blocks
+  return (all - factor * chosen) * pairs * pair_us <= 20.0;
 }
+void attn_selected_set_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 
-void attn_selected_plan(const AttnSelectedDesc& b, SelectedPlan* out) {
+void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) {
   SelectedPlan p = {};
   const AttnFusedDesc& d = b.base;
   const size_t blocks = (d.s + b.block - 1) / b.block, pairs = (size_t)d.s * b.count;
   p.mats = d.ndev * d.nb * d.nh;
   const size_t mats = p.mats;
-  p.masked = attn_selected_masked(b);
+  p.masked = attn_selected_masked(b, bwd);
   p.delta = round256(mats * d.s * 4);
   if (p.masked) {
     p.mask_words = (d.s + 31) / 32;
@@ -566,14 +585,15 @@ void attn_selected_plan(const AttnSelectedDesc& b, SelectedPlan* out) {
   *out = p;
 }
 size_t attn_selected_ws_bytes(const AttnSelectedDesc& b) {
-  SelectedPlan p;
-  attn_selected_plan(b, &p);
-  return p.total;
+  SelectedPlan fwd, bwd;
+  attn_selected_plan(b, false, &fwd);
+  attn_selected_plan(b, true, &bwd);
+  return fwd.total > bwd.total ? fwd.total : bwd.total;
 }
 
 int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
   SelectedPlan p;
-  attn_selected_plan(b, &p);
+  attn_selected_plan(b, false, &p);
   SelectedArgs a = with_workspace(b, p, false);
   if (p.masked) {
     launch_selected_masked(a, p.mats, b.base.d, false, st);
@@ -591,7 +611,7 @@ int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
 
 int launch_attn_selected_bwd(const AttnSelectedDesc& b, hipStream_t st) {
   SelectedPlan p;
-  attn_selected_plan(b, &p);
+  attn_selected_plan(b, true, &p);
   const SelectedArgs a = with_workspace(b, p, true);
   if (p.masked) {
     launch_selected_masked(a, p.mats, b.base.d, true, st);

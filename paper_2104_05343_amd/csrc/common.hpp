@@ -221,7 +221,8 @@ struct AttnSelectedDesc {
 };
 size_t attn_select_ws_bytes(const AttnSelectedDesc& d);     // of the choice
 size_t attn_selected_ws_bytes(const AttnSelectedDesc& d);   // of both directions
-bool attn_selected_masked(const AttnSelectedDesc& d);       // whether they are the fused attention with a mask, not lists
+bool attn_selected_masked(const AttnSelectedDesc& d, bool bwd);   // whether it is the fused attention with a mask, not lists
+void attn_selected_set_form(int form);
 int launch_attn_select(const AttnSelectedDesc& d, hipStream_t stream);
 int launch_attn_selected_fwd(const AttnSelectedDesc& d, hipStream_t stream);
 int launch_attn_selected_bwd(const AttnSelectedDesc& d, hipStream_t stream);

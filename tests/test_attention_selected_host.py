@@ -107,24 +107,42 @@ def test_refuses_more():
     assert _rc("bwd", opt.make_selection(64, 2), d_attn=None) == _rc("bwd", opt.make_selection(64, 2), d_qkv=None) == opt.EINVAL
 
 
-def test_workspace():
+@pytest.fixture
+def form():
+    yield opt.debug_set_attention_selected_form
+    opt.debug_set_attention_selected_form(-1)
+
+
+def test_workspace(form):
     size = lambda *a, sel=opt.make_selection(64, 3): opt.attention_selected_workspace_bytes(*a, sel)   # noqa: E731
     one, all_of = size(4, 200, 256, 4, 2, 0, 1), size(4, 200, 256, 4, 2, -1, -1)
     assert 4 * 200 * 4 <= one < all_of
     assert size(3, 200, 256, 4, 2, 0, 1) == size(4, 200, 320, 4, 2, 0, 1) == size(4, 200, 256, 4, 2, 0, 2) == 0
     assert size(4, 200, 256, 4, 2, 0, 1, sel=opt.make_selection(63, 3)) == 0
-    assert size(4, 5000, 256, 4, 2, 0, 1) >= 4 * 5000 * 3 * (64 * 2 + 12)                # lists: partial results of all pairs
+    form(0)
+    assert size(4, 5000, 256, 4, 2, 0, 1) >= 4 * 5000 * 3 * (64 * 2 + 12)               # lists: partial results of all pairs
+    form(-1)
     # of one (sequence, head) where 384 MiB do not hold them, not of all of them
     long = size(1, 1 << 18, 1024, 8, 1, 0, 0, sel=opt.make_selection(256, 16))
     assert (1 << 18) * 16 * (128 * 2 + 12) <= long < 2 * (1 << 18) * 16 * (128 * 2 + 12)
 
 
-def test_form():
-    """Every block with a mask where queries choose a third of what they could, at most 256 blocks; else lists."""
-    masked = lambda s, block, count, causal: opt.debug_attention_selected_masked(4, s, 256, 4, 2, 0, 1, causal, opt.make_selection(block, count))   # noqa: E731
-    assert masked(1, 64, 1, True) and masked(200, 64, 3, False) and masked(4096, 128, 8, True) and masked(1152, 64, 6, False)
-    assert not masked(5000, 64, 3, True) and not masked(1216, 64, 6, False) and not masked(32768, 128, 16, True)
-    assert masked(16384, 64, 64, True) and not masked(16385, 64, 64, True)              # 256 and 257 blocks
+def test_form(form):
+    """All blocks with a mask where queries choose much of what they could, or little is to do, at most 256 blocks; else lists."""
+    def masked(s, block, count, causal, backward=False, b=1, h=2048, n=16):
+        return opt.debug_attention_selected_masked(backward, b, s, h, n, 1, 0, 0, causal, opt.make_selection(block, count))
+    for backward in (False, True):
+        assert masked(1, 64, 1, True, backward) and masked(200, 64, 3, False, backward) and masked(4096, 128, 8, True, backward)
+        assert not masked(32768, 128, 16, True, backward) and not masked(8192, 128, 4, True, backward)
+        assert masked(16384, 64, 64, True, backward) and not masked(16385, 64, 64, True, backward)              # 256 and 257 blocks
+        # the same for one device, whatever the launch covers
+        sel = opt.make_selection(64, 6)
+        for s in (500, 1000, 2000, 3000):
+            assert len({opt.debug_attention_selected_masked(backward, 8, s, 2048, 16, 2, i, i, True, sel) for i in (-1, 0, 1)}) == 1
+        for forced in (0, 1):
+            form(forced)
+            assert masked(1, 64, 1, True, backward) == bool(forced) and not masked(16385, 64, 64, True, backward)
+        form(-1)
     with pytest.raises(opt.OptimusError):
         masked(200, 65, 3, True)
 

@@ -15,6 +15,21 @@ FP32 = 2e-5          # relative error of P: fp32 sums of 64 to 128 products, sco
 PART = 2.0 ** -12    # with lists, a block's part of an output or of dQ is rounded to fp16
 
 
+@pytest.fixture(params=["mask", "lists"])
+def form(request):
+    """Both ways to compute: all blocks with a mask, and lists of the queries of each block."""
+    opt.debug_set_attention_selected_form(1 if request.param == "mask" else 0)
+    yield
+    opt.debug_set_attention_selected_form(-1)
+
+
+@pytest.fixture
+def lists():
+    opt.debug_set_attention_selected_form(0)
+    yield
+    opt.debug_set_attention_selected_form(-1)
+
+
 class Run:
     """Choice, forward and backward on the device, and what the oracle makes of the same inputs (of the device's own attn and lse, backward).
     selected: a choice to attend to instead of the device's own, [b, n, s, count]."""
@@ -114,7 +129,7 @@ class Run:
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("s", [1, 2, 31, 33, 63, 64, 65, 127, 128, 129, 193, 257, 400])
-def test_block_boundaries(s, d, causal):
+def test_block_boundaries(s, d, causal, form):
     Run(2, s, 2 * d, 2, 1, causal, block=64, count=3).go().check()
     Run(2, s, 2 * d, 2, 1, causal, block=128, count=2).go().check()
     Run(2, s, 2 * d, 2, 1, causal, block=192, count=2).go().check()
@@ -123,19 +138,19 @@ def test_block_boundaries(s, d, causal):
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("block,count,s", [(64, 1, 300), (64, 2, 700), (64, 5, 1000), (64, 64, 1500), (128, 4, 1111), (192, 3, 1200), (256, 2, 1030), (512, 3, 2100),
                                            (4096, 2, 5000), (64, 12, 2300)])
-def test_blocks_and_counts(block, count, s, causal):
+def test_blocks_and_counts(block, count, s, causal, form):
     for d in (64, 128):
         Run(1, s, 2 * d, 2, 1, causal, block=block, count=count).go().check()
 
 
 @pytest.mark.parametrize("b,s,h,n,q", [(4, 328, 256, 4, 2), (8, 150, 1024, 8, 2), (4, 200, 512, 4, 4), (3, 500, 640, 5, 1)])
-def test_grids(b, s, h, n, q):
+def test_grids(b, s, h, n, q, form):
     Run(b, s, h, n, q, True, block=64, count=3).go().check()
 
 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("d", [64, 128])
-def test_lengths(d, causal):
+def test_lengths(d, causal, form):
     """Padded batches: what lies behind a sequence's end is full of NaN and infinities."""
     lengths = [500, 0, 1, 63, 64, 65, 130, 499, 1000, -5]
     for block, count in ((64, 3), (128, 2), (256, 2)):
@@ -148,7 +163,7 @@ def _given(b, n, s, count, low, high, seed=0):
 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("block", [64, 128, 256])
-def test_choices_of_the_callers_own(block, causal):
+def test_choices_of_the_callers_own(block, causal, form):
     """Any entries: repeated, unsorted, out of range on both sides, none at all, all queries the same block."""
     b, n, s, count = 2, 2, 700, 5
     for low, high in ((-3, 14), (0, 2), (-1, 0), (-2 ** 31, 2 ** 31 - 1)):
@@ -209,7 +224,7 @@ def test_scores_that_are_not_finite():
 
 
 @pytest.mark.parametrize("scale", [1e-3, 30.0, 1e4])
-def test_scores_of_any_size(scale):
+def test_scores_of_any_size(scale, form):
     """The forward at small and large scores: lse and the largest weights."""
     r = Run(1, 600, 128, 1, 1, True, block=64, count=3, stretch=scale)
     r.choose()
@@ -231,7 +246,7 @@ def test_larger_launches(b, s, h, n, block, count):
     Run(b, s, h, n, 1, True, block=block, count=count).go().check(which={(0, 0), (b - 1, n - 1), (b // 2, 1)})
 
 
-def test_one_device_has_the_bits_of_the_grid():
+def test_one_device_has_the_bits_of_the_grid(form):
     for h, block in ((256, 64), (512, 128), (256, 256)):
         full = Run(4, 520, h, 4, 2, True, block=block, count=3, lengths=[520, 300, 1, 519]).go()
         for dev in ((0, 1), (1, 0)):
@@ -244,7 +259,7 @@ def test_one_device_has_the_bits_of_the_grid():
                 assert (rest == -123).all() if name == "S" else torch.isnan(rest).all(), name     # nothing else is written
 
 
-def test_same_call_same_bits():
+def test_same_call_same_bits(form):
     a, b = (Run(4, 1000, 512, 8, 1, True, block=64, count=6).go() for _ in range(2))
     b.ws.fill_(0x55)
     b.go()
@@ -252,7 +267,7 @@ def test_same_call_same_bits():
         assert torch.equal(getattr(a, name).view(torch.uint8), getattr(b, name).view(torch.uint8)), name
 
 
-def test_captured_and_on_another_stream():
+def test_captured_and_on_another_stream(form):
     """A graph of all three replayed with other inputs and lengths, eager work and synchronisations between, and the same on a stream of its own."""
     r = Run(2, 700, 256, 4, 1, True, block=64, count=4, lengths=[700, 600]).go()
     first = [x.clone() for x in (r.S, r.O, r.L, r.G)]
@@ -333,34 +348,25 @@ def test_a_long_sequence():
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("s", [1025, 1087, 1088, 1089, 1119, 1120, 1121, 1151, 1152, 1153])
-def test_block_boundaries_with_lists(s, d):
+def test_block_boundaries_with_lists(s, d, lists):
     """Few of many blocks: lists of queries, around the tiles of 32, 64 and 128 rows and keys."""
     for block, count, causal in ((64, 2, True), (64, 4, False), (128, 1, True), (128, 2, False), (192, 1, True), (192, 1, False)):
         r = Run(2, s, 2 * d, 2, 1, causal, block=block, count=count, lengths=[s, 700])
-        assert not opt.debug_attention_selected_masked(2, s, 2 * d, 2, 1, -1, -1, causal, r.sel)
         r.go().check(which={(0, 0), (1, 1)})
 
 
-def test_all_forms_are_tested():
-    """Which of these tests' sizes take lists, which the mask: both, of every kind of block, in the boundary tests and in the grids."""
-    for block, count, s, want in ((64, 3, 400, True), (128, 2, 400, True), (192, 2, 400, True), (64, 2, 1089, False), (128, 1, 1089, False), (192, 1, 1089, False)):
-        assert opt.debug_attention_selected_masked(1, s, 128, 2, 1, 0, 0, True, opt.make_selection(block, count)) == want
-
-
 @pytest.mark.parametrize("block", [64, 128, 256])
-def test_choices_of_the_callers_own_with_lists(block):
+def test_choices_of_the_callers_own_with_lists(block, lists):
     """More blocks than a third of them named: repeated, unsorted, out of range, none, all queries the same one."""
     b, n, s, count = 2, 2, 26 * block + 17, 2
     for causal in (True, False):
         for low, high in ((-3, 29), (0, 2), (-1, 0), (-2 ** 31, 2 ** 31 - 1)):
             r = Run(b, s, n * 64, n, 1, causal, block=block, count=count, selected=_given(b, n, s, count, low, high))
-            assert not opt.debug_attention_selected_masked(b, s, n * 64, n, 1, -1, -1, causal, r.sel)
             r.go().check(which={(0, 0), (1, 1)} if block == 64 else {(1, 0)})
 
 
-def test_grids_and_lengths_with_lists():
+def test_grids_and_lengths_with_lists(lists):
     full = Run(4, 1300, 256, 4, 2, True, block=64, count=2, lengths=[1300, 700, 0, 1299], dirty=True).go().check(which={(0, 0), (1, 3), (2, 1), (3, 2)})
-    assert not opt.debug_attention_selected_masked(4, 1300, 256, 4, 2, -1, -1, True, full.sel)
     for dev in ((0, 1), (1, 0)):
         one = Run(4, 1300, 256, 4, 2, True, block=64, count=2, lengths=[1300, 700, 0, 1299], dirty=True, at=dev).go()
         k = dev[0] * 2 + dev[1]
@@ -371,7 +377,7 @@ def test_grids_and_lengths_with_lists():
             assert (rest == -123).all() if name == "S" else torch.isnan(rest).all(), name
 
 
-def test_captured_with_lists():
+def test_captured_with_lists(lists):
     r = Run(2, 1300, 256, 4, 1, True, block=64, count=2, lengths=[1300, 1100]).go()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):

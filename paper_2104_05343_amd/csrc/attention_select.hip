@@ -14,15 +14,15 @@
 namespace optimus {
 namespace {
 
-// Mean keys: a wavefront has a block, a lane 8 of its columns in every (64 / (d / 8))-th row.  Sums in 64 bits: their bf16 rounding does not
-// depend on the order then.
+// Mean keys, a workgroup a block: a lane has 8 columns of every (256 / (d / 8))-th row.  Sums in 64 bits: their bf16 rounding does not depend on
+// the order then.
 template <int D>
 __global__ __launch_bounds__(256) void block_means_kernel(SelectedArgs a) {
-  constexpr int CH = D / 8, ROWS = 64 / CH;
+  constexpr int CH = D / 8, ROWS = 256 / CH;
+  __shared__ double parts[3][D];
   const FusedArgs& f = a.f;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int v = blockIdx.x * 4 + wave, mm = blockIdx.y;
-  if (v >= a.blocks) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int v = blockIdx.x, mm = blockIdx.y;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const int row0 = v * a.block, rows = min(a.block, m.len - row0);
   if (rows <= 0) return;
@@ -31,20 +31,29 @@ __global__ __launch_bounds__(256) void block_means_kernel(SelectedArgs a) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) sum[k] = 0.0;
 #pragma unroll 4
-  for (int r = lane / CH; r < rows; r += ROWS) {
-    const bf16x8 x = *(const bf16x8*)(p + (long long)r * f.ld);
-    const u32x4 w = __builtin_bit_cast(u32x4, x);
+  for (int r = tid / CH; r < rows; r += ROWS) {
+    const u32x4 w = *(const u32x4*)(p + (long long)r * f.ld);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       sum[2 * k] += (double)__uint_as_float(w[k] << 16);
       sum[2 * k + 1] += (double)__uint_as_float(w[k] & 0xffff0000u);
     }
   }
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+#pragma unroll
+    for (int step = CH; step < 64; step <<= 1) sum[k] += __shfl_xor(sum[k], step);
+  if (wave > 0 && lane < CH) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) parts[wave - 1][lane * 8 + k] = sum[k];
+  }
+  __syncthreads();
+  if (wave > 0) return;
   float mean[8], size = 0.f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-#pragma unroll
-    for (int step = CH; step < 64; step <<= 1) sum[k] += __shfl_xor(sum[k], step);
+    const int c = lane % CH * 8 + k;
+    sum[k] += parts[0][c] + parts[1][c] + parts[2][c];
     mean[k] = bf16_to_f32(f32_to_bf16((float)(sum[k] / rows)));
     size = fmaf(mean[k], mean[k], size);
   }
@@ -127,13 +136,14 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
     }
     return;
   }
+  // (one wait for the workgroup: everything that is loaded is on its way before it)
   for (int k = tid; k < kRows * words; k += 256) contested[k] = 0;
-  if (tid == 0) *wild_rows = 0;
+  float mean_size = 0.f, q_size = 0.f;
+  for (int v = tid; v < others; v += 256) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
   const bf16_t* Q = f.qkv + m.qkv + (long long)min(t, m.len - 1) * f.ld + e * (D / 8);
   u32x4 qw[D / 64];
 #pragma unroll
   for (int k = 0; k < D / 64; ++k) qw[k] = *(const u32x4*)(Q + 8 * k);
-  __syncthreads();
   // Scores, 32 blocks a wavefront at a time; of no candidate: NaN, which is neither above nor below a threshold, largest nor least.
   {
     const int qrow = min(q0 + (lane & 31), m.len - 1);
@@ -142,6 +152,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(P + ks * 16);
     const bf16_t* means = a.means + (long long)mm * a.blocks * D;
+    unsigned long long bad = 0;
     const int end = (others + 8 * PART - 1) / (8 * PART) * (8 * PART);
     for (int v0 = wave * 32; v0 < end; v0 += 128) {
       const bf16_t* p = means + (long long)min(v0 + (lane & 31), others - 1) * D + g * 8;
@@ -151,7 +162,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
       float zero = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) zero = fmaf(acc[r], 0.f, zero);   // (an infinity or NaN: NaN)
-      if (!(zero == 0.f)) atomicOr(wild_rows, 1u << (lane & 31));
+      bad |= __builtin_amdgcn_ballot_w64(!(zero == 0.f));
       if (v0 + 32 > others || (own >= v0 && own < v0 + 32)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -163,10 +174,9 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
       for (int c = 0; c < 4; ++c)
         *(float4*)(scores + (lane & 31) * stride + v0 + 8 * c + 4 * g) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
     }
+    if (lane == 0) wild_rows[wave] = (unsigned)bad | (unsigned)(bad >> 32);
   }
   // E of the row: a query's size by its eight lanes, the largest mean by the workgroup
-  float mean_size = 0.f, q_size = 0.f;
-  for (int v = tid; v < others; v += 256) mean_size = fmaxf(mean_size, a.mean_sizes[(long long)mm * a.blocks + v]);
 #pragma unroll
   for (int step = 1; step < 64; step <<= 1) mean_size = fmaxf(mean_size, __shfl_xor(mean_size, step));
   if (lane == 0) sizes[wave] = mean_size;
@@ -182,7 +192,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
   mean_size = fmaxf(fmaxf(sizes[0], sizes[1]), fmaxf(sizes[2], sizes[3]));
   const float error = q_size * mean_size * (D * 1.1920929e-7f);
   // wild: a score or the bound is not finite, or too small for the bound: all scores are computed again
-  const bool wild = !(error < 1e30f) || error < 1e-30f || q_size < 1e-25f || mean_size < 1e-25f || (*wild_rows >> row & 1);
+  const bool wild = !(error < 1e30f) || error < 1e-30f || q_size < 1e-25f || mean_size < 1e-25f || ((wild_rows[0] | wild_rows[1] | wild_rows[2] | wild_rows[3]) >> row & 1);
   // a lane's scores: of blocks 4 e + j of every 32
   const float* mine = scores + row * stride + 4 * e;
   float x[NV];
@@ -399,7 +409,7 @@ void select_launch(const SelectedArgs& a, int mats, hipStream_t st) {
 template <int D>
 void choose(const SelectedArgs& a, int mats, hipStream_t st) {
   // (every block is chosen, or the own one alone: no scores)
-  if (a.count > 1 && a.count < a.blocks) block_means_kernel<D><<<dim3((a.blocks + 3) / 4, mats), 256, 0, st>>>(a);
+  if (a.count > 1 && a.count < a.blocks) block_means_kernel<D><<<dim3(a.blocks, mats), 256, 0, st>>>(a);
   if (a.blocks <= 32) select_launch<D, 4>(a, mats, st);
   else if (a.blocks <= 64) select_launch<D, 8>(a, mats, st);
   else if (a.blocks <= 128) select_launch<D, 16>(a, mats, st);

@@ -522,12 +522,12 @@ void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipSt
 // Which form.  The masked one computes all pairs of queries and keys (causal: half of them), lists the chosen ones, each of which costs as much
 // as some of the others: its part of a row goes through memory once for every block, and there are the lists to make.  Measured, us, masked /
 // lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
-//   width 128: 8192 queries, blocks of 128, 4 chosen 355 / 134, 1049 / 449; 8 302 / 222, 1056 / 653; 12 299 / 310, 1051 / 909; 16 296 / 377, 1060 / 1116;
+//   width 128: 8192 queries, blocks of 128, 4 chosen 355 / 134, 1049 / 410; 8 302 / 222, 1056 / 590; 12 299 / 310, 1051 / 820; 16 296 / 377, 1060 / 1010;
 //   16384, 256, 8 1112 / 631, 4311 / 2079; 4096, 64, 4 80 / 67, 276 / 190; 8 82 / 99, 288 / 292; 4096, 512, 2 76 / 105, 288 / 332;
 //   8 of 2048, 64, 3 36 / 33, 70 / 72
 //   width 64: 8192, 128, 8 164 / 128, 610 / 306; 16 169 / 219, 618 / 497; 16384, 256, 8 604 / 390, 2394 / 933; 4096, 64, 8 57 / 71, 175 / 153; 4096, 512, 2
 //   54 / 66, 173 / 162; 8 of 2048, 64, 3 22 / 30, 42 / 56
-// so a chosen pair costs (forward) 1.6 + 180 / block of the others, backward 1.5 + 150 / block, of width 64 1.2 + 120 / block, and lists some 20 us
+// so a chosen pair costs (forward) 1.6 + 180 / block of the others, backward 1.1 + 160 / block, of width 64 1.2 + 120 / block, and lists some 20 us
 // more, in which one pair of a device's matrices takes the time given below.  (One device's, whatever the launch covers: the forms add up in
 // different orders.)
 bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
@@ -538,7 +538,7 @@ bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
   if (forced >= 0) return forced != 0;
   const double all = d.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
   const double chosen = d.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
-  const double factor = !bwd ? 1.6 + 180 / B : d.d == 128 ? 1.5 + 150 / B : 1.2 + 120 / B;
+  const double factor = !bwd ? 1.6 + 180 / B : d.d == 128 ? 1.1 + 160 / B : 1.2 + 120 / B;
   const double pair_us = !bwd ? (d.d == 128 ? 5.5e-7 : 3.0e-7) : (d.d == 128 ? 1.9e-6 : 1.1e-6);
   const double pairs = (double)d.nb * d.nh * B * (d.s < b.block ? d.s : B);   // of queries and keys, of a pair of blocks
   return (all - factor * chosen) * pairs * pair_us <= 20.0;

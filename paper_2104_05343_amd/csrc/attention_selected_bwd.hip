@@ -156,6 +156,49 @@ struct GatherLoader {
   }
 };
 
+// 32 x 32 scores (rows: queries, columns: keys) and dP -> P and dS in their place.  l, d, t: of the lane's queries; masked: some are ahead of
+// the key
+__device__ __forceinline__ void list_scores(f32x16& sacc, f32x16& pacc, const float* l, const float* d, const int* t, float scale_log2, bool masked, int key) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const float4 l4 = *(const float4*)(l + 8 * c), d4 = *(const float4*)(d + 8 * c);
+    const int4 t4 = *(const int4*)(t + 8 * c);
+    const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+    const int tv[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * c + e;
+      float p = weight_of(fmaf(sacc[r], scale_log2, -lv[e]));
+      if (masked && tv[e] < key) p = 0.f;
+      sacc[r] = p;
+      pacc[r] = p * (pacc[r] - dv[e]);
+    }
+  }
+}
+__device__ __forceinline__ bool single_piece(const SelectedArgs& a, int mm, int block) {
+  const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1) + block;
+  return first[1] - first[0] == 1;
+}
+// A wavefront's sums of 32 keys from k0 on: of a block's only piece dK or dV themselves, at column `col`, a row after the other through LDS of the
+// wavefront's own (32 rows of D floats); else fp32 rows to `to`.
+template <int D>
+__device__ __forceinline__ void key_sums(const SelectedArgs& a, const SelMatrix& m, const f32x16 (&acc)[D / 32], int k0, int col, float w, bool only,
+                                         float* row, float* to, int lane) {
+  const int g = lane >> 5;
+  if (!only) {
+    store_rows<D / 32>(to, acc, m.len - k0, g, lane);
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) row[(slot(r) + 4 * g) * D + dt * 32 + (lane & 31)] = acc[dt][r] * w;
+  __builtin_amdgcn_wave_barrier();
+  for (int k = g; k < 32; k += 2)
+    write_ordered<D / 32>(a.f.d_qkv + m.qkv + (long long)(k0 + k) * a.f.ld + col, row + k * D, lane & 31, k0 + k < m.len);
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <int D>
 struct SelDkvLds {
   bf16_t tile[2][2][PAIR * D];   // [stage][Q, dO]
@@ -250,21 +293,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
                                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, k & 1 ? vf[k / 2] : kf[k / 2], acc, 0, 0, 0);
                              });
         const int at = par * BLK + t2 * 32 + 4 * g;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float4 l4 = *(const float4*)(lds.l[st] + at + 8 * c), d4 = *(const float4*)(lds.d[st] + at + 8 * c);
-          const int4 t4 = *(const int4*)(lds.t[st] + at + 8 * c);
-          const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
-          const int tv[4] = {t4.x, t4.y, t4.z, t4.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * c + e;
-            float p = weight_of(fmaf(sacc[r], f.scale_log2, -lv[e]));
-            if (masked && tv[e] < key) p = 0.f;
-            sacc[r] = p;
-            pacc[r] = p * (pacc[r] - dv[e]);
-          }
-        }
+        list_scores(sacc, pacc, lds.l[st] + at, lds.d[st] + at, lds.t[st] + at, f.scale_log2, masked, key);
         const bf16x8 pf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)}, dsf[2] = {pack_acc<0>(pacc), pack_acc<1>(pacc)};
         pipelined<4 * DT, 2>([&](int k) { return cols_at<D>(qc, (k & 1 ? 0 : PAIR) + t2 * 32 + k / (2 * DT) * 16, k / 2 % DT); },
                              [&](int k, const bf16x8& x) {
@@ -296,27 +325,150 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
       dkacc[dt][r] += xch[(dt * 16 + r) * 64 + lane];
       dvacc[dt][r] += xch[((DT + dt) * 16 + r) * 64 + lane];
     }
-  const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1) + it.block;
-  if (first[1] - first[0] == 1) {   // the block's only piece: dK and dV themselves, a row of 32 keys after the other through LDS
-    float* row = xch;               // (the wavefront's own part of it, which it has read)
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      const f32x16 (&acc)[DT] = which == 0 ? dkacc : dvacc;
-      const float w = which == 0 ? f.scale : 1.0f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) row[(slot(r) + 4 * g) * D + dt * 32 + (lane & 31)] = acc[dt][r] * w;
-      __builtin_amdgcn_wave_barrier();
-      for (int k = g; k < 32; k += 2)
-        write_ordered<DT>(f.d_qkv + m.qkv + (long long)(k0 + k) * f.ld + (which == 0 ? D : 2 * D), row + k * D, lane & 31, k0 + k < m.len);
-      __builtin_amdgcn_wave_barrier();
-    }
-    return;
-  }
+  const bool only = single_piece(a, mm, it.block);
   float* to = a.key_rows + (((long long)blockIdx.y * a.most[1] + item) * tiles + tile) * (2 * BLK * D) + rg * 32 * D;
-  store_rows<DT>(to, dkacc, m.len - k0, g, lane);
-  store_rows<DT>(to + BLK * D, dvacc, m.len - k0, g, lane);
+  key_sums<D>(a, m, dkacc, k0, D, f.scale, only, xch, to, lane);
+  key_sums<D>(a, m, dvacc, k0, 2 * D, 1.0f, only, xch, to + BLK * D, lane);
+}
+
+// Head width 128, blocks of whole 128 keys: 128 keys, eight wavefronts, as in the attention with changed scores: own V rows and half of the K
+// fragments in LDS, 64 queries at a time, a wavefront half of them.
+struct SelWideLds {
+  bf16_t block[2][2][BLK * 128];   // [stage][Q, dO]
+  bf16_t v[128 * 128], k[128 * 128];
+  alignas(16) float l[2][BLK];
+  alignas(16) float d[2][BLK];
+  alignas(16) int t[2][BLK];
+};
+__global__ __launch_bounds__(512, 2) void selected_dkv_wide_kernel(SelectedArgs a) {
+  constexpr int D = 128, KS = D / 16, DT = D / 32, BKW = 128, KREG = KS / 2;
+  __shared__ __attribute__((aligned(1024))) SelWideLds lds;
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave & 3, par = wave >> 2;
+  const int tiles = a.block / BKW, item = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+  const int mm = a.mat0 + blockIdx.y;
+  ListItem it;
+  if (!list_item(a, 1, mm, item, &it)) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int kt0 = it.block * a.block + tile * BKW;
+  if (kt0 >= m.len) return;
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const bf16_t* Gp = f.d_attn + m.attn;
+  const int k0 = kt0 + rg * 32, key = k0 + (lane & 31), krow = min(key, m.len - 1);
+  bf16x8 kf[KREG];
+#pragma unroll
+  for (int ks = 0; ks < KREG; ++ks) kf[ks] = *(const bf16x8*)(Qp + D + (long long)krow * f.ld + ks * 16 + g * 8);
+  {
+    TileLoader<D, 8, BKW, true> own;
+    own.init(f.ld, wave, lane);
+    own.issue(Qp + 2 * D, kt0, m.len, lds.v);
+    own.issue(Qp + D, kt0, m.len, lds.k);
+  }
+  const int* list = a.list + m.vec * a.count + it.start;
+  const int n_it = (it.pairs + BLK - 1) / BLK;
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    dkacc[dt] = zero16();
+    dvacc[dt] = zero16();
+  }
+  // (a wavefront's 32 rows of a block, and its own 32 rows of V and K)
+  const unsigned in_rows = lds_address(lds.block) + lane_rows<D>(lane) + par * 32 * D * 2, in_cols = lds_address(lds.block) + lane_cols<D>(lane) + par * 32 * D * 2;
+  const unsigned own_rows = lds_address(lds.v) + lane_rows<D>(lane) + rg * 32 * D * 2;
+  GatherLoader<D, 8, BLK> ldr;
+  ldr.wave = wave;
+  ldr.lane = lane;
+  int next_t = 0, row_t = 0;
+  float next_l = 0.f, next_d = 0.f;
+  auto load_numbers = [&](int n) {   // of iteration n
+    ldr.fetch(list, n * BLK, it.pairs);
+    if (tid < BLK) row_t = list[min(n * BLK + tid, it.pairs - 1)];
+  };
+  auto issue = [&](int st) {
+    if (tid < BLK) {
+      next_t = row_t;
+      next_l = f.lse[m.vec + row_t];
+      next_d = f.delta[m.vec + row_t];
+    }
+    ldr.issue(Qp, f.ld, lds.block[st][0]);
+    ldr.issue(Gp, f.ldo, lds.block[st][1]);
+  };
+  auto store_numbers = [&](int n, int st) {   // (past the end of the list: no P)
+    if (tid < BLK) {
+      lds.l[st][tid] = n * BLK + tid < it.pairs ? lse2_of(next_l) : INFINITY;
+      lds.d[st][tid] = next_d;
+      lds.t[st][tid] = next_t;
+    }
+  };
+  load_numbers(0);
+  issue(0);
+  if (n_it > 1) load_numbers(1);
+  store_numbers(0, 0);
+  wait_loads_and_barrier();
+  for (int n = 0; n < n_it; ++n) {
+    const int st = n & 1;
+    if (n + 1 < n_it) {
+      issue(st ^ 1);
+      if (n + 2 < n_it) load_numbers(n + 2);
+    }
+    // (the block's own queries come first: where the first of 32 is behind the keys, all are)
+    const int first_t = __builtin_amdgcn_readfirstlane(lds.t[st][par * 32]);
+    if (n * BLK + par * 32 < it.pairs && k0 < m.len) {
+      const unsigned stage = (unsigned)(st * 2 * BLK * D * 2);
+      const unsigned qt = in_rows + stage, qc = in_cols + stage;
+      const bool masked = a.causal && first_t < k0 + 31;
+      f32x16 sacc = zero16(), pacc = zero16();
+      struct Two { bf16x8 q, own; };
+      pipelined<2 * KS, 2>([&](int k) {
+                             const int ks = k / 2;
+                             Two x;
+                             x.q = rows_at<D>(qt, k & 1 ? BLK : 0, ks);
+                             if (k & 1) x.own = rows_at<D>(own_rows, 0, ks);
+                             else x.own = ks < KREG ? kf[ks < KREG ? ks : 0] : rows_at<D>(own_rows, BKW, ks);
+                             return x;
+                           },
+                           [&](int k, const Two& x) {
+                             f32x16& acc = k & 1 ? pacc : sacc;
+                             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.q, x.own, acc, 0, 0, 0);
+                           });
+      list_scores(sacc, pacc, lds.l[st] + par * 32 + 4 * g, lds.d[st] + par * 32 + 4 * g, lds.t[st] + par * 32 + 4 * g, f.scale_log2, masked, key);
+      const bf16x8 pf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)}, dsf[2] = {pack_acc<0>(pacc), pack_acc<1>(pacc)};
+      pipelined<4 * DT, 2>([&](int k) { return cols_at<D>(qc, (k & 1 ? 0 : BLK) + k / (2 * DT) * 16, k / 2 % DT); },
+                           [&](int k, const bf16x8& x) {
+                             const int dt = k / 2 % DT, u = k / (2 * DT);
+                             f32x16& acc = k & 1 ? dkacc[dt] : dvacc[dt];
+                             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k & 1 ? dsf[u] : pf[u], x, acc, 0, 0, 0);
+                           });
+    }
+    if (n + 1 < n_it) store_numbers(n + 1, st ^ 1);
+    wait_loads_and_barrier();
+  }
+  // the two halves' sums, dV first: the odd one hands over through LDS (64 KiB, all block tiles are free)
+  const bool only = single_piece(a, mm, it.block);
+  float* xch = (float*)&lds.block[0][0][0] + rg * (DT * 16) * 64;
+  float* to = a.key_rows + (((long long)blockIdx.y * a.most[1] + item) * (a.block / BLK) + tile * 2 + (rg >> 1)) * (2 * BLK * D) + (rg & 1) * 32 * D;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    f32x16 (&acc)[DT] = which == 0 ? dvacc : dkacc;
+    if (which == 1) __syncthreads();
+    if (par == 1) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) xch[(dt * 16 + r) * 64 + lane] = acc[dt][r];
+    }
+    __syncthreads();
+    if (par == 0) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[dt][r] += xch[(dt * 16 + r) * 64 + lane];
+      if (which == 0) key_sums<D>(a, m, acc, k0, 2 * D, 1.0f, only, xch, to + BLK * D, lane);
+      else key_sums<D>(a, m, acc, k0, D, f.scale, only, xch, to, lane);
+    }
+  }
 }
 
 // Sums over a key's pieces, in the order of the lists, to dK and dV; zeros where there is none.  (A single piece is written by its workgroup.)
@@ -368,7 +520,10 @@ int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
   }
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.key_portion) {
     const int portion = min(p.key_portion, p.mats - a.mat0);
-    selected_dkv_kernel<D><<<dim3(a.most[1] * (a.block / BLK), portion), 256, 0, st>>>(a);
+    bool wide = false;
+    if constexpr (D == 128) wide = a.block % 128 == 0;
+    if (wide) selected_dkv_wide_kernel<<<dim3(a.most[1] * (a.block / 128), portion), 512, 0, st>>>(a);
+    else selected_dkv_kernel<D><<<dim3(a.most[1] * (a.block / BLK), portion), 256, 0, st>>>(a);
     selected_dkv_combine_kernel<D><<<dim3((s + 7) / 8, portion), 256, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }

@@ -154,11 +154,18 @@ __global__ __launch_bounds__(256) void select_kernel(SelectedArgs a) {
     const bf16_t* means = a.means + (long long)mm * a.blocks * D;
     unsigned long long bad = 0;
     const int end = (others + 8 * PART - 1) / (8 * PART) * (8 * PART);
-    for (int v0 = wave * 32; v0 < end; v0 += 128) {
+    bf16x8 mf[KS];   // (the next 32 means are on their way while these are used)
+    auto load_means = [&](int v0) {
       const bf16_t* p = means + (long long)min(v0 + (lane & 31), others - 1) * D + g * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) mf[ks] = *(const bf16x8*)(p + ks * 16);
+    };
+    load_means(wave * 32);
+    for (int v0 = wave * 32; v0 < end; v0 += 128) {
       f32x16 acc = zero16();
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(p + ks * 16), qf[ks], acc, 0, 0, 0);
+      for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mf[ks], qf[ks], acc, 0, 0, 0);
+      load_means(v0 + 128);
       float zero = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) zero = fmaf(acc[r], 0.f, zero);   // (an infinity or NaN: NaN)

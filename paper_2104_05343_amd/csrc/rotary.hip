@@ -201,6 +201,7 @@ int run(const void* x, void* y, int b, int s, int h, int n, int q, int i, int j,
     const double power = r->shared_ladder ? (double)p / a.pairs : (double)done[k] / r->pairs[k];
     a.axis[p] = (unsigned char)k;
     a.turn[p] = r->scale[k] * pow(r->base, -power) / 6.283185307179586476925;
+    if (!(fabs(a.turn[p]) < 0x1p20)) return OPTIMUS_EINVAL;   // (past it 53 bits hold a large position's whole turns and nothing behind the point)
     --left[k];
     ++done[k];
     if (r->in_turn) k = (k + 1) % r->axes;

@@ -78,6 +78,8 @@ def test_refuses_axes():
     bad = _axes(pairs=(4, 4))
     bad.scale[1] = float("inf")
     assert _rc(bad) == opt.EINVAL
+    bad.scale[1] = 1e7                                    # a position of 2^31 would have no turn behind the point
+    assert _rc(bad) == opt.EINVAL and _rc(_axes(base=1e-9)) == opt.EINVAL
     assert _rc(_axes(pairs=(129,)), h=4 * 512) == opt.ESHAPE
     assert _rc(_axes(pairs=(3,), interleaved=1), h=4 * 9) == opt.ESHAPE        # a head of odd width
     for pairs, scale in (((), None), ((1, 1, 1, 1, 1), None), ((4, 4), [1.0])):

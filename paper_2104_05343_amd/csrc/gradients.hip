@@ -305,7 +305,7 @@ extern "C" size_t optimus_gradient_norm_workspace_bytes(const optimus_gradient* 
 
 extern "C" int optimus_gradient_norm(const optimus_gradient* gradients, int count, float max_norm, float* norm, float* scale, float* norms, void* ws,
                                      size_t ws_bytes, void* stream) {
-  if (!norm) return OPTIMUS_EINVAL;
+  if (!norm || ((uintptr_t)norm | (uintptr_t)scale | (uintptr_t)norms) & 3) return OPTIMUS_EINVAL;
   if (const int rc = check(gradients, count, false)) return rc;
   if (!(max_norm > 0)) return OPTIMUS_EINVAL;
   const long long piece = piece_of(gradients, count), pieces = pieces_of(gradients, count, piece);
@@ -332,7 +332,7 @@ extern "C" int optimus_gradient_norm(const optimus_gradient* gradients, int coun
 }
 
 extern "C" int optimus_gradient_clip(const optimus_gradient* gradients, int count, const float* scale, void* stream) {
-  if (!scale) return OPTIMUS_EINVAL;
+  if (!scale || (uintptr_t)scale & 3) return OPTIMUS_EINVAL;
   if (const int rc = check(gradients, count, true)) return rc;
   const hipStream_t st = (hipStream_t)stream;
   ClipArgs a = {};

@@ -46,6 +46,7 @@ def test_refuses_calls():
     assert _norm([], 0) == _clip([], 0) == opt.ESHAPE and _norm([_g()], -1) == opt.ESHAPE
     assert _norm([_g()], max_norm=0.0) == _norm([_g()], max_norm=-1.0) == _norm([_g()], max_norm=float("nan")) == opt.EINVAL
     assert _norm([_g()], norm=None) == opt.EINVAL and _clip([_g()], scale=None) == opt.EINVAL
+    assert _norm([_g()], norm=4098) == _clip([_g()], scale=4097) == opt.EINVAL
     need = opt.gradient_norm_workspace_bytes((opt.Gradient * 1)(_g()))
     assert need >= 16
     assert _norm([_g()], nbytes=need - 1) == _norm([_g()], ws=None) == _norm([_g()], ws=8196) == opt.EWORKSPACE

@@ -298,7 +298,9 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * lengths: int32 [b] device memory or NULL (all s): tokens of a sequence that count (clamped to 0 .. s).  What qkv and d_attn hold behind them
  * is not looked at, NaN included; there selected is -1, attn 0, lse -infinity and d_qkv 0.
  * P and dS are rounded to bf16 before their products, as the operands are, and what a query gets from one block may be rounded to 11 bits (fp16,
- * scaled) before the blocks' parts are added; scores and sums are fp32; lse enters as in optimus_attention_biased_bwd.  qkv, attn, lse, d_attn, d_qkv, coordinates and limits as in optimus_attention_fused_*; bf16 only;
+ * scaled) before the blocks' parts are added; scores and sums are fp32; lse enters as in optimus_attention_biased_bwd.  The values of tokens
+ * inside the lengths are taken to be finite: a pair that is left out has weight zero, and zero times an infinity or NaN is NaN.
+ * qkv, attn, d_attn, d_qkv (16-byte aligned: EINVAL), lse, coordinates and limits as in optimus_attention_fused_*; bf16 only;
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
  * from call to call: calls that may overlap need one each.  It holds up to 384 MiB of partial results, or one (sequence, head)'s:
@@ -325,7 +327,8 @@ size_t optimus_attention_selected_workspace_bytes(int b, int s, int h, int n, in
  * base^(-k / pairs[axis]) for the k-th pair of its axis, or with shared_ladder base^(-p / P).
  *   angle = positions[axis][token] * scale[axis] * frequency;  (x, y) -> (x cos - y sin, x sin + y cos)
  * The angle is a product of 64 bits, its whole turns are taken off before it is rounded to fp32.  positions: int32 device memory [axes][b*s]
- * (rows sequence-major, every device of a grid row reads the same ones), of any sign; host: scale and base > 0 (finite, EINVAL).
+ * (rows sequence-major, every device of a grid row reads the same ones), of any sign; host: scale and base > 0, finite, scale * frequency below
+ * 2 pi 2^20, 2^20 turns a position (EINVAL).
  * optimus_rotary writes the blocks of `out` whole, values too; out == qkv turns them in place; blocks that overlap otherwise: EINVAL.
  * optimus_rotary_bwd is the gradient, the turn by -angle: of d_out with respect to qkv, in place with d_qkv == d_out.
  * axes 1 .. 4, pairs[] >= 1, P <= 128, 2P <= h/n, even h/n with interleaved, 3h/q <= 2^18 (ESHAPE).  Pointers need the alignment of their elements

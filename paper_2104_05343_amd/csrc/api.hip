@@ -444,6 +444,8 @@ int run_attention_selected(int what, const void* qkv, int32_t* selected, void* a
   AttnDims a;
   AttnSelectedDesc d = {};
   if (const int rc = selected_desc(b, s, h, n, q, i, j, sel, &a, &d)) return rc;
+  // (rows are read, and written to LDS, sixteen bytes at a time)
+  if (((uintptr_t)qkv | (uintptr_t)attn | (uintptr_t)d_attn | (uintptr_t)d_qkv) & 15 || ((uintptr_t)selected | (uintptr_t)lse) & 3) return OPTIMUS_EINVAL;
   if (!ws || ws_bytes < selected_ws_bytes(d) || (uintptr_t)ws & 255) return OPTIMUS_EWORKSPACE;
   AttnFusedDesc& f = d.base;
   f.qkv = (const bf16_t*)qkv + d.dev0 * a.blk_qkv;

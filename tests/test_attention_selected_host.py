@@ -103,6 +103,10 @@ def test_refuses_more():
         for block, count in ((0, 2), (32, 2), (96, 2), (-64, 2), (4160, 2), (64, 0), (64, 65)):
             assert _rc(what, opt.make_selection(block, count)) == opt.ESHAPE
         assert _rc(what, opt.make_selection(64, 2, 4098)) == opt.EINVAL
+        for kw in (dict(qkv=(1 << 20) + 8), dict(selected=(1 << 22) + 2)):
+            assert _rc(what, opt.make_selection(64, 2), **kw) == opt.EINVAL
+    for kw in (dict(attn=(1 << 24) + 8), dict(lse=(1 << 26) + 2), dict(d_attn=(1 << 28) + 2), dict(d_qkv=(1 << 30) + 4)):
+        assert _rc("bwd", opt.make_selection(64, 2), **kw) == opt.EINVAL
     assert _rc("fwd", opt.make_selection(64, 2), attn=None) == _rc("fwd", opt.make_selection(64, 2), lse=None) == opt.EINVAL
     assert _rc("bwd", opt.make_selection(64, 2), d_attn=None) == _rc("bwd", opt.make_selection(64, 2), d_qkv=None) == opt.EINVAL
 

@@ -398,3 +398,103 @@ def test_captured_with_lists(lists):
         r.ws.fill_(0x55)
         r.go()
         assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(got, (r.S, r.O, r.L, r.G)))
+
+
+def test_gradients_of_any_size_with_lists(lists):
+    """Rows of dO from 2^-60 to 2^60 beside each other: a part of dQ is scaled by its row, so that a small row is as exact as a large one."""
+    s, d = 1300, 128
+    r = Run(1, s, d, 1, 1, True, block=64, count=4)
+    rows = 2.0 ** np.random.default_rng(5).integers(-60, 61, (s, 1))
+    r.d_attn = (r.d_attn * rows).astype(np.float32)      # (powers of two: bf16 still)
+    r.dO.copy_(mat_to_dev(r.d_attn, 1, "bf16"))
+    r.go()
+    Q, K, V = (r.qkv[:, k * d:(k + 1) * d].astype(np.float64) for k in range(3))
+    see = oas.seen(r.chosen()[0, 0], s, block=64, causal=True)
+    O, dO = mat_to_host(r.O, s, d, 1).astype(np.float64), r.d_attn.astype(np.float64)
+    want, _, _, P, dS = oas.backward(Q, K, V, dO, O, to_host(r.L).astype(np.float64), see)
+    spread = P * (np.abs(dO) @ np.abs(V).T + (np.abs(dO) * np.abs(O)).sum(1, keepdims=True))
+    raw = np.abs(dS) @ np.abs(K) / np.sqrt(d)
+    small = (FP32 * spread + PART * np.abs(dS)) @ np.abs(K) / np.sqrt(d)
+    got = mat_to_host(r.G, s, 3 * d, 1).astype(np.float64)[:, :d]
+    # (the first query sees itself alone: its dS, a difference of equal numbers, may be all rounding)
+    assert np.all(np.abs(got - want) <= HALF * (1.01 * np.abs(want) + raw) + 2 * small)
+
+
+def test_most_blocks_and_entries():
+    """1024 blocks and 64 of them, the most of both, captured too: more LDS than a launch has without asking."""
+    s, d = 65536, 64
+    r = Run(1, s, d, 1, 1, True, block=64, count=64)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.choose()
+    g.replay()
+    torch.cuda.synchronize()
+    first = r.chosen()[0, 0].copy()
+    r.S.fill_(-9)
+    r.go()
+    assert np.array_equal(first, r.chosen()[0, 0])
+    Q, K, V = (r.qkv[:, k * d:(k + 1) * d].astype(np.float64) for k in range(3))
+    O, L, mean = mat_to_host(r.O, s, d, 1).astype(np.float64), to_host(r.L).astype(np.float64), oas.means(K, 64, s)
+    for t in [0, 63, 64, 64 * 63, 64 * 64, 64 * 65, 30001, 65472, s - 1]:
+        score = mean[:t // 64] @ Q[t]
+        best = sorted(sorted(range(t // 64), key=lambda v: (-score[v], v))[:63] + [t // 64])
+        assert list(first[t]) == best + [-1] * (64 - len(best))
+        keys = np.concatenate([np.arange(v * 64, min((v + 1) * 64, t + 1)) for v in best])
+        x = K[keys] @ Q[t] / 8
+        p = np.exp(x - x.max())
+        lse, p = x.max() + np.log(p.sum()), p / p.sum()
+        assert abs(L[t] - lse) <= 1e-5 * max(1, abs(lse))
+        assert np.all(np.abs(O[t] - p @ V[keys]) <= HALF * (1.01 * np.abs(p @ V[keys]) + p @ np.abs(V[keys])) + (FP32 + PART) * (p @ np.abs(V[keys])))
+
+
+@pytest.mark.parametrize("form_of,block", [(0, 128), (0, 512), (1, 512)])
+def test_rows_past_four_gigabytes(form_of, block):
+    """131072 rows of 64 heads of 128: a matrix' last rows lie 6 GB behind its first.  A query attends to its own block and the one in front;
+    the last blocks' outputs and gradients against their own rows."""
+    s, n, d, count = 131072, 64, 128, 2
+    torch.manual_seed(3)
+    x = torch.randn(s, n, 3, d, dtype=torch.bfloat16, device=DEV)
+    dO = torch.randn(s, n, d, dtype=torch.bfloat16, device=DEV)
+    O, G, L = torch.empty_like(dO), torch.full_like(x, float("nan")), torch.empty(n, s, dtype=torch.float32, device=DEV)
+    own = torch.arange(s, dtype=torch.int32, device=DEV) // block
+    S = torch.stack((own - 1, own), 1).expand(n, s, count).contiguous()
+    sel = opt.make_selection(block, count)
+    ws = torch.empty(opt.attention_selected_workspace_bytes(1, s, n * d, n, 1, -1, -1, sel), dtype=torch.uint8, device=DEV)
+    args = (1, s, n * d, n, 1, -1, -1, True, opt.BF16, sel, ws)
+    opt.debug_set_attention_selected_form(form_of)
+    try:
+        print("far rows", form_of, block, flush=True)
+        opt.attention_selected_fwd(x, S, O, L, *args)
+        opt.attention_selected_bwd(x, S, O, L, dO, G, *args)
+        torch.cuda.synchronize()
+    finally:
+        opt.debug_set_attention_selected_form(-1)
+    assert not torch.isnan(G).any()
+    chosen = torch.empty_like(S)
+    opt.attention_select(x, chosen, *args)
+    torch.cuda.synchronize()
+    rows = 2 * block                                    # keys of the first of them are those of queries in front, too
+    lo = s - rows
+    q = np.arange(s - rows, s)
+    see = (q[:, None] >= q[None]) & (q[:, None] // block - q[None] // block <= 1)
+    for head in (0, 31, 63):
+        Q, K, V = (x[lo:, head, k].cpu().float().numpy().astype(np.float64) for k in range(3))
+        half = slice(block, rows)                       # queries that see these two blocks alone, keys that only they see
+        g, o = dO[lo:, head].cpu().float().numpy().astype(np.float64), O[lo:, head].cpu().float().numpy().astype(np.float64)
+        want, lse, P = oas.forward(Q, K, V, see)
+        size = P @ np.abs(V)
+        assert np.all(np.abs(L[head, lo:].cpu().numpy() - lse)[half] <= 1e-5 * np.maximum(1, np.abs(lse[half])))
+        assert np.all((np.abs(o - want) <= HALF * (1.01 * np.abs(want) + size) + (FP32 + PART) * size)[half])
+        dQ, dK, dV, P, dS = oas.backward(Q, K, V, g, o, L[head, lo:].cpu().numpy().astype(np.float64), see)
+        spread = P * (np.abs(g) @ np.abs(V).T + (np.abs(g) * np.abs(o)).sum(1, keepdims=True))
+        raw, fine = np.abs(dS), FP32 * spread
+        for k, (w, size, small) in enumerate(((dQ, raw @ np.abs(K) / np.sqrt(d), (fine + PART * raw) @ np.abs(K) / np.sqrt(d)),
+                                              (dK, raw.T @ np.abs(Q) / np.sqrt(d), fine.T @ np.abs(Q) / np.sqrt(d)),
+                                              (dV, P.T @ np.abs(g), FP32 * P.T @ np.abs(g)))):
+            got = G[lo:, head, k].cpu().float().numpy().astype(np.float64)
+            assert np.all((np.abs(got - w) <= HALF * (1.01 * np.abs(w) + size) + 2 * small + 1e-30)[half]), (head, "QKV"[k])
+        # the choice: the last row's, by its own scores
+        mean = oas.means(x[:, head, 1].cpu().float().numpy(), block, s)
+        score = mean[:-1] @ Q[-1]
+        best = int(np.argmax(score))
+        assert chosen[head, -1].tolist() == [best, (s - 1) // block]

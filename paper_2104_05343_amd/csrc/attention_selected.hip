@@ -171,9 +171,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int mm = a.mat0 + blockIdx.y;
+  const int unit = blockIdx.x / a.portion, matrix = blockIdx.x % a.portion, mm = a.mat0 + matrix;
   ListItem it;
-  if (!list_item(a, 0, mm, blockIdx.x, &it)) return;
+  if (!list_item(a, 0, mm, unit, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const bf16_t* Qp = f.qkv + m.qkv;
   const int key0 = it.block * a.block, last = m.len - 1;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
     ldr.issue(Qp + 2 * D, key0 + st * BLK, m.len, lds[st][1]);
   }
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
-  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
+  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = matrix * pairs + it.start;
   const int* list = a.list + first;
   // a tile's queries are requested a tile ahead, their numbers two, and past the end too: the last one again
   const int row = wave * 32 + (lane & 31);
@@ -259,9 +259,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int mm = a.mat0 + blockIdx.y;
+  const int unit = blockIdx.x / a.portion, matrix = blockIdx.x % a.portion, mm = a.mat0 + matrix;
   ListItem it;
-  if (!list_item(a, 0, mm, blockIdx.x, &it)) return;
+  if (!list_item(a, 0, mm, unit, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const bf16_t* Qp = f.qkv + m.qkv;
   const int key0 = it.block * a.block, last = m.len - 1;
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
   };
   issue(0, 0);
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane) + BLK * D * 2;
-  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
+  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = matrix * pairs + it.start;
   const int* list = a.list + first;
   const int row = wave * 32 + (lane & 31);
   wait_loads_and_barrier();
@@ -503,8 +503,9 @@ void launch_lists(const SelectedArgs& a, hipStream_t st) {
 }
 
 template <int D>
-void fwd_launch(const SelectedArgs& a, int portion, hipStream_t st) {
-  const dim3 grid(a.most[0], portion);
+void fwd_launch(const SelectedArgs& a, hipStream_t st) {
+  const int portion = a.portion;
+  const dim3 grid(a.most[0] * portion);
   if (a.block == 64) selected_fwd_kernel<D, 2><<<grid, 256, 0, st>>>(a);
   else if (a.block == 128) selected_fwd_kernel<D, 4><<<grid, 256, 0, st>>>(a);
   else selected_fwd_long_kernel<D><<<grid, 256, 0, st>>>(a);
@@ -513,8 +514,8 @@ void fwd_launch(const SelectedArgs& a, int portion, hipStream_t st) {
 
 }  // namespace
 
-void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipStream_t st) {
-  const dim3 grid((a.f.s + 7) / 8, portion);
+void launch_selected_dq_combine(const SelectedArgs& a, int d, hipStream_t st) {
+  const dim3 grid((a.f.s + 7) / 8, a.portion);
   if (d == 64) selected_combine_kernel<64, false><<<grid, 256, 0, st>>>(a);
   else selected_combine_kernel<128, false><<<grid, 256, 0, st>>>(a);
 }
@@ -601,9 +602,9 @@ int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
   }
   launch_lists(a, st);
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
-    const int portion = min(p.portion, p.mats - a.mat0);
-    if (b.base.d == 64) fwd_launch<64>(a, portion, st);
-    else fwd_launch<128>(a, portion, st);
+    a.portion = min(p.portion, p.mats - a.mat0);
+    if (b.base.d == 64) fwd_launch<64>(a, st);
+    else fwd_launch<128>(a, st);
     if (const int rc = hip_launch_status()) return rc;
   }
   return OPTIMUS_OK;

@@ -57,9 +57,9 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int mm = a.mat0 + blockIdx.y;
+  const int unit = blockIdx.x / a.portion, matrix = blockIdx.x % a.portion, mm = a.mat0 + matrix;
   ListItem it;
-  if (!list_item(a, 0, mm, blockIdx.x, &it)) return;
+  if (!list_item(a, 0, mm, unit, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
   const bf16_t* Qp = f.qkv + m.qkv;
   const bf16_t* Gp = f.d_attn + m.attn;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
 #pragma unroll
   for (int st = 0; st < (KT ? STAGES : 1); ++st) issue(st, st);
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane);
-  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = blockIdx.y * pairs + it.start;
+  const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = matrix * pairs + it.start;
   const int* list = a.list + first;
   const int row = wave * 32 + (lane & 31);
   bf16x8 qf[KS], dof[KS];
@@ -215,8 +215,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % NRG, par = wave / NRG;
-  const int tiles = a.block / BLK, item = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-  const int mm = a.mat0 + blockIdx.y;
+  const int unit = blockIdx.x / a.portion, matrix = blockIdx.x % a.portion, mm = a.mat0 + matrix;
+  const int tiles = a.block / BLK, item = unit / tiles, tile = unit % tiles;
   ListItem it;
   if (!list_item(a, 1, mm, item, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
       dvacc[dt][r] += xch[((DT + dt) * 16 + r) * 64 + lane];
     }
   const bool only = single_piece(a, mm, it.block);
-  float* to = a.key_rows + (((long long)blockIdx.y * a.most[1] + item) * tiles + tile) * (2 * BLK * D) + rg * 32 * D;
+  float* to = a.key_rows + (((long long)matrix * a.most[1] + item) * tiles + tile) * (2 * BLK * D) + rg * 32 * D;
   key_sums<D>(a, m, dkacc, k0, D, f.scale, only, xch, to, lane);
   key_sums<D>(a, m, dvacc, k0, 2 * D, 1.0f, only, xch, to + BLK * D, lane);
 }
@@ -347,8 +347,8 @@ __global__ __launch_bounds__(512, 2) void selected_dkv_wide_kernel(SelectedArgs 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave & 3, par = wave >> 2;
-  const int tiles = a.block / BKW, item = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-  const int mm = a.mat0 + blockIdx.y;
+  const int unit = blockIdx.x / a.portion, matrix = blockIdx.x % a.portion, mm = a.mat0 + matrix;
+  const int tiles = a.block / BKW, item = unit / tiles, tile = unit % tiles;
   ListItem it;
   if (!list_item(a, 1, mm, item, &it)) return;
   const SelMatrix m = selected_matrix<D>(a, mm);
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(512, 2) void selected_dkv_wide_kernel(SelectedArgs 
   // the two halves' sums, dV first: the odd one hands over through LDS (64 KiB, all block tiles are free)
   const bool only = single_piece(a, mm, it.block);
   float* xch = (float*)&lds.block[0][0][0] + rg * (DT * 16) * 64;
-  float* to = a.key_rows + (((long long)blockIdx.y * a.most[1] + item) * (a.block / BLK) + tile * 2 + (rg >> 1)) * (2 * BLK * D) + (rg & 1) * 32 * D;
+  float* to = a.key_rows + (((long long)matrix * a.most[1] + item) * (a.block / BLK) + tile * 2 + (rg >> 1)) * (2 * BLK * D) + (rg & 1) * 32 * D;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     f32x16 (&acc)[DT] = which == 0 ? dvacc : dkacc;
@@ -510,20 +510,20 @@ int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
   const int s = a.f.s;
   selected_delta_kernel<D><<<dim3((s + 127) / 128, p.mats), 256, 0, st>>>(a);
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
-    const int portion = min(p.portion, p.mats - a.mat0);
-    const dim3 grid(a.most[0], portion);
+    a.portion = min(p.portion, p.mats - a.mat0);
+    const dim3 grid(a.most[0] * a.portion);
     if (a.block == 64) selected_dq_kernel<D, 2><<<grid, 256, 0, st>>>(a);
     else if (a.block == 128) selected_dq_kernel<D, 4><<<grid, 256, 0, st>>>(a);
     else selected_dq_kernel<D, 0><<<grid, 256, 0, st>>>(a);
-    launch_selected_dq_combine(a, D, portion, st);
+    launch_selected_dq_combine(a, D, st);
     if (const int rc = hip_launch_status()) return rc;
   }
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.key_portion) {
-    const int portion = min(p.key_portion, p.mats - a.mat0);
+    const int portion = a.portion = min(p.key_portion, p.mats - a.mat0);
     bool wide = false;
     if constexpr (D == 128) wide = a.block % 128 == 0;
-    if (wide) selected_dkv_wide_kernel<<<dim3(a.most[1] * (a.block / 128), portion), 512, 0, st>>>(a);
-    else selected_dkv_kernel<D><<<dim3(a.most[1] * (a.block / BLK), portion), 256, 0, st>>>(a);
+    if (wide) selected_dkv_wide_kernel<<<a.most[1] * (a.block / 128) * portion, 512, 0, st>>>(a);
+    else selected_dkv_kernel<D><<<a.most[1] * (a.block / BLK) * portion, 256, 0, st>>>(a);
     selected_dkv_combine_kernel<D><<<dim3((s + 7) / 8, portion), 256, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }

@@ -39,7 +39,7 @@ struct SelectedArgs {
   int mask_words;                      // of a block's queries, 32 a word
   unsigned* mask;                      // [matrix][block][mask_words]: whether a query has chosen the block
   // lists
-  int mats, mat0;                      // matrices of the call, first one of this launch
+  int mats, mat0, portion;             // matrices of the call, first one of this launch, how many it has
   int chunks;                          // kListChunk pieces of a sequence
   int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, most items of a matrix
   int* counts;                         // [matrix][chunk][block]: pairs; then pairs of earlier chunks of the block
@@ -65,7 +65,7 @@ struct SelectedPlan {
 
 // csrc/attention_selected*.hip
 int launch_selected_bwd_kernels(const SelectedArgs& a, const SelectedPlan& p, int d, hipStream_t st);
-void launch_selected_dq_combine(const SelectedArgs& a, int d, int portion, hipStream_t st);
+void launch_selected_dq_combine(const SelectedArgs& a, int d, hipStream_t st);
 void launch_selected_masked(const SelectedArgs& a, int mats, int d, bool bwd, hipStream_t st);
 
 namespace {
@@ -224,7 +224,8 @@ __device__ __forceinline__ void write_row(bf16_t* to, const typename RowPart<DT>
   __builtin_amdgcn_wave_barrier();
 }
 
-// Work of a workgroup: a block and a piece of its list.
+// Work of a workgroup: a block and a piece of its list.  Workgroups count the matrices of a launch first: neighbours go to the eight dies in turn,
+// so that (of a multiple of eight) each die's L2 has the queries of its own ones.
 struct ListItem {
   int block, start, pairs;
 };

@@ -520,29 +520,38 @@ void launch_selected_dq_combine(const SelectedArgs& a, int d, hipStream_t st) {
   else selected_combine_kernel<128, false><<<grid, 256, 0, st>>>(a);
 }
 
-// Which form.  The masked one computes all pairs of queries and keys (causal: half of them), lists the chosen ones, each of which costs as much
-// as some of the others: its part of a row goes through memory once for every block, and there are the lists to make.  Measured, us, masked /
-// lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
-//   width 128: 8192 queries, blocks of 128, 4 chosen 355 / 134, 1049 / 410; 8 302 / 222, 1056 / 590; 12 299 / 310, 1051 / 820; 16 296 / 377, 1060 / 1010;
-//   16384, 256, 8 1112 / 631, 4311 / 2079; 4096, 64, 4 80 / 67, 276 / 190; 8 82 / 99, 288 / 292; 4096, 512, 2 76 / 105, 288 / 332;
-//   8 of 2048, 64, 3 36 / 33, 70 / 72
-//   width 64: 8192, 128, 8 164 / 128, 610 / 306; 16 169 / 219, 618 / 497; 16384, 256, 8 604 / 390, 2394 / 933; 4096, 64, 8 57 / 71, 175 / 153; 4096, 512, 2
-//   54 / 66, 173 / 162; 8 of 2048, 64, 3 22 / 30, 42 / 56
-// so a chosen pair costs (forward) 1.6 + 180 / block of the others, backward 1.1 + 160 / block, of width 64 1.2 + 120 / block, and lists some 20 us
-// more, in which one pair of a device's matrices takes the time given below.  (One device's, whatever the launch covers: the forms add up in
-// different orders.)
+// Which form: the one that should take less time, by what both have taken.  The masked one computes all pairs of queries and keys (causal: half of
+// them) at a rate, and its longest workgroup walks over all keys.  Lists compute the chosen pairs at more each, as a block's part of a row goes
+// through memory once a block, and have a price a call and a query for the lists and the sums.
+// Measured, us, masked / lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
+//   width 128: 8192 queries, blocks of 128, 4 chosen 350 / 126, 1044 / 327; 8 303 / 203, 1060 / 490; 12 291 / 293, 1060 / 682; 16 294 / 354, 1066 / 829;
+//   16384, 256, 8 1129 / 627, 4298 / 1516; 4096, 64, 4 82 / 60, 278 / 162; 14 83 / 141, 295 / 349; 4096, 512, 2 80 / 81, 290 / 204;
+//   one of 1024, 64, 4 21 / 24, 38 / 58; 8192, 128, 24 116 / 67, 213 / 128; no mask, 4096, 128, 10 145 / 121, 548 / 329
+//   width 64: 8192, 128, 8 167 / 120, 614 / 274; 16 173 / 204, 623 / 455; 16384, 256, 8 597 / 351, 2424 / 868; 4096, 64, 8 57 / 64, 177 / 131; 4096, 512, 2
+//   56 / 61, 176 / 142; one of 1024, 64, 4 14 / 25, 24 / 46; 8192, 128, 24 70 / 55, 133 / 95
+// (104 such pairs: the form taken was never more than 1.06 times the other one's time.  Queries are those of one device's matrices, whatever the
+// launch covers: the forms add up in different orders.)
+struct FormCost {
+  double masked_pair, masked_call, masked_row;          // us: a pair; the longest workgroup's start and each row that it walks over
+  double lists_call, lists_query, lists_pair, by_block; // us; a chosen pair, in masked ones, lists_pair + by_block / block
+};
+constexpr FormCost kFormCost[2][2] = {   // [forward, backward][width 64, 128]
+    {{2.8e-7, 6, 0.008, 25, 1.2e-4, 1.6, 128}, {5.0e-7, 6, 0.0138, 25, 1.2e-4, 1.55, 137}},
+    {{1.1e-6, 10, 0.015, 50, 3.5e-4, 1.1, 45}, {1.9e-6, 12, 0.024, 60, 6e-4, 1.05, 65}}};
 bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
   const AttnFusedDesc& d = b.base;
   const double blocks = (d.s + b.block - 1) / b.block, k = b.count < blocks ? b.count : blocks, B = b.block;
   if (blocks > kMaskedBlocks) return false;
   const int forced = g_form.load(std::memory_order_relaxed);
   if (forced >= 0) return forced != 0;
+  FormCost c = kFormCost[bwd][d.d == 128];
+  if (bwd && d.d == 128 && b.block % 128 != 0) c.by_block = 105;   // (dK and dV of 64 keys at a time)
   const double all = d.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
   const double chosen = d.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
-  const double factor = !bwd ? 1.6 + 180 / B : d.d == 128 ? 1.1 + 160 / B : 1.2 + 120 / B;
-  const double pair_us = !bwd ? (d.d == 128 ? 5.5e-7 : 3.0e-7) : (d.d == 128 ? 1.9e-6 : 1.1e-6);
-  const double pairs = (double)d.nb * d.nh * B * (d.s < b.block ? d.s : B);   // of queries and keys, of a pair of blocks
-  return (all - factor * chosen) * pairs * pair_us <= 20.0;
+  const double matrices = (double)d.nb * d.nh, pairs = matrices * B * (d.s < b.block ? d.s : B);   // of queries and keys, of a pair of blocks
+  const double masked = hypot(all * pairs * c.masked_pair, c.masked_call + d.s * c.masked_row);   // (the longest one counts where few run)
+  const double lists = c.lists_call + matrices * d.s * c.lists_query + chosen * pairs * c.masked_pair * (c.lists_pair + c.by_block / B);
+  return masked <= lists;
 }
 void attn_selected_set_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 

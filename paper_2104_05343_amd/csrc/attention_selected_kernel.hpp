@@ -4,7 +4,7 @@
 // The choice is one step (attention_select.hip), the attention over any chosen blocks another (attention_selected.hip forward,
 // attention_selected_bwd.hip backward); tiles, fragments and layouts are those of the fused attention (attention_fused_kernel.hpp).
 //
-// Where queries choose a third and more of the blocks that they could, it is the fused attention with a mask (attention_selected_masked.hip).
+// Where queries choose many of the blocks that they could, it is the fused attention with a mask (attention_selected_masked.hip).
 //
 // How the work is cut otherwise.  Neighbouring queries choose different blocks, so a tile of queries has no common keys to load and a tile of the dense
 // attention would be mostly masked.  The other way round a block of keys has a list of the queries that chose it.  A workgroup takes a

@@ -1,5 +1,5 @@
-// Attention over chosen blocks as the fused attention with a mask (attention_selected_kernel.hpp): where queries choose a third and more of
-// the blocks that they could, all tiles of the matrix are computed and blocks that a row has not chosen get weight zero.  No lists, no
+// Attention over chosen blocks as the fused attention with a mask (attention_selected_kernel.hpp): where queries choose many of the blocks that
+// they could, all tiles of the matrix are computed and blocks that a row has not chosen get weight zero.  No lists, no
 // partial results.  A row's choice is a bit a block; that a row has not chosen a block costs nothing a score: its maximum, or the
 // log-sum-exp that is subtracted, is infinite for the time of the block.
 #include "attention_selected_kernel.hpp"

@@ -136,7 +136,7 @@ def test_form(form):
     def masked(s, block, count, causal, backward=False, b=1, h=2048, n=16):
         return opt.debug_attention_selected_masked(backward, b, s, h, n, 1, 0, 0, causal, opt.make_selection(block, count))
     for backward in (False, True):
-        assert masked(1, 64, 1, True, backward) and masked(200, 64, 3, False, backward) and masked(4096, 128, 8, True, backward)
+        assert masked(1, 64, 1, True, backward) and masked(200, 64, 3, False, backward) and masked(4096, 128, 8, True, backward) != backward
         assert not masked(32768, 128, 16, True, backward) and not masked(8192, 128, 4, True, backward)
         assert masked(16384, 64, 64, True, backward) and not masked(16385, 64, 64, True, backward)              # 256 and 257 blocks
         # the same for one device, whatever the launch covers

@@ -301,7 +301,7 @@ def test_captured_and_on_another_stream(form):
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(got, (r.S, r.O, r.L, r.G)))
 
 
-def test_portions():
+def test_portions(lists):
     """Partial results beyond the workspace's portion: more (sequence, head)s than go at a time, the same bits as one of them alone."""
     b, s, n, d = 8, 4096, 4, 128
     many = Run(b, s, n * d, n, 1, True, block=128, count=8).go()          # 32 times 17 MB

@@ -219,13 +219,13 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
     }
     float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int t2 = 0; t2 < KT; ++t2) mx = scale_scores(sacc[t2], f.scale_log2, mx);
-    mx = halfwave_max(mx);   // (a listed query sees the block's first key)
+    for (int t2 = 0; t2 < KT; ++t2) mx = largest(sacc[t2], mx);
+    mx = halfwave_max(mx) * f.scale_log2;   // (a listed query sees the block's first key)
 #pragma unroll
     for (int t2 = 0; t2 < KT; ++t2)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(sacc[t2][r] - mx);
+        const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], f.scale_log2, -mx));
         sacc[t2][r] = p;
         sum += p;
       }
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
 #pragma unroll
             for (int r = 0; r < 16; ++r) sacc[t2][r] = 32 * t2 + slot(r) > reach ? -INFINITY : sacc[t2][r];
         }
-        const float mx = halfwave_max(scale_scores(sacc[1], f.scale_log2, scale_scores(sacc[0], f.scale_log2, -INFINITY)));
+        const float mx = halfwave_max(largest(sacc[1], largest(sacc[0], -INFINITY))) * f.scale_log2;
         // The maximum follows the step's when that is above it by more than 8: a step's largest term is at most 2^8 then.
         const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
         const float m_new = move ? fmaxf(m_run, mx) : m_run;
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
         for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(sacc[t2][r] - m_new);
+            const float e = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], f.scale_log2, -m_new));
             sacc[t2][r] = e;
             sum += e;
           }

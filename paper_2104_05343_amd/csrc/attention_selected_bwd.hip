@@ -39,12 +39,13 @@ __device__ __forceinline__ void dq_scores(bf16x8 (&dsf)[2], unsigned kt, const b
                          f32x16& acc = n & 1 ? pacc : sacc;
                          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, n & 1 ? dof[n / 2] : qf[n / 2], acc, 0, 0, 0);
                        });
+  if (masked) {   // (few tiles: the asm keeps the compiler from comparing in all of them)
+    asm volatile("");
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    float p = weight_of(fmaf(sacc[r], scale_log2, -lse2));
-    if (masked && slot(r) > reach) p = 0.f;
-    sacc[r] = p * (pacc[r] - delta);
+    for (int r = 0; r < 16; ++r) sacc[r] = slot(r) > reach ? -INFINITY : sacc[r];
   }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) sacc[r] = weight_of(fmaf(sacc[r], scale_log2, -lse2)) * (pacc[r] - delta);
   dsf[0] = pack_acc<0>(sacc);
   dsf[1] = pack_acc<1>(sacc);
 }
@@ -159,17 +160,24 @@ struct GatherLoader {
 // 32 x 32 scores (rows: queries, columns: keys) and dP -> P and dS in their place.  l, d, t: of the lane's queries; masked: some are ahead of
 // the key
 __device__ __forceinline__ void list_scores(f32x16& sacc, f32x16& pacc, const float* l, const float* d, const int* t, float scale_log2, bool masked, int key) {
+  if (masked) {   // (few tiles: the asm keeps the compiler from comparing in all of them)
+    asm volatile("");
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int4 t4 = *(const int4*)(t + 8 * c);
+      const int tv[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sacc[4 * c + e] = tv[e] < key ? -INFINITY : sacc[4 * c + e];
+    }
+  }
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const float4 l4 = *(const float4*)(l + 8 * c), d4 = *(const float4*)(d + 8 * c);
-    const int4 t4 = *(const int4*)(t + 8 * c);
     const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
-    const int tv[4] = {t4.x, t4.y, t4.z, t4.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 4 * c + e;
-      float p = weight_of(fmaf(sacc[r], scale_log2, -lv[e]));
-      if (masked && tv[e] < key) p = 0.f;
+      const float p = weight_of(fmaf(sacc[r], scale_log2, -lv[e]));
       sacc[r] = p;
       pacc[r] = p * (pacc[r] - dv[e]);
     }

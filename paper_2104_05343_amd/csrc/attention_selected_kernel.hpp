@@ -127,14 +127,12 @@ __device__ __forceinline__ void swap_rows(float& a, float& b) {
   a = __uint_as_float(r[0]);
   b = __uint_as_float(r[1]);
 }
-// scores times w, and the largest of them and m: products are known to be no signalling NaN, of which every maximum of a matrix instruction's
-// results would be cleared by an instruction of its own, and rounded before the maximum is subtracted scores of any size have exponents up to zero
-__device__ __forceinline__ float scale_scores(f32x16& v, float w, float m) {
+// The maximum that passes NaN on: two operands or three an instruction.  (fmaxf first clears signalling NaN out of every operand that might be one,
+// such as a matrix instruction's result, by an instruction of its own.)
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+__device__ __forceinline__ float largest(const f32x16& v, float m) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    v[r] *= w;
-    m = fmaxf(m, v[r]);
-  }
+  for (int r = 0; r < 16; r += 2) m = larger(larger(m, v[r]), v[r + 1]);
   return m;
 }
 template <int DT>
@@ -145,30 +143,29 @@ __device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x1
   float most[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    most[r] = fabsf(acc[0][r]);
-#pragma unroll
-    for (int dt = 1; dt < DT; ++dt) most[r] = fmaxf(most[r], fabsf(acc[dt][r]));
+    most[r] = larger(fabsf(acc[0][r]), fabsf(acc[1][r]));
+    if constexpr (DT == 4) most[r] = larger(larger(most[r], fabsf(acc[2][r])), fabsf(acc[3][r]));
   }
 #pragma unroll
   for (int r = 0; r < 8; ++r) {   // rows r and r + 8: lanes 0 .. 15 keep the first
     swap_rows(most[r], most[r + 8]);
-    most[r] = fmaxf(most[r], most[r + 8]);
+    most[r] = larger(most[r], most[r + 8]);
   }
   const bool upper = lane & 8;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {   // rows r and r + 4: every other eight lanes
     const float keep = upper ? most[r + 4] : most[r], give = upper ? most[r] : most[r + 4];
-    most[r] = fmaxf(keep, lane_moved<0x128>(give));
-    most[r] = fmaxf(most[r], lane_moved<0xB1>(most[r]));
-    most[r] = fmaxf(most[r], lane_moved<0x4E>(most[r]));
-    most[r] = fmaxf(most[r], lane_moved<0x141>(most[r]));
+    most[r] = larger(keep, lane_moved<0x128>(give));
+    most[r] = larger(most[r], lane_moved<0xB1>(most[r]));
+    most[r] = larger(most[r], lane_moved<0x4E>(most[r]));
+    most[r] = larger(most[r], lane_moved<0x141>(most[r]));
   }
   // a lane's four rows are r + 4 (lane / 8 % 4).  2^(141 - e) for a largest number of biased exponent e
   float scale[16];
   float4 unit;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const int e = min(max((int)(__float_as_uint(most[r]) >> 23), 16), 254);
+    const int e = min(max((int)(__float_as_uint(most[r]) >> 23 & 255), 16), 254);
     scale[r] = __uint_as_float((unsigned)(268 - e) << 23);
     (&unit.x)[r] = __uint_as_float((unsigned)(e - 14) << 23);
   }

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
 #pragma unroll
           for (int r = 0; r < 16; ++r) sacc[t2][r] = 32 * t2 + slot(r) > reach ? -INFINITY : sacc[t2][r];
       }
-      float mx = halfwave_max(scale_scores(sacc[1], f.scale_log2, scale_scores(sacc[0], f.scale_log2, -INFINITY)));
+      float mx = halfwave_max(largest(sacc[1], largest(sacc[0], -INFINITY))) * f.scale_log2;
       mx = chosen ? mx : -INFINITY;
       const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
       const float m_new = move ? fmaxf(m_run, mx) : m_run;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
       for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(sacc[t2][r] + off);
+          const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], f.scale_log2, off));
           sacc[t2][r] = p;
           sum += p;
         }

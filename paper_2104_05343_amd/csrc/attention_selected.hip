@@ -17,16 +17,30 @@ constexpr size_t kPortion = (size_t)384 << 20;    // bytes of partial results in
 __device__ __forceinline__ bool sees(const SelectedArgs& a, int len, int t, int v) {
   return v >= 0 && v < a.blocks && v * a.block < len && (!a.causal || v * a.block <= t);
 }
+// eight of a query's entries from e0 on, -1 behind the last; as found: a choice may start at any element
+__device__ __forceinline__ void load_entries(const int* own, int e0, int count, int v[8]) {
+  typedef __attribute__((ext_vector_type(4), aligned(4))) int Four;
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    if (e0 + h + 4 <= count) {
+      const Four x = *(const Four*)(own + e0 + h);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[h + u] = x[u];
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[h + u] = e0 + h + u < count ? own[e0 + h + u] : -1;
+    }
+  }
+}
 // The thread's query's entries into `bits` (zeroed); of the same block the first counts: entry(e, block, counts).
 template <class F>
 __device__ __forceinline__ void chunk_pairs(const SelectedArgs& a, int mm, int len, int t, unsigned* bits, F entry) {
   const int tid = threadIdx.x;
   if (t >= len) return;
   const int* own = a.selected + ((long long)mm * a.f.s + t) * a.count;
-  for (int e0 = 0; e0 < a.count; e0 += 8) {   // eight loads in flight
+  for (int e0 = 0; e0 < a.count; e0 += 8) {
     int v[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = e0 + u < a.count ? own[e0 + u] : -1;
+    load_entries(own, e0, a.count, v);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       bool counts = false;
@@ -77,18 +91,45 @@ __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
   return before + in - x;
 }
 
+// rowsum(dO * O) of a wavefront's 32 queries from t0 on, 0 past the end of a sequence
+template <int D>
+__device__ __forceinline__ void delta_rows(const SelectedArgs& a, int mm, int t0) {
+  const FusedArgs& f = a.f;
+  const int lane = threadIdx.x & 63, g = lane >> 5;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int t = t0 + (lane & 31), row = min(t, f.s - 1);
+  float delta = 0.f;
+  if (t < m.len) {
+    const bf16_t* G = f.d_attn + m.attn + (long long)row * f.ldo + g * 8;
+    const bf16_t* O = f.attn + m.attn + (long long)row * f.ldo + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) delta += delta_piece(*(const bf16x8*)(G + ks * 16), *(const bf16x8*)(O + ks * 16));
+  }
+  delta = halfwave_sum(delta);
+  if (g == 0 && t < f.s) f.delta[m.vec + t] = delta;
+}
+
+// A workgroup a matrix.  D > 0, ahead of a backward pass: workgroups behind them take 512 queries' delta, which needs no list.
+template <int D>
 __global__ __launch_bounds__(1024) void list_places_kernel(SelectedArgs a) {
   __shared__ int lds[16];
+  if constexpr (D > 0) {
+    if ((int)blockIdx.x >= a.mats) {
+      const int groups = (a.f.s + 511) / 512, k = blockIdx.x - a.mats;
+      delta_rows<D>(a, k / groups, k % groups * 512 + (threadIdx.x >> 6) * 32);
+      return;
+    }
+  }
   const int mm = blockIdx.x, v = threadIdx.x;
   int n = 0;
   if (v < a.blocks) {
     int* c = a.counts + (long long)mm * a.chunks * a.blocks + v;
-    for (int k = 0; k < a.chunks; k += 8) {   // eight loads in flight
-      int x[8];
+    for (int k = 0; k < a.chunks; k += 16) {   // sixteen loads in flight
+      int x[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = k + u < a.chunks ? c[(long long)(k + u) * a.blocks] : 0;
+      for (int u = 0; u < 16; ++u) x[u] = k + u < a.chunks ? c[(long long)(k + u) * a.blocks] : 0;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < 16; ++u) {
         if (k + u < a.chunks) c[(long long)(k + u) * a.blocks] = n;
         n += x[u];
       }
@@ -139,17 +180,26 @@ __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
   const int* own = a.selected + first + (long long)t * a.count;
   const int word = (tid >> 5) * a.blocks;
   for (int e0 = 0; e0 < a.count; e0 += 8) {
-    int v[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = e0 + u < a.count ? own[e0 + u] : -1;
+    int v[8], place[8];
+    load_entries(own, e0, a.count, v);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      int place = -1;
+      place[u] = -1;
       if (counted >> (e0 + u) & 1) {
-        place = place_of[word + v[u]] + __popc(bits[word + v[u]] & ((1u << (tid & 31)) - 1));
-        a.list[first + place] = t;
+        place[u] = place_of[word + v[u]] + __popc(bits[word + v[u]] & ((1u << (tid & 31)) - 1));
+        a.list[first + place[u]] = t;
       }
-      if (e0 + u < a.count) places[e0 + u] = place;
+    }
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      if (e0 + h + 4 <= a.count) {
+        typedef __attribute__((ext_vector_type(4), aligned(4))) int Four;
+        *(Four*)(places + e0 + h) = Four{place[h], place[h + 1], place[h + 2], place[h + 3]};
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (e0 + h + u < a.count) places[e0 + h + u] = place[h + u];
+      }
     }
   }
 }
@@ -495,10 +545,13 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
   return a;
 }
 
-void launch_lists(const SelectedArgs& a, hipStream_t st) {
+void launch_lists(const SelectedArgs& a, int d, bool bwd, hipStream_t st) {
   const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 32 KiB
   list_count_kernel<<<dim3(a.chunks, a.mats), kListChunk, bits, st>>>(a);
-  list_places_kernel<<<a.mats, 1024, 0, st>>>(a);
+  const int all = a.mats + a.mats * ((a.f.s + 511) / 512);
+  if (!bwd) list_places_kernel<0><<<a.mats, 1024, 0, st>>>(a);
+  else if (d == 64) list_places_kernel<64><<<all, 1024, 0, st>>>(a);
+  else list_places_kernel<128><<<all, 1024, 0, st>>>(a);
   list_fill_kernel<<<dim3(a.chunks, a.mats), kListChunk, 2 * bits, st>>>(a);
 }
 
@@ -609,7 +662,7 @@ int launch_attn_selected_fwd(const AttnSelectedDesc& b, hipStream_t st) {
     launch_selected_masked(a, p.mats, b.base.d, false, st);
     return hip_launch_status();
   }
-  launch_lists(a, st);
+  launch_lists(a, b.base.d, false, st);
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
     a.portion = min(p.portion, p.mats - a.mat0);
     if (b.base.d == 64) fwd_launch<64>(a, st);
@@ -627,7 +680,7 @@ int launch_attn_selected_bwd(const AttnSelectedDesc& b, hipStream_t st) {
     launch_selected_masked(a, p.mats, b.base.d, true, st);
     return hip_launch_status();
   }
-  launch_lists(a, st);
+  launch_lists(a, b.base.d, true, st);
   return launch_selected_bwd_kernels(a, p, b.base.d, st);
 }
 

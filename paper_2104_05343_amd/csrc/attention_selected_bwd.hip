@@ -10,24 +10,6 @@ __device__ __forceinline__ float weight_of(float x) { return __builtin_amdgcn_fm
 // what is subtracted from a row's scores; a row that saw nothing: +infinity, which makes every P of it zero
 __device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
 
-// rowsum(dO * O) of every query, 0 past the end of a sequence
-template <int D>
-__global__ __launch_bounds__(256) void selected_delta_kernel(SelectedArgs a) {
-  const FusedArgs& f = a.f;
-  const int lane = threadIdx.x & 63, g = lane >> 5, wave = threadIdx.x >> 6, mm = blockIdx.y;
-  const SelMatrix m = selected_matrix<D>(a, mm);
-  const int t = blockIdx.x * 128 + wave * 32 + (lane & 31), row = min(t, f.s - 1);
-  float delta = 0.f;
-  if (t < m.len) {
-    const bf16_t* G = f.d_attn + m.attn + (long long)row * f.ldo + g * 8;
-    const bf16_t* O = f.attn + m.attn + (long long)row * f.ldo + g * 8;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) delta += delta_piece(*(const bf16x8*)(G + ks * 16), *(const bf16x8*)(O + ks * 16));
-  }
-  delta = halfwave_sum(delta);
-  if (g == 0 && t < f.s) f.delta[m.vec + t] = delta;
-}
-
 // dS^T of 32 keys in LDS (rows_at from kt; V 64 rows behind) against the wavefront's queries, packed as fragments
 template <int D>
 __device__ __forceinline__ void dq_scores(bf16x8 (&dsf)[2], unsigned kt, const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16], float lse2, float delta,
@@ -516,7 +498,6 @@ __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs 
 template <int D>
 int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
   const int s = a.f.s;
-  selected_delta_kernel<D><<<dim3((s + 127) / 128, p.mats), 256, 0, st>>>(a);
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
     a.portion = min(p.portion, p.mats - a.mat0);
     const dim3 grid(a.most[0] * a.portion);

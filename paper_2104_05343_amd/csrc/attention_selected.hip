@@ -624,7 +624,12 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
     return;
   }
   p.chunks = (d.s + kListChunk - 1) / kListChunk;
-  p.seg[1] = 1024;
+  // Pieces of dK and dV: longer ones are fewer sums through memory, shorter ones fill the card.  Backward, us, with pieces of 256 / 512 / 1024 / 2048:
+  // width 128, blocks of 128, one of 4096 queries, 8 blocks 65 / 68 / 77 / 99; one of 8192, 8 88 / 78 / 86 / 107; two of 8192, 8 122 / 113 / 104 / 125; one
+  // of 16384, 16 178 / 163 / 158 / 149; 16 of 4096, 8 - / 275 / 250 / 240 (4096: 240).  (One device's pairs: sums depend on it.)
+  const size_t all_pairs = pairs * d.nb * d.nh;
+  p.seg[1] = 256;
+  while (p.seg[1] < 2048 && all_pairs / p.seg[1] >= 256) p.seg[1] *= 2;
   const size_t row_bytes = pairs * (d.d * 2 + 12);   // of a matrix
   auto fit = [&](size_t bytes) { return (int)(kPortion / bytes < 1 ? 1 : kPortion / bytes > mats ? mats : kPortion / bytes); };
   p.portion = fit(row_bytes);

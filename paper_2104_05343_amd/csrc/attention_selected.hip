@@ -577,12 +577,12 @@ void launch_selected_dq_combine(const SelectedArgs& a, int d, hipStream_t st) {
 // them) at a rate, and its longest workgroup walks over all keys.  Lists compute the chosen pairs at more each, as a block's part of a row goes
 // through memory once a block, and have a price a call and a query for the lists and the sums.
 // Measured, us, masked / lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
-//   width 128: 8192 queries, blocks of 128, 4 chosen 350 / 126, 1044 / 327; 8 303 / 203, 1060 / 490; 12 291 / 293, 1060 / 682; 16 294 / 354, 1066 / 829;
-//   16384, 256, 8 1129 / 627, 4298 / 1516; 4096, 64, 4 82 / 60, 278 / 162; 14 83 / 141, 295 / 349; 4096, 512, 2 80 / 81, 290 / 204;
-//   one of 1024, 64, 4 21 / 24, 38 / 58; 8192, 128, 24 116 / 67, 213 / 128; no mask, 4096, 128, 10 145 / 121, 548 / 329
-//   width 64: 8192, 128, 8 167 / 120, 614 / 274; 16 173 / 204, 623 / 455; 16384, 256, 8 597 / 351, 2424 / 868; 4096, 64, 8 57 / 64, 177 / 131; 4096, 512, 2
-//   56 / 61, 176 / 142; one of 1024, 64, 4 14 / 25, 24 / 46; 8192, 128, 24 70 / 55, 133 / 95
-// (104 such pairs: the form taken was never more than 1.06 times the other one's time.  Queries are those of one device's matrices, whatever the
+//   width 128: 8192 queries, blocks of 128, 4 chosen 341 / 125, 1086 / 298; 8 296 / 195, 1068 / 455; 12 285 / 288, 1055 / 640; 16 284 / 348, 1064 / 782;
+//   16384, 256, 8 1091 / 610, 4423 / 1421; 4096, 64, 4 79 / 60, 276 / 162; 14 80 / 138, 295 / 324; 4096, 512, 2 76 / 82, 291 / 197;
+//   one of 1024, 64, 4 20 / 23, 39 / 50; 8192, 128, 24 112 / 61, 212 / 117; no mask, 4096, 128, 10 142 / 125, 541 / 279
+//   width 64: 8192, 128, 8 158 / 111, 609 / 252; 16 162 / 193, 616 / 402; 16384, 256, 8 579 / 324, 2479 / 779; 4096, 64, 8 55 / 59, 175 / 114; 4096, 512, 2
+//   51 / 64, 171 / 134; one of 1024, 64, 4 12 / 23, 25 / 39; 8192, 128, 24 66 / 50, 132 / 85
+// (104 such pairs: the form taken was never more than 1.08 times the other one's time.  Queries are those of one device's matrices, whatever the
 // launch covers: the forms add up in different orders.)
 struct FormCost {
   double masked_pair, masked_call, masked_row;          // us: a pair; the longest workgroup's start and each row that it walks over
@@ -590,7 +590,7 @@ struct FormCost {
 };
 constexpr FormCost kFormCost[2][2] = {   // [forward, backward][width 64, 128]
     {{2.8e-7, 6, 0.008, 25, 1.2e-4, 1.6, 128}, {5.0e-7, 6, 0.0138, 25, 1.2e-4, 1.55, 137}},
-    {{1.1e-6, 10, 0.015, 50, 3.5e-4, 1.1, 45}, {1.9e-6, 12, 0.024, 60, 6e-4, 1.05, 65}}};
+    {{1.1e-6, 10, 0.015, 42, 3.8e-4, 0.92, 36}, {1.9e-6, 12, 0.024, 50, 5e-4, 0.98, 60}}};
 bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
   const AttnFusedDesc& d = b.base;
   const double blocks = (d.s + b.block - 1) / b.block, k = b.count < blocks ? b.count : blocks, B = b.block;
@@ -598,7 +598,7 @@ bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
   const int forced = g_form.load(std::memory_order_relaxed);
   if (forced >= 0) return forced != 0;
   FormCost c = kFormCost[bwd][d.d == 128];
-  if (bwd && d.d == 128 && b.block % 128 != 0) c.by_block = 105;   // (dK and dV of 64 keys at a time)
+  if (bwd && d.d == 128 && b.block % 128 != 0) c.by_block = 92;   // (dK and dV of 64 keys at a time)
   const double all = d.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
   const double chosen = d.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
   const double matrices = (double)d.nb * d.nh, pairs = matrices * B * (d.s < b.block ? d.s : B);   // of queries and keys, of a pair of blocks

@@ -462,37 +462,51 @@ __global__ __launch_bounds__(512, 2) void selected_dkv_wide_kernel(SelectedArgs 
 }
 
 // Sums over a key's pieces, in the order of the lists, to dK and dV; zeros where there is none.  (A single piece is written by its workgroup.)
+// A half-wavefront has four of a workgroup's 32 keys, which are of one block: with eight keys a workgroup 30 us to find single pieces for most of
+// 200000 keys, where few workgroups had anything to add.
 template <int D>
 __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs a) {
-  constexpr int DT = D / 32;
+  constexpr int DT = D / 32, KEYS = 4;
   typedef typename RowPart<DT>::V V;
   __shared__ __attribute__((aligned(16))) float lds[8][D];
   const FusedArgs& f = a.f;
   const int half = threadIdx.x >> 5, n = threadIdx.x & 31;
-  const int mm = a.mat0 + blockIdx.y;
-  const int key = blockIdx.x * 8 + half;
-  const bool inside = key < f.s;
+  const int mm = a.mat0 + blockIdx.y, key0 = blockIdx.x * (8 * KEYS);
   const SelMatrix m = selected_matrix<D>(a, mm);
-  const int v = min(key, f.s - 1) / a.block, in_block = key - v * a.block, tiles = a.block / BLK;
-  V dk, dv;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = 0.f;
+  const int v = key0 / a.block, tiles = a.block / BLK;
   const int* first = a.first_item + ((long long)a.mats + mm) * (a.blocks + 1);
   const int from = first[v], to = first[v + 1];
-  const bool write = inside && (key >= m.len || to - from != 1);
-  if (key < m.len && write) {
-#pragma unroll 2
+  const bool single = to - from == 1;
+  if (single && min(key0 + 8 * KEYS, f.s) <= m.len) return;
+  V dk[KEYS], dv[KEYS];
+#pragma unroll
+  for (int u = 0; u < KEYS; ++u)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dk[u][dt] = dv[u][dt] = 0.f;
+  const int in_block = key0 - v * a.block + half;
+  if (!single) {   // (rows past the end of the sequence are not written: read, and not used)
     for (int k = from; k < to; ++k) {
       const float* p = a.key_rows + (((long long)blockIdx.y * a.most[1] + k) * tiles + in_block / BLK) * (2 * BLK * D) + in_block % BLK * D + n * DT;
-      dk += *(const V*)p;
-      dv += *(const V*)(p + BLK * D);
+#pragma unroll
+      for (int u = 0; u < KEYS; ++u) {
+        dk[u] += *(const V*)(p + u * 8 * D);
+        dv[u] += *(const V*)(p + BLK * D + u * 8 * D);
+      }
     }
   }
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) dk[dt] *= f.scale;
-  bf16_t* out = f.d_qkv + m.qkv + (long long)key * f.ld + D;
-  write_row<DT>(out, dk, lds[half], n, write);
-  write_row<DT>(out + D, dv, lds[half], n, write);
+  for (int u = 0; u < KEYS; ++u) {
+    const int key = key0 + u * 8 + half;
+    const bool write = key < f.s && (key >= m.len || !single);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      dk[u][dt] = key < m.len ? dk[u][dt] * f.scale : 0.f;
+      dv[u][dt] = key < m.len ? dv[u][dt] : 0.f;
+    }
+    bf16_t* out = f.d_qkv + m.qkv + (long long)key * f.ld + D;
+    write_row<DT>(out, dk[u], lds[half], n, write);
+    write_row<DT>(out + D, dv[u], lds[half], n, write);
+  }
 }
 
 template <int D>
@@ -513,7 +527,7 @@ int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
     if constexpr (D == 128) wide = a.block % 128 == 0;
     if (wide) selected_dkv_wide_kernel<<<a.most[1] * (a.block / 128) * portion, 512, 0, st>>>(a);
     else selected_dkv_kernel<D><<<a.most[1] * (a.block / BLK) * portion, 256, 0, st>>>(a);
-    selected_dkv_combine_kernel<D><<<dim3((s + 7) / 8, portion), 256, 0, st>>>(a);
+    selected_dkv_combine_kernel<D><<<dim3((s + 31) / 32, portion), 256, 0, st>>>(a);
     if (const int rc = hip_launch_status()) return rc;
   }
   return OPTIMUS_OK;

@@ -12,7 +12,7 @@ namespace {
 // make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
 constexpr int kWords = kListChunk / 32;
 std::atomic<int> g_form{-1};                      // forced by a tuning hook: 1 masked, 0 lists
-constexpr size_t kPortion = (size_t)384 << 20;    // bytes of partial results in memory at a time
+constexpr size_t kPortion = (size_t)1 << 30;    // bytes of partial results in memory at a time
 
 __device__ __forceinline__ bool sees(const SelectedArgs& a, int len, int t, int v) {
   return v >= 0 && v < a.blocks && v * a.block < len && (!a.causal || v * a.block <= t);
@@ -411,8 +411,8 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
 }
 
 // A query's rows to its output, a half-wavefront each.  FORWARD: weighted by their maxima, divided by the sum; the others: added, times
-// 1 / sqrt(d), to dQ.  A row is 16 bytes of 16 lanes (8 of width 64), so that two or four come at a time, and four times as many are in flight.
-template <int D, bool FORWARD>
+// 1 / sqrt(d), to dQ.  JOINT: rows in the order of their columns, 32 of which have a scale.  A row is 16 bytes of 16 lanes (8 of width 64), so that two or four come at a time, and four times as many are in flight.
+template <int D, bool FORWARD, bool JOINT>
 __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   constexpr int DT = D / 32, LANES = D / 8, PARTS = 32 / LANES;
   typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -433,6 +433,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   for (int k = 0; k < 2; ++k) place[k] = inside && n + 32 * k < a.count ? places[n + 32 * k] : -1;
   // rows of entries e0 .. e0 + 4 PARTS - 1; the first ones are on their way while the weights are computed
   f16x8 x[4];
+  float unit[4];
   auto load_rows = [&](int e0) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -442,12 +443,13 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[u][k] = 0;
       if (p >= 0) x[u] = *(const f16x8*)(a.rows + (rows + p) * D + c * 8);
+      if (JOINT) unit[u] = p >= 0 ? a.units[(rows + p) * DT + c / 4] : 0.f;
     }
   };
   load_rows(0);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    weight[k] = place[k] >= 0 ? a.units[rows + place[k]] : 0.f;
+    weight[k] = !JOINT && place[k] >= 0 ? a.units[rows + place[k]] : 0.f;
     if (FORWARD) ml[k] = place[k] >= 0 ? a.ml[rows + place[k]] : make_float2(-INFINITY, 0.f);
   }
   float total = 0.f, top = -INFINITY;
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
     for (int u = 0; u < 4; ++u) {
       const int e = e0 + u * PARTS + part;
       const float w0 = __shfl(weight[0], e & 31, 32), w1 = __shfl(weight[1], e & 31, 32);
-      const float w = e < 32 ? w0 : w1;
+      const float w = JOINT ? unit[u] : e < 32 ? w0 : w1;
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum[k] = fmaf(w, (float)x[u][k], sum[k]);
     }
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
     for (int k = 0; k < 8; ++k) sum[k] += __shfl_xor(sum[k], step);
   if (part == 0) {   // numbers 8c .. of a row are [column % 32][column / 32]
 #pragma unroll
-    for (int k = 0; k < 8; ++k) lds[half][(8 * c + k) % DT * 32 + (8 * c + k) / DT] = FORWARD ? sum[k] : sum[k] * f.scale;
+    for (int k = 0; k < 8; ++k) lds[half][JOINT ? 8 * c + k : (8 * c + k) % DT * 32 + (8 * c + k) / DT] = FORWARD ? sum[k] : sum[k] * f.scale;
   }
   __builtin_amdgcn_wave_barrier();
   bf16_t* to = FORWARD ? f.attn + m.attn + (long long)t * f.ldo : f.d_qkv + m.qkv + (long long)t * f.ld;
@@ -536,12 +538,13 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
     a.items[k] = (i32x4_t*)take(p.items[k]);
   }
   if (!bwd) a.items[1] = nullptr;
+  if (p.joint) a.items[0] = nullptr;
   a.list = (int*)take(p.list);
   a.places = (int*)take(p.places);
   a.rows = (f16_t*)take(p.rows);
   a.units = (float*)take(p.units);
   a.ml = (float2*)take(p.ml);
-  a.key_rows = (float*)a.rows;   // (dK and dV come when the rows of dQ are done with)
+  a.key_rows = p.joint ? (float*)take(p.keys) : (float*)a.rows;   // (otherwise dK and dV come when the rows of dQ are done with)
   return a;
 }
 
@@ -562,15 +565,17 @@ void fwd_launch(const SelectedArgs& a, hipStream_t st) {
   if (a.block == 64) selected_fwd_kernel<D, 2><<<grid, 256, 0, st>>>(a);
   else if (a.block == 128) selected_fwd_kernel<D, 4><<<grid, 256, 0, st>>>(a);
   else selected_fwd_long_kernel<D><<<grid, 256, 0, st>>>(a);
-  selected_combine_kernel<D, true><<<dim3((a.f.s + 7) / 8, portion), 256, 0, st>>>(a);
+  selected_combine_kernel<D, true, false><<<dim3((a.f.s + 7) / 8, portion), 256, 0, st>>>(a);
 }
 
 }  // namespace
 
-void launch_selected_dq_combine(const SelectedArgs& a, int d, hipStream_t st) {
+void launch_selected_dq_combine(const SelectedArgs& a, int d, bool joint, hipStream_t st) {
   const dim3 grid((a.f.s + 7) / 8, a.portion);
-  if (d == 64) selected_combine_kernel<64, false><<<grid, 256, 0, st>>>(a);
-  else selected_combine_kernel<128, false><<<grid, 256, 0, st>>>(a);
+  if (joint && d == 64) selected_combine_kernel<64, false, true><<<grid, 256, 0, st>>>(a);
+  else if (joint) selected_combine_kernel<128, false, true><<<grid, 256, 0, st>>>(a);
+  else if (d == 64) selected_combine_kernel<64, false, false><<<grid, 256, 0, st>>>(a);
+  else selected_combine_kernel<128, false, false><<<grid, 256, 0, st>>>(a);
 }
 
 // Which form: the one that should take less time, by what both have taken.  The masked one computes all pairs of queries and keys (causal: half of
@@ -624,32 +629,36 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
     return;
   }
   p.chunks = (d.s + kListChunk - 1) / kListChunk;
+  p.joint = bwd && b.block <= 128;
   // Pieces of dK and dV: longer ones are fewer sums through memory, shorter ones fill the card.  Backward, us, with pieces of 256 / 512 / 1024 / 2048:
   // width 128, blocks of 128, one of 4096 queries, 8 blocks 65 / 68 / 77 / 99; one of 8192, 8 88 / 78 / 86 / 107; two of 8192, 8 122 / 113 / 104 / 125; one
   // of 16384, 16 178 / 163 / 158 / 149; 16 of 4096, 8 - / 275 / 250 / 240 (4096: 240).  (One device's pairs: sums depend on it.)
   const size_t all_pairs = pairs * d.nb * d.nh;
   p.seg[1] = 256;
   while (p.seg[1] < 2048 && all_pairs / p.seg[1] >= 256) p.seg[1] *= 2;
-  const size_t row_bytes = pairs * (d.d * 2 + 12);   // of a matrix
+  p.most[1] = (int)(blocks + pairs / p.seg[1]);
+  const size_t row_bytes = pairs * (d.d * 2 + (p.joint ? d.d / 8 : 12));   // of a matrix
+  const size_t key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;
   auto fit = [&](size_t bytes) { return (int)(kPortion / bytes < 1 ? 1 : kPortion / bytes > mats ? mats : kPortion / bytes); };
-  p.portion = fit(row_bytes);
+  p.portion = fit(p.joint ? row_bytes + key_bytes : row_bytes);
+  p.key_portion = p.joint ? p.portion : fit(key_bytes);
   // Pieces of a list as long as some 2000 of them leave no compute unit without work, 256 to 1024 rows (no bits depend on it): a launch of 10^6
   // pairs (two matrices of 32768 queries, 16 blocks each) 1006 us with 256 in all, 932 with 1024; 2.4 * 10^6 of width 64 395 with 256, 376 with 512.
   p.seg[0] = 256;
   while (p.seg[0] < 1024 && p.portion * pairs / p.seg[0] >= 4096) p.seg[0] *= 2;
-  for (int k = 0; k < 2; ++k) p.most[k] = (int)(blocks + pairs / p.seg[k]);
-  const size_t key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;   // of a matrix
-  p.key_portion = fit(key_bytes);
+  p.most[0] = (int)(blocks + pairs / p.seg[0]);
   p.counts = round256(mats * p.chunks * blocks * 4);
   p.offsets = round256(mats * (blocks + 1) * 4);
   p.first_item = round256(2 * mats * (blocks + 1) * 4);
-  for (int k = 0; k < 2; ++k) p.items[k] = round256(mats * p.most[k] * 16);
+  p.items[0] = p.joint ? 0 : round256(mats * p.most[0] * 16);
+  p.items[1] = bwd ? round256(mats * p.most[1] * 16) : 0;
   p.list = p.places = round256(mats * pairs * 4);
-  const size_t rows = p.portion * pairs * d.d * 2, keys = p.key_portion * key_bytes;
-  p.rows = round256(rows > keys ? rows : keys);
-  p.units = round256(p.portion * pairs * 4);
-  p.ml = round256(p.portion * pairs * 8);
-  p.total = p.delta + p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.units + p.ml;
+  const size_t rows = p.portion * pairs * d.d * 2, keys = bwd ? p.key_portion * key_bytes : 0;
+  p.rows = round256(p.joint || rows > keys ? rows : keys);
+  p.keys = p.joint ? round256(keys) : 0;
+  p.units = round256(p.portion * pairs * (p.joint ? d.d / 32 : 1) * 4);
+  p.ml = bwd ? 0 : round256(p.portion * pairs * 8);
+  p.total = p.delta + p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.units + p.ml + p.keys;
   *out = p;
 }
 size_t attn_selected_ws_bytes(const AttnSelectedDesc& b) {

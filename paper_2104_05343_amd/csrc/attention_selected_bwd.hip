@@ -32,11 +32,11 @@ __device__ __forceinline__ void dq_scores(bf16x8 (&dsf)[2], unsigned kt, const b
   dsf[1] = pack_acc<1>(sacc);
 }
 
-// dQ rows.  KT > 0: the block's K and V stay in LDS (64 or 128 keys); 0: 64 keys at a time through two stages.
-template <int D, int KT>
+// dQ rows of larger blocks: 64 keys at a time through two stages.
+template <int D>
 __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
-  constexpr int KS = D / 16, DT = D / 32, STAGES = KT == 2 ? 1 : 2;
-  __shared__ __attribute__((aligned(1024))) bf16_t lds[STAGES][2][BLK * D];   // [stage][K, V]
+  constexpr int KS = D / 16, DT = D / 32;
+  __shared__ __attribute__((aligned(1024))) bf16_t lds[2][2][BLK * D];   // [stage][K, V]
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
   const bf16_t* Qp = f.qkv + m.qkv;
   const bf16_t* Gp = f.d_attn + m.attn;
   const int key0 = it.block * a.block, last = m.len - 1;
-  const int steps = KT ? KT / 2 : (min(a.block, m.len - key0) + BLK - 1) / BLK;
+  const int steps = (min(a.block, m.len - key0) + BLK - 1) / BLK;
   const int rounds = (it.pairs + kQueries - 1) / kQueries;
   TileLoader<D, 4, BLK, true> ldr;
   ldr.init(f.ld, wave, lane);
@@ -55,8 +55,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
     ldr.issue(Qp + D, key0 + step * BLK, m.len, lds[st][0]);
     ldr.issue(Qp + 2 * D, key0 + step * BLK, m.len, lds[st][1]);
   };
-#pragma unroll
-  for (int st = 0; st < (KT ? STAGES : 1); ++st) issue(st, st);
+  issue(0, 0);
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane);
   const long long pairs = (long long)f.s * a.count, first = mm * pairs + it.start, out = matrix * pairs + it.start;
   const int* list = a.list + first;
@@ -83,17 +82,16 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
   int stage = 0;
   for (int round = 0; round < rounds; ++round) {
     const int base = round * kQueries, left = it.pairs - base - wave * 32;
-    if (KT && left <= 0) break;
     const int limit = a.causal ? min(t, last) : last;
     const float lse2 = lse2_of(lse);
     f32x16 acc[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
     for (int step = 0; step < steps; ++step, stage ^= 1) {
-      if (!KT && (step + 1 < steps || round + 1 < rounds)) issue(step + 1 < steps ? step + 1 : 0, stage ^ 1);
+      if (step + 1 < steps || round + 1 < rounds) issue(step + 1 < steps ? step + 1 : 0, stage ^ 1);
       const int kbase = key0 + step * BLK;
-      if (KT || (left > 0 && __builtin_amdgcn_ballot_w64(limit >= kbase) != 0)) {
-        const unsigned at = (unsigned)((KT ? step : stage) * (2 * BLK * D * 2));
+      if (left > 0 && __builtin_amdgcn_ballot_w64(limit >= kbase) != 0) {
+        const unsigned at = (unsigned)(stage * (2 * BLK * D * 2));
         const bool masked = __builtin_amdgcn_ballot_w64(limit < kbase + BLK - 1) != 0;
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2) {
@@ -105,7 +103,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
                                });
         }
       }
-      if (!KT) wait_loads_and_barrier();
+      wait_loads_and_barrier();
     }
     load_queries(base + kQueries);
     if (left > 0) {
@@ -321,6 +319,232 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
   key_sums<D>(a, m, dvacc, k0, 2 * D, 1.0f, only, xch, to + BLK * D, lane);
 }
 
+// Blocks of 64 or 128 keys: all three gradients in one pass over the list, 64 queries at a time.  P and dS are computed once, with a wavefront's 32 keys
+// as columns, which is what dK and dV take; dS goes through LDS as [key][query], where the transposing reads fetch it and K for dQ, a
+// 32 x 32 tile (or two) a wavefront.  A lane has one query's 16 numbers of a tile, 32 columns of dQ, which get a scale of their own.
+template <int D, int KEYS>
+struct SelectedBwd {
+  static constexpr bool WIDE = D == 128 && KEYS == 128;
+  static constexpr int WAVES = WIDE ? 8 : 4, THREADS = 64 * WAVES, RG = KEYS / 32, PARW = WAVES / RG;   // RG: groups of 32 keys; PARW: wavefronts of one
+  static constexpr int TILES = 2 * (D / 32) / WAVES;   // of dQ a wavefront
+  static constexpr int MOST = D == 64 && KEYS == 64 ? 3 : 2;   // wavefronts a SIMD (width 128, 64 keys: one, LDS)
+  static constexpr int KREG = WIDE ? 4 : KEYS == 64 ? 0 : D / 16, VREG = D == 128 ? 0 : D / 16;   // own fragments in registers, others in LDS
+  struct Lds {
+    bf16_t block[2][2][BLK * D];       // [stage][Q, dO]
+    bf16_t k[KEYS * D];
+    bf16_t v[VREG ? 512 : KEYS * D];
+    bf16_t ds[KEYS * BLK];             // [key][query of the block], laid out as a tile of width 64
+    alignas(16) float l[2][BLK];
+    alignas(16) float d[2][BLK];
+    alignas(16) int t[2][BLK];
+  };
+};
+// A lane's 16 numbers of a query's 32 columns from 32 dt on (slot r is column slot(r) + 4 g) to fp16, scaled as in store_parts: two stores of 16 bytes, one
+// of the scale.
+template <int DT>
+__device__ __forceinline__ void store_part(const f32x16& acc, int row, int dt, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t units, int g) {
+  float most = larger(fabsf(acc[0]), fabsf(acc[1]));
+#pragma unroll
+  for (int r = 2; r < 16; r += 2) most = larger(larger(most, fabsf(acc[r])), fabsf(acc[r + 1]));
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+  most = larger(__uint_as_float(both[0]), __uint_as_float(both[1]));
+  const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 16), 254);
+  const float scale = __uint_as_float((unsigned)(268 - e) << 23);
+  typedef __attribute__((ext_vector_type(4))) _Float16 Four;
+  u32x2 h[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    Four x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = (f16_t)(acc[4 * c + k] * scale);
+    h[c] = __builtin_bit_cast(u32x2, x);
+  }
+#pragma unroll
+  for (int c = 0; c < 4; c += 2) {   // lanes 0 .. 31: eight columns from 8 c on, the others the next eight
+    const auto lo = __builtin_amdgcn_permlane32_swap(h[c][0], h[c + 1][0], false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(h[c][1], h[c + 1][1], false, false);
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{lo[0], hi[0], lo[1], hi[1]}, rows, row * (64 * DT) + dt * 64 + (c + g) * 16, 0, 0);
+  }
+  __builtin_amdgcn_raw_buffer_store_b32((int)((unsigned)(e - 14) << 23), units, g == 0 ? (row * DT + dt) * 4 : 0x7fffffff, 0, 0);
+}
+
+template <int D, int KEYS>
+__global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), (SelectedBwd<D, KEYS>::MOST)) void selected_bwd_kernel(SelectedArgs a) {
+  typedef SelectedBwd<D, KEYS> B;
+  constexpr int KS = D / 16, DT = D / 32, NW = B::WAVES, KREG = B::KREG, VREG = B::VREG;
+  __shared__ __attribute__((aligned(1024))) typename B::Lds lds;
+  const FusedArgs& f = a.f;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave % B::RG, par = wave / B::RG;
+  const int item = blockIdx.x / a.portion, matrix = blockIdx.x % a.portion, mm = a.mat0 + matrix;
+  ListItem it;
+  if (!list_item(a, 1, mm, item, &it)) return;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int kt0 = it.block * KEYS;
+  const bf16_t* Qp = f.qkv + m.qkv;
+  const bf16_t* Gp = f.d_attn + m.attn;
+  const int k0 = kt0 + rg * 32, key = k0 + (lane & 31), krow = min(key, m.len - 1);
+  bf16x8 kf[KREG > 0 ? KREG : 1], vf[VREG > 0 ? VREG : 1];
+#pragma unroll
+  for (int ks = 0; ks < KREG; ++ks) kf[ks] = *(const bf16x8*)(Qp + D + (long long)krow * f.ld + ks * 16 + g * 8);
+#pragma unroll
+  for (int ks = 0; ks < VREG; ++ks) vf[ks] = *(const bf16x8*)(Qp + 2 * D + (long long)krow * f.ld + ks * 16 + g * 8);
+  {
+    TileLoader<D, NW, KEYS, true> own;   // (keys past the end of the sequence: zeros, which whatever their dS is adds nothing to dQ)
+    own.init(f.ld, wave, lane);
+    own.issue(Qp + D, kt0, m.len, lds.k);
+    if constexpr (VREG == 0) own.issue(Qp + 2 * D, kt0, m.len, lds.v);
+  }
+  const long long pairs = (long long)f.s * a.count;
+  const int* list = a.list + mm * pairs + it.start;
+  f16_t* const rows = a.rows + (matrix * pairs + it.start) * D;
+  float* const units = a.units + (matrix * pairs + it.start) * DT;
+  const int n_it = (it.pairs + BLK - 1) / BLK;
+  f32x16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    dkacc[dt] = zero16();
+    dvacc[dt] = zero16();
+  }
+  const unsigned in_rows = lds_address(lds.block) + lane_rows<D>(lane), in_cols = lds_address(lds.block) + lane_cols<D>(lane);
+  const unsigned own_k = lds_address(lds.k) + lane_rows<D>(lane) + rg * 32 * D * 2, own_v = lds_address(lds.v) + lane_rows<D>(lane) + rg * 32 * D * 2;
+  const unsigned k_cols = lds_address(lds.k) + lane_cols<D>(lane), ds_cols = lds_address(lds.ds) + lane_cols<64>(lane);
+  const int ds_row = rg * 32 + (lane & 31);
+  const unsigned ds_at = lds_address(lds.ds) + (unsigned)(ds_row * 128 + (swz<64>(ds_row) << 4) + g * 8);
+  const int q_half = wave / (NW / 2), dt0 = wave % (NW / 2) * B::TILES;   // of dQ
+  GatherLoader<D, NW, BLK> ldr;
+  ldr.wave = wave;
+  ldr.lane = lane;
+  // a row's numbers go through registers and reach LDS at the end of an iteration
+  int next_t = 0, row_t = 0;
+  float next_l = 0.f, next_d = 0.f;
+  auto load_numbers = [&](int n) {   // of iteration n
+    ldr.fetch(list, n * BLK, it.pairs);
+    if (tid < BLK) row_t = list[min(n * BLK + tid, it.pairs - 1)];
+  };
+  auto issue = [&](int st) {
+    if (tid < BLK) {
+      next_t = row_t;
+      next_l = f.lse[m.vec + row_t];
+      next_d = f.delta[m.vec + row_t];
+    }
+    ldr.issue(Qp, f.ld, lds.block[st][0]);
+    ldr.issue(Gp, f.ldo, lds.block[st][1]);
+  };
+  auto store_numbers = [&](int n, int st) {   // (past the end of the list: no P)
+    if (tid < BLK) {
+      lds.l[st][tid] = n * BLK + tid < it.pairs ? lse2_of(next_l) : INFINITY;
+      lds.d[st][tid] = next_d;
+      lds.t[st][tid] = next_t;
+    }
+  };
+  load_numbers(0);
+  issue(0);
+  if (n_it > 1) load_numbers(1);
+  store_numbers(0, 0);
+  wait_loads_and_barrier();
+  for (int n = 0; n < n_it; ++n) {
+    const int st = n & 1;
+    if (n + 1 < n_it) {
+      issue(st ^ 1);
+      if (n + 2 < n_it) load_numbers(n + 2);
+    }
+    const unsigned stage = (unsigned)(st * 2 * BLK * D * 2);
+#pragma unroll
+    for (int u2 = 0; u2 < 2 / B::PARW; ++u2) {
+      const int half = B::PARW == 2 ? par : u2;
+      if (n * BLK + half * 32 >= it.pairs) continue;   // (dQ of these rows is not stored)
+      const unsigned qt = in_rows + stage + half * (32 * D * 2), qc = in_cols + stage + half * (32 * D * 2);
+      // (the block's own queries come first: where the first of 32 is behind the keys, all are)
+      const bool masked = a.causal && __builtin_amdgcn_readfirstlane(lds.t[st][half * 32]) < k0 + 31;
+      f32x16 sacc = zero16(), pacc = zero16();
+      struct Two { bf16x8 q, own; };
+      pipelined<2 * KS, 2>([&](int k) {
+                             const int ks = k / 2;
+                             Two x;
+                             x.q = rows_at<D>(qt, k & 1 ? BLK : 0, ks);
+                             if (k & 1) x.own = ks < VREG ? vf[ks < VREG ? ks : 0] : rows_at<D>(own_v, 0, ks);
+                             else x.own = ks < KREG ? kf[ks < KREG ? ks : 0] : rows_at<D>(own_k, 0, ks);
+                             return x;
+                           },
+                           [&](int k, const Two& x) {
+                             f32x16& acc = k & 1 ? pacc : sacc;
+                             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.q, x.own, acc, 0, 0, 0);
+                           });
+      const int at = half * 32 + 4 * g;
+      list_scores(sacc, pacc, lds.l[st] + at, lds.d[st] + at, lds.t[st] + at, f.scale_log2, masked, key);
+      const bf16x8 pf[2] = {pack_acc<0>(sacc), pack_acc<1>(sacc)}, dsf[2] = {pack_acc<0>(pacc), pack_acc<1>(pacc)};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {   // queries 8 c + 4 g .. of the lane's key
+        const u32x4 w = __builtin_bit_cast(u32x4, dsf[c >> 1]);
+        *(__attribute__((address_space(3))) u32x2*)(size_t)(ds_at ^ (unsigned)((half * 4 + c) << 4)) = u32x2{w[2 * (c & 1)], w[2 * (c & 1) + 1]};
+      }
+      pipelined<4 * DT, 2>([&](int k) { return cols_at<D>(qc, (k & 1 ? 0 : BLK) + k / (2 * DT) * 16, k / 2 % DT); },
+                           [&](int k, const bf16x8& x) {
+                             const int dt = k / 2 % DT, u = k / (2 * DT);
+                             f32x16& acc = k & 1 ? dkacc[dt] : dvacc[dt];
+                             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k & 1 ? dsf[u] : pf[u], x, acc, 0, 0, 0);
+                           });
+    }
+    __syncthreads();
+    f32x16 dq[B::TILES];
+#pragma unroll
+    for (int i = 0; i < B::TILES; ++i) dq[i] = zero16();
+    struct Pair { bf16x8 ds, k[B::TILES]; };
+    pipelined<KEYS / 16, 2>([&](int k) {
+                              Pair x;
+                              x.ds = cols_at<64>(ds_cols ^ (unsigned)(q_half * 64), k * 16, 0);
+#pragma unroll
+                              for (int i = 0; i < B::TILES; ++i) x.k[i] = cols_at<D>(k_cols ^ (unsigned)((dt0 + i) * 64), k * 16, 0);
+                              return x;
+                            },
+                            [&](int, const Pair& x) {
+#pragma unroll
+                              for (int i = 0; i < B::TILES; ++i) dq[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.k[i], x.ds, dq[i], 0, 0, 0);
+                            });
+    if (n + 1 < n_it) store_numbers(n + 1, st ^ 1);
+    const int left = __builtin_amdgcn_readfirstlane(min(it.pairs - n * BLK, BLK));
+    const auto to_rows = __builtin_amdgcn_make_buffer_rsrc(rows + (long long)n * BLK * D, 0, left * (2 * D), 0x00020000);
+    const auto to_units = __builtin_amdgcn_make_buffer_rsrc(units + (long long)n * BLK * DT, 0, left * (4 * DT), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < B::TILES; ++i) store_part<DT>(dq[i], q_half * 32 + (lane & 31), dt0 + i, to_rows, to_units, g);
+    // all but this iteration's stores, three a tile, have ended: the loads into the other stage were issued ahead of them
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((3 * B::TILES) | (7 << 4) | (15 << 8));
+    asm volatile("" ::: "memory");
+    __syncthreads();
+  }
+  // the halves' sums of 32 keys, dV first: the odd one hands over through LDS (all block tiles are free)
+  const bool only = single_piece(a, mm, it.block);
+  float* xch = (float*)&lds.block[0][0][0] + rg * (DT * 16) * 64;
+  float* to = a.key_rows + (((long long)matrix * a.most[1] + item) * (KEYS / BLK) + (rg >> 1)) * (2 * BLK * D) + (rg & 1) * 32 * D;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    f32x16 (&acc)[DT] = which == 0 ? dvacc : dkacc;
+    if (B::PARW == 2) {
+      if (which == 1) __syncthreads();
+      if (par == 1) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) xch[(dt * 16 + r) * 64 + lane] = acc[dt][r];
+      }
+      __syncthreads();
+      if (par == 0) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[dt][r] += xch[(dt * 16 + r) * 64 + lane];
+      }
+    }
+    if (par == 0) {
+      if (which == 0) key_sums<D>(a, m, acc, k0, 2 * D, 1.0f, only, xch, to + BLK * D, lane);
+      else key_sums<D>(a, m, acc, k0, D, f.scale, only, xch, to, lane);
+    }
+  }
+}
+
 // Head width 128, blocks of whole 128 keys: 128 keys, eight wavefronts, as in the attention with changed scores: own V rows and half of the K
 // fragments in LDS, 64 queries at a time, a wavefront half of them.
 struct SelWideLds {
@@ -512,13 +736,21 @@ __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs 
 template <int D>
 int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
   const int s = a.f.s;
+  if (p.joint) {
+    for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
+      a.portion = min(p.portion, p.mats - a.mat0);
+      if (a.block == 64) selected_bwd_kernel<D, 64><<<a.most[1] * a.portion, SelectedBwd<D, 64>::THREADS, 0, st>>>(a);
+      else selected_bwd_kernel<D, 128><<<a.most[1] * a.portion, SelectedBwd<D, 128>::THREADS, 0, st>>>(a);
+      launch_selected_dq_combine(a, D, true, st);
+      selected_dkv_combine_kernel<D><<<dim3((s + 31) / 32, a.portion), 256, 0, st>>>(a);
+      if (const int rc = hip_launch_status()) return rc;
+    }
+    return OPTIMUS_OK;
+  }
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
     a.portion = min(p.portion, p.mats - a.mat0);
-    const dim3 grid(a.most[0] * a.portion);
-    if (a.block == 64) selected_dq_kernel<D, 2><<<grid, 256, 0, st>>>(a);
-    else if (a.block == 128) selected_dq_kernel<D, 4><<<grid, 256, 0, st>>>(a);
-    else selected_dq_kernel<D, 0><<<grid, 256, 0, st>>>(a);
-    launch_selected_dq_combine(a, D, st);
+    selected_dq_kernel<D><<<a.most[0] * a.portion, 256, 0, st>>>(a);
+    launch_selected_dq_combine(a, D, false, st);
     if (const int rc = hip_launch_status()) return rc;
   }
   for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.key_portion) {

@@ -49,7 +49,7 @@ struct SelectedArgs {
   int* list;                           // [matrix][s * count]: query of every pair
   int* places;                         // [matrix][s][count]: place of the pair in list, -1: none
   f16_t* rows;                         // [matrix - mat0][s * count][d]: partial results, see store_parts
-  float* units;                        // [matrix - mat0][s * count]: what a row's numbers are to be multiplied by
+  float* units;                        // [matrix - mat0][s * count]: what a row's numbers are to be multiplied by; joint: [d / 32] of 32 columns each
   float2* ml;                          // [matrix - mat0][s * count]: maximum of log2(e) Q K^T / sqrt(d), sum of exponentials
   float* key_rows;                     // [matrix - mat0][item][block / 64][dK, dV][64][d]
 };
@@ -57,15 +57,16 @@ struct SelectedArgs {
 // What the host decides; bytes of the workspace, in this order
 struct SelectedPlan {
   bool masked;
+  bool joint;                          // lists, all gradients in one pass
   int mats, chunks, mask_words;
   int portion, key_portion;            // matrices whose partial results are in memory at a time: of queries, of keys
   int seg[2], most[2];
-  size_t delta, mask, counts, offsets, first_item, items[2], list, places, rows, units, ml, total;
+  size_t delta, mask, counts, offsets, first_item, items[2], list, places, rows, units, ml, keys, total;
 };
 
 // csrc/attention_selected*.hip
 int launch_selected_bwd_kernels(const SelectedArgs& a, const SelectedPlan& p, int d, hipStream_t st);
-void launch_selected_dq_combine(const SelectedArgs& a, int d, hipStream_t st);
+void launch_selected_dq_combine(const SelectedArgs& a, int d, bool joint, hipStream_t st);
 void launch_selected_masked(const SelectedArgs& a, int mats, int d, bool bwd, hipStream_t st);
 
 namespace {

@@ -303,8 +303,8 @@ def test_captured_and_on_another_stream(form):
 
 def test_portions(lists):
     """Partial results beyond the workspace's portion: more (sequence, head)s than go at a time, the same bits as one device's alone."""
-    b, s, n, d = 8, 4096, 4, 128
-    many = Run(b, s, n * d, n, 2, True, block=128, count=8).go()          # 32 times 17 MB
+    b, s, n, d = 8, 8192, 4, 128
+    many = Run(b, s, n * d, n, 2, True, block=128, count=8).go()          # 32 times 36 MB and more
     one = Run(b, s, n * d, n, 2, True, block=128, count=8, at=(1, 0)).go()
     for name in "SOLG":
         assert torch.equal(getattr(one, name).view(4, -1)[2].view(torch.uint8), getattr(many, name).view(4, -1)[2].view(torch.uint8)), name

@@ -143,12 +143,14 @@ __global__ __launch_bounds__(1024) void list_places_kernel(SelectedArgs a) {
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
     if (!a.items[kind]) continue;
-    const int items = (n + a.seg[kind] - 1) / a.seg[kind], first = exclusive_sum(items, lds, &all);
+    // equal items of at most 1.25 seg rows, no short one at the end of a list
+    const int most = a.seg[kind] * 5 / 4, wanted = max((n + most - 1) / most, 1), size = ((n + wanted - 1) / wanted + 127) & ~127;
+    const int items = n > 0 ? (n + size - 1) / size : 0, first = exclusive_sum(items, lds, &all);
     int* firsts = a.first_item + ((long long)kind * a.mats + mm) * (a.blocks + 1);
     if (v < a.blocks) firsts[v] = first;
     if (v == 0) firsts[a.blocks] = all;
     for (int k = 0; k < items; ++k)
-      a.items[kind][(long long)mm * a.most[kind] + first + k] = i32x4_t{v, at + k * a.seg[kind], min(a.seg[kind], n - k * a.seg[kind]), 0};
+      a.items[kind][(long long)mm * a.most[kind] + first + k] = i32x4_t{v, at + k * size, min(size, n - k * size), 0};
   }
 }
 
@@ -582,28 +584,29 @@ void launch_selected_dq_combine(const SelectedArgs& a, int d, bool joint, hipStr
 // them) at a rate, and its longest workgroup walks over all keys.  Lists compute the chosen pairs at more each, as a block's part of a row goes
 // through memory once a block, and have a price a call and a query for the lists and the sums.
 // Measured, us, masked / lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
-//   width 128: 8192 queries, blocks of 128, 4 chosen 341 / 125, 1086 / 298; 8 296 / 195, 1068 / 455; 12 285 / 288, 1055 / 640; 16 284 / 348, 1064 / 782;
-//   16384, 256, 8 1091 / 610, 4423 / 1421; 4096, 64, 4 79 / 60, 276 / 162; 14 80 / 138, 295 / 324; 4096, 512, 2 76 / 82, 291 / 197;
-//   one of 1024, 64, 4 20 / 23, 39 / 50; 8192, 128, 24 112 / 61, 212 / 117; no mask, 4096, 128, 10 142 / 125, 541 / 279
-//   width 64: 8192, 128, 8 158 / 111, 609 / 252; 16 162 / 193, 616 / 402; 16384, 256, 8 579 / 324, 2479 / 779; 4096, 64, 8 55 / 59, 175 / 114; 4096, 512, 2
-//   51 / 64, 171 / 134; one of 1024, 64, 4 12 / 23, 25 / 39; 8192, 128, 24 66 / 50, 132 / 85
+//   width 128: 8192 queries, blocks of 128, 4 chosen 341 / 125, 1086 / 223; 8 296 / 195, 1068 / 354; 12 285 / 288, 1055 / 471; 16 284 / 348, 1064 / 569;
+//   16384, 256, 8 1091 / 610, 4423 / 1283; 4096, 64, 4 79 / 60, 276 / 128; 14 80 / 138, 295 / 253; 4096, 512, 2 76 / 82, 291 / 210;
+//   one of 1024, 64, 4 20 / 23, 39 / 48; 8192, 128, 24 112 / 61, 212 / 105; no mask, 4096, 128, 10 142 / 125, 541 / 208
+//   width 64: 8192, 128, 8 158 / 111, 609 / 178; 16 162 / 193, 616 / 305; 16384, 256, 8 579 / 324, 2479 / 744; 4096, 64, 8 55 / 59, 175 / 85; 4096, 512, 2
+//   51 / 64, 171 / 145; one of 1024, 64, 4 12 / 23, 25 / 36; 8192, 128, 24 66 / 50, 132 / 84
 // (104 such pairs: the form taken was never more than 1.08 times the other one's time.  Queries are those of one device's matrices, whatever the
 // launch covers: the forms add up in different orders.)
 struct FormCost {
   double masked_pair, masked_call, masked_row;          // us: a pair; the longest workgroup's start and each row that it walks over
   double lists_call, lists_query, lists_pair, by_block; // us; a chosen pair, in masked ones, lists_pair + by_block / block
 };
-constexpr FormCost kFormCost[2][2] = {   // [forward, backward][width 64, 128]
+constexpr FormCost kFormCost[3][2] = {   // [forward, backward of blocks of 64 and 128, of larger ones][width 64, 128]
     {{2.8e-7, 6, 0.008, 25, 1.2e-4, 1.6, 128}, {5.0e-7, 6, 0.0138, 25, 1.2e-4, 1.55, 137}},
-    {{1.1e-6, 10, 0.015, 42, 3.8e-4, 0.92, 36}, {1.9e-6, 12, 0.024, 50, 5e-4, 0.98, 60}}};
+    {{1.1e-6, 10, 0.015, 38, 1.4e-4, 0.82, 18}, {1.9e-6, 12, 0.024, 46, 3.6e-4, 0.27, 101}},
+    {{1.1e-6, 10, 0.015, 38, 3e-4, 1.05, 30}, {1.9e-6, 12, 0.024, 46, 4e-4, 0.98, 60}}};
 bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
   const AttnFusedDesc& d = b.base;
   const double blocks = (d.s + b.block - 1) / b.block, k = b.count < blocks ? b.count : blocks, B = b.block;
   if (blocks > kMaskedBlocks) return false;
   const int forced = g_form.load(std::memory_order_relaxed);
   if (forced >= 0) return forced != 0;
-  FormCost c = kFormCost[bwd][d.d == 128];
-  if (bwd && d.d == 128 && b.block % 128 != 0) c.by_block = 92;   // (dK and dV of 64 keys at a time)
+  FormCost c = kFormCost[!bwd ? 0 : b.block <= 128 ? 1 : 2][d.d == 128];
+  if (bwd && d.d == 128 && b.block > 128 && b.block % 128 != 0) c.by_block = 92;   // (dK and dV of 64 keys at a time)
   const double all = d.causal ? blocks * (blocks + 1) / 2 : blocks * blocks;
   const double chosen = d.causal ? k * (k + 1) / 2 + (blocks - k) * k : blocks * k;
   const double matrices = (double)d.nb * d.nh, pairs = matrices * B * (d.s < b.block ? d.s : B);   // of queries and keys, of a pair of blocks
@@ -630,12 +633,13 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
   }
   p.chunks = (d.s + kListChunk - 1) / kListChunk;
   p.joint = bwd && b.block <= 128;
-  // Pieces of dK and dV: longer ones are fewer sums through memory, shorter ones fill the card.  Backward, us, with pieces of 256 / 512 / 1024 / 2048:
-  // width 128, blocks of 128, one of 4096 queries, 8 blocks 65 / 68 / 77 / 99; one of 8192, 8 88 / 78 / 86 / 107; two of 8192, 8 122 / 113 / 104 / 125; one
-  // of 16384, 16 178 / 163 / 158 / 149; 16 of 4096, 8 - / 275 / 250 / 240 (4096: 240).  (One device's pairs: sums depend on it.)
+  // Pieces of a block's list: longer ones are fewer sums of dK and dV through memory, shorter ones fill the card.  Backward, us, with pieces chosen
+  // so that a device's pairs make 256 / 384 / 512 of them and more: width 128, one of 8192 queries, 8 blocks of 128 69 / 63 / 64; 24 104 / 103 / 117; one of
+  // 16384, 16 144 / 109 / 117; two of 8192, 8 93 / 79 / 85; width 64, one of 16384, 16 118 / 85 / 94; at most 2048 queries: 16 of 4096 x 128, 8 blocks
+  // 215 with 1024, 178, 175 with 4096.  (One device's pairs: sums depend on it.)
   const size_t all_pairs = pairs * d.nb * d.nh;
   p.seg[1] = 256;
-  while (p.seg[1] < 2048 && all_pairs / p.seg[1] >= 256) p.seg[1] *= 2;
+  while (p.seg[1] < 2048 && all_pairs / p.seg[1] >= 384) p.seg[1] *= 2;
   p.most[1] = (int)(blocks + pairs / p.seg[1]);
   const size_t row_bytes = pairs * (d.d * 2 + (p.joint ? d.d / 8 : 12));   // of a matrix
   const size_t key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;

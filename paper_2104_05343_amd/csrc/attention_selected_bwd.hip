@@ -327,8 +327,7 @@ struct SelectedBwd {
   static constexpr bool WIDE = D == 128 && KEYS == 128;
   static constexpr int WAVES = WIDE ? 8 : 4, THREADS = 64 * WAVES, RG = KEYS / 32, PARW = WAVES / RG;   // RG: groups of 32 keys; PARW: wavefronts of one
   static constexpr int TILES = 2 * (D / 32) / WAVES;   // of dQ a wavefront
-  static constexpr int MOST = D == 64 && KEYS == 64 ? 3 : 2;   // wavefronts a SIMD (width 128, 64 keys: one, LDS)
-  static constexpr int KREG = WIDE ? 4 : KEYS == 64 ? 0 : D / 16, VREG = D == 128 ? 0 : D / 16;   // own fragments in registers, others in LDS
+  static constexpr int KREG = WIDE ? 4 : D == 128 ? 0 : D / 16, VREG = D == 128 ? 0 : D / 16;   // own fragments in registers, others in LDS
   struct Lds {
     bf16_t block[2][2][BLK * D];       // [stage][Q, dO]
     bf16_t k[KEYS * D];
@@ -369,7 +368,7 @@ __device__ __forceinline__ void store_part(const f32x16& acc, int row, int dt, _
 }
 
 template <int D, int KEYS>
-__global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), (SelectedBwd<D, KEYS>::MOST)) void selected_bwd_kernel(SelectedArgs a) {
+__global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), 2) void selected_bwd_kernel(SelectedArgs a) {
   typedef SelectedBwd<D, KEYS> B;
   constexpr int KS = D / 16, DT = D / 32, NW = B::WAVES, KREG = B::KREG, VREG = B::VREG;
   __shared__ __attribute__((aligned(1024))) typename B::Lds lds;

@@ -41,7 +41,7 @@ struct SelectedArgs {
   // lists
   int mats, mat0, portion;             // matrices of the call, first one of this launch, how many it has
   int chunks;                          // kListChunk pieces of a sequence
-  int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, most items of a matrix
+  int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, about; most items of a matrix
   int* counts;                         // [matrix][chunk][block]: pairs; then pairs of earlier chunks of the block
   int* offsets;                        // [matrix][blocks + 1]: place of a block's first pair
   int* first_item;                     // [kind][matrix][blocks + 1]

@@ -138,7 +138,7 @@ def test_form(form):
     for backward in (False, True):
         assert masked(1, 64, 1, True, backward) and masked(200, 64, 3, False, backward) and masked(4096, 128, 8, True, backward) != backward
         assert not masked(32768, 128, 16, True, backward) and not masked(8192, 128, 4, True, backward)
-        assert masked(16384, 64, 64, True, backward) and not masked(16385, 64, 64, True, backward)              # 256 and 257 blocks
+        assert masked(16384, 64, 64, True, backward) != backward and not masked(16385, 64, 64, True, backward)  # 256 and 257 blocks
         # the same for one device, whatever the launch covers
         sel = opt.make_selection(64, 6)
         for s in (500, 1000, 2000, 3000):

@@ -303,7 +303,7 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * qkv, attn, d_attn, d_qkv (16-byte aligned: EINVAL), lse, coordinates and limits as in optimus_attention_fused_*; bf16 only;
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
- * from call to call: calls that may overlap need one each.  It holds up to 384 MiB of partial results, or one (sequence, head)'s:
+ * from call to call: calls that may overlap need one each.  It holds up to 1 GiB of partial results, or one (sequence, head)'s:
  * s * count * (2 d + 12) bytes. */
 typedef struct {
   int block, count;

@@ -52,6 +52,26 @@ __device__ __forceinline__ void chunk_pairs(const SelectedArgs& a, int mm, int l
     }
   }
 }
+// rowsum(dO * O) of a wavefront's 32 queries from t0 on, 0 past the end of a sequence
+template <int D>
+__device__ __forceinline__ void delta_rows(const SelectedArgs& a, int mm, int t0) {
+  const FusedArgs& f = a.f;
+  const int lane = threadIdx.x & 63, g = lane >> 5;
+  const SelMatrix m = selected_matrix<D>(a, mm);
+  const int t = t0 + (lane & 31), row = min(t, f.s - 1);
+  float delta = 0.f;
+  if (t < m.len) {
+    const bf16_t* G = f.d_attn + m.attn + (long long)row * f.ldo + g * 8;
+    const bf16_t* O = f.attn + m.attn + (long long)row * f.ldo + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) delta += delta_piece(*(const bf16x8*)(G + ks * 16), *(const bf16x8*)(O + ks * 16));
+  }
+  delta = halfwave_sum(delta);
+  if (g == 0 && t < f.s) f.delta[m.vec + t] = delta;
+}
+
+// D > 0, ahead of a backward pass: the queries' delta too.
+template <int D>
 __global__ __launch_bounds__(kListChunk) void list_count_kernel(SelectedArgs a) {
   extern __shared__ unsigned bits[];
   const int chunk = blockIdx.x, mm = blockIdx.y;
@@ -65,6 +85,10 @@ __global__ __launch_bounds__(kListChunk) void list_count_kernel(SelectedArgs a) 
 #pragma unroll
     for (int w = 0; w < kWords; ++w) n += __popc(bits[w * a.blocks + v]);
     a.counts[((long long)mm * a.chunks + chunk) * a.blocks + v] = n;
+  }
+  if constexpr (D > 0) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) delta_rows<D>(a, mm, chunk * kListChunk + (threadIdx.x >> 6) * 64 + 32 * k);
   }
 }
 
@@ -91,35 +115,8 @@ __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
   return before + in - x;
 }
 
-// rowsum(dO * O) of a wavefront's 32 queries from t0 on, 0 past the end of a sequence
-template <int D>
-__device__ __forceinline__ void delta_rows(const SelectedArgs& a, int mm, int t0) {
-  const FusedArgs& f = a.f;
-  const int lane = threadIdx.x & 63, g = lane >> 5;
-  const SelMatrix m = selected_matrix<D>(a, mm);
-  const int t = t0 + (lane & 31), row = min(t, f.s - 1);
-  float delta = 0.f;
-  if (t < m.len) {
-    const bf16_t* G = f.d_attn + m.attn + (long long)row * f.ldo + g * 8;
-    const bf16_t* O = f.attn + m.attn + (long long)row * f.ldo + g * 8;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) delta += delta_piece(*(const bf16x8*)(G + ks * 16), *(const bf16x8*)(O + ks * 16));
-  }
-  delta = halfwave_sum(delta);
-  if (g == 0 && t < f.s) f.delta[m.vec + t] = delta;
-}
-
-// A workgroup a matrix.  D > 0, ahead of a backward pass: workgroups behind them take 512 queries' delta, which needs no list.
-template <int D>
 __global__ __launch_bounds__(1024) void list_places_kernel(SelectedArgs a) {
   __shared__ int lds[16];
-  if constexpr (D > 0) {
-    if ((int)blockIdx.x >= a.mats) {
-      const int groups = (a.f.s + 511) / 512, k = blockIdx.x - a.mats;
-      delta_rows<D>(a, k / groups, k % groups * 512 + (threadIdx.x >> 6) * 32);
-      return;
-    }
-  }
   const int mm = blockIdx.x, v = threadIdx.x;
   int n = 0;
   if (v < a.blocks) {
@@ -552,12 +549,12 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
 
 void launch_lists(const SelectedArgs& a, int d, bool bwd, hipStream_t st) {
   const size_t bits = (size_t)kWords * a.blocks * sizeof(unsigned);   // at most 32 KiB
-  list_count_kernel<<<dim3(a.chunks, a.mats), kListChunk, bits, st>>>(a);
-  const int all = a.mats + a.mats * ((a.f.s + 511) / 512);
-  if (!bwd) list_places_kernel<0><<<a.mats, 1024, 0, st>>>(a);
-  else if (d == 64) list_places_kernel<64><<<all, 1024, 0, st>>>(a);
-  else list_places_kernel<128><<<all, 1024, 0, st>>>(a);
-  list_fill_kernel<<<dim3(a.chunks, a.mats), kListChunk, 2 * bits, st>>>(a);
+  const dim3 grid(a.chunks, a.mats);
+  if (!bwd) list_count_kernel<0><<<grid, kListChunk, bits, st>>>(a);
+  else if (d == 64) list_count_kernel<64><<<grid, kListChunk, bits, st>>>(a);
+  else list_count_kernel<128><<<grid, kListChunk, bits, st>>>(a);
+  list_places_kernel<<<a.mats, 1024, 0, st>>>(a);
+  list_fill_kernel<<<grid, kListChunk, 2 * bits, st>>>(a);
 }
 
 template <int D>

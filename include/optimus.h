@@ -304,7 +304,9 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
  * from call to call: calls that may overlap need one each.  It holds up to 1 GiB of partial results, or one (sequence, head)'s:
- * s * count * (2 d + 12) bytes. */
+ * some s * count * (2 d + 16) bytes.
+ * How it is computed (all blocks with a mask, or lists of each block's queries), and with it the last bits, follows the sizes, those of one
+ * device whatever the call covers. */
 typedef struct {
   int block, count;
   const int32_t* lengths;

@@ -589,7 +589,7 @@ void launch_selected_dq_combine(const SelectedArgs& a, int d, bool joint, hipStr
 // through memory once a block, and have a price a call and a query for the lists and the sums.
 // Measured, us, masked / lists, causal, 16 (sequence, head)s unless said otherwise; forward, backward:
 //   width 128: 8192 queries, blocks of 128, 4 chosen 341 / 125, 1086 / 223; 8 296 / 195, 1068 / 354; 12 285 / 288, 1055 / 471; 16 284 / 348, 1064 / 569;
-//   16384, 256, 8 1091 / 610, 4423 / 1283; 4096, 64, 4 79 / 60, 276 / 128; 14 80 / 138, 295 / 253; 4096, 512, 2 76 / 82, 291 / 210;
+//   16384, 256, 8 1091 / 610, 4423 / 1283; 4096, 64, 4 79 / 60, 276 / 122; 14 80 / 138, 295 / 226; 4096, 512, 2 76 / 82, 291 / 210;
 //   one of 1024, 64, 4 20 / 23, 39 / 48; 8192, 128, 24 112 / 61, 212 / 105; no mask, 4096, 128, 10 142 / 125, 541 / 208
 //   width 64: 8192, 128, 8 158 / 111, 609 / 178; 16 162 / 193, 616 / 305; 16384, 256, 8 579 / 324, 2479 / 744; 4096, 64, 8 55 / 59, 175 / 85; 4096, 512, 2
 //   51 / 64, 171 / 145; one of 1024, 64, 4 12 / 23, 25 / 36; 8192, 128, 24 66 / 50, 132 / 84
@@ -601,7 +601,7 @@ struct FormCost {
 };
 constexpr FormCost kFormCost[3][2] = {   // [forward, backward of blocks of 64 and 128, of larger ones][width 64, 128]
     {{2.8e-7, 6, 0.008, 25, 1.2e-4, 1.6, 128}, {5.0e-7, 6, 0.0138, 25, 1.2e-4, 1.55, 137}},
-    {{1.1e-6, 10, 0.015, 38, 1.4e-4, 0.82, 18}, {1.9e-6, 12, 0.024, 46, 3.6e-4, 0.27, 101}},
+    {{1.1e-6, 10, 0.015, 38, 1.4e-4, 0.82, 18}, {1.9e-6, 12, 0.024, 46, 3.6e-4, 0.62, 56}},
     {{1.1e-6, 10, 0.015, 38, 3e-4, 1.05, 30}, {1.9e-6, 12, 0.024, 46, 4e-4, 0.98, 60}}};
 bool attn_selected_masked(const AttnSelectedDesc& b, bool bwd) {
   const AttnFusedDesc& d = b.base;

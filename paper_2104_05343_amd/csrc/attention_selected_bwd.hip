@@ -377,7 +377,8 @@ template <int D, int KEYS>
 __global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), 2) void selected_bwd_kernel(SelectedArgs a) {
   typedef SelectedBwd<D, KEYS> B;
   constexpr int KS = D / 16, DT = D / 32, NW = B::WAVES, KREG = B::KREG, VREG = B::VREG;
-  __shared__ __attribute__((aligned(1024))) typename B::Lds lds;
+  extern __shared__ __attribute__((aligned(1024))) char selected_bwd_lds[];   // (of a size that the compiler does not know: where it holds one wavefront
+  typename B::Lds& lds = *(typename B::Lds*)selected_bwd_lds;                 // a SIMD, 512 registers are half of them moves)
   const FusedArgs& f = a.f;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -738,14 +739,21 @@ __global__ __launch_bounds__(256) void selected_dkv_combine_kernel(SelectedArgs 
   }
 }
 
+template <int D, int KEYS>
+void launch_joint(const SelectedArgs& a, hipStream_t st) {
+  typedef SelectedBwd<D, KEYS> B;
+  constexpr int lds = sizeof(typename B::Lds);
+  if (lds > 65536) (void)hipFuncSetAttribute((const void*)selected_bwd_kernel<D, KEYS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  selected_bwd_kernel<D, KEYS><<<a.most[1] * a.portion, B::THREADS, lds, st>>>(a);
+}
 template <int D>
 int bwd_launch(SelectedArgs a, const SelectedPlan& p, hipStream_t st) {
   const int s = a.f.s;
   if (p.joint) {
     for (a.mat0 = 0; a.mat0 < p.mats; a.mat0 += p.portion) {
       a.portion = min(p.portion, p.mats - a.mat0);
-      if (a.block == 64) selected_bwd_kernel<D, 64><<<a.most[1] * a.portion, SelectedBwd<D, 64>::THREADS, 0, st>>>(a);
-      else selected_bwd_kernel<D, 128><<<a.most[1] * a.portion, SelectedBwd<D, 128>::THREADS, 0, st>>>(a);
+      if (a.block == 64) launch_joint<D, 64>(a, st);
+      else launch_joint<D, 128>(a, st);
       launch_selected_dq_combine(a, D, true, st);
       selected_dkv_combine_kernel<D><<<dim3((s + 31) / 32, a.portion), 256, 0, st>>>(a);
       if (const int rc = hip_launch_status()) return rc;

@@ -495,3 +495,40 @@ def test_rows_past_four_gigabytes(form_of, block):
         score = mean[:-1] @ Q[-1]
         best = int(np.argmax(score))
         assert chosen[head, -1].tolist() == [best, (s - 1) // block]
+
+
+def test_two_calls_at_once_and_graphs_that_share_a_workspace(form):
+    """Two streams with a workspace each; two graphs over one workspace, replayed in turn."""
+    a, b = (Run(2, 1500, 256, 4, 1, True, block=64, count=4, seed=k, lengths=[1500, 900 + k]) for k in range(2))
+    want = [[x.clone() for x in (r.S, r.O, r.L, r.G)] for r in (a.go(), b.go())]
+    same = lambda r, w: all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip((r.S, r.O, r.L, r.G), w))
+
+    def clear():
+        for r in (a, b):
+            r.S.fill_(-9)
+            for x in (r.O, r.L, r.G):
+                x.fill_(float("nan"))
+        torch.cuda.synchronize()
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    clear()
+    for step in ("choose", "forward", "backward"):
+        for r, st in zip((a, b), streams):
+            getattr(r, step)(stream=st)
+    torch.cuda.synchronize()
+    assert same(a, want[0]) and same(b, want[1])
+    b.args = b.args[:-1] + (a.ws,)
+    graphs = []
+    for r in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r.choose()
+            r.forward()
+            r.backward()
+        graphs.append(g)
+    for k in range(3):
+        clear()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert same(a, want[0]) and same(b, want[1])

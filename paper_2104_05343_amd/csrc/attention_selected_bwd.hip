@@ -333,7 +333,11 @@ struct SelectedBwd {
   static constexpr bool WIDE = D == 128 && KEYS == 128;
   static constexpr int WAVES = WIDE ? 8 : 4, THREADS = 64 * WAVES, RG = KEYS / 32, PARW = WAVES / RG;   // RG: groups of 32 keys; PARW: wavefronts of one
   static constexpr int TILES = 2 * (D / 32) / WAVES;   // of dQ a wavefront
-  static constexpr int KREG = WIDE ? 4 : D == 128 ? 0 : D / 16, VREG = D == 128 ? 0 : D / 16;   // own fragments in registers, others in LDS
+  static constexpr bool SMALL = D == 64 && KEYS == 64;
+  static constexpr int KREG = WIDE ? 4 : D == 128 || SMALL ? 0 : D / 16, VREG = D == 128 ? 0 : D / 16;   // own fragments in registers, others in LDS
+  // Wavefronts a SIMD.  SMALL: three, with K from LDS and its fragments one step ahead, 168 registers (20 (sequence, head)s of up to 10000, 12 of 157
+  // blocks: 265 us a call with two, 253 with three, 271 with fragments two ahead, which spill)
+  static constexpr int MOST = SMALL ? 3 : 2, AHEAD = SMALL ? 1 : 2;
   struct Lds {
     bf16_t block[2][2][BLK * D];       // [stage][Q, dO]
     bf16_t k[KEYS * D];
@@ -374,7 +378,7 @@ __device__ __forceinline__ void store_part(const f32x16& acc, int row, int dt, _
 }
 
 template <int D, int KEYS>
-__global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), 2) void selected_bwd_kernel(SelectedArgs a) {
+__global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), (SelectedBwd<D, KEYS>::MOST)) void selected_bwd_kernel(SelectedArgs a) {
   typedef SelectedBwd<D, KEYS> B;
   constexpr int KS = D / 16, DT = D / 32, NW = B::WAVES, KREG = B::KREG, VREG = B::VREG;
   extern __shared__ __attribute__((aligned(1024))) char selected_bwd_lds[];   // (of a size that the compiler does not know: where it holds one wavefront
@@ -466,7 +470,7 @@ __global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), 2) void selected_b
       const bool masked = a.causal && __builtin_amdgcn_readfirstlane(lds.t[st][half * 32]) < k0 + 31;
       f32x16 sacc = zero16(), pacc = zero16();
       struct Two { bf16x8 q, own; };
-      pipelined<2 * KS, 2>([&](int k) {
+      pipelined<2 * KS, B::AHEAD>([&](int k) {
                              const int ks = k / 2;
                              Two x;
                              x.q = rows_at<D>(qt, k & 1 ? BLK : 0, ks);

@@ -8,8 +8,8 @@ namespace optimus {
 namespace {
 
 // ---------------------------------------------------------------- lists
-// Bound: round trips to memory (the choice read twice, lists and places written once, one workgroup a matrix between them): 20, 13 and 31 us for 8
-// (sequence, head)s of 32768 queries with 16 entries each (17 MB), 5, 5 and 6 for 16 of 4096 with 8.
+// Bound: round trips to memory (the choice read twice, lists and places written once): 21 and 42 us for 8 (sequence, head)s of 32768 queries with 16
+// entries each (17 MB), 5 (10 with the backward pass' sums) and 8 for 16 of 4096 with 8.
 // Pairs of 256 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
 // make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
 constexpr int kWords = kListChunk / 32;
@@ -94,8 +94,9 @@ __global__ __launch_bounds__(kListChunk) void list_count_kernel(SelectedArgs a) 
   }
 }
 
-// exclusive sums of x over the 1024 threads, the sum of all in *total
+// exclusive sums of x over the workgroup's threads, the sum of all in *total
 __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
+  constexpr int kWaves = kListChunk / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int in = x;
 #pragma unroll
@@ -107,7 +108,7 @@ __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < 16; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     const int y = lds[w];
     before += w < wave ? y : 0;
     all += y;
@@ -117,45 +118,12 @@ __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
   return before + in - x;
 }
 
-__global__ __launch_bounds__(1024) void list_places_kernel(SelectedArgs a) {
-  __shared__ int lds[16];
-  const int mm = blockIdx.x, v = threadIdx.x;
-  int n = 0;
-  if (v < a.blocks) {
-    int* c = a.counts + (long long)mm * a.chunks * a.blocks + v;
-    for (int k = 0; k < a.chunks; k += 16) {   // sixteen loads in flight
-      int x[16];
-#pragma unroll
-      for (int u = 0; u < 16; ++u) x[u] = k + u < a.chunks ? c[(long long)(k + u) * a.blocks] : 0;
-#pragma unroll
-      for (int u = 0; u < 16; ++u) {
-        if (k + u < a.chunks) c[(long long)(k + u) * a.blocks] = n;
-        n += x[u];
-      }
-    }
-  }
-  int all;
-  const int at = exclusive_sum(n, lds, &all);
-  int* offsets = a.offsets + (long long)mm * (a.blocks + 1);
-  if (v < a.blocks) offsets[v] = at;
-  if (v == 0) offsets[a.blocks] = all;
-#pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    if (!a.items[kind]) continue;
-    // equal items of at most 1.25 seg rows, no short one at the end of a list
-    const int most = a.seg[kind] * 5 / 4, wanted = max((n + most - 1) / most, 1), size = ((n + wanted - 1) / wanted + 127) & ~127;
-    const int items = n > 0 ? (n + size - 1) / size : 0, first = exclusive_sum(items, lds, &all);
-    int* firsts = a.first_item + ((long long)kind * a.mats + mm) * (a.blocks + 1);
-    if (v < a.blocks) firsts[v] = first;
-    if (v == 0) firsts[a.blocks] = all;
-    for (int k = 0; k < items; ++k)
-      a.items[kind][(long long)mm * a.most[kind] + first + k] = i32x4_t{v, at + k * size, min(size, n - k * size), 0};
-  }
-}
-
+// Places and entries of a chunk.  Every workgroup adds up its matrix' counts itself (a launch of its own for them: 5 to 13 us); the first one of a
+// matrix writes the items too.
 __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
   extern __shared__ unsigned bits[];
   int* place_of = (int*)(bits + kWords * a.blocks);   // [word][block]: place of a word's first pair
+  int* lds = place_of + kWords * a.blocks;            // [kListChunk / 64]
   const int chunk = blockIdx.x, mm = blockIdx.y, tid = threadIdx.x;
   const int len = selected_matrix<64>(a, mm).len;
   const int t = chunk * kListChunk + tid;
@@ -164,14 +132,47 @@ __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
   unsigned long long counted = 0;   // (at most 64 entries)
   chunk_pairs(a, mm, len, t, bits, [&](int e, int, bool counts) { counted |= counts ? 1ull << e : 0; });
   __syncthreads();
-  const int* offsets = a.offsets + (long long)mm * (a.blocks + 1);
-  const int* before = a.counts + ((long long)mm * a.chunks + chunk) * a.blocks;
-  for (int v = tid; v < a.blocks; v += kListChunk) {
-    int n = offsets[v] + before[v];
+  int earlier_pairs = 0, earlier_items[2] = {0, 0};   // of the blocks below
+  for (int v0 = 0; v0 < a.blocks; v0 += kListChunk) {
+    const int v = v0 + tid;
+    int pairs = 0, before = 0;   // of the block, in earlier chunks
+    if (v < a.blocks) {
+      const int* c = a.counts + (long long)mm * a.chunks * a.blocks + v;
+      for (int k = 0; k < a.chunks; k += 16) {   // sixteen loads in flight
+        int x[16];
 #pragma unroll
-    for (int w = 0; w < kWords; ++w) {
-      place_of[w * a.blocks + v] = n;
-      n += __popc(bits[w * a.blocks + v]);
+        for (int u = 0; u < 16; ++u) x[u] = k + u < a.chunks ? c[(long long)(k + u) * a.blocks] : 0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          pairs += x[u];
+          before += k + u < chunk ? x[u] : 0;
+        }
+      }
+    }
+    int all;
+    const int at = earlier_pairs + exclusive_sum(pairs, lds, &all);
+    earlier_pairs += all;
+    if (v < a.blocks) {
+      int n = at + before;
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) {
+        place_of[w * a.blocks + v] = n;
+        n += __popc(bits[w * a.blocks + v]);
+      }
+    }
+    if (chunk > 0) continue;
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      if (!a.items[kind]) continue;
+      // equal items of at most 1.25 seg rows, no short one at the end of a list
+      const int most = a.seg[kind] * 5 / 4, wanted = max((pairs + most - 1) / most, 1), size = ((pairs + wanted - 1) / wanted + 127) & ~127;
+      const int items = pairs > 0 ? (pairs + size - 1) / size : 0, first = earlier_items[kind] + exclusive_sum(items, lds, &all);
+      earlier_items[kind] += all;
+      int* firsts = a.first_item + ((long long)kind * a.mats + mm) * (a.blocks + 1);
+      if (v < a.blocks) firsts[v] = first;
+      if (tid == 0) firsts[min(v0 + kListChunk, a.blocks)] = earlier_items[kind];
+      for (int k = 0; k < items; ++k)
+        a.items[kind][(long long)mm * a.most[kind] + first + k] = i32x4_t{v, at + k * size, min(size, pairs - k * size), 0};
     }
   }
   __syncthreads();
@@ -536,7 +537,6 @@ SelectedArgs with_workspace(const AttnSelectedDesc& b, const SelectedPlan& p, bo
   a.f.delta = (float*)take(p.delta);
   a.mask = (unsigned*)take(p.mask);
   a.counts = (int*)take(p.counts);
-  a.offsets = (int*)take(p.offsets);
   a.first_item = (int*)take(p.first_item);
   for (int k = 0; k < 2; ++k) {
     a.seg[k] = p.seg[k];
@@ -560,8 +560,9 @@ void launch_lists(const SelectedArgs& a, int d, bool bwd, hipStream_t st) {
   if (!bwd) list_count_kernel<0><<<grid, kListChunk, bits, st>>>(a);
   else if (d == 64) list_count_kernel<64><<<grid, kListChunk, bits, st>>>(a);
   else list_count_kernel<128><<<grid, kListChunk, bits, st>>>(a);
-  list_places_kernel<<<a.mats, 1024, 0, st>>>(a);
-  list_fill_kernel<<<grid, kListChunk, 2 * bits, st>>>(a);
+  const size_t fill = 2 * bits + kListChunk / 64 * sizeof(int);
+  if (fill > 65536) (void)hipFuncSetAttribute((const void*)list_fill_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)fill);
+  list_fill_kernel<<<grid, kListChunk, fill, st>>>(a);
 }
 
 template <int D>
@@ -656,7 +657,6 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
   while (p.seg[0] < 1024 && p.portion * pairs / p.seg[0] >= 4096) p.seg[0] *= 2;
   p.most[0] = (int)(blocks + pairs / p.seg[0]);
   p.counts = round256(mats * p.chunks * blocks * 4);
-  p.offsets = round256(mats * (blocks + 1) * 4);
   p.first_item = round256(2 * mats * (blocks + 1) * 4);
   p.items[0] = p.joint ? 0 : round256(mats * p.most[0] * 16);
   p.items[1] = bwd ? round256(mats * p.most[1] * 16) : 0;
@@ -666,7 +666,7 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
   p.keys = p.joint ? round256(keys) : 0;
   p.units = round256(p.portion * pairs * (p.joint ? d.d / 32 : 1) * 4);
   p.ml = bwd ? 0 : round256(p.portion * pairs * 8);
-  p.total = p.delta + p.counts + p.offsets + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.units + p.ml + p.keys;
+  p.total = p.delta + p.counts + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.units + p.ml + p.keys;
   *out = p;
 }
 size_t attn_selected_ws_bytes(const AttnSelectedDesc& b) {

@@ -44,8 +44,7 @@ struct SelectedArgs {
   int mats, mat0, portion;             // matrices of the call, first one of this launch, how many it has
   int chunks;                          // kListChunk pieces of a sequence
   int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, about; most items of a matrix
-  int* counts;                         // [matrix][chunk][block]: pairs; then pairs of earlier chunks of the block
-  int* offsets;                        // [matrix][blocks + 1]: place of a block's first pair
+  int* counts;                         // [matrix][chunk][block]: pairs
   int* first_item;                     // [kind][matrix][blocks + 1]
   i32x4_t* items[2];                   // [matrix][most]: block, place of the first pair, pairs, -
   int* list;                           // [matrix][s * count]: query of every pair
@@ -63,7 +62,7 @@ struct SelectedPlan {
   int mats, chunks, mask_words;
   int portion, key_portion;            // matrices whose partial results are in memory at a time: of queries, of keys
   int seg[2], most[2];
-  size_t delta, mask, counts, offsets, first_item, items[2], list, places, rows, units, ml, keys, total;
+  size_t delta, mask, counts, first_item, items[2], list, places, rows, units, ml, keys, total;
 };
 
 // csrc/attention_selected*.hip

@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
     pipelined<2 * KT * DT, AHEAD>([&](int n) { return cols_at<D>(in_cols, n / DT / 4 * (2 * BLK) + n / DT % 4 * 16, n % DT); },
                                   [&](int n, const bf16x8& x) {
                                     const int k = n / DT;
-                                    oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf[k / 2][k & 1], x, oacc[n % DT], 0, 0, 0);
+                                    oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[k / 2][k & 1], oacc[n % DT], 0, 0, 0);
                                   });
     const long long at = out + base + wave * 32;
     const int left = min(it.pairs - base - wave * 32, 32);
@@ -385,11 +385,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
           const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);   // (m_new is a score: the first step holds a key of every row)
           l_run *= alpha;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float of_row = __shfl(alpha, slot(r) + 4 * g);
+          for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) oacc[dt][r] *= of_row;
-          }
+            for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
           m_run = m_new;
         }
         l_run += sum;
@@ -402,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
         pipelined<4 * DT, AHEAD>([&](int n) { return cols_at<D>(vt, n / DT * 16, n % DT); },
                                  [&](int n, const bf16x8& x) {
                                    const int k = n / DT;
-                                   oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf[k / 2][k & 1], x, oacc[n % DT], 0, 0, 0);
+                                   oacc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[k / 2][k & 1], oacc[n % DT], 0, 0, 0);
                                  });
       }
       wait_loads_and_barrier();
@@ -416,14 +414,13 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
 }
 
 // A query's rows to its output, a half-wavefront each.  FORWARD: weighted by their maxima, divided by the sum; the others: added, times
-// 1 / sqrt(d), to dQ.  JOINT: rows in the order of their columns, 32 of which have a scale.
+// 1 / sqrt(d), to dQ.  JOINT: 32 columns of a row have a scale.
 // A row is 16 bytes of 16 lanes (8 of width 64), so that two or four come at a time, and four times as many are in flight.
 // Bound: memory, 4.3 TB/s of scattered rows of 256 bytes forward, 5 and 6.8 TB/s backward (width 128, 64), where the cache still holds some.
 template <int D, bool FORWARD, bool JOINT>
 __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
-  constexpr int DT = D / 32, LANES = D / 8, PARTS = 32 / LANES;
+  constexpr int LANES = D / 8, PARTS = 32 / LANES;
   typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-  __shared__ __attribute__((aligned(16))) float lds[8][D];
   const FusedArgs& f = a.f;
   const int half = threadIdx.x >> 5, n = threadIdx.x & 31, part = n / LANES, c = n % LANES;
   const int mm = a.mat0 + blockIdx.y;
@@ -450,7 +447,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[u][k] = 0;
       if (p >= 0) x[u] = *(const f16x8*)(a.rows + (rows + p) * D + c * 8);
-      if (JOINT) unit[u] = p >= 0 ? a.units[(rows + p) * DT + c / 4] : 0.f;
+      if (JOINT) unit[u] = p >= 0 ? a.units[(rows + p) * (D / 32) + c / 4] : 0.f;
     }
   };
   load_rows(0);
@@ -495,13 +492,13 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   for (int step = LANES; step < 32; step <<= 1)
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] += __shfl_xor(sum[k], step);
-  if (part == 0) {   // numbers 8c .. of a row are [column % 32][column / 32]
+  if (inside && part == 0) {
+    bf16_t* to = FORWARD ? f.attn + m.attn + (long long)t * f.ldo : f.d_qkv + m.qkv + (long long)t * f.ld;
+    u32x4 w;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) lds[half][JOINT ? 8 * c + k : (8 * c + k) % DT * 32 + (8 * c + k) / DT] = FORWARD ? sum[k] : sum[k] * f.scale;
+    for (int k = 0; k < 4; ++k) w[k] = FORWARD ? pack2_bf16(sum[2 * k], sum[2 * k + 1]) : pack2_bf16(sum[2 * k] * f.scale, sum[2 * k + 1] * f.scale);
+    *(u32x4*)(to + 8 * c) = w;
   }
-  __builtin_amdgcn_wave_barrier();
-  bf16_t* to = FORWARD ? f.attn + m.attn + (long long)t * f.ldo : f.d_qkv + m.qkv + (long long)t * f.ld;
-  write_ordered<DT>(to, lds[half], n, inside);
   if (FORWARD && inside && n == 0) f.lse[m.vec + t] = total > 0.f ? (top + __log2f(total)) * LN2 : -INFINITY;
 }
 

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void selected_dq_kernel(SelectedArgs a) {
           dq_scores<D>(dsf, in_rows + at + t2 * (32 * D * 2), qf, dof, lse2, delta, f.scale_log2, masked, limit - kbase - 32 * t2 - 4 * g);
           pipelined<2 * DT, 2>([&](int n) { return cols_at<D>(in_cols + at, t2 * 32 + n / DT * 16, n % DT); },
                                [&](int n, const bf16x8& x) {
-                                 acc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dsf[n / DT], x, acc[n % DT], 0, 0, 0);
+                                 acc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, dsf[n / DT], acc[n % DT], 0, 0, 0);
                                });
         }
       }
@@ -348,33 +348,16 @@ struct SelectedBwd {
     alignas(16) int t[2][BLK];
   };
 };
-// A lane's 16 numbers of a query's 32 columns from 32 dt on (slot r is column slot(r) + 4 g) to fp16, scaled as in store_parts: two stores of 16 bytes, one
-// of the scale.
+// A lane's 16 numbers of a query's 32 columns from 32 dt on, with a scale of their own: three stores
 template <int DT>
-__device__ __forceinline__ void store_part(const f32x16& acc, int row, int dt, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t units, int g) {
-  float most = larger(fabsf(acc[0]), fabsf(acc[1]));
-#pragma unroll
-  for (int r = 2; r < 16; r += 2) most = larger(larger(most, fabsf(acc[r])), fabsf(acc[r + 1]));
-  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
-  most = larger(__uint_as_float(both[0]), __uint_as_float(both[1]));
-  const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 16), 254);
-  const float scale = __uint_as_float((unsigned)(268 - e) << 23);
-  typedef __attribute__((ext_vector_type(4))) _Float16 Four;
-  u32x2 h[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    Four x;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = (f16_t)(acc[4 * c + k] * scale);
-    h[c] = __builtin_bit_cast(u32x2, x);
-  }
-#pragma unroll
-  for (int c = 0; c < 4; c += 2) {   // lanes 0 .. 31: eight columns from 8 c on, the others the next eight
-    const auto lo = __builtin_amdgcn_permlane32_swap(h[c][0], h[c + 1][0], false, false);
-    const auto hi = __builtin_amdgcn_permlane32_swap(h[c][1], h[c + 1][1], false, false);
-    __builtin_amdgcn_raw_buffer_store_b128(u32x4{lo[0], hi[0], lo[1], hi[1]}, rows, row * (64 * DT) + dt * 64 + (c + g) * 16, 0, 0);
-  }
-  __builtin_amdgcn_raw_buffer_store_b32((int)((unsigned)(e - 14) << 23), units, g == 0 ? (row * DT + dt) * 4 : 0x7fffffff, 0, 0);
+__device__ __forceinline__ void store_part(const f32x16& acc, int row0, int dt, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t units, int lane) {
+  const RowScale s = row_scale(largest_size(acc, 0.f));
+  u32x4 w[2];   // (64 whole bytes of sixteen rows a store)
+  pack_columns(acc, s.scale, w);
+  const int at = (row0 + (lane & 15)) * (64 * DT) + dt * 64 + (lane >> 4 & 1) * 32 + (lane >> 5) * 16;
+  __builtin_amdgcn_raw_buffer_store_b128(w[0], rows, at, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(w[1], rows, at + 16 * 64 * DT, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b32((int)s.unit, units, lane < 32 ? ((row0 + lane) * DT + dt) * 4 : 0x7fffffff, 0, 0);
 }
 
 template <int D, int KEYS>
@@ -518,7 +501,7 @@ __global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), (SelectedBwd<D, KE
     const auto to_rows = __builtin_amdgcn_make_buffer_rsrc(rows + (long long)n * BLK * D, 0, left * (2 * D), 0x00020000);
     const auto to_units = __builtin_amdgcn_make_buffer_rsrc(units + (long long)n * BLK * DT, 0, left * (4 * DT), 0x00020000);
 #pragma unroll
-    for (int i = 0; i < B::TILES; ++i) store_part<DT>(dq[i], q_half * 32 + (lane & 31), dt0 + i, to_rows, to_units, g);
+    for (int i = 0; i < B::TILES; ++i) store_part<DT>(dq[i], q_half * 32, dt0 + i, to_rows, to_units, lane);
     // all but this iteration's stores, three a tile, have ended: the loads into the other stage were issued ahead of them
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt((3 * B::TILES) | (7 << 4) | (15 << 8));

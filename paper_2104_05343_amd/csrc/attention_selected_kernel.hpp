@@ -115,20 +115,6 @@ __device__ __forceinline__ void store_rows(float* to, const f32x16 (&acc)[DT], i
 // and dS to bf16 has left it off by some 2^-9; the sums over a block's keys and over the blocks stay fp32.  (8 (sequence, head)s of 32768 x 128,
 // 16 of 256 blocks: 2.2 GB of fp32 rows cost 300 us to write beside the products' 417, and 389 to read.)  Each row is scaled by a power of
 // two that brings its largest number to 2^14, so that nothing is lost to fp16's range but what is below 2^-28 of that.
-template <int DT> struct RowHalves;
-template <> struct RowHalves<4> { typedef __attribute__((ext_vector_type(4))) _Float16 V; };
-template <> struct RowHalves<2> { typedef __attribute__((ext_vector_type(2))) _Float16 V; };
-
-template <int CTRL>
-__device__ __forceinline__ float lane_moved(float x) {
-  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
-}
-// first: [a's row of 16 lanes 0, b's 0, a's 2, b's 2]; second: [a's 1, b's 1, a's 3, b's 3]
-__device__ __forceinline__ void swap_rows(float& a, float& b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-  a = __uint_as_float(r[0]);
-  b = __uint_as_float(r[1]);
-}
 // The maximum that passes NaN on: two operands or three an instruction.  (fmaxf first clears signalling NaN out of every operand that might be one,
 // such as a matrix instruction's result, by an instruction of its own.)
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
@@ -137,69 +123,77 @@ __device__ __forceinline__ float largest(const f32x16& v, float m) {
   for (int r = 0; r < 16; r += 2) m = larger(larger(m, v[r]), v[r + 1]);
   return m;
 }
+// A lane has one row's numbers: products with the rows' operand in the B slot, slot r of a 32 x 32 tile is column slot(r) + 4 g.  What scales them, the
+// reciprocal of what they are to be multiplied by later: 2^(141 - e) for a largest number of biased exponent e.
+struct RowScale { float scale; unsigned unit; };
+__device__ __forceinline__ RowScale row_scale(float most) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+  most = larger(__uint_as_float(both[0]), __uint_as_float(both[1]));
+  const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 16), 254);
+  return {__uint_as_float((unsigned)(268 - e) << 23), (unsigned)(e - 14) << 23};
+}
+__device__ __forceinline__ float largest_size(const f32x16& v, float m) {
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) m = larger(larger(m, fabsf(v[r])), fabsf(v[r + 1]));
+  return m;
+}
+// 32 columns of a wavefront's 32 rows as fp16: lane n % 16 of w[k] has row 16 k + n % 16, columns 16 (n / 16 % 2) + 8 (n / 32) .. + 7
+__device__ __forceinline__ void pack_columns(const f32x16& acc, float scale, u32x4 (&w)[2]) {
+  typedef __attribute__((ext_vector_type(4))) _Float16 Four;
+  u32x2 h[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    Four x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = (f16_t)(acc[4 * c + k] * scale);
+    h[c] = __builtin_bit_cast(u32x2, x);
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {   // lanes 0 .. 31: columns 16 c .. + 7, the others the next eight
+    const auto lo = __builtin_amdgcn_permlane32_swap(h[2 * c][0], h[2 * c + 1][0], false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(h[2 * c][1], h[2 * c + 1][1], false, false);
+    w[c] = u32x4{lo[0], hi[0], lo[1], hi[1]};
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {   // lanes 16 .. 31 and 48 .. 63 of the first with the sixteen before them of the second: rows 0 .. 15, rows 16 .. 31
+    const auto r = __builtin_amdgcn_permlane16_swap(w[0][k], w[1][k], false, false);
+    w[0][k] = r[0];
+    w[1][k] = r[1];
+  }
+}
+template <int CTRL, int BANKS>
+__device__ __forceinline__ unsigned moved_into(unsigned old, unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, 0xf, BANKS, false); }
+
+// A wavefront's 32 rows, `rows` of them there, whole.
+// Through buffer resources that end behind the last row: a store under a condition would have the wait for the next tile's queries, which are
+// requested ahead of it, wait for the stores too.
 template <int DT>
 __device__ __forceinline__ void store_parts(f16_t* to, float* units, const f32x16 (&acc)[DT], int rows, int g, int lane) {
-  const int left = __builtin_amdgcn_readfirstlane(rows);
-  typedef typename RowHalves<DT>::V V;
-  // largest of row r over 32 lanes, 16 rows at once: with every step a lane keeps half as many of them
-  float most[16];
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    most[r] = larger(fabsf(acc[0][r]), fabsf(acc[1][r]));
-    if constexpr (DT == 4) most[r] = larger(larger(most[r], fabsf(acc[2][r])), fabsf(acc[3][r]));
-  }
-#pragma unroll
-  for (int r = 0; r < 8; ++r) {   // rows r and r + 8: lanes 0 .. 15 keep the first
-    swap_rows(most[r], most[r + 8]);
-    most[r] = larger(most[r], most[r + 8]);
-  }
-  const bool upper = lane & 8;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {   // rows r and r + 4: every other eight lanes
-    const float keep = upper ? most[r + 4] : most[r], give = upper ? most[r] : most[r + 4];
-    most[r] = larger(keep, lane_moved<0x128>(give));
-    most[r] = larger(most[r], lane_moved<0xB1>(most[r]));
-    most[r] = larger(most[r], lane_moved<0x4E>(most[r]));
-    most[r] = larger(most[r], lane_moved<0x141>(most[r]));
-  }
-  // a lane's four rows are r + 4 (lane / 8 % 4).  2^(141 - e) for a largest number of biased exponent e
-  float scale[16];
-  float4 unit;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int e = min(max((int)(__float_as_uint(most[r]) >> 23 & 255), 16), 254);
-    scale[r] = __uint_as_float((unsigned)(268 - e) << 23);
-    (&unit.x)[r] = __uint_as_float((unsigned)(e - 14) << 23);
-  }
-  const int first_row = 8 * (lane >> 3 & 3) + 4 * g;   // slot(r) + 4 g of them
-  // Through buffer resources that end behind the last row: a store under a condition would have the wait for the next tile's queries, which are
-  // requested ahead of it, wait for the stores too.
+  const int left = __builtin_amdgcn_readfirstlane(rows), row = lane & 31;
   const auto to_units = __builtin_amdgcn_make_buffer_rsrc(units, 0, left * 4, 0x00020000);
   const auto to_rows = __builtin_amdgcn_make_buffer_rsrc(to, 0, left * (64 * DT), 0x00020000);
+  float most = 0.f;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    __builtin_amdgcn_raw_buffer_store_b32((int)__float_as_uint((&unit.x)[r]), to_units, (lane & 7) == 0 ? (first_row + r) * 4 : 0x7fffffff, 0, 0);
-  // and back to all lanes
+  for (int dt = 0; dt < DT; ++dt) most = largest_size(acc[dt], most);
+  const RowScale s = row_scale(most);
+  __builtin_amdgcn_raw_buffer_store_b32((int)s.unit, to_units, g == 0 ? row * 4 : 0x7fffffff, 0, 0);
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const float other = lane_moved<0x128>(scale[r]);
-    scale[r + 4] = upper ? scale[r] : other;
-    scale[r] = upper ? other : scale[r];
-  }
+  for (int dt = 0; dt < DT; dt += 2) {   // 64 columns: stores of eight rows' whole 128 bytes
+    u32x4 w[2][2];
+    pack_columns(acc[dt], s.scale, w[0]);
+    pack_columns(acc[dt + 1], s.scale, w[1]);
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    scale[r + 8] = scale[r];
-    swap_rows(scale[r], scale[r + 8]);
-  }
+    for (int h = 0; h < 2; ++h) {
+      u32x4 first, second;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int row = slot(r) + 4 * g;
-    V v;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) v[dt] = (f16_t)(acc[dt][r] * scale[r]);
-    const int at = row * (64 * DT) + (lane & 31) * (2 * DT);
-    if constexpr (DT == 4) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), to_rows, at, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, v), to_rows, at, 0, 0);
+      for (int k = 0; k < 4; ++k) {   // eight lanes of sixteen trade: rows 0 .. 7 with both column halves, rows 8 .. 15
+        first[k] = moved_into<0x128, 0xc>(w[0][h][k], w[1][h][k]);
+        second[k] = moved_into<0x128, 0x3>(w[1][h][k], w[0][h][k]);
+      }
+      const int at = (16 * h + (lane & 7)) * (64 * DT) + dt * 64 + (lane >> 3 & 1) * 64 + (lane >> 4 & 1) * 32 + (lane >> 5) * 16;
+      __builtin_amdgcn_raw_buffer_store_b128(first, to_rows, at, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(second, to_rows, at + 8 * 64 * DT, 0, 0);
+    }
   }
 }
 // A half-wavefront's row of D numbers in LDS, columns in order -> bf16 at `to`.

@@ -216,7 +216,7 @@ __device__ __forceinline__ void store_ml(float2* to, float m, float l, int rows,
 // A wavefront has 32 queries of a tile of 128.  KT > 0: the block is at most 32 KT = 64 or 128 keys, stays in LDS for all of the workgroup's
 // queries, and a row's scores are all there before the maximum is taken: no barrier behind the loads, no rescaling.  The next tile's
 // queries are requested as soon as the products of this one have read theirs, and ahead of its stores: the wait for them is no wait for stores.
-// Bound: nothing alone (1.1 GB of rows in 466 us, the matrix units at 24 %, the vector units at 40 %): a wavefront's products, its soft-max and its
+// Bound: nothing alone (1.1 GB of rows in 470 us, the matrix units at 24 %, the vector units at 40 %): a wavefront's products, its soft-max and its
 // row's scaling follow each other, two wavefronts a SIMD hide part of one behind the other.  Without the stores 330 us, with stores that are
 // dropped 413; exponentials left out 480; other cache policies of the stores 0 to 2 % (all of 510).
 template <int D, int KT>

@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
 // as columns, which is what dK and dV take; dS goes through LDS as [key][query], where the transposing reads fetch it and K for dQ, a
 // 32 x 32 tile (or two) a wavefront.  A lane has one query's 16 numbers of a tile, 32 columns of dQ, which get a scale of their own.
 // Bound: the steps of a block of queries one after the other, two barriers, two wavefronts a SIMD.  16 (sequence, head)s of 4096 x 128, 8 of 32 blocks:
-// 119 us, 640 TFLOP/s of five products (dQ in a pass of its own 83, dK and dV 95); 20 of up to 10000 x 64, 12 of 157 blocks 157 (118 and 127).
+// 119 us, 640 TFLOP/s of five products (dQ in a pass of its own 83, dK and dV 95); 20 of up to 10000 x 64, 12 of 157 blocks 136 (118 and 127).
 // The wait at the end of an iteration counts: dQ's stores, three a tile, are the last to be issued and may stay on their way.
 template <int D, int KEYS>
 struct SelectedBwd {

@@ -13,7 +13,7 @@
 // (backward): a row of fp16 numbers that goes to memory at the pair's place in the list, and a second kernel adds up each query's rows, at the
 // places that the step which makes the lists has noted.  dK and dV stay in the workgroup; blocks of several pieces are added up behind it.
 // The rows are count * s * d * 2 bytes a matrix, written and read: this, beside the products, bounds the form; they are made for 1 GiB at a time.
-// Measured, 8 (sequence, head)s of 32768 x 128, 16 of 256 blocks of 128 keys: lists 65 us, products 466 (590 TFLOP/s of the chosen pairs), sums 255 (1.1 GB,
+// Measured, 8 (sequence, head)s of 32768 x 128, 16 of 256 blocks of 128 keys: lists 62 us, products 470 (585 TFLOP/s of the chosen pairs), sums 258 (1.1 GB,
 // 4.3 TB/s); without the rows' stores the products take 330.
 #pragma once
 #include "attention_biased_kernel.hpp"
@@ -115,6 +115,9 @@ __device__ __forceinline__ void store_rows(float* to, const f32x16 (&acc)[DT], i
 // and dS to bf16 has left it off by some 2^-9; the sums over a block's keys and over the blocks stay fp32.  (8 (sequence, head)s of 32768 x 128,
 // 16 of 256 blocks: 2.2 GB of fp32 rows cost 300 us to write beside the products' 417, and 389 to read.)  Each row is scaled by a power of
 // two that brings its largest number to 2^14, so that nothing is lost to fp16's range but what is below 2^-28 of that.
+// Lanes trade their numbers until a store has 128 whole bytes of a row: the forward products of the case above take 536 us with 32 bytes of a row in a
+// store, 490 with 64, 474 with 128; 464 with 256, whose lanes have a column each, and 100 instructions more a tile for the scales (width 64: 2 to 5 % slower).
+
 // The maximum that passes NaN on: two operands or three an instruction.  (fmaxf first clears signalling NaN out of every operand that might be one,
 // such as a matrix instruction's result, by an instruction of its own.)
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }

@@ -532,3 +532,23 @@ def test_two_calls_at_once_and_graphs_that_share_a_workspace(form):
             g.replay()
         torch.cuda.synchronize()
         assert same(a, want[0]) and same(b, want[1])
+
+
+@pytest.mark.parametrize("block", [64, 128, 256])
+def test_captured_at_width_128(block, lists):
+    """The passes whose LDS is sized at launch, captured and replayed, against eager calls."""
+    r = Run(2, 1100, 512, 4, 1, True, block=block, count=3, lengths=[1100, 777]).go()
+    want = [x.clone() for x in (r.S, r.O, r.L, r.G)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.choose()
+        r.forward()
+        r.backward()
+    for k in range(3):
+        r.S.fill_(-9)
+        for x in (r.O, r.L, r.G):
+            x.fill_(float("nan"))
+        r.ws.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip((r.S, r.O, r.L, r.G), want))

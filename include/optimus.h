@@ -298,8 +298,9 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * lengths: int32 [b] device memory or NULL (all s): tokens of a sequence that count (clamped to 0 .. s).  What qkv and d_attn hold behind them
  * is not looked at, NaN included; there selected is -1, attn 0, lse -infinity and d_qkv 0.
  * P and dS are rounded to bf16 before their products, as the operands are, and what a query gets from one block may be rounded to 11 bits (fp16,
- * scaled) before the blocks' parts are added; scores and sums are fp32; lse enters as in optimus_attention_biased_bwd.  The values of tokens
- * inside the lengths are taken to be finite: a pair that is left out has weight zero, and zero times an infinity or NaN is NaN.
+ * scaled) before the blocks' parts are added; scores and sums are fp32; lse enters as in optimus_attention_biased_bwd: the
+ * forward takes finite scores of any size, the gradients of a row mean something up to scores of 1e7.  The values of tokens inside the lengths
+ * are taken to be finite: a pair that is left out has weight zero, and zero times an infinity or NaN is NaN.
  * qkv, attn, d_attn, d_qkv (16-byte aligned: EINVAL), lse, coordinates and limits as in optimus_attention_fused_*; bf16 only;
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it

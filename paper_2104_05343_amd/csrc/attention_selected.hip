@@ -276,11 +276,12 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_kernel(SelectedArgs a) {
 #pragma unroll
     for (int t2 = 0; t2 < KT; ++t2) mx = largest(sacc[t2], mx);
     mx = halfwave_max(mx) * f.scale_log2;   // (a listed query sees the block's first key)
+    const float weight = score_weight(sacc, f.scale_log2, large_scores(mx));
 #pragma unroll
     for (int t2 = 0; t2 < KT; ++t2)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], f.scale_log2, -mx));
+        const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], weight, -mx));
         sacc[t2][r] = p;
         sum += p;
       }
@@ -347,6 +348,7 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
+    bool large = false;
     for (int step = 0; step < steps; ++step, stage ^= 1) {
       const int next = step + 1 < steps ? step + 1 : 0;
       if (step + 1 < steps || round + 1 < rounds) issue(next, stage ^ 1);
@@ -371,12 +373,14 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_long_kernel(SelectedArgs 
         // The maximum follows the step's when that is above it by more than 8: a step's largest term is at most 2^8 then.
         const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
         const float m_new = move ? fmaxf(m_run, mx) : m_run;
+        if (move) large = large_scores(m_new);
+        const float weight = score_weight(sacc, f.scale_log2, large);
         float sum = 0.f;
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], f.scale_log2, -m_new));
+            const float e = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], weight, -m_new));
             sacc[t2][r] = e;
             sum += e;
           }

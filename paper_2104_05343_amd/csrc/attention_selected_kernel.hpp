@@ -126,6 +126,22 @@ __device__ __forceinline__ float largest(const f32x16& v, float m) {
   for (int r = 0; r < 16; r += 2) m = larger(larger(m, v[r]), v[r + 1]);
   return m;
 }
+// Whether a wavefront's scores have to be rounded before what is subtracted from them, a rounded score itself: that is off by up to 2^-24 of itself, and
+// scores times the factor less it are not, so that from 2^31 on an exponent above zero overflows, and one below leaves a row nothing.  (Finite: a
+// row that has seen nothing has -infinity.  Choice and forward of 128 (sequence, head)s of 4096 x 64 with a mask 438 us without this, 444 with it; lists as before.)
+__device__ __forceinline__ bool large_scores(float subtracted) {
+  const float size = fabsf(subtracted);
+  return __builtin_amdgcn_ballot_w64(size > 0x1p28f && size < INFINITY) != 0;
+}
+template <int N>
+__device__ __forceinline__ float score_weight(f32x16 (&scores)[N], float weight, bool large) {   // what the scores are to be multiplied by then
+  if (!large) return weight;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) scores[t][r] *= weight;
+  return 1.0f;
+}
 // A lane has one row's numbers: products with the rows' operand in the B slot, slot r of a 32 x 32 tile is column slot(r) + 4 g.  What scales them, the
 // reciprocal of what they are to be multiplied by later: 2^(141 - e) for a largest number of biased exponent e.
 struct RowScale { float scale; unsigned unit; };

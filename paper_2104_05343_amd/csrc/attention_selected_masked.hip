@@ -64,6 +64,7 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
   float m_run = -INFINITY, l_run = 0.f;
+  bool large = false;
   const unsigned in_rows = lds_address(lds) + lane_rows<D>(lane), in_cols = lds_address(lds) + lane_cols<D>(lane);
   TileLoader<D, 2 * NRG, PAIR, true> ldr;
   ldr.init(f.ld, wave, lane);
@@ -103,6 +104,8 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
       mx = chosen ? mx : -INFINITY;
       const bool move = __builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0;
       const float m_new = move ? fmaxf(m_run, mx) : m_run;
+      if (move) large = large_scores(m_new);
+      const float weight = score_weight(sacc, f.scale_log2, large);
       const float m_sub = m_new == -INFINITY ? 0.f : m_new;
       const float off = chosen ? -m_sub : -INFINITY;
       float sum = 0.f;
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(NRG * 128, D == 64 && NRG == 4 ? 4 : NRG == 4 || D 
       for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], f.scale_log2, off));
+          const float p = __builtin_amdgcn_exp2f(fmaf(sacc[t2][r], weight, off));
           sacc[t2][r] = p;
           sum += p;
         }

@@ -304,8 +304,8 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * qkv, attn, d_attn, d_qkv (16-byte aligned: EINVAL), lse, coordinates and limits as in optimus_attention_fused_*; bf16 only;
  * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
- * from call to call: calls that may overlap need one each.  It holds up to 1 GiB of partial results, or one (sequence, head)'s:
- * some s * count * (2 d + 16) bytes.
+ * from call to call: calls that may overlap need one each.  It holds some 9 bytes an entry of the choice, 40 a query and 1024 a (sequence, head),
+ * and up to 1 GiB of partial results, or where that is more one (sequence, head)'s: at most d * (3 s * count + 8 (s + block)) bytes.
  * How it is computed (all blocks with a mask, or lists of each block's queries), and with it the last bits, follows the sizes, those of one
  * device whatever the call covers. */
 typedef struct {

@@ -646,9 +646,13 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
   const size_t all_pairs = pairs * d.nb * d.nh;
   p.seg[1] = 256;
   while (p.seg[1] < 2048 && all_pairs / p.seg[1] >= 384) p.seg[1] *= 2;
+  const size_t row_bytes = pairs * (d.d * 2 + (p.joint ? d.d / 8 : 12)), key_row = d.d * 8;   // of a matrix; of a key
+  // A piece leaves sums of all of its block's keys, whatever its length: where those of one matrix would be more than a portion and more than a
+  // block's only piece and its queries' rows take, pieces are longer.  (One of 262144 x 128, 4 of 64 blocks of 4096: workspace 2317 MiB and backward 7.6 ms
+  // without this, 777 MiB and 7.0 ms.)
+  while ((blocks + pairs / p.seg[1]) * b.block * key_row > kPortion && pairs / p.seg[1] * b.block * key_row > row_bytes) p.seg[1] *= 2;
   p.most[1] = (int)(blocks + pairs / p.seg[1]);
-  const size_t row_bytes = pairs * (d.d * 2 + (p.joint ? d.d / 8 : 12));   // of a matrix
-  const size_t key_bytes = (size_t)p.most[1] * (b.block / 64) * 2 * 64 * d.d * 4;
+  const size_t key_bytes = p.most[1] * b.block * key_row;
   auto fit = [&](size_t bytes) { return (int)(kPortion / bytes < 1 ? 1 : kPortion / bytes > mats ? mats : kPortion / bytes); };
   p.portion = fit(p.joint ? row_bytes + key_bytes : row_bytes);
   p.key_portion = p.joint ? p.portion : fit(key_bytes);
@@ -662,10 +666,11 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
   p.items[0] = p.joint ? 0 : round256(mats * p.most[0] * 16);
   p.items[1] = bwd ? round256(mats * p.most[1] * 16) : 0;
   p.list = p.places = round256(mats * pairs * 4);
-  const size_t rows = p.portion * pairs * d.d * 2, keys = bwd ? p.key_portion * key_bytes : 0;
-  p.rows = round256(p.joint || rows > keys ? rows : keys);
-  p.keys = p.joint ? round256(keys) : 0;
+  const size_t keys = bwd ? p.key_portion * key_bytes : 0;
+  p.rows = round256(p.portion * pairs * d.d * 2);
   p.units = round256(p.portion * pairs * (p.joint ? d.d / 32 : 1) * 4);
+  if (p.joint) p.keys = round256(keys);
+  else if (keys > p.rows + p.units) p.units = round256(keys - p.rows);   // (in the place of both, when dQ is done)
   p.ml = bwd ? 0 : round256(p.portion * pairs * 8);
   p.total = p.delta + p.counts + p.first_item + p.items[0] + p.items[1] + p.list + p.places + p.rows + p.units + p.ml + p.keys;
   *out = p;

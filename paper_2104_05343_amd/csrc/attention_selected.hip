@@ -8,11 +8,15 @@ namespace optimus {
 namespace {
 
 // ---------------------------------------------------------------- lists
-// Bound: round trips to memory (the choice read twice, lists and places written once): 21 and 42 us for 8 (sequence, head)s of 32768 queries with 16
-// entries each (17 MB), 5 (10 with the backward pass' sums) and 8 for 16 of 4096 with 8.
+// Bound: round trips to memory (the choice read twice, lists and places written once; the table of counts, a row a chunk, see kFewChunks): 17 and 33 us for 8
+// (sequence, head)s of 32768 queries with 16 entries each (17 MB), 5 (10 with the backward pass' sums) and 7 for 16 of 4096 with 8.
 // Pairs of 256 queries as a bit a (block, query) in LDS: entries that name a block twice, none, or one that the query does not see
 // make no pair, and a query's place among a block's is a count of bits.  bits[word of 32 queries][block].
 constexpr int kWords = kListChunk / 32;
+// Chunks of a sequence up to which list_fill_kernel adds up the counts by itself, which grows with their square.  Fill, or a launch for the sums and fill, us: width
+// 128, 16 (sequence, head)s of 4096, 8 blocks of 128 (16 chunks) 7 / 11; 8 of 16384, 16 entries (64) 19 / 21; of 24576 (96) 26 / 26; of 32768 (128) 34 / 32; of
+// 65536 (256) 117 / 63; of 131072 (512) 1042 / 157; one of 2^20, 4 of 1024 (4096) 6884 / 135.
+constexpr int kFewChunks = 96;
 std::atomic<int> g_form{-1};                      // forced by a tuning hook: 1 masked, 0 lists
 constexpr size_t kPortion = (size_t)1 << 30;    // bytes of partial results in memory at a time
 
@@ -86,11 +90,47 @@ __global__ __launch_bounds__(kListChunk) void list_count_kernel(SelectedArgs a) 
     int n = 0;
 #pragma unroll
     for (int w = 0; w < kWords; ++w) n += __popc(bits[w * a.blocks + v]);
-    a.counts[((long long)mm * a.chunks + chunk) * a.blocks + v] = n;
+    a.counts[((long long)mm * (a.chunks + 1) + chunk) * a.blocks + v] = n;
   }
   if constexpr (D > 0) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) delta_rows<D>(a, mm, chunk * kListChunk + (threadIdx.x >> 6) * 64 + 32 * k);
+  }
+}
+
+// Counts of many chunks -> each block's pairs in earlier chunks, and behind the last chunk in all of them.  A workgroup has 64 blocks, each of its
+// wavefronts a run of chunks.
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(64 * kSumWaves) void list_sums_kernel(SelectedArgs a) {
+  __shared__ int sums[kSumWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, v = blockIdx.x * 64 + lane;
+  const bool mine = v < a.blocks;
+  int* c = a.counts + (long long)blockIdx.y * (a.chunks + 1) * a.blocks + v;
+  const int each = (a.chunks + kSumWaves - 1) / kSumWaves, from = min(wave * each, a.chunks), to = min(from + each, a.chunks);
+  auto load = [&](int k, int x[16]) {   // sixteen in flight
+#pragma unroll
+    for (int u = 0; u < 16; ++u) x[u] = mine && k + u < to ? c[(long long)(k + u) * a.blocks] : 0;
+  };
+  int sum = 0;
+  for (int k = from; k < to; k += 16) {
+    int x[16];
+    load(k, x);
+#pragma unroll
+    for (int u = 0; u < 16; ++u) sum += x[u];
+  }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < wave; ++w) before += sums[w][lane];
+  if (mine && wave == kSumWaves - 1) c[(long long)a.chunks * a.blocks] = before + sum;
+  for (int k = from; k < to; k += 16) {
+    int x[16];
+    load(k, x);
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      if (mine && k + u < to) c[(long long)(k + u) * a.blocks] = before;
+      before += x[u];
+    }
   }
 }
 
@@ -118,8 +158,9 @@ __device__ __forceinline__ int exclusive_sum(int x, int* lds, int* total) {
   return before + in - x;
 }
 
-// Places and entries of a chunk.  Every workgroup adds up its matrix' counts itself (a launch of its own for them: 5 to 13 us); the first one of a
-// matrix writes the items too.
+// Places and entries of a chunk.  SUMMED: list_sums_kernel has added up the counts; otherwise every workgroup does so itself, with its matrix' whole
+// table.  The first one of a matrix writes the items too.
+template <bool SUMMED>
 __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
   extern __shared__ unsigned bits[];
   int* place_of = (int*)(bits + kWords * a.blocks);   // [word][block]: place of a word's first pair
@@ -137,8 +178,12 @@ __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
     const int v = v0 + tid;
     int pairs = 0, before = 0;   // of the block, in earlier chunks
     if (v < a.blocks) {
-      const int* c = a.counts + (long long)mm * a.chunks * a.blocks + v;
-      for (int k = 0; k < a.chunks; k += 16) {   // sixteen loads in flight
+      const int* c = a.counts + (long long)mm * (a.chunks + 1) * a.blocks + v;
+      if (SUMMED) {
+        pairs = c[(long long)a.chunks * a.blocks];
+        before = c[(long long)chunk * a.blocks];
+      }
+      for (int k = 0; !SUMMED && k < a.chunks; k += 16) {   // sixteen loads in flight
         int x[16];
 #pragma unroll
         for (int u = 0; u < 16; ++u) x[u] = k + u < a.chunks ? c[(long long)(k + u) * a.blocks] : 0;
@@ -562,8 +607,11 @@ void launch_lists(const SelectedArgs& a, int d, bool bwd, hipStream_t st) {
   else if (d == 64) list_count_kernel<64><<<grid, kListChunk, bits, st>>>(a);
   else list_count_kernel<128><<<grid, kListChunk, bits, st>>>(a);
   const size_t fill = 2 * bits + kListChunk / 64 * sizeof(int);
-  if (fill > 65536) (void)hipFuncSetAttribute((const void*)list_fill_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)fill);
-  list_fill_kernel<<<grid, kListChunk, fill, st>>>(a);
+  const bool summed = a.chunks > kFewChunks;
+  if (summed) list_sums_kernel<<<dim3((a.blocks + 63) / 64, a.mats), 64 * kSumWaves, 0, st>>>(a);
+  auto kernel = summed ? list_fill_kernel<true> : list_fill_kernel<false>;
+  if (fill > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)fill);
+  kernel<<<grid, kListChunk, fill, st>>>(a);
 }
 
 template <int D>
@@ -661,7 +709,7 @@ void attn_selected_plan(const AttnSelectedDesc& b, bool bwd, SelectedPlan* out) 
   p.seg[0] = 256;
   while (p.seg[0] < 1024 && p.portion * pairs / p.seg[0] >= 4096) p.seg[0] *= 2;
   p.most[0] = (int)(blocks + pairs / p.seg[0]);
-  p.counts = round256(mats * p.chunks * blocks * 4);
+  p.counts = round256(mats * (p.chunks + 1) * blocks * 4);
   p.first_item = round256(2 * mats * (blocks + 1) * 4);
   p.items[0] = p.joint ? 0 : round256(mats * p.most[0] * 16);
   p.items[1] = bwd ? round256(mats * p.most[1] * 16) : 0;

@@ -44,7 +44,7 @@ struct SelectedArgs {
   int mats, mat0, portion;             // matrices of the call, first one of this launch, how many it has
   int chunks;                          // kListChunk pieces of a sequence
   int seg[2], most[2];                 // kind 0: forward and dQ, 1: dK and dV: list rows of an item, about; most items of a matrix
-  int* counts;                         // [matrix][chunk][block]: pairs
+  int* counts;                         // [matrix][chunks + 1][block]: pairs, or (list_sums_kernel) those of earlier chunks
   int* first_item;                     // [kind][matrix][blocks + 1]
   i32x4_t* items[2];                   // [matrix][most]: block, place of the first pair, pairs, -
   int* list;                           // [matrix][s * count]: query of every pair

@@ -327,7 +327,6 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void selected_dkv_kernel(Sele
 // 32 x 32 tile (or two) a wavefront.  A lane has one query's 16 numbers of a tile, 32 columns of dQ, which get a scale of their own.
 // Bound: the steps of a block of queries one after the other, two barriers, two wavefronts a SIMD.  16 (sequence, head)s of 4096 x 128, 8 of 32 blocks:
 // 119 us, 640 TFLOP/s of five products (dQ in a pass of its own 83, dK and dV 95); 20 of up to 10000 x 64, 12 of 157 blocks 136 (118 and 127).
-// The wait at the end of an iteration counts: dQ's stores, three a tile, are the last to be issued and may stay on their way.
 template <int D, int KEYS>
 struct SelectedBwd {
   static constexpr bool WIDE = D == 128 && KEYS == 128;
@@ -348,7 +347,7 @@ struct SelectedBwd {
     alignas(16) int t[2][BLK];
   };
 };
-// A lane's 16 numbers of a query's 32 columns from 32 dt on, with a scale of their own: three stores
+// A lane's 16 numbers of a query's 32 columns from 32 dt on, with a scale of their own
 template <int DT>
 __device__ __forceinline__ void store_part(const f32x16& acc, int row0, int dt, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t units, int lane) {
   const RowScale s = row_scale(largest_size(acc, 0.f));
@@ -497,15 +496,15 @@ __global__ __launch_bounds__((SelectedBwd<D, KEYS>::THREADS), (SelectedBwd<D, KE
                               for (int i = 0; i < B::TILES; ++i) dq[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.k[i], x.ds, dq[i], 0, 0, 0);
                             });
     if (n + 1 < n_it) store_numbers(n + 1, st ^ 1);
+    // The loads into the other stage have ended, and with them the stores of the iteration before: this one's come behind the wait and stay on their way,
+    // however many instructions they are.  (A wait behind them that leaves
+    // just as many takes as long: 16 (sequence, head)s of 4096 x 128 165 us a call, 16 of 8192 in blocks of 64 325 for 327.)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const int left = __builtin_amdgcn_readfirstlane(min(it.pairs - n * BLK, BLK));
     const auto to_rows = __builtin_amdgcn_make_buffer_rsrc(rows + (long long)n * BLK * D, 0, left * (2 * D), 0x00020000);
     const auto to_units = __builtin_amdgcn_make_buffer_rsrc(units + (long long)n * BLK * DT, 0, left * (4 * DT), 0x00020000);
 #pragma unroll
     for (int i = 0; i < B::TILES; ++i) store_part<DT>(dq[i], q_half * 32, dt0 + i, to_rows, to_units, lane);
-    // all but this iteration's stores, three a tile, have ended: the loads into the other stage were issued ahead of them
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((3 * B::TILES) | (7 << 4) | (15 << 8));
-    asm volatile("" ::: "memory");
     __syncthreads();
   }
   // the halves' sums of 32 keys, dV first: the odd one hands over through LDS (all block tiles are free)

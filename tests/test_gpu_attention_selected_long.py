@@ -128,3 +128,22 @@ def test_lists_grow_with_the_sequence(lists):  # noqa: F811
         took.append(best)
     print("us", took)
     assert took[1] <= 8 * took[0]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [64, 128])
+def test_same_gradients_beside_other_traffic(d, block, lists):  # noqa: F811
+    """The pass for all three gradients hands tiles of queries from iteration to iteration: the same bits whatever else the memory is busy with."""
+    r = Run(1, 6000, 4 * d, 4, 1, True, block=block, count=8).go()
+    want = r.G.clone()
+    a, b = (torch.zeros(1 << 28, dtype=torch.uint8, device=DEV) for _ in range(2))
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(12):
+        with torch.cuda.stream(other):
+            for _ in range(4):
+                b.copy_(a)
+        r.G.fill_(float("nan"))
+        r.backward()
+        torch.cuda.synchronize()
+        assert torch.equal(r.G.view(torch.uint8), want.view(torch.uint8))

@@ -302,7 +302,7 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * forward takes finite scores of any size, the gradients of a row mean something up to scores of 1e7.  The values of tokens inside the lengths
  * are taken to be finite: a pair that is left out has weight zero, and zero times an infinity or NaN is NaN.
  * qkv, attn, d_attn, d_qkv (16-byte aligned: EINVAL), lse, coordinates and limits as in optimus_attention_fused_*; bf16 only;
- * b*n (whole grid) or b/q * n/q (one device) up to 65535 (ESHAPE).
+ * b*n (whole grid) or b/q * n/q (one device) up to 65535, q up to 46340, 3h < 2^31 (ESHAPE).
  * ws: optimus_attention_selected_workspace_bytes(...) bytes for all three (0 for arguments that are refused), 256-byte aligned, nothing kept in it
  * from call to call: calls that may overlap need one each.  It holds some 9 bytes an entry of the choice, 40 a query and 1024 a (sequence, head),
  * and up to 1 GiB of partial results, or where that is more one (sequence, head)'s: at most d * (3 s * count + 8 (s + block)) bytes.
@@ -334,7 +334,7 @@ size_t optimus_attention_selected_workspace_bytes(int b, int s, int h, int n, in
  * 2 pi 2^20, 2^20 turns a position (EINVAL).
  * optimus_rotary writes the blocks of `out` whole, values too; out == qkv turns them in place; blocks that overlap otherwise: EINVAL.
  * optimus_rotary_bwd is the gradient, the turn by -angle: of d_out with respect to qkv, in place with d_qkv == d_out.
- * axes 1 .. 4, pairs[] >= 1, P <= 128, 2P <= h/n, even h/n with interleaved, 3h/q <= 2^18 (ESHAPE).  Pointers need the alignment of their elements
+ * axes 1 .. 4, pairs[] >= 1, P <= 128, 2P <= h/n, even h/n with interleaved, 3h/q <= 2^18, 3h < 2^31, q <= 46340 (ESHAPE).  Pointers need the alignment of their elements
  * only.  The struct is read before the call returns; one row (s = 1) is a call like any other. */
 typedef struct {
   const int32_t* positions;

@@ -414,6 +414,7 @@ int run_attention_biased(bool bwd, const void* qkv, void* attn, float* lse, cons
 
 // ---- attention over chosen blocks ----
 int selected_desc(int b, int s, int h, int n, int q, int i, int j, const optimus_selection* sel, AttnDims* a, AttnSelectedDesc* d) {
+  if (!fits_int(h, q)) return OPTIMUS_ESHAPE;
   if (const int rc = attn_fused_dims(b, s, h, n, q, a)) return rc;
   if (const int rc = check_coords(q, i, j)) return rc;
   if (!sel) return OPTIMUS_EINVAL;

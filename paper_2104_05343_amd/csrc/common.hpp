@@ -209,6 +209,9 @@ int launch_attn_biased_bwd(const AttnBiasedDesc& d, hipStream_t stream);
 bool attn_biased_fwd_wide(const AttnBiasedDesc& d);   // whether workgroups have 128 rows, not 64
 bool attn_biased_bwd_wide(const AttnBiasedDesc& d);
 
+// Whether the devices of a grid and the columns of qkv are numbers of 32 bits.
+inline bool fits_int(int h, int q) { return q <= 46340 && h <= 0x7fffffff / 3; }
+
 // Attention over chosen blocks of keys (attention_selected_kernel.hpp).
 struct AttnSelectedDesc {
   AttnFusedDesc base;       // lse, selected: first device of the launch; delta: not used

@@ -170,7 +170,7 @@ void launch(const RotaryArgs& a, bool beside, dim3 grid, hipStream_t st) {
 int run(const void* x, void* y, int b, int s, int h, int n, int q, int i, int j, int dtype, const optimus_rotary_axes* r, bool back, void* stream) {
   if (!x || !y || !r || !r->positions) return OPTIMUS_EINVAL;
   if (dtype != OPTIMUS_BF16 && dtype != OPTIMUS_FP32) return OPTIMUS_EDTYPE;
-  if (q <= 0 || b <= 0 || s <= 0 || h <= 0 || n <= 0 || b % q || n % q || h % n) return OPTIMUS_ESHAPE;
+  if (q <= 0 || !fits_int(h, q) || b <= 0 || s <= 0 || h <= 0 || n <= 0 || b % q || n % q || h % n) return OPTIMUS_ESHAPE;
   const bool all = i == OPTIMUS_ALL && j == OPTIMUS_ALL;
   if (!all && (i < 0 || j < 0 || i >= q || j >= q)) return OPTIMUS_ECOORD;
   if (r->axes < 1 || r->axes > kMaxAxes || !(r->base > 0) || !isfinite(r->base)) return OPTIMUS_EINVAL;

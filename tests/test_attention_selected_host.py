@@ -165,3 +165,12 @@ def test_refuses_tensors():
             with pytest.raises(opt.OptimusError) as e:
                 call()
             assert e.value.code == code
+
+
+@pytest.mark.parametrize("kw", [dict(b=65536, s=1, n=65536, h=65536 * 64, q=65536, i=-1, j=-1), dict(b=46341, s=1, n=46341, h=46341 * 64, q=46341, i=0, j=0),
+                                dict(b=200, s=1, n=200 * 60000, h=200 * 60000 * 64, q=200, i=0, j=0)])
+def test_refuses_sizes_past_32_bits(kw):
+    """Grids of 2^31 devices and more, rows of 2^31 columns."""
+    for what in ("select", "fwd", "bwd"):
+        assert _rc(what, opt.make_selection(64, 2), **kw) == opt.ESHAPE, what
+    assert opt.attention_selected_workspace_bytes(*(kw[k] for k in "b s h n q i j".split()), opt.make_selection(64, 2)) == 0

@@ -94,3 +94,10 @@ def test_refuses_tensors():
         with pytest.raises(opt.OptimusError) as e:
             opt.make_rotary(t, (4, 4))
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("kw", [dict(b=65536, s=1, n=65536, h=65536 * 32, q=65536, i=-1, j=-1), dict(b=46341, s=1, n=46341, h=46341 * 32, q=46341, i=0, j=0),
+                                dict(b=8192, s=1, n=8192 * 2, h=8192 * 87382, q=8192, i=0, j=0)])
+def test_refuses_sizes_past_32_bits(kw):
+    """Grids of 2^31 devices and more, rows of 2^31 columns."""
+    assert _rc(_axes(), **kw) == opt.ESHAPE

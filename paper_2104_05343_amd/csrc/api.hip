@@ -418,7 +418,8 @@ int selected_desc(int b, int s, int h, int n, int q, int i, int j, const optimus
   if (const int rc = attn_fused_dims(b, s, h, n, q, a)) return rc;
   if (const int rc = check_coords(q, i, j)) return rc;
   if (!sel) return OPTIMUS_EINVAL;
-  if (sel->block < 64 || sel->block % 64 || sel->block > 4096 || (s - 1) / sel->block >= 1024 || sel->count < 1 || sel->count > 64) return OPTIMUS_ESHAPE;
+  if (sel->block < 64 || sel->block % 64 || sel->block > kMostBlock || (s - 1) / sel->block >= kMostBlocks) return OPTIMUS_ESHAPE;
+  if (sel->count < 1 || sel->count > kMostCount) return OPTIMUS_ESHAPE;
   if ((uintptr_t)sel->lengths & 3) return OPTIMUS_EINVAL;
   AttnFusedDesc& f = d->base;
   f.s = s; f.d = a->d; f.nb = a->nb; f.nh = a->nh; f.ld = a->ld; f.ldo = a->ldo;

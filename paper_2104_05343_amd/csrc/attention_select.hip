@@ -425,6 +425,7 @@ void choose(const SelectedArgs& a, int mats, hipStream_t st) {
   else if (a.blocks <= 256) select_launch<D, 32>(a, mats, st);
   else if (a.blocks <= 512) select_launch<D, 64>(a, mats, st);
   else select_launch<D, 128>(a, mats, st);
+  static_assert(kMostBlocks <= 8 * 128, "a lane's scores");
 }
 
 size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -447,7 +448,6 @@ int launch_attn_select(const AttnSelectedDesc& b, hipStream_t st) {
   a.nb = d.nb; a.nmat = d.nb * d.nh; a.q = b.q; a.dev0 = b.dev0; a.causal = d.causal;
   a.block = b.block; a.count = b.count; a.blocks = (d.s + b.block - 1) / b.block;
   const int mats = d.ndev * a.nmat;
-  if (mats > 65535 || a.blocks > kMostBlocks) return OPTIMUS_ESHAPE;
   a.means = (bf16_t*)b.ws;
   a.mean_sizes = (float*)((char*)b.ws + round256((size_t)mats * a.blocks * d.d * 2));
   if (d.d == 64) choose<64>(a, mats, st);

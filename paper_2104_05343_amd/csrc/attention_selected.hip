@@ -170,7 +170,8 @@ __global__ __launch_bounds__(kListChunk) void list_fill_kernel(SelectedArgs a) {
   const int t = chunk * kListChunk + tid;
   for (int k = tid; k < kWords * a.blocks; k += kListChunk) bits[k] = 0;
   __syncthreads();
-  unsigned long long counted = 0;   // (at most 64 entries)
+  static_assert(kMostCount <= 64, "an entry is a bit");
+  unsigned long long counted = 0;
   chunk_pairs(a, mm, len, t, bits, [&](int e, int, bool counts) { counted |= counts ? 1ull << e : 0; });
   __syncthreads();
   int earlier_pairs = 0, earlier_items[2] = {0, 0};   // of the blocks below
@@ -478,6 +479,7 @@ __global__ __launch_bounds__(256) void selected_combine_kernel(SelectedArgs a) {
   const SelMatrix m = selected_matrix<D>(a, mm);
   const long long rows = (long long)blockIdx.y * f.s * a.count;
   const int* places = a.places + (m.vec + t) * a.count;
+  static_assert(kMostCount <= 64, "two entries a lane");
   // entries n and n + 32
   int place[2];
   float weight[2];
@@ -558,7 +560,7 @@ SelectedArgs make_args(const AttnSelectedDesc& b) {
   f.qkv = (const bf16_t*)d.qkv; f.attn = (bf16_t*)d.attn; f.lse = d.lse;
   f.d_attn = (const bf16_t*)d.d_attn; f.d_qkv = (bf16_t*)d.d_qkv;
   f.s = d.s; f.nh = d.nh; f.ld = d.ld; f.ldo = d.ldo;
-  f.dev_qkv = d.dev_qkv; f.dev_attn = d.dev_attn; f.dev_vec = (long long)d.nb * d.nh * d.s;
+  f.dev_qkv = d.dev_qkv; f.dev_attn = d.dev_attn;
   f.scale = 1.0f / sqrtf((float)d.d);
   f.scale_log2 = (float)(1.4426950408889634 / sqrt((double)d.d));
   a.selected = b.selected; a.lengths = b.lengths;

@@ -21,7 +21,6 @@
 namespace optimus {
 
 constexpr int kListChunk = 256;        // queries of a workgroup that makes the lists
-constexpr int kMostBlocks = 1024, kMostCount = 64;
 constexpr int kMaskedBlocks = 256;     // most blocks of a sequence in the masked form
 constexpr int kQueries = 128;          // list rows of a tile
 

@@ -213,6 +213,7 @@ bool attn_biased_bwd_wide(const AttnBiasedDesc& d);
 inline bool fits_int(int h, int q) { return q <= 46340 && h <= 0x7fffffff / 3; }
 
 // Attention over chosen blocks of keys (attention_selected_kernel.hpp).
+constexpr int kMostBlocks = 1024, kMostCount = 64, kMostBlock = 4096;   // blocks of a sequence, of a query; keys of a block
 struct AttnSelectedDesc {
   AttnFusedDesc base;       // lse, selected: first device of the launch; delta: not used
   int q, dev0;              // grid, first device of the launch

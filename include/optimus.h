@@ -307,7 +307,7 @@ size_t optimus_attention_biased_workspace_bytes(int b, int s, int h, int n, int 
  * from call to call: calls that may overlap need one each.  It holds some 9 bytes an entry of the choice, 40 a query and 1024 a (sequence, head),
  * and up to 1 GiB of partial results, or where that is more one (sequence, head)'s: at most d * (3 s * count + 8 (s + block)) bytes.
  * How it is computed (all blocks with a mask, or lists of each block's queries), and with it the last bits, follows the sizes, those of one
- * device whatever the call covers. */
+ * device whatever the call covers: b/q and n/q too, so that a sequence alone and the same one in a batch may differ in their last bits. */
 typedef struct {
   int block, count;
   const int32_t* lengths;
@@ -334,7 +334,8 @@ size_t optimus_attention_selected_workspace_bytes(int b, int s, int h, int n, in
  * 2 pi 2^20, 2^20 turns a position (EINVAL).
  * optimus_rotary writes the blocks of `out` whole, values too; out == qkv turns them in place; blocks that overlap otherwise: EINVAL.
  * optimus_rotary_bwd is the gradient, the turn by -angle: of d_out with respect to qkv, in place with d_qkv == d_out.
- * axes 1 .. 4, pairs[] >= 1, P <= 128, 2P <= h/n, even h/n with interleaved, 3h/q <= 2^18, 3h < 2^31, q <= 46340 (ESHAPE).  Pointers need the alignment of their elements
+ * axes 1 .. 4, pairs[] >= 1, P <= 128, 2P <= h/n, even h/n with interleaved, 3h/q <= 2^18, 3h < 2^31, q <= 46340, b/q * s below 2^24
+ * (up to eight times as many where rows are narrow) (ESHAPE).  Pointers need the alignment of their elements
  * only.  The struct is read before the call returns; one row (s = 1) is a call like any other. */
 typedef struct {
   const int32_t* positions;
@@ -510,9 +511,10 @@ int optimus_cross_entropy2d_bwd(const void* logits, const int32_t* labels, const
                                 float scale, int64_t M, int64_t v, int q, int i, int j, int dtype, void* stream);
 
 /* ---- the norm of all gradients, and clipping by it, between the backward pass and the update ----
- * norm = sqrt(sum over tensors and elements of g^2), g the sum of an element's parts (partial gradients [q][q][N/q] of optimus_layer_bwd
- * are q parts of N elements); squares and sums in 64 bits.  scale = max_norm / norm where norm is above max_norm, else 1: what
- * optimus_adamw_cfg.grad_scale takes, so that an update clips without a pass of its own.  A gradient that holds an infinity or NaN: scale
+ * norm = sqrt(sum over tensors and elements of g^2), g the sum of an element's parts in fp32, in their order (partial gradients [q][q][N/q] of
+ * optimus_layer_bwd are q parts of N elements); squares and their sums in 64 bits.  scale = max_norm / norm where norm is above max_norm, else 1:
+ * what optimus_adamw_cfg.grad_scale takes, so that an optimus_adamw_step behind optimus_stack_bwd clips without a pass of its own
+ * (optimus_stack_bwd_adamw updates a layer before the gradients of all are there).  A gradient that holds an infinity or NaN: scale
  * is NaN.  norm: 1 float; scale: 1 float or NULL; norms: [count], each tensor's own, or NULL: device memory, written.  max_norm > 0, infinity
  * included (EINVAL).  ws: optimus_gradient_norm_workspace_bytes(...) bytes (0 for a list that is refused), 8-byte aligned.
  * optimus_gradient_clip: clipped = *scale * g, in the gradient's dtype, the parts added (in fp32, in order): clipped[n] may be grad

@@ -13,7 +13,7 @@
 // (backward): a row of fp16 numbers that goes to memory at the pair's place in the list, and a second kernel adds up each query's rows, at the
 // places that the step which makes the lists has noted.  dK and dV stay in the workgroup; blocks of several pieces are added up behind it.
 // The rows are count * s * d * 2 bytes a matrix, written and read: this, beside the products, bounds the form; they are made for 1 GiB at a time.
-// Measured, 8 (sequence, head)s of 32768 x 128, 16 of 256 blocks of 128 keys: lists 62 us, products 470 (585 TFLOP/s of the chosen pairs), sums 258 (1.1 GB,
+// Measured, 8 (sequence, head)s of 32768 x 128, 16 of 256 blocks of 128 keys: lists 61 us, products 470 (585 TFLOP/s of the chosen pairs), sums 258 (1.1 GB,
 // 4.3 TB/s); without the rows' stores the products take 330.
 #pragma once
 #include "attention_biased_kernel.hpp"

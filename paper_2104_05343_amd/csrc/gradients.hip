@@ -1,12 +1,12 @@
 // The norm of the gradients of many tensors, and their clipping.
-//   norm = sqrt(sum over tensors and elements of g^2), g the sum of an element's parts;  scale = min(1, max_norm / norm)
+//   norm = sqrt(sum over tensors and elements of g^2), g the fp32 sum of an element's parts;  scale = min(1, max_norm / norm)
 // Squares and their sums are 64 bits: in fp32 a gradient below 1e-19 or above 1e19 would have no square, and a long sum loses digits.
 // (An element costs a conversion and a fused multiply-add of full rate, a quarter of what memory takes to deliver it.)  A workgroup adds
 // its piece of one tensor, a last one adds the pieces in their order: the same list gives the same bits.
 //
 // Bound: memory.  The clipping reads the gradients a second time, last ones first: those the norm has read last are in the
-// Infinity Cache still.  50 * 10^6 fp32 numbers: 40 us (5.0 TB/s), 5 for the last workgroup, 67 for the clipping (6.0 TB/s of its own bytes);
-// 8 * 10^8 in bf16: 312 (5.2), 7, 546 (5.9).
+// Infinity Cache still.  50 * 10^6 fp32 numbers: 40 us (5.0 TB/s), 5 for the last workgroup, 67 for the clipping (6.0 TB/s of its own bytes),
+// 126 for the two calls; 8 * 10^8 in bf16: 312 (5.2), 7, 546 (5.9), 867.
 #include <math.h>
 #include <stdlib.h>
 
